@@ -208,7 +208,8 @@ def _run_plain(state):
         return {"x": x, "v": v}
     if k == "layer":
         x = state["x"].float()
-        sa = x.abs().amax(1) / 127.0
+        mx = x.abs().amax(1)
+        sa = mx / torch.full_like(mx, 127.0)   # by a number torch would multiply with its reciprocal, a step off at times
         A = torch.round(x / sa[:, None])
     else:
         sa, A = state["sa"], state["A"][:, :case["K"]].float()
