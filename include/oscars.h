@@ -75,6 +75,12 @@ typedef enum {
  * n images of H*W*Cin fp32 values (NHWC) and n labels.
  */
 
+/* Element types of the context-free operators that take more than one. */
+typedef enum {
+  OSCARS_F32 = 0,
+  OSCARS_BF16 = 1
+} oscars_dtype;
+
 typedef enum {
   OSCARS_W_UNIFORM = 0,    /* w_k = 1/N: the average of Eq. 4 (first branch)        */
   OSCARS_W_LOCALSTEPS = 1, /* w_k = tau_k / sum_j tau_j: NOT in the paper            */
@@ -486,6 +492,99 @@ oscars_status oscars_softreg_steps_noalloc(const float* params_in, float* params
                                            const int32_t* y, int64_t n, int64_t cursor, int32_t tau,
                                            int32_t dim, int32_t classes, int32_t batch, float lr,
                                            float* loss_out, void* stream);
+
+/*
+ * oscars_orthogonalize - replace every singular value of an update by (about)
+ * one, by Newton-Schulz steps: the update rule of the Muon optimiser for weight
+ * matrices, which a server may apply to a merged update before it adds it to
+ * the model (the paper's server averages, Eq. 4; this rule is not in it).
+ *   X = G / (|G|_F + eps);  `steps` times:  A = X X^T,
+ *   X <- a X + (b A + c A A) X;  O = scale X.
+ * G: device, `batch` matrices [rows][cols], element (z, i, j) at
+ * G[z batch_stride_g + i ldg + j]; O likewise, written in [rows][cols] only.
+ * O may be G itself with the same strides, else they must not overlap; a
+ * batch_stride_g of 0 reads one matrix for all.  dtype (oscars_dtype) is that
+ * of both; any alignment (16-byte aligned rows take the vector path).
+ * coeff: host, 3 floats {a, b, c}, each at most 8 in magnitude, or NULL for
+ * {3.4445, -4.7750, 2.0315}, which keep singular values in [0, 1] below 1.21.
+ * Others have to keep them below 2 in every step, or the result may overflow.
+ * eps > 0: a matrix of zeros gives zeros.  A matrix that holds an infinity or
+ * NaN gives NaN throughout.  The norm neither overflows nor underflows.
+ * Accuracy: fp32 results are fp32 throughout; bf16 results round the factors
+ * (b A + c A A) to 11 bits and keep X in 22, about 1e-3 of a result's size.
+ * The arithmetic is fixed: equal inputs give equal bits.
+ * workspace: device, 256-byte aligned, at least the bytes that
+ * oscars_orthogonalize_workspace gives for the same sizes; the call leaves
+ * nothing in it that a later call needs, and calls (or captured graphs) that
+ * may run at the same time need one each.  The call allocates nothing and can
+ * be captured.  Ordered on `stream`.  batch = 0 does nothing.
+ * Errors: EINVAL (NULL or misaligned pointers, batch outside [0, 65535], rows
+ * or cols outside [1, 65536], ldg or ldo < cols, a negative batch_stride_g, a
+ * batch_stride_o below a matrix's extent with batch > 1, steps outside [1, 64],
+ * coefficients or eps out of range, a workspace that is too small), ECUDA.
+ */
+oscars_status oscars_orthogonalize_workspace(int32_t batch, int32_t rows, int32_t cols, int32_t dtype,
+                                             int64_t* bytes);
+oscars_status oscars_orthogonalize(const void* G, int64_t ldg, int64_t batch_stride_g, void* O, int64_t ldo,
+                                   int64_t batch_stride_o, int32_t batch, int32_t rows, int32_t cols,
+                                   int32_t dtype, int32_t steps, const float* coeff, float eps, float scale,
+                                   void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * oscars_merge_orthogonal - the server step on one weight matrix with an
+ * orthogonalised update, in place of oscars_merge's average:
+ *   d = sum_k w[k] deltas[k] (in worker order);  v <- mu v + d;
+ *   u = nesterov ? d + mu v : v;
+ *   x_g <- x_g + server_lr O(u), O as in oscars_orthogonalize.
+ * x_g, momentum (v) and the W deltas: device, [rows][cols] fp32 without
+ * padding (a weight of the canonical layout), any alignment, not overlapping;
+ * x_g and momentum are updated in place.  momentum == NULL: u = d (mu is not
+ * read, nesterov must be 0).  deltas: host array of W device pointers, w: host,
+ * W floats, W <= 256.  Everything in fp32.  Workspace, coeff, eps, determinism
+ * and capture as for oscars_orthogonalize.
+ * Errors: EINVAL, ECUDA.
+ */
+oscars_status oscars_merge_orthogonal_workspace(int32_t rows, int32_t cols, int64_t* bytes);
+oscars_status oscars_merge_orthogonal(float* x_g, const float* const* deltas, const float* w, int32_t W,
+                                      int32_t rows, int32_t cols, float* momentum, float mu, int32_t nesterov,
+                                      float server_lr, int32_t steps, const float* coeff, float eps,
+                                      void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * oscars_quantize_i8 - rows in 8 bits with a scale each: the tokens (samples)
+ * of a layer's input, or the output channels of its weight matrix.
+ *   scale[i] = max_j |x[i][j]| / 127;  q[i][j] = x[i][j] / scale[i], rounded to
+ * fp32 and then to the nearest integer (ties to even), within [-127, 127].
+ * x: device, element (i, j) at x[i ldx + j], of `dtype`, any alignment.  q:
+ * device int8, element (i, j) at q[i ldq + j], any alignment; bytes past
+ * column cols of a row are left as they were.  scale: device, rows floats.  A
+ * row of zeros, or whose scale underflows to zero, has scale 0 and codes 0.  A
+ * row that holds an infinity or NaN has that (NaN first) for its scale and codes
+ * 0, so that its products are NaN.  rows = 0 does nothing.  Ordered on `stream`.
+ * Errors: EINVAL (NULL pointers, x or scale not aligned to its elements, rows
+ * < 0, cols < 1, ldx or ldq < cols), ECUDA.
+ */
+oscars_status oscars_quantize_i8(const void* x, int64_t ldx, int32_t dtype, int32_t rows, int32_t cols, int8_t* q,
+                                 int64_t ldq, float* scale, void* stream);
+
+/*
+ * oscars_gemm_i8_nt - the product of a dense layer kept in 8 bits,
+ *   C[m][n] = act(scale_a[m] scale_b[n] sum_k A[m][k] B[n][k] + bias[n]),
+ * with the sum exact in 32-bit integers.  A: device int8, row m (a token) at
+ * A + m lda; B: device int8, row n (an output channel) at B + n ldb; both
+ * 16-byte aligned with lda and ldb multiples of 16 (bytes past column K are not
+ * used).  scale_a [M], scale_b [N]: device fp32.  bias: device, N fp32, or NULL.
+ * relu != 0: act = max(0, .) (NaN stays), else none.  C: device, element (m, n) at
+ * C[m ldc + n], of `dtype`, any alignment; scale, bias and act are fp32, rounded
+ * once.  M = 0 (no tokens) does nothing; 1 <= N; 1 <= K <= 131071 (the sum of
+ * products of -128 stays within 32 bits).  Ordered on `stream`; allocates
+ * nothing.
+ * Errors: EINVAL (NULL or misaligned pointers, sizes or strides out of range),
+ * ECUDA.
+ */
+oscars_status oscars_gemm_i8_nt(const int8_t* A, int64_t lda, const float* scale_a, const int8_t* B, int64_t ldb,
+                                const float* scale_b, const float* bias, int32_t relu, void* C, int64_t ldc,
+                                int32_t dtype, int32_t M, int32_t N, int32_t K, void* stream);
 
 #ifdef __cplusplus
 }

@@ -17,6 +17,7 @@ LIB_PATH = os.path.join(HERE, "_lib", "liboscars.so")
 
 OSCARS_OK, OSCARS_EINVAL, OSCARS_ENOMEM, OSCARS_ECUDA, OSCARS_ESTATE, OSCARS_ETIMEOUT, OSCARS_ENOTSUP = range(7)
 MODEL_FLAT, MODEL_MLP, MODEL_CNN = 0, 1, 2
+F32, BF16 = 0, 1
 W_UNIFORM, W_LOCALSTEPS, W_EXPLICIT = 0, 1, 2
 SEARCH_CAPPED, SEARCH_LITERAL = 0, 1
 POLICY_OSCARS, POLICY_BSP, POLICY_LOCAL_SGD = 0, 1, 2
@@ -87,6 +88,17 @@ _SIGS = {
                                         POINTER(c_int32)]),
     "oscars_train": (c_int32, [c_void_p, c_int32, c_void_p, c_void_p, c_int64, c_float, POINTER(OscarsRoundLog),
                                POINTER(c_int32)]),
+    "oscars_orthogonalize_workspace": (c_int32, [c_int32, c_int32, c_int32, c_int32, POINTER(c_int64)]),
+    "oscars_orthogonalize": (c_int32, [c_void_p, c_int64, c_int64, c_void_p, c_int64, c_int64, c_int32, c_int32, c_int32,
+                                       c_int32, c_int32, POINTER(c_float), c_float, c_float, c_void_p, c_int64, c_void_p]),
+    "oscars_merge_orthogonal_workspace": (c_int32, [c_int32, c_int32, POINTER(c_int64)]),
+    "oscars_merge_orthogonal": (c_int32, [c_void_p, POINTER(c_void_p), POINTER(c_float), c_int32, c_int32, c_int32,
+                                          c_void_p, c_float, c_int32, c_float, c_int32, POINTER(c_float), c_float,
+                                          c_void_p, c_int64, c_void_p]),
+    "oscars_quantize_i8": (c_int32, [c_void_p, c_int64, c_int32, c_int32, c_int32, c_void_p, c_int64, c_void_p,
+                                     c_void_p]),
+    "oscars_gemm_i8_nt": (c_int32, [c_void_p, c_int64, c_void_p, c_void_p, c_int64, c_void_p, c_void_p, c_int32, c_void_p,
+                                    c_int64, c_int32, c_int32, c_int32, c_int32, c_void_p]),
     "oscars_merge": (c_int32, [c_void_p, POINTER(c_void_p), POINTER(c_float), c_int32, c_int64, c_float, c_void_p]),
 }
 
@@ -291,6 +303,64 @@ def oscars_check_wait_timeout(ctx: int, polls: int):
 def oscars_gemm_bf16_nt(a_ptr: int, b_ptr: int, c_ptr: int, M: int, N: int, K: int, stream: Optional[int] = None):
     _check(lib().oscars_gemm_bf16_nt(c_void_p(a_ptr), c_void_p(b_ptr), c_void_p(c_ptr), M, N, K,
                                      c_void_p(stream or 0)))
+
+
+def oscars_orthogonalize_workspace(batch: int, rows: int, cols: int, dtype: int) -> int:
+    """Bytes of workspace that oscars_orthogonalize wants for these sizes."""
+    out = c_int64()
+    _check(lib().oscars_orthogonalize_workspace(batch, rows, cols, dtype, ctypes.byref(out)))
+    return out.value
+
+
+def oscars_orthogonalize(g_ptr: int, ldg: int, batch_stride_g: int, o_ptr: int, ldo: int, batch_stride_o: int, batch: int,
+                         rows: int, cols: int, dtype: int, steps: int, workspace_ptr: int, workspace_bytes: int,
+                         coeff: Optional[Sequence[float]] = None, eps: float = 1e-7, scale: float = 1.0,
+                         stream: Optional[int] = None):
+    """Newton-Schulz steps on a batch of matrices (strides in elements)."""
+    _check(lib().oscars_orthogonalize(g_ptr, ldg, batch_stride_g, o_ptr, ldo, batch_stride_o, batch, rows, cols, dtype, steps,
+                                      _coeff(coeff), eps, scale, workspace_ptr, workspace_bytes, stream))
+
+
+def oscars_merge_orthogonal_workspace(rows: int, cols: int) -> int:
+    """Bytes of workspace that oscars_merge_orthogonal wants for these sizes."""
+    out = c_int64()
+    _check(lib().oscars_merge_orthogonal_workspace(rows, cols, ctypes.byref(out)))
+    return out.value
+
+
+def oscars_merge_orthogonal(x_g_ptr: int, delta_ptrs: Sequence[int], w: Sequence[float], rows: int, cols: int,
+                            momentum_ptr: Optional[int], mu: float, nesterov: bool, server_lr: float, steps: int,
+                            workspace_ptr: int, workspace_bytes: int, coeff: Optional[Sequence[float]] = None,
+                            eps: float = 1e-7, stream: Optional[int] = None):
+    """Merge deltas into the momentum, orthogonalise it, apply it to x_g."""
+    W = len(delta_ptrs)
+    if len(w) != W:
+        raise OscarsError(OSCARS_EINVAL, "one weight for each delta")
+    _check(lib().oscars_merge_orthogonal(x_g_ptr, _arr(c_void_p, delta_ptrs), _arr(c_float, w), W, rows, cols, momentum_ptr,
+                                         mu, int(nesterov), server_lr, steps, _coeff(coeff), eps, workspace_ptr,
+                                         workspace_bytes, stream))
+
+
+def _coeff(coeff):
+    if coeff is None:
+        return None
+    if len(coeff) != 3:
+        raise OscarsError(OSCARS_EINVAL, "three coefficients")
+    return (c_float * 3)(*coeff)
+
+
+def oscars_quantize_i8(x_ptr: int, ldx: int, dtype: int, rows: int, cols: int, q_ptr: int, ldq: int, scale_ptr: int,
+                       stream: Optional[int] = None):
+    """Rows in 8 bits with a scale each (strides in elements)."""
+    _check(lib().oscars_quantize_i8(x_ptr, ldx, dtype, rows, cols, q_ptr, ldq, scale_ptr, stream))
+
+
+def oscars_gemm_i8_nt(a_ptr: int, lda: int, scale_a_ptr: int, b_ptr: int, ldb: int, scale_b_ptr: int, c_ptr: int, ldc: int,
+                      dtype: int, M: int, N: int, K: int, bias_ptr: Optional[int] = None, relu: bool = False,
+                      stream: Optional[int] = None):
+    """8-bit product with scales, bias and ReLU (strides in elements)."""
+    _check(lib().oscars_gemm_i8_nt(a_ptr, lda, scale_a_ptr, b_ptr, ldb, scale_b_ptr, bias_ptr, int(relu), c_ptr, ldc, dtype,
+                                   M, N, K, stream))
 
 
 def oscars_profile_read(ctx: int):

@@ -55,6 +55,10 @@ EncodeTiledFn encode_fn() {
   return fn.load(std::memory_order_relaxed);
 }
 
+}  // namespace
+
+namespace oscars {
+
 // One tensor map.  A host thread that has made no CUDA call yet has no context
 // bound, which the driver's encoder wants (the runtime's calls bind it
 // themselves): bind the device's primary one then.
@@ -74,6 +78,10 @@ bool encode_map(CUtensorMap* m, CUtensorMapDataType type, uint32_t rank, const v
   }
   return r == CUDA_SUCCESS;
 }
+
+}  // namespace oscars
+
+namespace {
 
 // 3-D bf16 tensor map: element (x, y, z) at base + z*stride_z + y*stride_y +
 // 2x bytes; boxes of 64 (x) by box_y rows, 128-byte swizzle, zero fill

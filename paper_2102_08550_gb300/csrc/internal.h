@@ -36,6 +36,11 @@ constexpr int kMaxWorkersMLP = 64;
 constexpr int kMaxClasses = 32;
 constexpr int kRowsPerLossChunk = 16;   // rows per loss partial in the head kernel
 
+// Tiled tensor map of up to 4 dimensions (strides of dimensions 1.. in bytes),
+// zero fill outside the extents; false if the driver refuses it (csrc/capi.cu).
+bool encode_map(CUtensorMap* m, CUtensorMapDataType type, uint32_t rank, const void* base, const cuuint64_t* dims,
+                const cuuint64_t* strides, const cuuint32_t* box, CUtensorMapSwizzle swz);
+
 // ---------------------------------------------------------------- merge
 struct MergeArgs {
   const float* src[kMaxMergeWorkers];  // delta_k, or replica x^k
