@@ -3,6 +3,7 @@
 
 #include <cuda.h>
 #include <cuda_bf16.h>
+#include <cuda_fp16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
 
@@ -217,6 +218,36 @@ RowsPlan gemm_rows_plan(int epi, int M, int N, int K);
 // with 128-byte swizzle
 cudaError_t launch_gemm_rows(int epi, const RowsPlan& p, const CUtensorMap& mA, const CUtensorMap& mB,
                              const CUtensorMap& mD, RowsArgs a, cudaStream_t s);
+
+// The products of a Newton-Schulz step (csrc/orth_product.cu).  Operands are fp16,
+// [half][batch][rows][ld]: one half, or two whose sum is the value.
+enum NsEpi {
+  kNsGram,     // D = A = X X^T or X^T X, symmetric: the tiles of one triangle and their mirror images
+  kNsSquare,   // D = a I + b A + c A A, the same
+  kNsStep,     // D = the next X, two halves
+  kNsLast      // the last step's X, times a, to `out`
+};
+enum NsOut { kNsF32, kNsBf16, kNsAdd };   // kNsAdd: out += a X, fp32
+// values are stored times these, which keeps the second half out of fp16's subnormal range
+constexpr float kNsScaleX = 1024.f, kNsScaleA = 256.f;
+struct NsArgs {
+  int batch, M, N, K;
+  int a_halves, b_halves;        // of the operands
+  int a_mn, b_mn;                // read MN-major (the transposed tensor)
+  int d_halves;                  // of D
+  __half* D;                     // kNsGram, kNsSquare: mirror images are written through this
+  const __half* Y;               // kNsSquare: A
+  int64_t ld, z, half;           // strides of D and Y in elements
+  float a, b, c;
+  void* out;                     // kNsLast
+  int64_t ldo, zo;
+  int out_type;                  // NsOut
+  int BN, stages, mt, nt, units; // set by the launcher
+};
+// mA, mB: the operands, boxes {64, 64, 1, 1} (inner, row, batch, half), 128-byte
+// swizzle; mD: D, boxes {32, 32, 1, 1}, 64-byte swizzle
+cudaError_t launch_ns_product(int epi, const CUtensorMap& mA, const CUtensorMap& mB, const CUtensorMap& mD, NsArgs a,
+                              cudaStream_t s);
 
 // Weight gradient + SGD of up to kDwMaxLayers hidden layers, persistent
 // (csrc/gemm_dw.cu): W[wid] = W[src] - lr * G^T X over the batch, its bf16

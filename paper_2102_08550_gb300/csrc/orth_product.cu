@@ -1,0 +1,548 @@
+// The three products of a Newton-Schulz step on the 5th-generation tensor cores
+// (tcgen05, sm_103a), for a batch of matrices in one launch:
+//
+//   kNsGram    A = X X^T (X K-major) or X^T X (X read MN-major)
+//   kNsSquare  B = a I + b A + c A A
+//   kNsStep    X <- B X (X read MN-major) or X B
+//   kNsLast    the same into the caller's matrix
+//
+// Precision.  tcgen05 multiplies 16-bit operands; a value is kept as one fp16 (11
+// bits) or as two whose sum has 22, and a product of values in two halves takes
+// three products, high x high, high x low and low x high (the fourth is below
+// fp32's last bit), into one fp32 accumulator.  fp32 results take two halves of
+// everything.  bf16 results take two halves of X and one of A and B: what X's
+// rounding leaves in the directions in which the update is near zero is
+// multiplied by a at every step (485 over five), while the roundings of A and B
+// multiply X and stay relative to it.  fp16 rather than bf16: three more bits at
+// the same rate, and the values are bounded (singular values below 2).
+//
+// The tensor core cuts what an addition to its accumulator leaves below fp32's last
+// bit.  Over 4096 products in three passes of 256 additions each that is a loss of
+// 1e-5 of a sum of squares, so for fp32 results the accumulator takes kChunk K-blocks
+// at a time, and the epilogue adds it, rounded to nearest, to a sum in registers.
+//
+// A and B are symmetric: only tiles on and above the diagonal are computed, and
+// the epilogue writes each tile and its mirror image, half the work of two of the
+// three products.
+//
+// Structure: persistent, one CTA per SM or a cluster of two (cta_group::2, a tile
+// of 256 x BN) striding over tiles; warp 0 lane 0 streams K-blocks of 64 by TMA
+// (128-byte swizzle), warp 1 issues into one of two TMEM accumulators, warps 4-11
+// (half of a tile's columns each group of four) run the epilogue of a tile, or the
+// sum of a chunk, under the products of the next.
+#include <atomic>
+
+#include "common.cuh"
+#include "internal.h"
+
+namespace oscars {
+
+namespace {
+
+constexpr int kK = 64, kThreads = 384, kMaxBN = 256, kMaxStages = 8;
+constexpr int kChunk = 2;                          // K-blocks of one accumulation of an fp32 result
+constexpr int kEpiWarps = 8;
+constexpr int kBox = 64 * 128;                     // one operand box: 64 rows of 128 bytes
+constexpr int kStg = 2048;                         // one staging box: 32 rows x 64 bytes
+constexpr int kStgBytes = kEpiWarps * 2 * kStg;    // two per epilogue warp
+constexpr int kBarBytes = 256;
+constexpr int kSmem = 227 * 1024;
+constexpr int kRing = kSmem - 1024 - kBarBytes - kStgBytes;
+// at least: one CTA an SM, and no other kernel's cluster beside it (tensor memory)
+constexpr size_t kLeast = 164 * 1024;
+static_assert(no_cluster_beside(kLeast), "no other cluster's CTA beside this kernel's");
+
+struct Bars {
+  uint64_t full[kMaxStages], empty[kMaxStages], accf[2], acce[2];
+  uint32_t tmem;
+};
+static_assert(sizeof(Bars) <= kBarBytes, "barriers fit");
+
+constexpr uint32_t kLeaderMask = 0xFEFFFFFFu;   // a pair's barrier of the leader at the same offset
+__device__ __forceinline__ void tma_load_4d_pair(void* smem_dst, const CUtensorMap* map, int c0, int c1, int c2, int c3,
+                                                 uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(smem_u32(smem_dst)),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(smem_u32(bar) & kLeaderMask)
+      : "memory");
+}
+// kind::f16 takes its operands' type from the instruction descriptor
+__device__ __forceinline__ void umma_f16_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
+                                              uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void umma_commit_pair(uint64_t* bar) {
+  asm volatile(
+      "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(
+          smem_u32(bar)),
+      "h"(static_cast<uint16_t>(0x3))
+      : "memory");
+}
+__device__ __forceinline__ void mbar_arrive_at(uint32_t cluster_bar) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+}
+// fp16 operands (format 0), fp32 accumulator; bits 15 and 16: A, B MN-major
+__host__ __device__ constexpr uint32_t idesc_f16(int M, int N, int a_mn, int b_mn) {
+  return (1u << 4) | (static_cast<uint32_t>(a_mn) << 15) | (static_cast<uint32_t>(b_mn) << 16) |
+         (static_cast<uint32_t>(N >> 3) << 17) | (static_cast<uint32_t>(M >> 4) << 24);
+}
+
+// tile of a work unit: the matrix, and row and column tile (i <= j on a triangle)
+struct Tile {
+  int z, i, j;
+};
+template <int CL, bool kSym>
+__device__ __forceinline__ Tile tile_of(const NsArgs& a, int u) {
+  Tile t;
+  if (kSym) {
+    const int per = a.nt * (a.nt + 1) / 2;
+    t.z = u / per;
+    int r = u - t.z * per;
+    t.i = 0;
+    while (r >= a.nt - t.i) r -= a.nt - t.i++;
+    t.j = t.i + r;
+  } else {
+    const int mu = a.mt / CL, per = mu * a.nt;
+    t.z = u / per;
+    const int r = u - t.z * per;
+    t.j = r / mu;   // rows fastest
+    t.i = r - t.j * mu;
+  }
+  return t;
+}
+
+__device__ __forceinline__ uint32_t pack_half2(__half lo, __half hi) {
+  const __half2 v = __halves2half2(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+template <int EPI, int CL, bool kSums>
+__global__ void __launch_bounds__(kThreads, 1) ns_product_kernel(const __grid_constant__ CUtensorMap mapA,
+                                                                 const __grid_constant__ CUtensorMap mapB,
+                                                                 const __grid_constant__ CUtensorMap mapD,
+                                                                 const __grid_constant__ NsArgs a) {
+  constexpr bool kSym = EPI == kNsGram || EPI == kNsSquare;
+  extern __shared__ uint8_t ns_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(ns_raw) + 1023) & ~uintptr_t(1023));
+  uint8_t* stg = smem;
+  uint8_t* ring = smem + kStgBytes;   // [stages][A: halves x 2 boxes | B: halves x BN / CL / 64 boxes]
+  const int b_boxes = a.BN / CL / 64, b_half = b_boxes * kBox;
+  const int a_bytes = a.a_halves * 2 * kBox, stage_bytes = a_bytes + a.b_halves * b_half;
+  Bars* bars = reinterpret_cast<Bars*>(ring + a.stages * stage_bytes);
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+  const int rank = CL > 1 ? static_cast<int>(cluster_ctarank()) : 0;
+  const int nk = (a.K + kK - 1) / kK;
+  const int chunk = kSums ? kChunk : nk;   // K-blocks of one accumulation
+  const int u0 = blockIdx.x / CL, ustep = gridDim.x / CL;
+
+  if (threadIdx.x == 0) {
+    prefetch_tmap(&mapA);
+    prefetch_tmap(&mapB);
+    if (EPI != kNsLast) prefetch_tmap(&mapD);
+    for (int i = 0; i < a.stages; ++i) {
+      mbar_init(&bars->full[i], 1);
+      mbar_init(&bars->empty[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&bars->accf[i], 1);
+      mbar_init(&bars->acce[i], kEpiWarps * CL);
+    }
+    fence_barrier_init();
+    fence_proxy_async_smem();
+  }
+  if (warp == 2) {
+    if (CL == 1) {
+      tmem_alloc(&bars->tmem, 512);
+      tmem_relinquish();
+    } else {
+      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars->tmem)), "r"(512)
+                   : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+  }
+  tc_fence_before();
+  if (CL > 1) cluster_sync();   // the peer's barriers are initialised before anything arrives on them
+  else __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = bars->tmem;
+  pdl_wait();
+  pdl_trigger();
+
+  if (warp == 0 && lane == 0) {
+    // ---- TMA producer
+    int it = 0, s = 0, ph = 1, armed = 0;
+    bool ok = true;
+    for (int u = u0; ok && u < a.units; u += ustep) {
+      const Tile t = tile_of<CL, kSym>(a, u);
+      const int m0 = (t.i * CL + rank) * 128, n0 = t.j * a.BN + rank * (a.BN / CL);
+      for (int kb = 0; kb < nk; ++kb, ++it) {
+        if (it >= a.stages && !(ok = mbar_wait(&bars->empty[s], ph, nullptr, kDevTimeoutEmpty))) break;
+        uint8_t* at = ring + s * stage_bytes;
+        if (rank == 0) mbar_arrive_expect_tx(&bars->full[s], CL * stage_bytes);   // a pair's bytes count on the leader's
+        armed = it + 1;
+        auto load = [&](const CUtensorMap* map, int mn, int row0, int half) {
+          const int c0 = mn ? row0 : kb * kK, c1 = mn ? kb * kK : row0;
+          if (CL > 1) tma_load_4d_pair(at, map, c0, c1, t.z, half, &bars->full[s]);
+          else tma_load_4d(at, map, c0, c1, t.z, half, &bars->full[s]);
+          at += kBox;
+        };
+        for (int h = 0; h < a.a_halves; ++h)
+          for (int b = 0; b < 2; ++b) load(&mapA, a.a_mn, m0 + 64 * b, h);
+        for (int h = 0; h < a.b_halves; ++h)
+          for (int b = 0; b < b_boxes; ++b) load(&mapB, a.b_mn, n0 + 64 * b, h);
+        if (++s == a.stages) {
+          s = 0;
+          ph ^= 1;
+        }
+      }
+    }
+    // no copy, and no commit of the leader, may still be on its way when this CTA ends
+    for (int i = armed > a.stages ? armed - a.stages : 0; i < armed; ++i) {
+      if (rank == 0) mbar_wait(&bars->full[i % a.stages], (i / a.stages) & 1, nullptr, kDevTimeoutFull);
+      if (!mbar_wait(&bars->empty[i % a.stages], (i / a.stages) & 1, nullptr, kDevTimeoutEmpty)) break;
+    }
+  } else if (warp == 1 && rank == 0) {
+    // ---- MMA issuer (the leader's, of a pair); the warp stays converged and one elected lane issues
+    const uint32_t idesc = idesc_f16(128 * CL, a.BN, a.a_mn, a.b_mn);
+    const uint32_t ring0 = smem_u32(ring);
+    const uint64_t astep = a.a_mn ? 128 : 2, bstep = a.b_mn ? 128 : 2;   // 16 of K in the address field
+    const uint64_t alo = 2 * kBox >> 4, blo = b_half >> 4;               // from the first half to the second
+    int s = 0, ph = 0, t = 0;   // t: accumulations begun
+    uint32_t limit = kSpinLimit;
+    for (int u = u0; u < a.units; u += ustep) {
+      for (int k0 = 0; k0 < nk; k0 += chunk, ++t) {
+        const int b = t & 1, k1 = k0 + chunk < nk ? k0 + chunk : nk;
+        if (t >= 2) mbar_wait_keep(limit, &bars->acce[b], ((t >> 1) + 1) & 1, nullptr, kDevTimeoutAccum);
+        tc_fence_after();
+        const uint32_t acc = tmem + static_cast<uint32_t>(b * kMaxBN);
+        for (int kb = k0; kb < k1; ++kb) {
+          mbar_wait_keep(limit, &bars->full[s], ph, nullptr, kDevTimeoutFull);
+          tc_fence_after();
+          const uint32_t at = ring0 + s * stage_bytes;
+          const uint64_t ad = a.a_mn ? smem_desc_mn128(at, kBox) : smem_desc_k128(at);
+          const uint64_t bd = a.b_mn ? smem_desc_mn128(at + a_bytes, kBox) : smem_desc_k128(at + a_bytes);
+          if (elect_one() && limit > 1) {
+            uint32_t more = kb == k0 ? 0u : 1u;
+            auto issue = [&](uint64_t x, uint64_t y) {
+#pragma unroll
+              for (int j = 0; j < kK / 16; ++j) {
+                if (CL > 1) umma_f16_pair(acc, x + j * astep, y + j * bstep, idesc, more);
+                else umma_bf16(acc, x + j * astep, y + j * bstep, idesc, more);
+                more = 1u;
+              }
+            };
+            if (a.b_halves == 2) issue(ad, bd + blo);
+            if (a.a_halves == 2) issue(ad + alo, bd);
+            issue(ad, bd);
+            if (CL > 1) umma_commit_pair(&bars->empty[s]);
+            else umma_commit(&bars->empty[s]);
+          }
+          __syncwarp();
+          if (++s == a.stages) {
+            s = 0;
+            ph ^= 1;
+          }
+        }
+        if (elect_one() && limit > 1) {
+          if (CL > 1) umma_commit_pair(&bars->accf[b]);
+          else umma_commit(&bars->accf[b]);
+        }
+        __syncwarp();
+      }
+    }
+  } else if (warp >= 4) {
+    // ---- epilogue: thread = one accumulator row and half of its columns
+    const int quarter = warp & 3, span = a.BN / 2, cb = (warp >> 2) == 1 ? 0 : span;
+    uint8_t* my = stg + (warp - 4) * 2 * kStg;
+    int t = 0;
+    // the accumulator may be written again (by accumulation t + 2)
+    auto release = [&](int b) {
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) {
+        if (CL > 1) mbar_arrive_at(cluster_addr(&bars->acce[b], 0));
+        else mbar_arrive(&bars->acce[b]);
+      }
+    };
+    for (int u = u0; u < a.units; u += ustep) {
+      const Tile tl = tile_of<CL, kSym>(a, u);
+      const int m0 = (tl.i * CL + rank) * 128 + 32 * quarter, n0 = tl.j * a.BN + cb;
+      const int r = m0 + lane;
+      const uint32_t row0 = tmem + (static_cast<uint32_t>(32 * quarter) << 16) + cb;
+      // 32 columns from column c0 on
+      auto finish = [&](int c0, const float (&v)[32]) {
+        if constexpr (EPI != kNsLast) {
+          const float scale = EPI == kNsGram ? kNsScaleA / (kNsScaleX * kNsScaleX)
+                              : EPI == kNsSquare ? a.c / kNsScaleA : 1.f / kNsScaleA;
+          if (lane == 0) bulk_wait_read_all();   // the last stores have read the boxes
+          __syncwarp();
+          __half* mirror = a.D + tl.z * a.z + static_cast<int64_t>(n0 + c0) * a.ld + r;
+          const __half* y = a.Y + tl.z * a.z + static_cast<int64_t>(r) * a.ld + n0 + c0;
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            __half hi[8], lo[8];
+            const int col = n0 + c0 + 8 * q;
+            float f[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[e] = v[8 * q + e] * scale;
+            if (EPI == kNsSquare && r < a.M && col < a.N) {   // + b A + a I; a row's 8 columns lie within its stride
+              for (int g = 0; g < a.d_halves; ++g) {
+                const uint4 w = *reinterpret_cast<const uint4*>(y + g * a.half + 8 * q);
+                const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  const float2 p = __half22float2(*reinterpret_cast<const __half2*>(&ws[e]));
+                  f[2 * e] = fmaf(a.b, p.x, f[2 * e]);
+                  f[2 * e + 1] = fmaf(a.b, p.y, f[2 * e + 1]);
+                }
+              }
+#pragma unroll
+              for (int e = 0; e < 8; ++e)
+                if (col + e == r) f[e] += a.a * kNsScaleA;
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              hi[e] = __float2half_rn(f[e]);
+              lo[e] = __float2half_rn(f[e] - __half2float(hi[e]));
+            }
+            const int swz = (q ^ ((lane >> 1) & 3)) << 4;
+            *reinterpret_cast<uint4*>(my + lane * 64 + swz) = make_uint4(
+                pack_half2(hi[0], hi[1]), pack_half2(hi[2], hi[3]), pack_half2(hi[4], hi[5]), pack_half2(hi[6], hi[7]));
+            if (a.d_halves == 2)
+              *reinterpret_cast<uint4*>(my + kStg + lane * 64 + swz) = make_uint4(
+                  pack_half2(lo[0], lo[1]), pack_half2(lo[2], lo[3]), pack_half2(lo[4], lo[5]), pack_half2(lo[6], lo[7]));
+            if (kSym && tl.i != tl.j && r < a.M) {   // the mirror image: a column's 32 rows are 64 bytes
+#pragma unroll
+              for (int e = 0; e < 8; ++e)
+                if (col + e < a.N) {
+                  mirror[static_cast<int64_t>(8 * q + e) * a.ld] = hi[e];
+                  if (a.d_halves == 2) mirror[a.half + static_cast<int64_t>(8 * q + e) * a.ld] = lo[e];
+                }
+            }
+          }
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0 && m0 < a.M) {
+            tma_store_4d(&mapD, my, n0 + c0, m0, tl.z, 0);
+            if (a.d_halves == 2) tma_store_4d(&mapD, my + kStg, n0 + c0, m0, tl.z, 1);
+            bulk_commit_group();
+          }
+        } else {
+          const float scale = a.a / (kNsScaleA * kNsScaleX);
+#pragma unroll
+          for (int q = 0; q < 8; ++q)
+            *reinterpret_cast<float4*>(my + lane * 128 + ((q ^ (lane & 7)) << 4)) =
+                make_float4(v[4 * q] * scale, v[4 * q + 1] * scale, v[4 * q + 2] * scale, v[4 * q + 3] * scale);
+          __syncwarp();
+          // rows of 32 columns, coalesced whatever the caller's alignment
+          const int col = n0 + c0 + lane;
+          const int64_t at0 = tl.z * a.zo + col;
+          const int rows = a.M - m0 < 32 ? a.M - m0 : 32;
+          if (col < a.N) {
+            for (int i0 = 0; i0 < rows; i0 += 8) {
+              float x[8];
+#pragma unroll
+              for (int i = 0; i < 8; ++i) {
+                const int rr = i0 + i;
+                x[i] = *reinterpret_cast<const float*>(my + rr * 128 + (((lane >> 2) ^ (rr & 7)) << 4) + (lane & 3) * 4);
+              }
+              if (a.out_type == kNsAdd) {
+                const float* o = static_cast<const float*>(a.out);
+                float old[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                  old[i] = i0 + i < rows ? o[at0 + static_cast<int64_t>(m0 + i0 + i) * a.ldo] : 0.f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] += old[i];
+              }
+#pragma unroll
+              for (int i = 0; i < 8; ++i) {
+                if (i0 + i >= rows) continue;
+                const int64_t at = at0 + static_cast<int64_t>(m0 + i0 + i) * a.ldo;
+                if (a.out_type == kNsBf16) static_cast<__nv_bfloat16*>(a.out)[at] = __float2bfloat16_rn(x[i]);
+                else static_cast<float*>(a.out)[at] = x[i];
+              }
+            }
+          }
+          __syncwarp();
+        }
+      };
+      if constexpr (kSums) {
+        float sum[kMaxBN / 64][32];
+#pragma unroll
+        for (int g = 0; g < kMaxBN / 64; ++g)
+#pragma unroll
+          for (int e = 0; e < 32; ++e) sum[g][e] = 0.f;
+        bool ok = true;
+        for (int k0 = 0; k0 < nk; k0 += chunk, ++t) {
+          const int b = t & 1;
+          if (!(ok = mbar_wait_warp(&bars->accf[b], (t >> 1) & 1, nullptr, kDevTimeoutAccum))) break;
+          tc_fence_after();
+#pragma unroll
+          for (int g = 0; g < kMaxBN / 64; ++g)
+            if (32 * g < span) {
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                float v[16];
+                tmem_ld_32x32b_x16(row0 + b * kMaxBN + 32 * g + 16 * h, v);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) sum[g][16 * h + e] += v[e];
+              }
+            }
+          release(b);
+        }
+        if (!ok) break;
+#pragma unroll
+        for (int g = 0; g < kMaxBN / 64; ++g)
+          if (32 * g < span && n0 + 32 * g < a.N) finish(32 * g, sum[g]);
+      } else {
+        const int b = t & 1;
+        if (!mbar_wait_warp(&bars->accf[b], (t >> 1) & 1, nullptr, kDevTimeoutAccum)) break;
+        tc_fence_after();
+        for (int c0 = 0; c0 < span && n0 + c0 < a.N; c0 += 32) {
+          float v[32];
+          tmem_ld_32x32b_x32(row0 + b * kMaxBN + c0, v);
+          finish(c0, v);
+        }
+        release(b);
+        ++t;
+      }
+    }
+    if (lane == 0) bulk_wait_all();
+  }
+  tc_fence_before();
+  if (CL > 1) cluster_sync();   // the pair's products and arrivals are done in both CTAs
+  else __syncthreads();
+  if (warp == 2) {
+    tc_fence_after();
+    if (CL == 1) tmem_dealloc(tmem, 512);
+    else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+  }
+}
+
+constexpr int kMaxDevices = 64;
+struct DevInfo {
+  std::atomic<int> sms{0}, pairs{0};
+};
+DevInfo g_dev[kMaxDevices];
+
+int stage_bytes(const NsArgs& a, int BN, int cl) { return (a.a_halves * 2 + a.b_halves * (BN / cl / 64)) * kBox; }
+int stages_of(const NsArgs& a, int BN, int cl) {
+  const int nk = (a.K + kK - 1) / kK;
+  int st = kRing / stage_bytes(a, BN, cl);
+  st = st > kMaxStages ? kMaxStages : st;
+  return st > nk ? (nk < 2 ? 2 : nk) : st;
+}
+
+template <int CL>
+cudaLaunchConfig_t config(cudaLaunchAttribute* attr, int grid, size_t smem, cudaStream_t s) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid, 1, 1);
+  cfg.blockDim = dim3(kThreads, 1, 1);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cfg.attrs = attr;
+  cfg.numAttrs = 0;
+  if (CL > 1) {
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = CL;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cfg.numAttrs = 1;
+  }
+  return cfg;
+}
+
+// {SMs, resident clusters of two} of the current device, queried once
+void device_room(int& sms, int& pairs) {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) dev = 0;
+  sms = g_dev[dev].sms.load(std::memory_order_relaxed);
+  pairs = g_dev[dev].pairs.load(std::memory_order_relaxed);
+  if (sms > 0 && pairs > 0) return;
+  if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || sms < 1) sms = 1;
+  cudaLaunchAttribute attr[1];
+  pairs = 0;
+  if (allow_smem(ns_product_kernel<kNsStep, 2, true>, kSmem) == cudaSuccess) {
+    cudaLaunchConfig_t cfg = config<2>(attr, 2, kSmem, nullptr);
+    if (cudaOccupancyMaxActiveClusters(&pairs, ns_product_kernel<kNsStep, 2, true>, &cfg) != cudaSuccess) pairs = 0;
+  }
+  cudaGetLastError();
+  if (pairs < 1) pairs = 1;
+  g_dev[dev].sms.store(sms, std::memory_order_relaxed);
+  g_dev[dev].pairs.store(pairs, std::memory_order_relaxed);
+}
+
+template <int EPI, int CL, bool kSums>
+cudaError_t launch_t(const CUtensorMap& mA, const CUtensorMap& mB, const CUtensorMap& mD, const NsArgs& a, int grid,
+                     cudaStream_t s) {
+  size_t smem = 1024 + kStgBytes + static_cast<size_t>(a.stages) * stage_bytes(a, a.BN, CL) + kBarBytes;
+  if (smem < kLeast) smem = kLeast;
+  cudaError_t e = allow_smem(ns_product_kernel<EPI, CL, kSums>, kSmem);
+  if (e != cudaSuccess) return e;
+  cudaLaunchAttribute attr[2];
+  cudaLaunchConfig_t cfg = config<CL>(attr, grid, smem, s);
+  attr[cfg.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[cfg.numAttrs].val.programmaticStreamSerializationAllowed = 1;
+  ++cfg.numAttrs;
+  return cudaLaunchKernelEx(&cfg, ns_product_kernel<EPI, CL, kSums>, mA, mB, mD, a);
+}
+
+template <int EPI>
+cudaError_t launch_e(int cl, const CUtensorMap& mA, const CUtensorMap& mB, const CUtensorMap& mD, const NsArgs& a, int grid,
+                     cudaStream_t s) {
+  if (a.a_halves + a.b_halves == 4)
+    return cl == 2 ? launch_t<EPI, 2, true>(mA, mB, mD, a, grid, s) : launch_t<EPI, 1, true>(mA, mB, mD, a, grid, s);
+  return cl == 2 ? launch_t<EPI, 2, false>(mA, mB, mD, a, grid, s) : launch_t<EPI, 1, false>(mA, mB, mD, a, grid, s);
+}
+
+}  // namespace
+
+cudaError_t launch_ns_product(int epi, const CUtensorMap& mA, const CUtensorMap& mB, const CUtensorMap& mD, NsArgs a,
+                              cudaStream_t s) {
+  int sms, pairs;
+  device_room(sms, pairs);
+  const bool sym = epi == kNsGram || epi == kNsSquare;
+  const int nk = (a.K + kK - 1) / kK, products = a.a_halves + a.b_halves - 1;
+  // The shape with the least estimated time: waves of tiles times the longer of a
+  // tile's products (2 BN clocks a K-block and product) and loads (60 bytes a clock
+  // into an SM), plus a tile's and a launch's fixed part.  Triangles take square tiles.
+  double best = 0.0;
+  int cl = 1;
+  for (int c = 1; c <= 2; ++c) {
+    const int mt = ((a.M + 127) / 128 + c - 1) / c * c;
+    for (int bn = 64; bn <= kMaxBN; bn += 64) {
+      if ((c == 2 && bn % 128) || (sym && bn != 128 * c)) continue;
+      const int nt = (a.N + bn - 1) / bn;
+      const int64_t units = static_cast<int64_t>(a.batch) * (sym ? nt * static_cast<int64_t>(nt + 1) / 2 : static_cast<int64_t>(mt / c) * nt);
+      const int room = c == 2 ? pairs : sms;
+      const double waves = static_cast<double>((units + room - 1) / room);
+      const double mma = 2.0 * bn * products, load = stage_bytes(a, bn, c) / 60.0;
+      const double cost = waves * (nk * (load > mma ? load : mma) + 600.0) + 12.0 * bn + (c == 2 ? 1500.0 : 0.0);
+      if (best == 0.0 || cost < best) {
+        best = cost;
+        cl = c;
+        a.BN = bn;
+        a.mt = mt;
+        a.nt = nt;
+        a.units = static_cast<int>(units);   // far below 2^31: a tile is 16 KB of workspace at least
+      }
+    }
+  }
+  a.stages = stages_of(a, a.BN, cl);
+  const int room = cl == 2 ? pairs : sms, grid = (a.units < room ? a.units : room) * cl;
+  switch (epi) {
+    case kNsGram: return launch_e<kNsGram>(cl, mA, mB, mD, a, grid, s);
+    case kNsSquare: return launch_e<kNsSquare>(cl, mA, mB, mD, a, grid, s);
+    case kNsStep: return launch_e<kNsStep>(cl, mA, mB, mD, a, grid, s);
+    default: return launch_e<kNsLast>(cl, mA, mB, mD, a, grid, s);
+  }
+}
+
+}  // namespace oscars

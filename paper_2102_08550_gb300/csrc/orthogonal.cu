@@ -11,7 +11,8 @@
 // copy is made of either.
 //
 // Launches: the sum of squares (with the merge of the deltas in the same pass),
-// X = G / norm, then three products a step.
+// X = G / norm, then three products a step (orth_product.cu, where the precision
+// of X, A and B is explained).
 #include <cmath>
 
 #include "../../include/oscars.h"
@@ -29,6 +30,7 @@ constexpr float kMaxCoeff = 8.f;
 
 struct Shape {
   int batch, rows, cols, s;         // s: the shorter side
+  int halves;                       // fp16 halves of A and B (X has two)
   int64_t ldx, lds;                 // rows of X and of A, B in the workspace, in elements
   int parts;                        // partial sums a matrix
   int64_t off_part, off_u, off_x[2], off_a, off_b, bytes;
@@ -36,12 +38,13 @@ struct Shape {
 
 int64_t up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 
-Shape make_shape(int batch, int rows, int cols, bool with_u) {
+Shape make_shape(int batch, int rows, int cols, int dtype, bool with_u) {
   Shape p;
   p.batch = batch;
   p.rows = rows;
   p.cols = cols;
   p.s = rows < cols ? rows : cols;
+  p.halves = dtype == OSCARS_F32 ? 2 : 1;
   p.ldx = up(cols, 8);
   p.lds = up(p.s, 8);
   const int64_t elems = static_cast<int64_t>(rows) * cols;
@@ -56,8 +59,8 @@ Shape make_shape(int batch, int rows, int cols, bool with_u) {
   p.off_part = take(static_cast<int64_t>(batch) * p.parts * 8);
   p.off_u = with_u ? take(elems * 4) : 0;
   for (int i = 0; i < 2; ++i) p.off_x[i] = take(static_cast<int64_t>(batch) * rows * p.ldx * 4);
-  p.off_a = take(static_cast<int64_t>(batch) * p.s * p.lds * 4);
-  p.off_b = take(static_cast<int64_t>(batch) * p.s * p.lds * 4);
+  p.off_a = take(static_cast<int64_t>(batch) * p.s * p.lds * 2 * p.halves);
+  p.off_b = take(static_cast<int64_t>(batch) * p.s * p.lds * 2 * p.halves);
   p.bytes = at;
   return p;
 }
@@ -207,11 +210,11 @@ __global__ void __launch_bounds__(kPasses) orth_merge_kernel(const __grid_consta
   if (threadIdx.x == 0) part[blockIdx.x] = sum;
 }
 
-// X = G / (norm + eps), the row padding of X zero
+// X = G / (norm + eps) as two fp16 halves, [half][z][rows][ldx], the row padding zero
 template <typename T>
 __global__ void __launch_bounds__(kPasses) orth_scale_kernel(const T* __restrict__ G, int64_t ldg, int64_t bsg, int rows,
                                                              int cols, int vec, const double* __restrict__ part, int parts,
-                                                             float eps, float* __restrict__ X, int64_t ldx) {
+                                                             float eps, __half* __restrict__ X, int64_t ldx) {
   __shared__ float inv_s[2];
   double t = 0.0;
   for (int i = threadIdx.x; i < parts; i += kPasses) t += part[blockIdx.y * static_cast<int64_t>(parts) + i];
@@ -226,87 +229,44 @@ __global__ void __launch_bounds__(kPasses) orth_scale_kernel(const T* __restrict
   __syncthreads();
   const float f = inv_s[0], pw = inv_s[1];
   const T* g = G + blockIdx.y * bsg;
-  float* x = X + blockIdx.y * rows * ldx;
+  __half* x = X + blockIdx.y * rows * ldx;
+  const int64_t second = static_cast<int64_t>(gridDim.y) * rows * ldx;
   const int per_row = static_cast<int>(ldx / 8);
   const int64_t n = static_cast<int64_t>(rows) * per_row, step = static_cast<int64_t>(gridDim.x) * kPasses;
   for (int64_t i = static_cast<int64_t>(blockIdx.x) * kPasses + threadIdx.x; i < n; i += step) {
     const int r = static_cast<int>(i / per_row), c = static_cast<int>(i - static_cast<int64_t>(r) * per_row) * 8;
     float v[8];
     load8(g + r * ldg + c, cols - c, vec, v);
+    __align__(16) __half hi[8], lo[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[r * ldx + c + j] = (v[j] * pw) * f;
+    for (int j = 0; j < 8; ++j) {
+      const float y = ((v[j] * pw) * f) * kNsScaleX;
+      hi[j] = __float2half_rn(y);
+      lo[j] = __float2half_rn(y - __half2float(hi[j]));
+    }
+    *reinterpret_cast<uint4*>(x + r * ldx + c) = *reinterpret_cast<const uint4*>(hi);
+    *reinterpret_cast<uint4*>(x + second + r * ldx + c) = *reinterpret_cast<const uint4*>(lo);
   }
-}
-
-// ------------------------------------------------------------------ products
-// D[i][j] = sum_k A(i, k) B(k, j), 64 x 64 a block, 4 x 4 a thread
-enum { kGram, kSquare, kStep, kLastF32, kLastBf16, kApply };
-struct ProdArgs {
-  const float *A, *B, *Y;            // Y: kSquare reads b Y[i][j]
-  void* D;
-  int64_t ai, ak, bk, bj, za, zb, zy, zd, ldy, ldd;
-  int M, N, K;
-  float a, b, c;                     // kSquare's coefficients; a: the scale of the last step
-};
-
-template <int EPI>
-__global__ void __launch_bounds__(256) orth_product_kernel(const __grid_constant__ ProdArgs p) {
-  __shared__ float sa[16][65], sb[16][65];
-  const float* A = p.A + blockIdx.z * p.za;
-  const float* B = p.B + blockIdx.z * p.zb;
-  const int m0 = blockIdx.y * 64, n0 = blockIdx.x * 64, tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  float acc[4][4] = {};
-  for (int k0 = 0; k0 < p.K; k0 += 16) {
-    for (int e = threadIdx.x; e < 64 * 16; e += 256) {
-      // the contiguous index of each operand runs along the threads
-      const int ka = p.ak == 1 ? e & 15 : e >> 6, ia = p.ak == 1 ? e >> 4 : e & 63;
-      const int kb = p.bk == 1 ? e & 15 : e >> 6, jb = p.bk == 1 ? e >> 4 : e & 63;
-      sa[ka][ia] = k0 + ka < p.K && m0 + ia < p.M ? A[(m0 + ia) * p.ai + (k0 + ka) * p.ak] : 0.f;
-      sb[kb][jb] = k0 + kb < p.K && n0 + jb < p.N ? B[(k0 + kb) * p.bk + (n0 + jb) * p.bj] : 0.f;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < 16; ++k) {
-      float x[4], y[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) x[i] = sa[k][ty + 16 * i], y[i] = sb[k][tx + 16 * i];
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(x[i], y[j], acc[i][j]);
-    }
-    __syncthreads();
-  }
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int r = m0 + ty + 16 * i, c = n0 + tx + 16 * j;
-      if (r >= p.M || c >= p.N) continue;
-      const int64_t at = blockIdx.z * p.zd + r * p.ldd + c;
-      const float v = acc[i][j];
-      if (EPI == kGram || EPI == kStep) static_cast<float*>(p.D)[at] = v;
-      if (EPI == kSquare)
-        static_cast<float*>(p.D)[at] = fmaf(p.c, v, fmaf(p.b, p.Y[blockIdx.z * p.zy + r * p.ldy + c], r == c ? p.a : 0.f));
-      if (EPI == kLastF32) static_cast<float*>(p.D)[at] = p.a * v;
-      if (EPI == kLastBf16) static_cast<__nv_bfloat16*>(p.D)[at] = __float2bfloat16_rn(p.a * v);
-      if (EPI == kApply) static_cast<float*>(p.D)[at] = fmaf(p.a, v, static_cast<float*>(p.D)[at]);
-    }
-}
-
-template <int EPI>
-cudaError_t product(const ProdArgs& p, int batch, cudaStream_t s) {
-  orth_product_kernel<EPI><<<dim3((p.N + 63) / 64, (p.M + 63) / 64, batch), 256, 0, s>>>(p);
-  return cudaGetLastError();
 }
 
 // where the last step's result goes
 struct Target {
   void* D;
   int64_t ldd, zd;
-  int epi;
+  int type;                         // NsOut
   float scale;
 };
+
+// fp16 [halves][batch][rows][ld]: loads in boxes of 64 x 64, stores of 32 x 32
+bool half_maps(CUtensorMap* load, CUtensorMap* store, const void* base, int64_t ld, int cols, int rows, int batch, int halves) {
+  const cuuint64_t dims[4] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows), static_cast<cuuint64_t>(batch),
+                              static_cast<cuuint64_t>(halves)};
+  const cuuint64_t strides[3] = {static_cast<cuuint64_t>(ld) * 2, static_cast<cuuint64_t>(ld) * rows * 2,
+                                 static_cast<cuuint64_t>(ld) * rows * batch * 2};
+  const cuuint32_t in[4] = {64, 64, 1, 1}, out[4] = {32, 32, 1, 1};
+  return encode_map(load, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, base, dims, strides, in, CU_TENSOR_MAP_SWIZZLE_128B) &&
+         encode_map(store, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, base, dims, strides, out, CU_TENSOR_MAP_SWIZZLE_64B);
+}
 
 int pass_blocks(int64_t units, int most) {
   const int64_t b = (units + kPasses - 1) / kPasses;
@@ -316,61 +276,54 @@ int pass_blocks(int64_t units, int most) {
 template <typename T>
 cudaError_t steps_from(const Shape& p, uint8_t* ws, const T* G, int64_t ldg, int64_t bsg, float eps, int steps,
                        const float (&co)[3], const Target& to, cudaStream_t s) {
-  float* X[2] = {reinterpret_cast<float*>(ws + p.off_x[0]), reinterpret_cast<float*>(ws + p.off_x[1])};
-  float *A = reinterpret_cast<float*>(ws + p.off_a), *B = reinterpret_cast<float*>(ws + p.off_b);
+  __half* X[2] = {reinterpret_cast<__half*>(ws + p.off_x[0]), reinterpret_cast<__half*>(ws + p.off_x[1])};
+  __half *A = reinterpret_cast<__half*>(ws + p.off_a), *B = reinterpret_cast<__half*>(ws + p.off_b);
+  CUtensorMap mX[2], mA, mB, sX[2], sA, sB;
+  for (int i = 0; i < 2; ++i)
+    if (!half_maps(&mX[i], &sX[i], X[i], p.ldx, p.cols, p.rows, p.batch, 2)) return cudaErrorInvalidValue;
+  if (!half_maps(&mA, &sA, A, p.lds, p.s, p.s, p.batch, p.halves) || !half_maps(&mB, &sB, B, p.lds, p.s, p.s, p.batch, p.halves))
+    return cudaErrorInvalidValue;
   const int vec = (reinterpret_cast<uintptr_t>(G) | (ldg * sizeof(T)) | (bsg * sizeof(T))) % 16 == 0;
   orth_scale_kernel<T><<<dim3(pass_blocks(p.rows * (p.ldx / 8), 1024), p.batch), kPasses, 0, s>>>(
       G, ldg, bsg, p.rows, p.cols, vec, reinterpret_cast<const double*>(ws + p.off_part), p.parts, eps, X[0], p.ldx);
   cudaError_t e = cudaGetLastError();
   const bool tall = p.rows > p.cols;
-  const int64_t zx = p.rows * p.ldx, zs = p.s * p.lds;
+  NsArgs g{};   // A = X X^T or X^T X
+  g.batch = p.batch;
+  g.M = g.N = p.s;
+  g.K = tall ? p.rows : p.cols;
+  g.a_halves = g.b_halves = g.d_halves = p.halves;
+  g.a_mn = g.b_mn = tall;
+  g.D = A;
+  g.ld = p.lds;
+  g.z = p.s * p.lds;
+  g.half = p.batch * g.z;
+  NsArgs q = g;   // B = a I + b A + c A A
+  q.K = p.s;
+  q.a_mn = q.b_mn = 0;
+  q.D = B;
+  q.Y = A;
+  q.a = co[0], q.b = co[1], q.c = co[2];
+  NsArgs u{};   // X <- B X or X B
+  u.batch = p.batch;
+  u.M = p.rows;
+  u.N = p.cols;
+  u.K = p.s;
+  u.a_halves = tall ? 2 : p.halves;
+  u.b_halves = tall ? p.halves : 2;
+  u.b_mn = !tall;
+  u.d_halves = 2;
+  u.a = to.scale;
+  u.out = to.D;
+  u.ldo = to.ldd;
+  u.zo = to.zd;
+  u.out_type = to.type;
   for (int k = 0; k < steps && e == cudaSuccess; ++k) {
-    const float* x = X[k & 1];
-    ProdArgs g{};   // A = X X^T or X^T X
-    g.A = g.B = x;
-    g.za = g.zb = zx;
-    g.D = A;
-    g.zd = zs;
-    g.ldd = p.lds;
-    g.M = g.N = p.s;
-    g.K = tall ? p.rows : p.cols;
-    g.ai = g.bj = tall ? 1 : p.ldx;
-    g.ak = g.bk = tall ? p.ldx : 1;
-    if ((e = product<kGram>(g, p.batch, s)) != cudaSuccess) break;
-    ProdArgs q{};   // B = a I + b A + c A A
-    q.A = q.B = q.Y = A;
-    q.za = q.zb = q.zy = q.zd = zs;
-    q.D = B;
-    q.ldy = q.ldd = q.ai = q.bj = p.lds;
-    q.ak = q.bk = 1;
-    q.M = q.N = q.K = p.s;
-    q.a = co[0], q.b = co[1], q.c = co[2];
-    if ((e = product<kSquare>(q, p.batch, s)) != cudaSuccess) break;
-    ProdArgs u{};   // X <- B X or X B
-    u.A = tall ? x : B;
-    u.B = tall ? B : x;
-    u.za = tall ? zx : zs;
-    u.zb = tall ? zs : zx;
-    u.ai = tall ? p.ldx : p.lds;
-    u.ak = 1;
-    u.bk = tall ? 1 : p.ldx;
-    u.bj = tall ? p.lds : 1;
-    u.M = p.rows;
-    u.N = p.cols;
-    u.K = p.s;
-    if (k + 1 < steps) {
-      u.D = X[(k + 1) & 1];
-      u.ldd = p.ldx;
-      u.zd = zx;
-      e = product<kStep>(u, p.batch, s);
-    } else {
-      u.D = to.D;
-      u.ldd = to.ldd;
-      u.zd = to.zd;
-      u.a = to.scale;
-      e = to.epi == kApply ? product<kApply>(u, p.batch, s)
-          : to.epi == kLastBf16 ? product<kLastBf16>(u, p.batch, s) : product<kLastF32>(u, p.batch, s);
-    }
+    const CUtensorMap& x = mX[k & 1];
+    e = launch_ns_product(kNsGram, x, x, sA, g, s);
+    if (e == cudaSuccess) e = launch_ns_product(kNsSquare, mA, mA, sB, q, s);
+    if (e == cudaSuccess)
+      e = launch_ns_product(k + 1 < steps ? kNsStep : kNsLast, tall ? x : mB, tall ? mB : x, sX[(k + 1) & 1], u, s);
   }
   return e;
 }
@@ -413,7 +366,7 @@ extern "C" {
 oscars_status oscars_orthogonalize_workspace(int32_t batch, int32_t rows, int32_t cols, int32_t dtype,
                                              int64_t* bytes) {
   if (!bytes || !sizes_ok(batch, rows, cols) || (dtype != OSCARS_F32 && dtype != OSCARS_BF16)) return OSCARS_EINVAL;
-  *bytes = make_shape(batch, rows, cols, false).bytes;
+  *bytes = make_shape(batch, rows, cols, dtype, false).bytes;
   return OSCARS_OK;
 }
 
@@ -429,10 +382,10 @@ oscars_status oscars_orthogonalize(const void* G, int64_t ldg, int64_t batch_str
   if (batch == 0) return OSCARS_OK;
   const uintptr_t size = dtype == OSCARS_F32 ? 4 : 2;
   if (!G || !O || (reinterpret_cast<uintptr_t>(G) | reinterpret_cast<uintptr_t>(O)) % size) return OSCARS_EINVAL;
-  const Shape p = make_shape(batch, rows, cols, false);
+  const Shape p = make_shape(batch, rows, cols, dtype, false);
   if (!workspace_ok(workspace, workspace_bytes, p.bytes)) return OSCARS_EINVAL;
   uint8_t* ws = static_cast<uint8_t*>(workspace);
-  const Target to{O, ldo, batch_stride_o, dtype == OSCARS_F32 ? kLastF32 : kLastBf16, scale};
+  const Target to{O, ldo, batch_stride_o, dtype == OSCARS_F32 ? kNsF32 : kNsBf16, scale};
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   if (dtype == OSCARS_F32)
     return orthogonalize<float>(p, G, ldg, batch_stride_g, ws, steps, co, eps, to, s);
@@ -441,7 +394,7 @@ oscars_status oscars_orthogonalize(const void* G, int64_t ldg, int64_t batch_str
 
 oscars_status oscars_merge_orthogonal_workspace(int32_t rows, int32_t cols, int64_t* bytes) {
   if (!bytes || !sizes_ok(1, rows, cols)) return OSCARS_EINVAL;
-  *bytes = make_shape(1, rows, cols, true).bytes;
+  *bytes = make_shape(1, rows, cols, OSCARS_F32, true).bytes;
   return OSCARS_OK;
 }
 
@@ -463,7 +416,7 @@ oscars_status oscars_merge_orthogonal(float* x_g, const float* const* deltas, co
     bits |= reinterpret_cast<uintptr_t>(deltas[k]);
   }
   if ((bits | reinterpret_cast<uintptr_t>(x_g)) & 3) return OSCARS_EINVAL;
-  const Shape p = make_shape(1, rows, cols, true);
+  const Shape p = make_shape(1, rows, cols, OSCARS_F32, true);
   if (!workspace_ok(workspace, workspace_bytes, p.bytes)) return OSCARS_EINVAL;
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   float* u = reinterpret_cast<float*>(ws + p.off_u);
@@ -473,7 +426,7 @@ oscars_status oscars_merge_orthogonal(float* x_g, const float* const* deltas, co
   if ((bits & 15) == 0) orth_merge_kernel<4><<<p.parts, kPasses, 0, s>>>(a, momentum, mu, nesterov != 0, u, n, part);
   else orth_merge_kernel<1><<<p.parts, kPasses, 0, s>>>(a, momentum, mu, nesterov != 0, u, n, part);
   if (cudaGetLastError() != cudaSuccess) return OSCARS_ECUDA;
-  const Target to{x_g, cols, 0, kApply, server_lr};
+  const Target to{x_g, cols, 0, kNsAdd, server_lr};
   return steps_from(p, ws, static_cast<const float*>(u), cols, 0, eps, steps, co, to, s) == cudaSuccess ? OSCARS_OK
                                                                                                        : OSCARS_ECUDA;
 }
