@@ -235,19 +235,21 @@ struct NsArgs {
   int a_halves, b_halves;        // of the operands
   int a_mn, b_mn;                // read MN-major (the transposed tensor)
   int d_halves;                  // of D
-  __half* D;                     // kNsGram, kNsSquare: mirror images are written through this
   const __half* Y;               // kNsSquare: A
-  int64_t ld, z, half;           // strides of D and Y in elements
+  int64_t ld, z, half;           // its strides in elements
   float a, b, c;
   void* out;                     // kNsLast
   int64_t ldo, zo;
   int out_type;                  // NsOut
-  int BN, stages, mt, nt, units; // set by the launcher
+  int BN, stages, mt, nt, units; // set by the launcher, and the rows of a load's box:
+  int a_rows, b_rows;
 };
-// mA, mB: the operands, boxes {64, 64, 1, 1} (inner, row, batch, half), 128-byte
-// swizzle; mD: D, boxes {32, 32, 1, 1}, 64-byte swizzle
-cudaError_t launch_ns_product(int epi, const CUtensorMap& mA, const CUtensorMap& mB, const CUtensorMap& mD, NsArgs a,
-                              cudaStream_t s);
+// maps of one tensor (inner, row, batch, half): loads in boxes of 64 x 64 and 64 x
+// 128 with 128-byte swizzle, stores in boxes of 32 x 32 with 64-byte swizzle
+struct NsMaps {
+  CUtensorMap load64, load128, store;
+};
+cudaError_t launch_ns_product(int epi, const NsMaps& A, const NsMaps& B, const NsMaps& D, NsArgs a, cudaStream_t s);
 
 // Weight gradient + SGD of up to kDwMaxLayers hidden layers, persistent
 // (csrc/gemm_dw.cu): W[wid] = W[src] - lr * G^T X over the batch, its bf16

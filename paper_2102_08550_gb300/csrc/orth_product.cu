@@ -117,11 +117,6 @@ __device__ __forceinline__ Tile tile_of(const NsArgs& a, int u) {
   return t;
 }
 
-__device__ __forceinline__ uint32_t pack_half2(__half lo, __half hi) {
-  const __half2 v = __halves2half2(lo, hi);
-  return *reinterpret_cast<const uint32_t*>(&v);
-}
-
 template <int EPI, int CL, bool kSums>
 __global__ void __launch_bounds__(kThreads, 1) ns_product_kernel(const __grid_constant__ CUtensorMap mapA,
                                                                  const __grid_constant__ CUtensorMap mapB,
@@ -181,21 +176,23 @@ __global__ void __launch_bounds__(kThreads, 1) ns_product_kernel(const __grid_co
     for (int u = u0; ok && u < a.units; u += ustep) {
       const Tile t = tile_of<CL, kSym>(a, u);
       const int m0 = (t.i * CL + rank) * 128, n0 = t.j * a.BN + rank * (a.BN / CL);
+      const bool same = kSym && t.i == t.j && b_boxes == 2;   // a tile on the diagonal: B is A
       for (int kb = 0; kb < nk; ++kb, ++it) {
         if (it >= a.stages && !(ok = mbar_wait(&bars->empty[s], ph, nullptr, kDevTimeoutEmpty))) break;
         uint8_t* at = ring + s * stage_bytes;
-        if (rank == 0) mbar_arrive_expect_tx(&bars->full[s], CL * stage_bytes);   // a pair's bytes count on the leader's
+        // a pair's bytes count on the leader's
+        if (rank == 0) mbar_arrive_expect_tx(&bars->full[s], CL * (same ? a_bytes : stage_bytes));
         armed = it + 1;
-        auto load = [&](const CUtensorMap* map, int mn, int row0, int half) {
-          const int c0 = mn ? row0 : kb * kK, c1 = mn ? kb * kK : row0;
-          if (CL > 1) tma_load_4d_pair(at, map, c0, c1, t.z, half, &bars->full[s]);
-          else tma_load_4d(at, map, c0, c1, t.z, half, &bars->full[s]);
-          at += kBox;
+        auto load = [&](const CUtensorMap* map, int mn, int boxes, int rows, int row0, int half) {
+          for (int i = 0; i < boxes; ++i, row0 += rows, at += rows * 128) {
+            const int c0 = mn ? row0 : kb * kK, c1 = mn ? kb * kK : row0;
+            if (CL > 1) tma_load_4d_pair(at, map, c0, c1, t.z, half, &bars->full[s]);
+            else tma_load_4d(at, map, c0, c1, t.z, half, &bars->full[s]);
+          }
         };
-        for (int h = 0; h < a.a_halves; ++h)
-          for (int b = 0; b < 2; ++b) load(&mapA, a.a_mn, m0 + 64 * b, h);
-        for (int h = 0; h < a.b_halves; ++h)
-          for (int b = 0; b < b_boxes; ++b) load(&mapB, a.b_mn, n0 + 64 * b, h);
+        for (int h = 0; h < a.a_halves; ++h) load(&mapA, a.a_mn, 128 / a.a_rows, a.a_rows, m0, h);
+        if (!same)
+          for (int h = 0; h < a.b_halves; ++h) load(&mapB, a.b_mn, 64 * b_boxes / a.b_rows, a.b_rows, n0, h);
         if (++s == a.stages) {
           s = 0;
           ph ^= 1;
@@ -216,6 +213,12 @@ __global__ void __launch_bounds__(kThreads, 1) ns_product_kernel(const __grid_co
     int s = 0, ph = 0, t = 0;   // t: accumulations begun
     uint32_t limit = kSpinLimit;
     for (int u = u0; u < a.units; u += ustep) {
+      bool same = false;
+      if (kSym) {
+        const Tile tl = tile_of<CL, kSym>(a, u);
+        same = tl.i == tl.j && b_boxes == 2;
+      }
+      const int b_off = same ? 0 : a_bytes;
       for (int k0 = 0; k0 < nk; k0 += chunk, ++t) {
         const int b = t & 1, k1 = k0 + chunk < nk ? k0 + chunk : nk;
         if (t >= 2) mbar_wait_keep(limit, &bars->acce[b], ((t >> 1) + 1) & 1, nullptr, kDevTimeoutAccum);
@@ -226,7 +229,7 @@ __global__ void __launch_bounds__(kThreads, 1) ns_product_kernel(const __grid_co
           tc_fence_after();
           const uint32_t at = ring0 + s * stage_bytes;
           const uint64_t ad = a.a_mn ? smem_desc_mn128(at, kBox) : smem_desc_k128(at);
-          const uint64_t bd = a.b_mn ? smem_desc_mn128(at + a_bytes, kBox) : smem_desc_k128(at + a_bytes);
+          const uint64_t bd = a.b_mn ? smem_desc_mn128(at + b_off, kBox) : smem_desc_k128(at + b_off);
           if (elect_one() && limit > 1) {
             uint32_t more = kb == k0 ? 0u : 1u;
             auto issue = [&](uint64_t x, uint64_t y) {
@@ -260,7 +263,7 @@ __global__ void __launch_bounds__(kThreads, 1) ns_product_kernel(const __grid_co
     // ---- epilogue: thread = one accumulator row and half of its columns
     const int quarter = warp & 3, span = a.BN / 2, cb = (warp >> 2) == 1 ? 0 : span;
     uint8_t* my = stg + (warp - 4) * 2 * kStg;
-    int t = 0;
+    int t = 0, nst = 0;
     // the accumulator may be written again (by accumulation t + 2)
     auto release = [&](int b) {
       tc_fence_before();
@@ -278,60 +281,46 @@ __global__ void __launch_bounds__(kThreads, 1) ns_product_kernel(const __grid_co
       // 32 columns from column c0 on
       auto finish = [&](int c0, const float (&v)[32]) {
         if constexpr (EPI != kNsLast) {
-          const float scale = EPI == kNsGram ? kNsScaleA / (kNsScaleX * kNsScaleX)
-                              : EPI == kNsSquare ? a.c / kNsScaleA : 1.f / kNsScaleA;
-          if (lane == 0) bulk_wait_read_all();   // the last stores have read the boxes
-          __syncwarp();
-          __half* mirror = a.D + tl.z * a.z + static_cast<int64_t>(n0 + c0) * a.ld + r;
-          const __half* y = a.Y + tl.z * a.z + static_cast<int64_t>(r) * a.ld + n0 + c0;
+          const float scale = EPI == kNsGram ? kNsScaleA / (kNsScaleX * kNsScaleX) : EPI == kNsSquare ? 1.f : 1.f / kNsScaleA;
+          uint32_t hi[16], lo[16];
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            __half hi[8], lo[8];
-            const int col = n0 + c0 + 8 * q;
-            float f[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) f[e] = v[8 * q + e] * scale;
-            if (EPI == kNsSquare && r < a.M && col < a.N) {   // + b A + a I; a row's 8 columns lie within its stride
-              for (int g = 0; g < a.d_halves; ++g) {
-                const uint4 w = *reinterpret_cast<const uint4*>(y + g * a.half + 8 * q);
-                const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                  const float2 p = __half22float2(*reinterpret_cast<const __half2*>(&ws[e]));
-                  f[2 * e] = fmaf(a.b, p.x, f[2 * e]);
-                  f[2 * e + 1] = fmaf(a.b, p.y, f[2 * e + 1]);
-                }
-              }
-#pragma unroll
-              for (int e = 0; e < 8; ++e)
-                if (col + e == r) f[e] += a.a * kNsScaleA;
-            }
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              hi[e] = __float2half_rn(f[e]);
-              lo[e] = __float2half_rn(f[e] - __half2float(hi[e]));
-            }
-            const int swz = (q ^ ((lane >> 1) & 3)) << 4;
-            *reinterpret_cast<uint4*>(my + lane * 64 + swz) = make_uint4(
-                pack_half2(hi[0], hi[1]), pack_half2(hi[2], hi[3]), pack_half2(hi[4], hi[5]), pack_half2(hi[6], hi[7]));
-            if (a.d_halves == 2)
-              *reinterpret_cast<uint4*>(my + kStg + lane * 64 + swz) = make_uint4(
-                  pack_half2(lo[0], lo[1]), pack_half2(lo[2], lo[3]), pack_half2(lo[4], lo[5]), pack_half2(lo[6], lo[7]));
-            if (kSym && tl.i != tl.j && r < a.M) {   // the mirror image: a column's 32 rows are 64 bytes
-#pragma unroll
-              for (int e = 0; e < 8; ++e)
-                if (col + e < a.N) {
-                  mirror[static_cast<int64_t>(8 * q + e) * a.ld] = hi[e];
-                  if (a.d_halves == 2) mirror[a.half + static_cast<int64_t>(8 * q + e) * a.ld] = lo[e];
-                }
-            }
+          for (int e = 0; e < 16; ++e) {
+            const float x = v[2 * e] * scale, y = v[2 * e + 1] * scale;
+            const __half2 h = __floats2half2_rn(x, y);
+            const float2 f = __half22float2(h);
+            const __half2 l = __floats2half2_rn(x - f.x, y - f.y);
+            hi[e] = *reinterpret_cast<const uint32_t*>(&h);
+            lo[e] = *reinterpret_cast<const uint32_t*>(&l);
           }
-          fence_proxy_async_smem();
-          __syncwarp();
-          if (lane == 0 && m0 < a.M) {
-            tma_store_4d(&mapD, my, n0 + c0, m0, tl.z, 0);
-            if (a.d_halves == 2) tma_store_4d(&mapD, my + kStg, n0 + c0, m0, tl.z, 1);
-            bulk_commit_group();
+          // one box of 32 x 32: rows as they are, or (kSym) the mirror image
+          auto store = [&](const uint32_t (&w)[16], int half, bool mirror) {
+            uint8_t* box = my + (nst & 1) * kStg;
+            if (lane == 0 && nst >= 2) bulk_wait_read_but_one();   // the store of two boxes ago has read this one
+            ++nst;
+            __syncwarp();
+            if (!mirror) {
+#pragma unroll
+              for (int q = 0; q < 4; ++q)
+                *reinterpret_cast<uint4*>(box + lane * 64 + ((q ^ ((lane >> 1) & 3)) << 4)) =
+                    make_uint4(w[4 * q], w[4 * q + 1], w[4 * q + 2], w[4 * q + 3]);
+            } else {
+#pragma unroll
+              for (int e = 0; e < 32; ++e)
+                *reinterpret_cast<uint16_t*>(box + e * 64 + (((lane >> 3) ^ ((e >> 1) & 3)) << 4) + (lane & 7) * 2) =
+                    static_cast<uint16_t>(w[e >> 1] >> (16 * (e & 1)));
+            }
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+              tma_store_4d(&mapD, box, mirror ? m0 : n0 + c0, mirror ? n0 + c0 : m0, tl.z, half);
+              bulk_commit_group();
+            }
+          };
+          store(hi, 0, false);
+          if (a.d_halves == 2) store(lo, 1, false);
+          if (kSym && tl.i != tl.j) {
+            store(hi, 0, true);
+            if (a.d_halves == 2) store(lo, 1, true);
           }
         } else {
           const float scale = a.a / (kNsScaleA * kNsScaleX);
@@ -373,12 +362,35 @@ __global__ void __launch_bounds__(kThreads, 1) ns_product_kernel(const __grid_co
           __syncwarp();
         }
       };
-      if constexpr (kSums) {
+      if constexpr (kSums || EPI == kNsSquare) {
         float sum[kMaxBN / 64][32];
 #pragma unroll
-        for (int g = 0; g < kMaxBN / 64; ++g)
+        for (int g = 0; g < kMaxBN / 64; ++g) {
 #pragma unroll
           for (int e = 0; e < 32; ++e) sum[g][e] = 0.f;
+          if constexpr (EPI == kNsSquare) {   // b A + a I, read while the products run; 8 columns lie within a row's stride
+            const __half* y = a.Y + tl.z * a.z + static_cast<int64_t>(r) * a.ld + n0 + 32 * g;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              const int col = n0 + 32 * g + 8 * q;
+              if (32 * g >= span || r >= a.M || col >= a.N) continue;
+              for (int h = 0; h < a.d_halves; ++h) {
+                const uint4 w = *reinterpret_cast<const uint4*>(y + h * a.half + 8 * q);
+                const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  const float2 p = __half22float2(*reinterpret_cast<const __half2*>(&ws[e]));
+                  sum[g][8 * q + 2 * e] = fmaf(a.b, p.x, sum[g][8 * q + 2 * e]);
+                  sum[g][8 * q + 2 * e + 1] = fmaf(a.b, p.y, sum[g][8 * q + 2 * e + 1]);
+                }
+              }
+#pragma unroll
+              for (int e = 0; e < 8; ++e)
+                if (col + e == r) sum[g][8 * q + e] += a.a * kNsScaleA;
+            }
+          }
+        }
+        const float factor = EPI == kNsSquare ? a.c / kNsScaleA : 1.f;
         bool ok = true;
         for (int k0 = 0; k0 < nk; k0 += chunk, ++t) {
           const int b = t & 1;
@@ -392,7 +404,7 @@ __global__ void __launch_bounds__(kThreads, 1) ns_product_kernel(const __grid_co
                 float v[16];
                 tmem_ld_32x32b_x16(row0 + b * kMaxBN + 32 * g + 16 * h, v);
 #pragma unroll
-                for (int e = 0; e < 16; ++e) sum[g][16 * h + e] += v[e];
+                for (int e = 0; e < 16; ++e) sum[g][16 * h + e] = fmaf(v[e], factor, sum[g][16 * h + e]);
               }
             }
           release(b);
@@ -400,12 +412,12 @@ __global__ void __launch_bounds__(kThreads, 1) ns_product_kernel(const __grid_co
         if (!ok) break;
 #pragma unroll
         for (int g = 0; g < kMaxBN / 64; ++g)
-          if (32 * g < span && n0 + 32 * g < a.N) finish(32 * g, sum[g]);
+          if (32 * g < span && n0 + 32 * g < a.N && m0 < a.M) finish(32 * g, sum[g]);
       } else {
         const int b = t & 1;
         if (!mbar_wait_warp(&bars->accf[b], (t >> 1) & 1, nullptr, kDevTimeoutAccum)) break;
         tc_fence_after();
-        for (int c0 = 0; c0 < span && n0 + c0 < a.N; c0 += 32) {
+        for (int c0 = 0; c0 < span && n0 + c0 < a.N && m0 < a.M; c0 += 32) {
           float v[32];
           tmem_ld_32x32b_x32(row0 + b * kMaxBN + c0, v);
           finish(c0, v);
@@ -504,14 +516,13 @@ cudaError_t launch_e(int cl, const CUtensorMap& mA, const CUtensorMap& mB, const
 
 }  // namespace
 
-cudaError_t launch_ns_product(int epi, const CUtensorMap& mA, const CUtensorMap& mB, const CUtensorMap& mD, NsArgs a,
-                              cudaStream_t s) {
+cudaError_t launch_ns_product(int epi, const NsMaps& A, const NsMaps& B, const NsMaps& D, NsArgs a, cudaStream_t s) {
   int sms, pairs;
   device_room(sms, pairs);
   const bool sym = epi == kNsGram || epi == kNsSquare;
   const int nk = (a.K + kK - 1) / kK, products = a.a_halves + a.b_halves - 1;
   // The shape with the least estimated time: waves of tiles times the longer of a
-  // tile's products (2 BN clocks a K-block and product) and loads (60 bytes a clock
+  // tile's products (2 BN clocks a K-block and product) and loads (45 bytes a clock
   // into an SM), plus a tile's and a launch's fixed part.  Triangles take square tiles.
   double best = 0.0;
   int cl = 1;
@@ -523,7 +534,7 @@ cudaError_t launch_ns_product(int epi, const CUtensorMap& mA, const CUtensorMap&
       const int64_t units = static_cast<int64_t>(a.batch) * (sym ? nt * static_cast<int64_t>(nt + 1) / 2 : static_cast<int64_t>(mt / c) * nt);
       const int room = c == 2 ? pairs : sms;
       const double waves = static_cast<double>((units + room - 1) / room);
-      const double mma = 2.0 * bn * products, load = stage_bytes(a, bn, c) / 60.0;
+      const double mma = 2.0 * bn * products, load = stage_bytes(a, bn, c) / 45.0;
       const double cost = waves * (nk * (load > mma ? load : mma) + 600.0) + 12.0 * bn + (c == 2 ? 1500.0 : 0.0);
       if (best == 0.0 || cost < best) {
         best = cost;
@@ -536,6 +547,10 @@ cudaError_t launch_ns_product(int epi, const CUtensorMap& mA, const CUtensorMap&
     }
   }
   a.stages = stages_of(a, a.BN, cl);
+  // K-major boxes of 128 rows where the tile has them: half as many copies
+  a.a_rows = a.a_mn ? 64 : 128;
+  a.b_rows = a.b_mn || a.BN / cl % 128 ? 64 : 128;
+  const CUtensorMap &mA = a.a_rows == 64 ? A.load64 : A.load128, &mB = a.b_rows == 64 ? B.load64 : B.load128, &mD = D.store;
   const int room = cl == 2 ? pairs : sms, grid = (a.units < room ? a.units : room) * cl;
   switch (epi) {
     case kNsGram: return launch_e<kNsGram>(cl, mA, mB, mD, a, grid, s);

@@ -257,15 +257,17 @@ struct Target {
   float scale;
 };
 
-// fp16 [halves][batch][rows][ld]: loads in boxes of 64 x 64, stores of 32 x 32
-bool half_maps(CUtensorMap* load, CUtensorMap* store, const void* base, int64_t ld, int cols, int rows, int batch, int halves) {
+// fp16 [halves][batch][rows][ld]
+bool half_maps(NsMaps* m, const void* base, int64_t ld, int cols, int rows, int batch, int halves) {
   const cuuint64_t dims[4] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows), static_cast<cuuint64_t>(batch),
                               static_cast<cuuint64_t>(halves)};
   const cuuint64_t strides[3] = {static_cast<cuuint64_t>(ld) * 2, static_cast<cuuint64_t>(ld) * rows * 2,
                                  static_cast<cuuint64_t>(ld) * rows * batch * 2};
-  const cuuint32_t in[4] = {64, 64, 1, 1}, out[4] = {32, 32, 1, 1};
-  return encode_map(load, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, base, dims, strides, in, CU_TENSOR_MAP_SWIZZLE_128B) &&
-         encode_map(store, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, base, dims, strides, out, CU_TENSOR_MAP_SWIZZLE_64B);
+  const cuuint32_t b64[4] = {64, 64, 1, 1}, b128[4] = {64, 128, 1, 1}, out[4] = {32, 32, 1, 1};
+  const CUtensorMapDataType t = CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+  return encode_map(&m->load64, t, 4, base, dims, strides, b64, CU_TENSOR_MAP_SWIZZLE_128B) &&
+         encode_map(&m->load128, t, 4, base, dims, strides, b128, CU_TENSOR_MAP_SWIZZLE_128B) &&
+         encode_map(&m->store, t, 4, base, dims, strides, out, CU_TENSOR_MAP_SWIZZLE_64B);
 }
 
 int pass_blocks(int64_t units, int most) {
@@ -278,10 +280,10 @@ cudaError_t steps_from(const Shape& p, uint8_t* ws, const T* G, int64_t ldg, int
                        const float (&co)[3], const Target& to, cudaStream_t s) {
   __half* X[2] = {reinterpret_cast<__half*>(ws + p.off_x[0]), reinterpret_cast<__half*>(ws + p.off_x[1])};
   __half *A = reinterpret_cast<__half*>(ws + p.off_a), *B = reinterpret_cast<__half*>(ws + p.off_b);
-  CUtensorMap mX[2], mA, mB, sX[2], sA, sB;
+  NsMaps mX[2], mA, mB;
   for (int i = 0; i < 2; ++i)
-    if (!half_maps(&mX[i], &sX[i], X[i], p.ldx, p.cols, p.rows, p.batch, 2)) return cudaErrorInvalidValue;
-  if (!half_maps(&mA, &sA, A, p.lds, p.s, p.s, p.batch, p.halves) || !half_maps(&mB, &sB, B, p.lds, p.s, p.s, p.batch, p.halves))
+    if (!half_maps(&mX[i], X[i], p.ldx, p.cols, p.rows, p.batch, 2)) return cudaErrorInvalidValue;
+  if (!half_maps(&mA, A, p.lds, p.s, p.s, p.batch, p.halves) || !half_maps(&mB, B, p.lds, p.s, p.s, p.batch, p.halves))
     return cudaErrorInvalidValue;
   const int vec = (reinterpret_cast<uintptr_t>(G) | (ldg * sizeof(T)) | (bsg * sizeof(T))) % 16 == 0;
   orth_scale_kernel<T><<<dim3(pass_blocks(p.rows * (p.ldx / 8), 1024), p.batch), kPasses, 0, s>>>(
@@ -294,14 +296,12 @@ cudaError_t steps_from(const Shape& p, uint8_t* ws, const T* G, int64_t ldg, int
   g.K = tall ? p.rows : p.cols;
   g.a_halves = g.b_halves = g.d_halves = p.halves;
   g.a_mn = g.b_mn = tall;
-  g.D = A;
   g.ld = p.lds;
   g.z = p.s * p.lds;
   g.half = p.batch * g.z;
   NsArgs q = g;   // B = a I + b A + c A A
   q.K = p.s;
   q.a_mn = q.b_mn = 0;
-  q.D = B;
   q.Y = A;
   q.a = co[0], q.b = co[1], q.c = co[2];
   NsArgs u{};   // X <- B X or X B
@@ -319,11 +319,11 @@ cudaError_t steps_from(const Shape& p, uint8_t* ws, const T* G, int64_t ldg, int
   u.zo = to.zd;
   u.out_type = to.type;
   for (int k = 0; k < steps && e == cudaSuccess; ++k) {
-    const CUtensorMap& x = mX[k & 1];
-    e = launch_ns_product(kNsGram, x, x, sA, g, s);
-    if (e == cudaSuccess) e = launch_ns_product(kNsSquare, mA, mA, sB, q, s);
+    const NsMaps& x = mX[k & 1];
+    e = launch_ns_product(kNsGram, x, x, mA, g, s);
+    if (e == cudaSuccess) e = launch_ns_product(kNsSquare, mA, mA, mB, q, s);
     if (e == cudaSuccess)
-      e = launch_ns_product(k + 1 < steps ? kNsStep : kNsLast, tall ? x : mB, tall ? mB : x, sX[(k + 1) & 1], u, s);
+      e = launch_ns_product(k + 1 < steps ? kNsStep : kNsLast, tall ? x : mB, tall ? mB : x, mX[(k + 1) & 1], u, s);
   }
   return e;
 }
