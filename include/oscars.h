@@ -505,13 +505,14 @@ oscars_status oscars_softreg_steps_noalloc(const float* params_in, float* params
  * O may be G itself with the same strides, else they must not overlap; a
  * batch_stride_g of 0 reads one matrix for all.  dtype (oscars_dtype) is that
  * of both; any alignment (16-byte aligned rows take the vector path).
- * coeff: host, 3 floats {a, b, c}, each at most 8 in magnitude, or NULL for
+ * coeff: host, 3 floats {a, b, c}, each at most 8 in magnitude, with c = 0 or
+ * both b^2 <= 32 |c| and |b| <= 64 |c| (terms of like size), or NULL for
  * {3.4445, -4.7750, 2.0315}, which keep singular values in [0, 1] below 1.21.
  * Others have to keep them below 2 in every step, or the result may overflow.
  * eps > 0: a matrix of zeros gives zeros.  A matrix that holds an infinity or
  * NaN gives NaN throughout.  The norm neither overflows nor underflows.
- * Accuracy: fp32 results are fp32 throughout; bf16 results round the factors
- * (b A + c A A) to 11 bits and keep X in 22, about 1e-3 of a result's size.
+ * Accuracy: fp32 results keep X and the factors in 22 bits and add in fp32; bf16
+ * results round the factors to 11 bits, about 1e-3 of a result's size.
  * The arithmetic is fixed: equal inputs give equal bits.
  * workspace: device, 256-byte aligned, at least the bytes that
  * oscars_orthogonalize_workspace gives for the same sizes; the call leaves

@@ -222,12 +222,11 @@ cudaError_t launch_gemm_rows(int epi, const RowsPlan& p, const CUtensorMap& mA, 
 // The products of a Newton-Schulz step (csrc/orth_product.cu).  Operands are fp16,
 // [half][batch][rows][ld]: one half, or two whose sum is the value.
 enum NsEpi {
-  kNsGram,     // D = A = X X^T or X^T X, symmetric: the tiles of one triangle and their mirror images
-  kNsSquare,   // D = a I + b A + c A A, the same
+  kNsSym,      // D = factor A B + diag I, symmetric: the tiles of one triangle and their mirror images
   kNsStep,     // D = the next X, two halves
-  kNsLast      // the last step's X, times a, to `out`
+  kNsLast      // the last step's X, times factor, to `out`
 };
-enum NsOut { kNsF32, kNsBf16, kNsAdd };   // kNsAdd: out += a X, fp32
+enum NsOut { kNsF32, kNsBf16, kNsAdd };   // kNsAdd: out += factor X, fp32
 // values are stored times these, which keeps the second half out of fp16's subnormal range
 constexpr float kNsScaleX = 1024.f, kNsScaleA = 256.f;
 struct NsArgs {
@@ -235,9 +234,7 @@ struct NsArgs {
   int a_halves, b_halves;        // of the operands
   int a_mn, b_mn;                // read MN-major (the transposed tensor)
   int d_halves;                  // of D
-  const __half* Y;               // kNsSquare: A
-  int64_t ld, z, half;           // its strides in elements
-  float a, b, c;
+  float factor, diag;            // factor includes the operands' and D's scales, diag D's
   void* out;                     // kNsLast
   int64_t ldo, zo;
   int out_type;                  // NsOut

@@ -1,10 +1,15 @@
 // The three products of a Newton-Schulz step on the 5th-generation tensor cores
 // (tcgen05, sm_103a), for a batch of matrices in one launch:
 //
-//   kNsGram    A = X X^T (X K-major) or X^T X (X read MN-major)
-//   kNsSquare  B = a I + b A + c A A
-//   kNsStep    X <- B X (X read MN-major) or X B
-//   kNsLast    the same into the caller's matrix
+//   kNsSym   A' = X X^T + beta I (X K-major) or X^T X + beta I (X read MN-major)
+//            B = c A' A' + gamma I
+//   kNsStep  X <- B X (X read MN-major) or X B
+//   kNsLast  the same into the caller's matrix
+//
+// With beta = b / 2c and gamma = a - b^2 / 4c, B is a I + b A + c A A: the
+// polynomial takes one product of A' with itself and nothing else (reading A in
+// that product's epilogue, 32 rows a load, took 10000 to 20000 clocks a tile, more
+// than the products of 1024 columns).
 //
 // Precision.  tcgen05 multiplies 16-bit operands; a value is kept as one fp16 (11
 // bits) or as two whose sum has 22, and a product of values in two halves takes
@@ -40,7 +45,7 @@ namespace oscars {
 namespace {
 
 constexpr int kK = 64, kThreads = 384, kMaxBN = 256, kMaxStages = 8;
-constexpr int kChunk = 2;                          // K-blocks of one accumulation of an fp32 result
+constexpr int kChunk = 1;                          // K-blocks of one accumulation of an fp32 result
 constexpr int kEpiWarps = 8;
 constexpr int kBox = 64 * 128;                     // one operand box: 64 rows of 128 bytes
 constexpr int kStg = 2048;                         // one staging box: 32 rows x 64 bytes
@@ -122,7 +127,7 @@ __global__ void __launch_bounds__(kThreads, 1) ns_product_kernel(const __grid_co
                                                                  const __grid_constant__ CUtensorMap mapB,
                                                                  const __grid_constant__ CUtensorMap mapD,
                                                                  const __grid_constant__ NsArgs a) {
-  constexpr bool kSym = EPI == kNsGram || EPI == kNsSquare;
+  constexpr bool kSym = EPI == kNsSym;
   extern __shared__ uint8_t ns_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(ns_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* stg = smem;
@@ -281,11 +286,15 @@ __global__ void __launch_bounds__(kThreads, 1) ns_product_kernel(const __grid_co
       // 32 columns from column c0 on
       auto finish = [&](int c0, const float (&v)[32]) {
         if constexpr (EPI != kNsLast) {
-          const float scale = EPI == kNsGram ? kNsScaleA / (kNsScaleX * kNsScaleX) : EPI == kNsSquare ? 1.f : 1.f / kNsScaleA;
           uint32_t hi[16], lo[16];
+          const int d = r - n0 - c0;   // the column on the diagonal
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
-            const float x = v[2 * e] * scale, y = v[2 * e + 1] * scale;
+            float x = v[2 * e] * a.factor, y = v[2 * e + 1] * a.factor;
+            if (kSym) {
+              x += d == 2 * e ? a.diag : 0.f;
+              y += d == 2 * e + 1 ? a.diag : 0.f;
+            }
             const __half2 h = __floats2half2_rn(x, y);
             const float2 f = __half22float2(h);
             const __half2 l = __floats2half2_rn(x - f.x, y - f.y);
@@ -323,11 +332,10 @@ __global__ void __launch_bounds__(kThreads, 1) ns_product_kernel(const __grid_co
             if (a.d_halves == 2) store(lo, 1, true);
           }
         } else {
-          const float scale = a.a / (kNsScaleA * kNsScaleX);
 #pragma unroll
           for (int q = 0; q < 8; ++q)
             *reinterpret_cast<float4*>(my + lane * 128 + ((q ^ (lane & 7)) << 4)) =
-                make_float4(v[4 * q] * scale, v[4 * q + 1] * scale, v[4 * q + 2] * scale, v[4 * q + 3] * scale);
+                make_float4(v[4 * q] * a.factor, v[4 * q + 1] * a.factor, v[4 * q + 2] * a.factor, v[4 * q + 3] * a.factor);
           __syncwarp();
           // rows of 32 columns, coalesced whatever the caller's alignment
           const int col = n0 + c0 + lane;
@@ -362,35 +370,12 @@ __global__ void __launch_bounds__(kThreads, 1) ns_product_kernel(const __grid_co
           __syncwarp();
         }
       };
-      if constexpr (kSums || EPI == kNsSquare) {
+      if constexpr (kSums) {
         float sum[kMaxBN / 64][32];
 #pragma unroll
-        for (int g = 0; g < kMaxBN / 64; ++g) {
+        for (int g = 0; g < kMaxBN / 64; ++g)
 #pragma unroll
           for (int e = 0; e < 32; ++e) sum[g][e] = 0.f;
-          if constexpr (EPI == kNsSquare) {   // b A + a I, read while the products run; 8 columns lie within a row's stride
-            const __half* y = a.Y + tl.z * a.z + static_cast<int64_t>(r) * a.ld + n0 + 32 * g;
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              const int col = n0 + 32 * g + 8 * q;
-              if (32 * g >= span || r >= a.M || col >= a.N) continue;
-              for (int h = 0; h < a.d_halves; ++h) {
-                const uint4 w = *reinterpret_cast<const uint4*>(y + h * a.half + 8 * q);
-                const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                  const float2 p = __half22float2(*reinterpret_cast<const __half2*>(&ws[e]));
-                  sum[g][8 * q + 2 * e] = fmaf(a.b, p.x, sum[g][8 * q + 2 * e]);
-                  sum[g][8 * q + 2 * e + 1] = fmaf(a.b, p.y, sum[g][8 * q + 2 * e + 1]);
-                }
-              }
-#pragma unroll
-              for (int e = 0; e < 8; ++e)
-                if (col + e == r) sum[g][8 * q + e] += a.a * kNsScaleA;
-            }
-          }
-        }
-        const float factor = EPI == kNsSquare ? a.c / kNsScaleA : 1.f;
         bool ok = true;
         for (int k0 = 0; k0 < nk; k0 += chunk, ++t) {
           const int b = t & 1;
@@ -404,7 +389,7 @@ __global__ void __launch_bounds__(kThreads, 1) ns_product_kernel(const __grid_co
                 float v[16];
                 tmem_ld_32x32b_x16(row0 + b * kMaxBN + 32 * g + 16 * h, v);
 #pragma unroll
-                for (int e = 0; e < 16; ++e) sum[g][16 * h + e] = fmaf(v[e], factor, sum[g][16 * h + e]);
+                for (int e = 0; e < 16; ++e) sum[g][16 * h + e] += v[e];
               }
             }
           release(b);
@@ -519,7 +504,7 @@ cudaError_t launch_e(int cl, const CUtensorMap& mA, const CUtensorMap& mB, const
 cudaError_t launch_ns_product(int epi, const NsMaps& A, const NsMaps& B, const NsMaps& D, NsArgs a, cudaStream_t s) {
   int sms, pairs;
   device_room(sms, pairs);
-  const bool sym = epi == kNsGram || epi == kNsSquare;
+  const bool sym = epi == kNsSym;
   const int nk = (a.K + kK - 1) / kK, products = a.a_halves + a.b_halves - 1;
   // The shape with the least estimated time: waves of tiles times the longer of a
   // tile's products (2 BN clocks a K-block and product) and loads (45 bytes a clock
@@ -553,8 +538,7 @@ cudaError_t launch_ns_product(int epi, const NsMaps& A, const NsMaps& B, const N
   const CUtensorMap &mA = a.a_rows == 64 ? A.load64 : A.load128, &mB = a.b_rows == 64 ? B.load64 : B.load128, &mD = D.store;
   const int room = cl == 2 ? pairs : sms, grid = (a.units < room ? a.units : room) * cl;
   switch (epi) {
-    case kNsGram: return launch_e<kNsGram>(cl, mA, mB, mD, a, grid, s);
-    case kNsSquare: return launch_e<kNsSquare>(cl, mA, mB, mD, a, grid, s);
+    case kNsSym: return launch_e<kNsSym>(cl, mA, mB, mD, a, grid, s);
     case kNsStep: return launch_e<kNsStep>(cl, mA, mB, mD, a, grid, s);
     default: return launch_e<kNsLast>(cl, mA, mB, mD, a, grid, s);
   }

@@ -2,7 +2,8 @@
 // server step that merges pushed deltas, orthogonalises the result and applies
 // it (the update rule of the Muon optimiser in place of the average of Eq. 4).
 //
-//   X = G / (|G|_F + eps);  steps times:  A = X X^T,  B = a I + b A + c A A,
+//   X = G / (|G|_F + eps);  steps times:  A = X X^T,  B = a I + b A + c A A
+//   (as c (A + beta I)^2 + gamma I, or a I + b A where c = 0),
 //   X <- B X;  O = scale X.
 //
 // With s = min(rows, cols) the Gram matrix is taken on the shorter side: A = X
@@ -11,7 +12,7 @@
 // copy is made of either.
 //
 // Launches: the sum of squares (with the merge of the deltas in the same pass),
-// X = G / norm, then three products a step (orth_product.cu, where the precision
+// X = G / norm, then three products a step, two where c = 0 (orth_product.cu, where the precision
 // of X, A and B is explained).
 #include <cmath>
 
@@ -290,20 +291,21 @@ cudaError_t steps_from(const Shape& p, uint8_t* ws, const T* G, int64_t ldg, int
       G, ldg, bsg, p.rows, p.cols, vec, reinterpret_cast<const double*>(ws + p.off_part), p.parts, eps, X[0], p.ldx);
   cudaError_t e = cudaGetLastError();
   const bool tall = p.rows > p.cols;
-  NsArgs g{};   // A = X X^T or X^T X
+  const bool cubic = co[2] == 0.f;
+  const float sums = kNsScaleA / (kNsScaleX * kNsScaleX);
+  NsArgs g{};   // A + beta I, or B itself where c = 0
   g.batch = p.batch;
   g.M = g.N = p.s;
   g.K = tall ? p.rows : p.cols;
   g.a_halves = g.b_halves = g.d_halves = p.halves;
   g.a_mn = g.b_mn = tall;
-  g.ld = p.lds;
-  g.z = p.s * p.lds;
-  g.half = p.batch * g.z;
-  NsArgs q = g;   // B = a I + b A + c A A
+  g.factor = cubic ? co[1] * sums : sums;
+  g.diag = (cubic ? co[0] : static_cast<float>(0.5 * co[1] / co[2])) * kNsScaleA;
+  NsArgs q = g;   // B = c (A + beta I)^2 + gamma I
   q.K = p.s;
   q.a_mn = q.b_mn = 0;
-  q.Y = A;
-  q.a = co[0], q.b = co[1], q.c = co[2];
+  q.factor = co[2] / kNsScaleA;
+  q.diag = static_cast<float>(co[0] - 0.25 * co[1] * co[1] / co[2]) * kNsScaleA;
   NsArgs u{};   // X <- B X or X B
   u.batch = p.batch;
   u.M = p.rows;
@@ -313,17 +315,20 @@ cudaError_t steps_from(const Shape& p, uint8_t* ws, const T* G, int64_t ldg, int
   u.b_halves = tall ? p.halves : 2;
   u.b_mn = !tall;
   u.d_halves = 2;
-  u.a = to.scale;
-  u.out = to.D;
-  u.ldo = to.ldd;
-  u.zo = to.zd;
-  u.out_type = to.type;
+  u.factor = 1.f / kNsScaleA;
+  NsArgs last = u;
+  last.factor = to.scale / (kNsScaleA * kNsScaleX);
+  last.out = to.D;
+  last.ldo = to.ldd;
+  last.zo = to.zd;
+  last.out_type = to.type;
   for (int k = 0; k < steps && e == cudaSuccess; ++k) {
     const NsMaps& x = mX[k & 1];
-    e = launch_ns_product(kNsGram, x, x, mA, g, s);
-    if (e == cudaSuccess) e = launch_ns_product(kNsSquare, mA, mA, mB, q, s);
+    const bool end = k + 1 == steps;
+    e = launch_ns_product(kNsSym, x, x, cubic ? mB : mA, g, s);
+    if (e == cudaSuccess && !cubic) e = launch_ns_product(kNsSym, mA, mA, mB, q, s);
     if (e == cudaSuccess)
-      e = launch_ns_product(k + 1 < steps ? kNsStep : kNsLast, tall ? x : mB, tall ? mB : x, mX[(k + 1) & 1], u, s);
+      e = launch_ns_product(end ? kNsLast : kNsStep, tall ? x : mB, tall ? mB : x, mX[(k + 1) & 1], end ? last : u, s);
   }
   return e;
 }
@@ -338,6 +343,8 @@ bool settings_ok(int32_t steps, const float* coeff, float eps, float scale, floa
     co[i] = coeff ? coeff[i] : muon[i];
     if (!(std::fabs(co[i]) <= kMaxCoeff)) return false;
   }
+  // (A + beta I)^2 must not lose what it adds up to: c beta^2 = b^2 / 4c
+  if (co[2] != 0.f && !(co[1] * co[1] <= 32.f * std::fabs(co[2]) && std::fabs(co[1]) <= 64.f * std::fabs(co[2]))) return false;
   return steps >= 1 && steps <= kMaxSteps && eps > 0.f && std::isfinite(eps) && std::isfinite(scale);
 }
 

@@ -61,7 +61,8 @@ def test_large(cuda_device, rows, cols, dtype):
     check(orth(G[None])[0], G, 5)
 
 
-@pytest.mark.parametrize("steps,coeff", [(1, None), (2, None), (8, None), (12, (1.5, -0.5, 0.0)), (6, (1.875, -1.25, 0.375))])
+@pytest.mark.parametrize("steps,coeff", [(1, None), (2, None), (8, None), (12, (1.5, -0.5, 0.0)), (6, (1.875, -1.25, 0.375)),
+                                         (4, (2.0, -1.5, 0.5)), (3, (1.0, 0.0, 0.0)), (3, (1.5, 0.0, -0.5)), (2, (3.0, -4.0, 0.5))])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_steps_and_coefficients(cuda_device, steps, coeff, dtype):
     G = update(150, 260, steps, cuda_device).to(dtype)

@@ -26,7 +26,7 @@ def orth(g=A, ldg=8, bsg=64, o=A, ldo=8, bso=64, batch=1, rows=8, cols=8, dtype=
     dict(bso=0, batch=2), dict(bso=-64, batch=2), dict(batch=-1), dict(batch=65536), dict(rows=0), dict(cols=0), dict(rows=-3), dict(cols=65537, ldg=1 << 20, ldo=1 << 20),
     dict(rows=65537), dict(steps=0), dict(steps=65), dict(steps=-1), dict(eps=0.0), dict(eps=-1e-7), dict(eps=NAN), dict(eps=INF),
     dict(scale=NAN), dict(scale=INF), dict(coeff=(9, 0, 0)), dict(coeff=(0, -8.5, 0)), dict(coeff=(0, 0, NAN)), dict(coeff=(INF, 0, 0)),
-    dict(coeff=(1, 2)), dict(coeff=(1, 2, 3, 4)),
+    dict(coeff=(1, 2)), dict(coeff=(1, 2, 3, 4)), dict(coeff=(1, 4, 0.25)), dict(coeff=(1, 0.5, 1e-3)), dict(coeff=(1, 1e-5, 1e-8)),
 ])
 def test_orthogonalize(oscars_lib, kw):
     refused(orth, **kw)
