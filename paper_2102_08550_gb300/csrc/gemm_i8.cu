@@ -1,7 +1,29 @@
 // The product of a dense layer kept in 8 bits, and the rows' quantisation.
 //
-//   C[m][n] = act(sa[m] sb[n] sum_k A[m][k] B[n][k] + bias[n]),  the sum in int32
+//   C[m][n] = act(sa[m] sb[n] sum_k A[m][k] B[n][k] + bias[n]),  the sum exact
 //   scale[i] = max_j |x[i][j]| / 127,  q[i][j] = rint(x[i][j] / scale[i])
+//
+// sm_103a's tensor cores have no 8-bit integer kind.  An 8-bit integer is exact in
+// fp16, a product of two is at most 2^14, and fp32 holds sums of 1024 such products
+// exactly.  So warps turn tiles of codes into fp16 in shared memory, tcgen05
+// (kind::f16) multiplies them, and every kChunk K-blocks (1024 of K) the
+// epilogue moves the accumulator, an exact integer, to a sum in int32.
+//
+// The product is computed as rows = channels (B), columns = tokens (A): the
+// accumulator's lanes then run along a row of C, so that a store of a token's 32
+// channels is coalesced as it leaves the registers, whatever C's alignment.
+//
+// gemm_i8_kernel: persistent, one CTA per SM or a cluster of two (cta_group::2),
+// 20 warps:
+//   0       TMA of code tiles (128 channels and BN tokens, 64 of K) into a ring
+//   1       issues the products from the operand ring into one of two accumulators
+//   4-11    codes -> fp16, into the operand ring (K-major, 128-byte swizzle)
+//   12-19   accumulators -> int32 sums -> C, under the products of the next tile
+// What bounds a large product is shared memory: a pair's K-block (256 x 256 x 64)
+// brings 16 KB of codes into an SM, which are written, read, written as 32 KB and read
+// by the tensor core: 96 KB, 768 clocks at 128 bytes a clock, to 512 of products.
+#include <atomic>
+
 #include "../../include/oscars.h"
 #include "common.cuh"
 #include "internal.h"
@@ -46,51 +68,393 @@ __global__ void __launch_bounds__(256) quantize_i8_kernel(const T* __restrict__ 
 
 // ------------------------------------------------------------------ product
 struct I8Args {
-  const int8_t *A, *B;
   const float *sa, *sb, *bias;
   void* C;
-  int64_t lda, ldb, ldc;
-  int M, N, K, relu;
+  int64_t ldc;
+  int M, N, K, relu, bf16;
+  int BN, nt, mt, units, raw_stages, op_stages;   // set by the launcher
 };
 
-// four codes of a row from column k on, zero past column K
-__device__ __forceinline__ int codes4(const int8_t* row, int k, int K) {
-  const int v = *reinterpret_cast<const int*>(row + k);
-  return K - k >= 4 ? v : v & ((1 << (8 * (K - k))) - 1);
+constexpr int kK = 64, kThreads = 640, kMaxBN = 256;
+constexpr int kChunk = 16;                       // K-blocks whose sums fp32 holds exactly
+constexpr int kMaxStages = 8, kConvWarps = 8, kEpiWarps = 8;
+constexpr int kBarBytes = 512;
+constexpr int kSmem = 227 * 1024;
+// at least: one CTA an SM, and no other kernel's cluster beside it (tensor memory)
+constexpr size_t kLeast = 164 * 1024;
+static_assert(no_cluster_beside(kLeast), "no other cluster's CTA beside this kernel's");
+static_assert(kChunk * kK * 128 * 128 <= 1 << 24, "a chunk's sums are exact in fp32");
+
+struct Bars {
+  uint64_t raw_full[kMaxStages], raw_empty[kMaxStages], op_full[kMaxStages], op_empty[kMaxStages], accf[2], acce[2];
+  uint32_t tmem;
+};
+static_assert(sizeof(Bars) <= kBarBytes, "barriers fit");
+
+__device__ __forceinline__ void umma_f16_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
+                                              uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void umma_commit_pair(uint64_t* bar) {
+  asm volatile(
+      "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(
+          smem_u32(bar)),
+      "h"(static_cast<uint16_t>(0x3))
+      : "memory");
+}
+__device__ __forceinline__ void mbar_arrive_at(uint32_t cluster_bar) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+}
+// mbar_wait_keep for a barrier on which the peer CTA arrives after writing its shared memory
+__device__ __forceinline__ void mbar_wait_keep_cluster(uint32_t& limit, uint64_t* bar, uint32_t parity) {
+  uint32_t i = 0, ok = 0;
+  while (true) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(smem_u32(bar)), "r"(parity)
+        : "memory");
+    if (ok) break;
+    if (++i >= limit) {
+      limit = 1;
+      break;
+    }
+    if (i > 64) __nanosleep(64);
+  }
+}
+template <int N>
+__device__ __forceinline__ void regs_down() {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
+}
+template <int N>
+__device__ __forceinline__ void regs_up() {
+  asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
+}
+// registers: 640 threads at 96; the warps that keep sums take what the others leave
+constexpr int kLowRegs = 48, kHighRegs = 168;
+static_assert(kThreads / 128 * 96 == 3 * kLowRegs + 2 * kHighRegs, "the shares add up to the launch's registers");
+
+// four codes as fp16: a code plus 128 in the mantissa of 1024, less 1152
+__device__ __forceinline__ void codes_to_half(uint32_t w, uint32_t& lo, uint32_t& hi) {
+  const uint32_t u = w ^ 0x80808080u;
+  const uint32_t a = __byte_perm(u, 0x64646464u, 0x4140), b = __byte_perm(u, 0x64646464u, 0x4342);
+  const __half2 off = __half2half2(__ushort_as_half(0x6480));   // 1152
+  const __half2 x = __hsub2(*reinterpret_cast<const __half2*>(&a), off), y = __hsub2(*reinterpret_cast<const __half2*>(&b), off);
+  lo = *reinterpret_cast<const uint32_t*>(&x);
+  hi = *reinterpret_cast<const uint32_t*>(&y);
 }
 
-// 64 x 64 a block, 4 x 4 a thread
-template <typename T>
-__global__ void __launch_bounds__(256) gemm_i8_kernel(const __grid_constant__ I8Args p) {
-  __shared__ int sa[16][65], sb[16][65];
-  const int m0 = blockIdx.x * 64, n0 = blockIdx.y * 64, tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  int acc[4][4] = {};
-  for (int k0 = 0; k0 < p.K; k0 += 64) {
-    for (int e = threadIdx.x; e < 64 * 16; e += 256) {
-      const int kq = e & 15, i = e >> 4, k = k0 + 4 * kq;
-      sa[kq][i] = k < p.K && m0 + i < p.M ? codes4(p.A + (m0 + i) * p.lda, k, p.K) : 0;
-      sb[kq][i] = k < p.K && n0 + i < p.N ? codes4(p.B + (n0 + i) * p.ldb, k, p.K) : 0;
+// fp16 operands (format 0), K-major, fp32 accumulator
+__host__ __device__ constexpr uint32_t idesc_f16(int M, int N) {
+  return (1u << 4) | (static_cast<uint32_t>(N >> 3) << 17) | (static_cast<uint32_t>(M >> 4) << 24);
+}
+
+__device__ __forceinline__ float finish(const I8Args& a, int sum, float sa, float sb, float bias) {
+  float v = static_cast<float>(sum) * sa * sb;
+  if (a.bias) v += bias;
+  return a.relu && v < 0.f ? 0.f : v;
+}
+
+template <int CL>
+__global__ void __launch_bounds__(kThreads, 1) gemm_i8_kernel(const __grid_constant__ CUtensorMap mapW,
+                                                              const __grid_constant__ CUtensorMap mapX,
+                                                              const __grid_constant__ I8Args a) {
+  extern __shared__ uint8_t i8_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(i8_raw) + 1023) & ~uintptr_t(1023));
+  const int bn = a.BN / CL, rows = 128 + bn;       // this CTA's tokens of a tile; rows of codes of a K-block
+  const int raw_bytes = rows * kK, op_bytes = 2 * raw_bytes;
+  uint8_t* op = smem;                              // [op stages][128 channels | bn tokens][128 bytes]
+  uint8_t* raw = smem + a.op_stages * op_bytes;    // [raw stages][128 channels | bn tokens][64 bytes]
+  Bars* bars = reinterpret_cast<Bars*>(raw + a.raw_stages * raw_bytes);
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+  const int rank = CL > 1 ? static_cast<int>(cluster_ctarank()) : 0;
+  const int nk = (a.K + kK - 1) / kK;
+  const int u0 = blockIdx.x / CL, ustep = gridDim.x / CL;
+  const int mu = a.mt / CL;                        // row tiles (of channels); rows fastest
+
+  if (threadIdx.x == 0) {
+    prefetch_tmap(&mapW);
+    prefetch_tmap(&mapX);
+    for (int i = 0; i < a.raw_stages; ++i) {
+      mbar_init(&bars->raw_full[i], 1);
+      mbar_init(&bars->raw_empty[i], kConvWarps);
     }
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < 16; ++k)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = __dp4a(sa[k][ty + 16 * i], sb[k][tx + 16 * j], acc[i][j]);
-    __syncthreads();
+    for (int i = 0; i < a.op_stages; ++i) {
+      mbar_init(&bars->op_full[i], kConvWarps * CL);
+      mbar_init(&bars->op_empty[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&bars->accf[i], 1);
+      mbar_init(&bars->acce[i], kEpiWarps * CL);
+    }
+    fence_barrier_init();
+    fence_proxy_async_smem();
   }
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int m = m0 + ty + 16 * i, n = n0 + tx + 16 * j;
-      if (m >= p.M || n >= p.N) continue;
-      float v = static_cast<float>(acc[i][j]) * p.sa[m] * p.sb[n];
-      if (p.bias) v += p.bias[n];
-      if (p.relu) v = v < 0.f ? 0.f : v;
-      static_cast<T*>(p.C)[m * p.ldc + n] = static_cast<T>(v);
+  if (warp == 2) {
+    if (CL == 1) {
+      tmem_alloc(&bars->tmem, 512);
+      tmem_relinquish();
+    } else {
+      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars->tmem)), "r"(512)
+                   : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
     }
+  }
+  tc_fence_before();
+  if (CL > 1) cluster_sync();   // the peer's barriers are initialised before anything arrives on them
+  else __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = bars->tmem;
+  pdl_wait();
+  pdl_trigger();
+
+  if (warp < 4) {
+    regs_down<kLowRegs>();
+    if (warp == 0 && lane == 0) {
+      // ---- TMA of codes
+      int it = 0, s = 0, ph = 1;
+      bool ok = true;
+      for (int u = u0; ok && u < a.units; u += ustep) {
+        const int n0 = ((u % mu) * CL + rank) * 128, m0 = (u / mu) * a.BN + rank * bn;
+        for (int kb = 0; kb < nk; ++kb, ++it) {
+          if (it >= a.raw_stages && !(ok = mbar_wait(&bars->raw_empty[s], ph, nullptr, kDevTimeoutEmpty))) break;
+          uint8_t* at = raw + s * raw_bytes;
+          mbar_arrive_expect_tx(&bars->raw_full[s], raw_bytes);
+          tma_load_3d(at, &mapW, kb * kK, n0, 0, &bars->raw_full[s]);
+          tma_load_3d(at + 128 * kK, &mapX, kb * kK, m0, 0, &bars->raw_full[s]);
+          if (++s == a.raw_stages) {
+            s = 0;
+            ph ^= 1;
+          }
+        }
+      }
+      // the copies have landed before this CTA ends: the converting warps wait for each of them, and after a
+      // timeout of theirs this thread's waits on the freed slots run out later than any copy takes
+      for (int i = it > a.raw_stages ? it - a.raw_stages : 0; i < it; ++i) {
+        if (!mbar_wait(&bars->raw_full[i % a.raw_stages], (i / a.raw_stages) & 1, nullptr, kDevTimeoutFull)) break;
+      }
+    } else if (warp == 1 && rank == 0) {
+      // ---- MMA issuer (the leader's, of a pair); the warp stays converged and one elected lane issues
+      const uint32_t idesc = idesc_f16(128 * CL, a.BN);
+      const uint32_t op0 = smem_u32(op);
+      int s = 0, ph = 0, t = 0;   // t: accumulations begun
+      uint32_t limit = kSpinLimit;
+      for (int u = u0; u < a.units; u += ustep) {
+        for (int k0 = 0; k0 < nk; k0 += kChunk, ++t) {
+          const int b = t & 1, k1 = k0 + kChunk < nk ? k0 + kChunk : nk;
+          if (t >= 2) mbar_wait_keep(limit, &bars->acce[b], ((t >> 1) + 1) & 1, nullptr, kDevTimeoutAccum);
+          tc_fence_after();
+          const uint32_t acc = tmem + static_cast<uint32_t>(b * kMaxBN);
+          for (int kb = k0; kb < k1; ++kb) {
+            if (CL > 1) mbar_wait_keep_cluster(limit, &bars->op_full[s], ph);
+            else mbar_wait_keep(limit, &bars->op_full[s], ph, nullptr, kDevTimeoutFull);
+            tc_fence_after();
+            const uint64_t wd = smem_desc_k128(op0 + s * op_bytes), xd = smem_desc_k128(op0 + s * op_bytes + 128 * 128);
+            if (elect_one() && limit > 1) {
+#pragma unroll
+              for (int j = 0; j < kK / 16; ++j) {
+                if (CL > 1) umma_f16_pair(acc, wd + 2 * j, xd + 2 * j, idesc, (kb - k0) | j ? 1u : 0u);
+                else umma_bf16(acc, wd + 2 * j, xd + 2 * j, idesc, (kb - k0) | j ? 1u : 0u);
+              }
+              if (CL > 1) umma_commit_pair(&bars->op_empty[s]);
+              else umma_commit(&bars->op_empty[s]);
+            }
+            __syncwarp();
+            if (++s == a.op_stages) {
+              s = 0;
+              ph ^= 1;
+            }
+          }
+          if (elect_one() && limit > 1) {
+            if (CL > 1) umma_commit_pair(&bars->accf[b]);
+            else umma_commit(&bars->accf[b]);
+          }
+          __syncwarp();
+        }
+      }
+    }
+  } else if (warp < 4 + kConvWarps) {
+    // ---- codes to fp16: 16 codes of a row a thread and turn, a row's 64 in four neighbouring lanes
+    regs_down<kLowRegs>();
+    const int th = threadIdx.x - 128, c = th & 3;
+    int rs = 0, rph = 0, os = 0, oph = 1, it = 0;
+    bool ok = true;
+    for (int u = u0; ok && u < a.units; u += ustep) {
+      for (int kb = 0; kb < nk; ++kb, ++it) {
+        ok = mbar_wait_warp(&bars->raw_full[rs], rph, nullptr, kDevTimeoutFull);
+        if (ok && it >= a.op_stages) ok = mbar_wait_warp(&bars->op_empty[os], oph, nullptr, kDevTimeoutEmpty);
+        if (!ok) break;
+        const uint8_t* from = raw + rs * raw_bytes;
+        uint8_t* to = op + os * op_bytes;
+#pragma unroll 2
+        for (int r = th >> 2; r < rows; r += kConvWarps * 8) {
+          const uint4 w = *reinterpret_cast<const uint4*>(from + r * kK + 16 * c);
+          uint4 x, y;
+          codes_to_half(w.x, x.x, x.y);
+          codes_to_half(w.y, x.z, x.w);
+          codes_to_half(w.z, y.x, y.y);
+          codes_to_half(w.w, y.z, y.w);
+          *reinterpret_cast<uint4*>(to + r * 128 + (((2 * c) ^ (r & 7)) << 4)) = x;
+          *reinterpret_cast<uint4*>(to + r * 128 + (((2 * c + 1) ^ (r & 7)) << 4)) = y;
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(&bars->raw_empty[rs]);
+          if (CL > 1) mbar_arrive_at(cluster_addr(&bars->op_full[os], 0));
+          else mbar_arrive(&bars->op_full[os]);
+        }
+        if (++rs == a.raw_stages) {
+          rs = 0;
+          rph ^= 1;
+        }
+        if (++os == a.op_stages) {
+          os = 0;
+          oph ^= 1;
+        }
+      }
+    }
+    // no commit of the leader may still be on its way to this CTA when it ends
+    for (int i = it > a.op_stages ? it - a.op_stages : 0; ok && i < it; ++i)
+      ok = mbar_wait_warp(&bars->op_empty[i % a.op_stages], (i / a.op_stages) & 1, nullptr, kDevTimeoutEmpty);
+  } else {
+    // ---- sums and C: thread = one channel and half of the tile's tokens
+    regs_up<kHighRegs>();
+    const int quarter = warp & 3, span = a.BN / 2, cb = warp < 16 ? 0 : span;
+    int t = 0;
+    bool ok = true;
+    for (int u = u0; ok && u < a.units; u += ustep) {
+      const int n = ((u % mu) * CL + rank) * 128 + 32 * quarter + lane, m0 = (u / mu) * a.BN + cb;
+      const uint32_t row0 = tmem + (static_cast<uint32_t>(32 * quarter) << 16) + cb;
+      const float sb = n < a.N ? __ldg(a.sb + n) : 0.f, bias = a.bias && n < a.N ? __ldg(a.bias + n) : 0.f;
+      float sa[kMaxBN / 64];   // lane l: tokens l, 32 + l, ...
+#pragma unroll
+      for (int i = 0; i < kMaxBN / 64; ++i) sa[i] = m0 + 32 * i + lane < a.M && 32 * i < span ? __ldg(a.sa + m0 + 32 * i + lane) : 0.f;
+      int sum[kMaxBN / 32][16];
+#pragma unroll
+      for (int g = 0; g < kMaxBN / 32; ++g)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sum[g][e] = 0;
+      for (int k0 = 0; k0 < nk; k0 += kChunk, ++t) {
+        const int b = t & 1;
+        if (!(ok = mbar_wait_warp(&bars->accf[b], (t >> 1) & 1, nullptr, kDevTimeoutAccum))) break;
+        tc_fence_after();
+#pragma unroll
+        for (int g = 0; g < kMaxBN / 32; ++g)
+          if (16 * g < span) {
+            float v[16];
+            tmem_ld_32x32b_x16(row0 + b * kMaxBN + 16 * g, v);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) sum[g][e] += __float2int_rn(v[e]);
+          }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          if (CL > 1) mbar_arrive_at(cluster_addr(&bars->acce[b], 0));
+          else mbar_arrive(&bars->acce[b]);
+        }
+      }
+      if (!ok) break;
+#pragma unroll
+      for (int g = 0; g < kMaxBN / 32; ++g)
+        if (16 * g < span) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const float s = __shfl_sync(0xffffffffu, sa[g / 2], (g & 1) * 16 + e);
+            const int m = m0 + 16 * g + e;
+            if (m < a.M && n < a.N) {
+              const float v = finish(a, sum[g][e], s, sb, bias);
+              if (a.bf16) static_cast<__nv_bfloat16*>(a.C)[m * a.ldc + n] = __float2bfloat16_rn(v);
+              else static_cast<float*>(a.C)[m * a.ldc + n] = v;
+            }
+          }
+        }
+    }
+  }
+  tc_fence_before();
+  if (CL > 1) cluster_sync();   // the pair's products and arrivals are done in both CTAs
+  else __syncthreads();
+  if (warp == 2) {
+    tc_fence_after();
+    if (CL == 1) tmem_dealloc(tmem, 512);
+    else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+  }
+}
+
+constexpr int kMaxDevices = 64;
+struct DevInfo {
+  std::atomic<int> sms{0}, pairs{0};
+};
+DevInfo g_dev[kMaxDevices];
+
+template <int CL>
+cudaLaunchConfig_t config(cudaLaunchAttribute* attr, int grid, size_t smem, cudaStream_t s) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid, 1, 1);
+  cfg.blockDim = dim3(kThreads, 1, 1);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cfg.attrs = attr;
+  cfg.numAttrs = 0;
+  if (CL > 1) {
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = CL;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cfg.numAttrs = 1;
+  }
+  return cfg;
+}
+
+// {SMs, resident clusters of two} of the current device, queried once
+void device_room(int& sms, int& pairs) {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) dev = 0;
+  sms = g_dev[dev].sms.load(std::memory_order_relaxed);
+  pairs = g_dev[dev].pairs.load(std::memory_order_relaxed);
+  if (sms > 0 && pairs > 0) return;
+  if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || sms < 1) sms = 1;
+  cudaLaunchAttribute attr[1];
+  pairs = 0;
+  if (allow_smem(gemm_i8_kernel<2>, kSmem) == cudaSuccess) {
+    cudaLaunchConfig_t cfg = config<2>(attr, 2, kSmem, nullptr);
+    if (cudaOccupancyMaxActiveClusters(&pairs, gemm_i8_kernel<2>, &cfg) != cudaSuccess) pairs = 0;
+  }
+  cudaGetLastError();
+  if (pairs < 1) pairs = 1;
+  g_dev[dev].sms.store(sms, std::memory_order_relaxed);
+  g_dev[dev].pairs.store(pairs, std::memory_order_relaxed);
+}
+
+template <int CL>
+cudaError_t launch_i8(const CUtensorMap& mW, const CUtensorMap& mX, I8Args a, int grid, cudaStream_t s) {
+  const int raw = (128 + a.BN / CL) * kK, room = kSmem - 1024 - kBarBytes;
+  // operand stages in twice as many bytes as code stages, up to 4 and 6
+  a.op_stages = 4;
+  while (a.op_stages * 2 * raw + 2 * raw > room) --a.op_stages;
+  a.raw_stages = (room - a.op_stages * 2 * raw) / raw;
+  if (a.raw_stages > 6) a.raw_stages = 6;
+  size_t smem = 1024 + static_cast<size_t>(a.op_stages) * 2 * raw + static_cast<size_t>(a.raw_stages) * raw + kBarBytes;
+  if (smem < kLeast) smem = kLeast;
+  cudaError_t e = allow_smem(gemm_i8_kernel<CL>, kSmem);
+  if (e != cudaSuccess) return e;
+  cudaLaunchAttribute attr[1];
+  const cudaLaunchConfig_t cfg = config<CL>(attr, grid, smem, s);
+  return cudaLaunchKernelEx(&cfg, gemm_i8_kernel<CL>, mW, mX, a);
+}
+
+bool code_map(CUtensorMap* m, const int8_t* base, int64_t ld, int K, int rows, int box_rows) {
+  const cuuint64_t dims[3] = {static_cast<cuuint64_t>(K), static_cast<cuuint64_t>(rows), 1};
+  const cuuint64_t strides[2] = {static_cast<cuuint64_t>(ld), static_cast<cuuint64_t>(ld)};   // the third dimension has one entry
+  const cuuint32_t box[3] = {kK, static_cast<cuuint32_t>(box_rows), 1};
+  return encode_map(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, base, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_NONE);
 }
 
 }  // namespace
@@ -128,12 +492,43 @@ oscars_status oscars_gemm_i8_nt(const int8_t* A, int64_t lda, const float* scale
   if ((reinterpret_cast<uintptr_t>(scale_a) | reinterpret_cast<uintptr_t>(scale_b) | reinterpret_cast<uintptr_t>(bias)) & 3)
     return OSCARS_EINVAL;
   if (reinterpret_cast<uintptr_t>(C) & (dtype == OSCARS_F32 ? 3 : 1)) return OSCARS_EINVAL;
-  const I8Args p{A, B, scale_a, scale_b, bias, C, lda, ldb, ldc, M, N, K, relu};
-  const dim3 grid((M + 63) / 64, (N + 63) / 64);
+  I8Args p{scale_a, scale_b, bias, C, ldc, M, N, K, relu, dtype == OSCARS_BF16, 0, 0, 0, 0, 0, 0};
+  int sms, pairs;
+  device_room(sms, pairs);
+  // the shape with the least estimated time: waves of tiles times the longer of a K-block's products (2 BN
+  // clocks), shared-memory traffic (3 clocks a row of codes) and loads (45 bytes a clock), plus fixed parts
+  const int nk = (K + kK - 1) / kK;
+  double best = 0.0;
+  int cl = 1;
+  for (int c = 1; c <= 2; ++c) {
+    const int mt = ((N + 127) / 128 + c - 1) / c * c;
+    for (int bn = 32; bn <= kMaxBN; bn *= 2) {
+      const int nt = (M + bn - 1) / bn, rows = 128 + bn / c;
+      const int64_t units = static_cast<int64_t>(mt / c) * nt;
+      const int room = c == 2 ? pairs : sms;
+      const double waves = static_cast<double>((units + room - 1) / room);
+      double kb = 2.0 * bn;
+      kb = kb > 3.0 * rows ? kb : 3.0 * rows;
+      kb = kb > rows * kK / 45.0 ? kb : rows * kK / 45.0;
+      const double cost = waves * (nk * kb + 600.0) + 15.0 * bn + (c == 2 ? 1500.0 : 0.0);
+      if (best == 0.0 || cost < best) {
+        best = cost;
+        cl = c;
+        p.BN = bn;
+        p.mt = mt;
+        p.nt = nt;
+      }
+    }
+  }
+  const int64_t units = static_cast<int64_t>(p.mt / cl) * p.nt;
+  if (units > INT32_MAX / 2) return OSCARS_EINVAL;
+  p.units = static_cast<int>(units);
+  CUtensorMap mW, mX;
+  if (!code_map(&mW, B, ldb, K, N, 128) || !code_map(&mX, A, lda, K, M, p.BN / cl)) return OSCARS_ECUDA;
+  const int room = cl == 2 ? pairs : sms, grid = (p.units < room ? p.units : room) * cl;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (dtype == OSCARS_F32) gemm_i8_kernel<float><<<grid, 256, 0, s>>>(p);
-  else gemm_i8_kernel<__nv_bfloat16><<<grid, 256, 0, s>>>(p);
-  return cudaGetLastError() == cudaSuccess ? OSCARS_OK : OSCARS_ECUDA;
+  const cudaError_t e = cl == 2 ? launch_i8<2>(mW, mX, p, grid, s) : launch_i8<1>(mW, mX, p, grid, s);
+  return e == cudaSuccess ? OSCARS_OK : OSCARS_ECUDA;
 }
 
 }  // extern "C"
