@@ -72,7 +72,7 @@ struct I8Args {
   void* C;
   int64_t ldc;
   int M, N, K, relu, bf16;
-  int BN, nt, mt, units, raw_stages, op_stages;   // set by the launcher
+  int BN, nt, mt, units, split, raw_stages, op_stages;   // set by the launcher
 };
 
 constexpr int kK = 64, kThreads = 640, kMaxBN = 256;
@@ -162,7 +162,7 @@ __device__ __forceinline__ float finish(const I8Args& a, int sum, float sa, floa
   return a.relu && v < 0.f ? 0.f : v;
 }
 
-template <int CL>
+template <int CL, bool kSplit>
 __global__ void __launch_bounds__(kThreads, 1) gemm_i8_kernel(const __grid_constant__ CUtensorMap mapW,
                                                               const __grid_constant__ CUtensorMap mapX,
                                                               const __grid_constant__ I8Args a) {
@@ -174,9 +174,12 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_i8_kernel(const __grid_const
   uint8_t* raw = smem + a.op_stages * op_bytes;    // [raw stages][128 channels | bn tokens][64 bytes]
   Bars* bars = reinterpret_cast<Bars*>(raw + a.raw_stages * raw_bytes);
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+  const int part = kSplit ? static_cast<int>(cluster_ctarank()) : 0;
   const int rank = CL > 1 ? static_cast<int>(cluster_ctarank()) : 0;
   const int nk = (a.K + kK - 1) / kK;
-  const int u0 = blockIdx.x / CL, ustep = gridDim.x / CL;
+  const int kb0 = kSplit ? nk * part / a.split : 0, kb1 = kSplit ? nk * (part + 1) / a.split : nk;   // K-blocks of this CTA
+  const int per = kSplit ? a.split : CL;           // CTAs of a tile
+  const int u0 = blockIdx.x / per, ustep = gridDim.x / per;
   const int mu = a.mt / CL;                        // row tiles (of channels); rows fastest
 
   if (threadIdx.x == 0) {
@@ -184,10 +187,10 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_i8_kernel(const __grid_const
     prefetch_tmap(&mapX);
     for (int i = 0; i < a.raw_stages; ++i) {
       mbar_init(&bars->raw_full[i], 1);
-      mbar_init(&bars->raw_empty[i], kConvWarps);
+      mbar_init(&bars->raw_empty[i], kConvWarps / 2);
     }
     for (int i = 0; i < a.op_stages; ++i) {
-      mbar_init(&bars->op_full[i], kConvWarps * CL);
+      mbar_init(&bars->op_full[i], kConvWarps / 2 * CL);
       mbar_init(&bars->op_empty[i], 1);
     }
     for (int i = 0; i < 2; ++i) {
@@ -208,12 +211,10 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_i8_kernel(const __grid_const
     }
   }
   tc_fence_before();
-  if (CL > 1) cluster_sync();   // the peer's barriers are initialised before anything arrives on them
+  if (CL > 1 || kSplit) cluster_sync();   // the peers run, and their barriers are initialised
   else __syncthreads();
   tc_fence_after();
   const uint32_t tmem = bars->tmem;
-  pdl_wait();
-  pdl_trigger();
 
   if (warp < 4) {
     regs_down<kLowRegs>();
@@ -223,7 +224,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_i8_kernel(const __grid_const
       bool ok = true;
       for (int u = u0; ok && u < a.units; u += ustep) {
         const int n0 = ((u % mu) * CL + rank) * 128, m0 = (u / mu) * a.BN + rank * bn;
-        for (int kb = 0; kb < nk; ++kb, ++it) {
+        for (int kb = kb0; kb < kb1; ++kb, ++it) {
           if (it >= a.raw_stages && !(ok = mbar_wait(&bars->raw_empty[s], ph, nullptr, kDevTimeoutEmpty))) break;
           uint8_t* at = raw + s * raw_bytes;
           mbar_arrive_expect_tx(&bars->raw_full[s], raw_bytes);
@@ -247,8 +248,8 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_i8_kernel(const __grid_const
       int s = 0, ph = 0, t = 0;   // t: accumulations begun
       uint32_t limit = kSpinLimit;
       for (int u = u0; u < a.units; u += ustep) {
-        for (int k0 = 0; k0 < nk; k0 += kChunk, ++t) {
-          const int b = t & 1, k1 = k0 + kChunk < nk ? k0 + kChunk : nk;
+        for (int k0 = kb0; k0 < kb1; k0 += kChunk, ++t) {
+          const int b = t & 1, k1 = k0 + kChunk < kb1 ? k0 + kChunk : kb1;
           if (t >= 2) mbar_wait_keep(limit, &bars->acce[b], ((t >> 1) + 1) & 1, nullptr, kDevTimeoutAccum);
           tc_fence_after();
           const uint32_t acc = tmem + static_cast<uint32_t>(b * kMaxBN);
@@ -281,28 +282,38 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_i8_kernel(const __grid_const
       }
     }
   } else if (warp < 4 + kConvWarps) {
-    // ---- codes to fp16: 16 codes of a row a thread and turn, a row's 64 in four neighbouring lanes
+    // ---- codes to fp16: two groups of four warps take K-blocks in turn, so that one's waits and stores run under
+    // the other's; 16 codes of a row a thread and turn, a row's 64 in four neighbouring lanes
     regs_down<kLowRegs>();
-    const int th = threadIdx.x - 128, c = th & 3;
-    int rs = 0, rph = 0, os = 0, oph = 1, it = 0;
+    const int th = threadIdx.x & 127, c = th & 3, group = (warp >> 2) - 1;
+    int it = 0;
     bool ok = true;
     for (int u = u0; ok && u < a.units; u += ustep) {
-      for (int kb = 0; kb < nk; ++kb, ++it) {
-        ok = mbar_wait_warp(&bars->raw_full[rs], rph, nullptr, kDevTimeoutFull);
-        if (ok && it >= a.op_stages) ok = mbar_wait_warp(&bars->op_empty[os], oph, nullptr, kDevTimeoutEmpty);
+      for (int kb = kb0; kb < kb1; ++kb, ++it) {
+        if ((it & 1) != group) continue;
+        const int rs = it % a.raw_stages, os = it % a.op_stages;
+        ok = mbar_wait_warp(&bars->raw_full[rs], (it / a.raw_stages) & 1, nullptr, kDevTimeoutFull);
+        if (ok && it >= a.op_stages) ok = mbar_wait_warp(&bars->op_empty[os], (it / a.op_stages + 1) & 1, nullptr, kDevTimeoutEmpty);
         if (!ok) break;
-        const uint8_t* from = raw + rs * raw_bytes;
+        const uint8_t* from = raw + rs * raw_bytes + 16 * c;
         uint8_t* to = op + os * op_bytes;
-#pragma unroll 2
-        for (int r = th >> 2; r < rows; r += kConvWarps * 8) {
-          const uint4 w = *reinterpret_cast<const uint4*>(from + r * kK + 16 * c);
-          uint4 x, y;
-          codes_to_half(w.x, x.x, x.y);
-          codes_to_half(w.y, x.z, x.w);
-          codes_to_half(w.z, y.x, y.y);
-          codes_to_half(w.w, y.z, y.w);
-          *reinterpret_cast<uint4*>(to + r * 128 + (((2 * c) ^ (r & 7)) << 4)) = x;
-          *reinterpret_cast<uint4*>(to + r * 128 + (((2 * c + 1) ^ (r & 7)) << 4)) = y;
+        for (int r0 = th >> 2; r0 < rows; r0 += 128) {
+          uint4 w[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (r0 + 32 * i < rows) w[i] = *reinterpret_cast<const uint4*>(from + (r0 + 32 * i) * kK);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int r = r0 + 32 * i;
+            if (r >= rows) break;
+            uint4 x, y;
+            codes_to_half(w[i].x, x.x, x.y);
+            codes_to_half(w[i].y, x.z, x.w);
+            codes_to_half(w[i].z, y.x, y.y);
+            codes_to_half(w[i].w, y.z, y.w);
+            *reinterpret_cast<uint4*>(to + r * 128 + (((2 * c) ^ (r & 7)) << 4)) = x;
+            *reinterpret_cast<uint4*>(to + r * 128 + (((2 * c + 1) ^ (r & 7)) << 4)) = y;
+          }
         }
         fence_proxy_async_smem();
         __syncwarp();
@@ -310,14 +321,6 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_i8_kernel(const __grid_const
           mbar_arrive(&bars->raw_empty[rs]);
           if (CL > 1) mbar_arrive_at(cluster_addr(&bars->op_full[os], 0));
           else mbar_arrive(&bars->op_full[os]);
-        }
-        if (++rs == a.raw_stages) {
-          rs = 0;
-          rph ^= 1;
-        }
-        if (++os == a.op_stages) {
-          os = 0;
-          oph ^= 1;
         }
       }
     }
@@ -342,7 +345,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_i8_kernel(const __grid_const
       for (int g = 0; g < kMaxBN / 32; ++g)
 #pragma unroll
         for (int e = 0; e < 16; ++e) sum[g][e] = 0;
-      for (int k0 = 0; k0 < nk; k0 += kChunk, ++t) {
+      for (int k0 = kb0; k0 < kb1; k0 += kChunk, ++t) {
         const int b = t & 1;
         if (!(ok = mbar_wait_warp(&bars->accf[b], (t >> 1) & 1, nullptr, kDevTimeoutAccum))) break;
         tc_fence_after();
@@ -362,25 +365,57 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_i8_kernel(const __grid_const
         }
       }
       if (!ok) break;
+      if constexpr (kSplit) {   // partial sums [token][channel] where the operands were: the products have read them
+        int* out = reinterpret_cast<int*>(op) + cb * 128 + 32 * quarter + lane;
 #pragma unroll
-      for (int g = 0; g < kMaxBN / 32; ++g)
-        if (16 * g < span) {
+        for (int g = 0; g < kMaxBN / 32; ++g)
+          if (16 * g < span) {
 #pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const float s = __shfl_sync(0xffffffffu, sa[g / 2], (g & 1) * 16 + e);
-            const int m = m0 + 16 * g + e;
-            if (m < a.M && n < a.N) {
-              const float v = finish(a, sum[g][e], s, sb, bias);
-              if (a.bf16) static_cast<__nv_bfloat16*>(a.C)[m * a.ldc + n] = __float2bfloat16_rn(v);
-              else static_cast<float*>(a.C)[m * a.ldc + n] = v;
+            for (int e = 0; e < 16; ++e) out[(16 * g + e) * 128] = sum[g][e];
+          }
+      } else {
+#pragma unroll
+        for (int g = 0; g < kMaxBN / 32; ++g)
+          if (16 * g < span) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const float s = __shfl_sync(0xffffffffu, sa[g / 2], (g & 1) * 16 + e);
+              const int m = m0 + 16 * g + e;
+              if (m < a.M && n < a.N) {
+                const float v = finish(a, sum[g][e], s, sb, bias);
+                if (a.bf16) static_cast<__nv_bfloat16*>(a.C)[m * a.ldc + n] = __float2bfloat16_rn(v);
+                else static_cast<float*>(a.C)[m * a.ldc + n] = v;
+              }
             }
           }
-        }
+      }
     }
   }
   tc_fence_before();
-  if (CL > 1) cluster_sync();   // the pair's products and arrivals are done in both CTAs
+  if (CL > 1 || kSplit) cluster_sync();   // the pair's products and arrivals are done in both CTAs; every part's sums are there
   else __syncthreads();
+  if constexpr (kSplit) {
+    // each CTA adds up its tokens of the tile over the parts, four channels a thread
+    const int n0 = (u0 % mu) * 128, m0 = (u0 / mu) * a.BN, tokens = a.BN / a.split;
+    for (int i = threadIdx.x; i < tokens * 32; i += kThreads) {
+      const int tok = part * tokens + i / 32, ch = (i % 32) * 4, m = m0 + tok;
+      int4 s = make_int4(0, 0, 0, 0);
+      for (int p = 0; p < a.split; ++p) {
+        const float4 f = ld_dsmem_f32x4(reinterpret_cast<const float*>(op) + tok * 128 + ch, p);
+        s.x += __float_as_int(f.x), s.y += __float_as_int(f.y), s.z += __float_as_int(f.z), s.w += __float_as_int(f.w);
+      }
+      const int v[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int n = n0 + ch + e;
+        if (m >= a.M || n >= a.N) continue;
+        const float y = finish(a, v[e], __ldg(a.sa + m), __ldg(a.sb + n), a.bias ? __ldg(a.bias + n) : 0.f);
+        if (a.bf16) static_cast<__nv_bfloat16*>(a.C)[m * a.ldc + n] = __float2bfloat16_rn(y);
+        else static_cast<float*>(a.C)[m * a.ldc + n] = y;
+      }
+    }
+    cluster_sync();   // no CTA ends while a peer reads its sums
+  }
   if (warp == 2) {
     tc_fence_after();
     if (CL == 1) tmem_dealloc(tmem, 512);
@@ -394,8 +429,7 @@ struct DevInfo {
 };
 DevInfo g_dev[kMaxDevices];
 
-template <int CL>
-cudaLaunchConfig_t config(cudaLaunchAttribute* attr, int grid, size_t smem, cudaStream_t s) {
+cudaLaunchConfig_t config(cudaLaunchAttribute* attr, int cluster, int grid, size_t smem, cudaStream_t s) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(grid, 1, 1);
   cfg.blockDim = dim3(kThreads, 1, 1);
@@ -403,9 +437,9 @@ cudaLaunchConfig_t config(cudaLaunchAttribute* attr, int grid, size_t smem, cuda
   cfg.stream = s;
   cfg.attrs = attr;
   cfg.numAttrs = 0;
-  if (CL > 1) {
+  if (cluster > 1) {
     attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = CL;
+    attr[0].val.clusterDim.x = cluster;
     attr[0].val.clusterDim.y = 1;
     attr[0].val.clusterDim.z = 1;
     cfg.numAttrs = 1;
@@ -423,9 +457,9 @@ void device_room(int& sms, int& pairs) {
   if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || sms < 1) sms = 1;
   cudaLaunchAttribute attr[1];
   pairs = 0;
-  if (allow_smem(gemm_i8_kernel<2>, kSmem) == cudaSuccess) {
-    cudaLaunchConfig_t cfg = config<2>(attr, 2, kSmem, nullptr);
-    if (cudaOccupancyMaxActiveClusters(&pairs, gemm_i8_kernel<2>, &cfg) != cudaSuccess) pairs = 0;
+  if (allow_smem(gemm_i8_kernel<2, false>, kSmem) == cudaSuccess) {
+    cudaLaunchConfig_t cfg = config(attr, 2, 2, kSmem, nullptr);
+    if (cudaOccupancyMaxActiveClusters(&pairs, gemm_i8_kernel<2, false>, &cfg) != cudaSuccess) pairs = 0;
   }
   cudaGetLastError();
   if (pairs < 1) pairs = 1;
@@ -433,21 +467,20 @@ void device_room(int& sms, int& pairs) {
   g_dev[dev].pairs.store(pairs, std::memory_order_relaxed);
 }
 
-template <int CL>
+template <int CL, bool kSplit>
 cudaError_t launch_i8(const CUtensorMap& mW, const CUtensorMap& mX, I8Args a, int grid, cudaStream_t s) {
   const int raw = (128 + a.BN / CL) * kK, room = kSmem - 1024 - kBarBytes;
-  // operand stages in twice as many bytes as code stages, up to 4 and 6
-  a.op_stages = 4;
-  while (a.op_stages * 2 * raw + 2 * raw > room) --a.op_stages;
-  a.raw_stages = (room - a.op_stages * 2 * raw) / raw;
-  if (a.raw_stages > 6) a.raw_stages = 6;
+  // even numbers: a slot belongs to one of the two converting groups, which sees each of its phases
+  a.op_stages = 8 * raw + 2 * raw > room ? 2 : 4;
+  a.raw_stages = (room - a.op_stages * 2 * raw) / raw / 2 * 2;
+  if (a.raw_stages > kMaxStages) a.raw_stages = kMaxStages;
   size_t smem = 1024 + static_cast<size_t>(a.op_stages) * 2 * raw + static_cast<size_t>(a.raw_stages) * raw + kBarBytes;
   if (smem < kLeast) smem = kLeast;
-  cudaError_t e = allow_smem(gemm_i8_kernel<CL>, kSmem);
+  cudaError_t e = allow_smem(gemm_i8_kernel<CL, kSplit>, kSmem);
   if (e != cudaSuccess) return e;
   cudaLaunchAttribute attr[1];
-  const cudaLaunchConfig_t cfg = config<CL>(attr, grid, smem, s);
-  return cudaLaunchKernelEx(&cfg, gemm_i8_kernel<CL>, mW, mX, a);
+  const cudaLaunchConfig_t cfg = config(attr, kSplit ? a.split : CL, grid, smem, s);
+  return cudaLaunchKernelEx(&cfg, gemm_i8_kernel<CL, kSplit>, mW, mX, a);
 }
 
 bool code_map(CUtensorMap* m, const int8_t* base, int64_t ld, int K, int rows, int box_rows) {
@@ -492,7 +525,7 @@ oscars_status oscars_gemm_i8_nt(const int8_t* A, int64_t lda, const float* scale
   if ((reinterpret_cast<uintptr_t>(scale_a) | reinterpret_cast<uintptr_t>(scale_b) | reinterpret_cast<uintptr_t>(bias)) & 3)
     return OSCARS_EINVAL;
   if (reinterpret_cast<uintptr_t>(C) & (dtype == OSCARS_F32 ? 3 : 1)) return OSCARS_EINVAL;
-  I8Args p{scale_a, scale_b, bias, C, ldc, M, N, K, relu, dtype == OSCARS_BF16, 0, 0, 0, 0, 0, 0};
+  I8Args p{scale_a, scale_b, bias, C, ldc, M, N, K, relu, dtype == OSCARS_BF16, 0, 0, 0, 0, 1, 0, 0};
   int sms, pairs;
   device_room(sms, pairs);
   // the shape with the least estimated time: waves of tiles times the longer of a K-block's products (2 BN
@@ -506,17 +539,22 @@ oscars_status oscars_gemm_i8_nt(const int8_t* A, int64_t lda, const float* scale
       const int nt = (M + bn - 1) / bn, rows = 128 + bn / c;
       const int64_t units = static_cast<int64_t>(mt / c) * nt;
       const int room = c == 2 ? pairs : sms;
-      const double waves = static_cast<double>((units + room - 1) / room);
       double kb = 2.0 * bn;
       kb = kb > 3.0 * rows ? kb : 3.0 * rows;
       kb = kb > rows * kK / 45.0 ? kb : rows * kK / 45.0;
-      const double cost = waves * (nk * kb + 600.0) + 15.0 * bn + (c == 2 ? 1500.0 : 0.0);
-      if (best == 0.0 || cost < best) {
-        best = cost;
-        cl = c;
-        p.BN = bn;
-        p.mt = mt;
-        p.nt = nt;
+      // few tiles: the K-blocks of each over a cluster of `split` CTAs, whose sums meet in shared memory
+      for (int split = 1; split <= (c == 1 ? 8 : 1); split *= 2) {
+        if (split > 1 && (units * split > (split == 8 ? sms * 3 / 4 : sms * 7 / 8) || nk < 2 * split || bn < 4 * split)) break;
+        const double waves = split > 1 ? 1.0 : static_cast<double>((units + room - 1) / room);
+        const double cost = waves * ((nk + split - 1) / split * kb + 600.0) + 15.0 * bn + (c == 2 ? 1500.0 : 0.0) + (split > 1 ? 3000.0 : 0.0);
+        if (best == 0.0 || cost < best) {
+          best = cost;
+          cl = c;
+          p.BN = bn;
+          p.mt = mt;
+          p.nt = nt;
+          p.split = split;
+        }
       }
     }
   }
@@ -527,7 +565,9 @@ oscars_status oscars_gemm_i8_nt(const int8_t* A, int64_t lda, const float* scale
   if (!code_map(&mW, B, ldb, K, N, 128) || !code_map(&mX, A, lda, K, M, p.BN / cl)) return OSCARS_ECUDA;
   const int room = cl == 2 ? pairs : sms, grid = (p.units < room ? p.units : room) * cl;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  const cudaError_t e = cl == 2 ? launch_i8<2>(mW, mX, p, grid, s) : launch_i8<1>(mW, mX, p, grid, s);
+  const cudaError_t e = p.split > 1 ? launch_i8<1, true>(mW, mX, p, p.units * p.split, s)
+                        : cl == 2   ? launch_i8<2, false>(mW, mX, p, grid, s)
+                                    : launch_i8<1, false>(mW, mX, p, grid, s);
   return e == cudaSuccess ? OSCARS_OK : OSCARS_ECUDA;
 }
 
