@@ -15,7 +15,7 @@
 //
 // gemm_i8_kernel: persistent, one CTA per SM or a cluster of two (cta_group::2),
 // 20 warps:
-//   0       TMA of code tiles (128 channels and BN tokens, 64 of K) into a ring
+//   0       TMA of code tiles (128 channels and BN tokens, 128 of K) into a ring
 //   1       issues the products from the operand ring into one of two accumulators
 //   4-11    codes -> fp16, into the operand ring (K-major, 128-byte swizzle)
 //   12-19   accumulators -> int32 sums -> C, under the products of the next tile
@@ -169,15 +169,17 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_i8_kernel(const __grid_const
   extern __shared__ uint8_t i8_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(i8_raw) + 1023) & ~uintptr_t(1023));
   const int bn = a.BN / CL, rows = 128 + bn;       // this CTA's tokens of a tile; rows of codes of a K-block
-  const int raw_bytes = rows * kK, op_bytes = 2 * raw_bytes;
+  const int raw_bytes = rows * 128, op_bytes = rows * 128;   // 128 codes, or 64 in fp16
   uint8_t* op = smem;                              // [op stages][128 channels | bn tokens][128 bytes]
-  uint8_t* raw = smem + a.op_stages * op_bytes;    // [raw stages][128 channels | bn tokens][64 bytes]
+  uint8_t* raw = smem + a.op_stages * op_bytes;    // [raw stages][128 channels | bn tokens][128 bytes]
   Bars* bars = reinterpret_cast<Bars*>(raw + a.raw_stages * raw_bytes);
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const int part = kSplit ? static_cast<int>(cluster_ctarank()) : 0;
   const int rank = CL > 1 ? static_cast<int>(cluster_ctarank()) : 0;
   const int nk = (a.K + kK - 1) / kK;
-  const int kb0 = kSplit ? nk * part / a.split : 0, kb1 = kSplit ? nk * (part + 1) / a.split : nk;   // K-blocks of this CTA
+  // this CTA's pairs of K-blocks (a code tile each); the last one's second half may lie behind nk: it takes its
+  // turn in the operand ring, but nothing is multiplied
+  const int np = (nk + 1) / 2, p0 = kSplit ? np * part / a.split : 0, p1 = kSplit ? np * (part + 1) / a.split : np;
   const int per = kSplit ? a.split : CL;           // CTAs of a tile
   const int u0 = blockIdx.x / per, ustep = gridDim.x / per;
   const int mu = a.mt / CL;                        // row tiles (of channels); rows fastest
@@ -187,7 +189,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_i8_kernel(const __grid_const
     prefetch_tmap(&mapX);
     for (int i = 0; i < a.raw_stages; ++i) {
       mbar_init(&bars->raw_full[i], 1);
-      mbar_init(&bars->raw_empty[i], kConvWarps / 2);
+      mbar_init(&bars->raw_empty[i], kConvWarps);
     }
     for (int i = 0; i < a.op_stages; ++i) {
       mbar_init(&bars->op_full[i], kConvWarps / 2 * CL);
@@ -224,12 +226,12 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_i8_kernel(const __grid_const
       bool ok = true;
       for (int u = u0; ok && u < a.units; u += ustep) {
         const int n0 = ((u % mu) * CL + rank) * 128, m0 = (u / mu) * a.BN + rank * bn;
-        for (int kb = kb0; kb < kb1; ++kb, ++it) {
+        for (int p = p0; p < p1; ++p, ++it) {
           if (it >= a.raw_stages && !(ok = mbar_wait(&bars->raw_empty[s], ph, nullptr, kDevTimeoutEmpty))) break;
           uint8_t* at = raw + s * raw_bytes;
           mbar_arrive_expect_tx(&bars->raw_full[s], raw_bytes);
-          tma_load_3d(at, &mapW, kb * kK, n0, 0, &bars->raw_full[s]);
-          tma_load_3d(at + 128 * kK, &mapX, kb * kK, m0, 0, &bars->raw_full[s]);
+          tma_load_3d(at, &mapW, p * 2 * kK, n0, 0, &bars->raw_full[s]);
+          tma_load_3d(at + 128 * 128, &mapX, p * 2 * kK, m0, 0, &bars->raw_full[s]);
           if (++s == a.raw_stages) {
             s = 0;
             ph ^= 1;
@@ -248,8 +250,8 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_i8_kernel(const __grid_const
       int s = 0, ph = 0, t = 0;   // t: accumulations begun
       uint32_t limit = kSpinLimit;
       for (int u = u0; u < a.units; u += ustep) {
-        for (int k0 = kb0; k0 < kb1; k0 += kChunk, ++t) {
-          const int b = t & 1, k1 = k0 + kChunk < kb1 ? k0 + kChunk : kb1;
+        for (int k0 = 2 * p0; k0 < 2 * p1; k0 += kChunk, ++t) {
+          const int b = t & 1, k1 = k0 + kChunk < 2 * p1 ? k0 + kChunk : 2 * p1;
           if (t >= 2) mbar_wait_keep(limit, &bars->acce[b], ((t >> 1) + 1) & 1, nullptr, kDevTimeoutAccum);
           tc_fence_after();
           const uint32_t acc = tmem + static_cast<uint32_t>(b * kMaxBN);
@@ -259,8 +261,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_i8_kernel(const __grid_const
             tc_fence_after();
             const uint64_t wd = smem_desc_k128(op0 + s * op_bytes), xd = smem_desc_k128(op0 + s * op_bytes + 128 * 128);
             if (elect_one() && limit > 1) {
-#pragma unroll
-              for (int j = 0; j < kK / 16; ++j) {
+              for (int j = 0; kb < nk && j < kK / 16; ++j) {
                 if (CL > 1) umma_f16_pair(acc, wd + 2 * j, xd + 2 * j, idesc, (kb - k0) | j ? 1u : 0u);
                 else umma_bf16(acc, wd + 2 * j, xd + 2 * j, idesc, (kb - k0) | j ? 1u : 0u);
               }
@@ -282,48 +283,62 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_i8_kernel(const __grid_const
       }
     }
   } else if (warp < 4 + kConvWarps) {
-    // ---- codes to fp16: two groups of four warps take K-blocks in turn, so that one's waits and stores run under
-    // the other's; 16 codes of a row a thread and turn, a row's 64 in four neighbouring lanes
+    // ---- codes to fp16: two groups of four warps take the two K-blocks of a code tile, so that one's waits and
+    // stores run under the other's; 16 codes of a row a thread and turn, a row's 64 in four neighbouring lanes.
+    // Eight lanes, which move 16 bytes each at once, take rows p and p ^ 5 of eight: with the 128-byte swizzle
+    // their reads (half a row each) and writes (every second chunk of a row) fall on different banks
     regs_down<kLowRegs>();
     const int th = threadIdx.x & 127, c = th & 3, group = (warp >> 2) - 1;
-    int it = 0;
+    const int p8 = lane >> 3, r8 = lane & 4 ? p8 ^ 5 : p8, row = (th >> 5) * 8 + r8;   // rows row, row + 32, ...
+    const int from = row * 128 + (((4 * group + c) ^ r8) << 4);
+    const int to0 = row * 128 + (((2 * c) ^ r8) << 4), to1 = row * 128 + (((2 * c + 1) ^ r8) << 4);
+    int it = 0, rs = 0, rph = 0, os = group, oph = 1;
     bool ok = true;
     for (int u = u0; ok && u < a.units; u += ustep) {
-      for (int kb = kb0; kb < kb1; ++kb, ++it) {
-        if ((it & 1) != group) continue;
-        const int rs = it % a.raw_stages, os = it % a.op_stages;
-        ok = mbar_wait_warp(&bars->raw_full[rs], (it / a.raw_stages) & 1, nullptr, kDevTimeoutFull);
-        if (ok && it >= a.op_stages) ok = mbar_wait_warp(&bars->op_empty[os], (it / a.op_stages + 1) & 1, nullptr, kDevTimeoutEmpty);
+      for (int p = p0; p < p1; ++p, ++it) {
+        ok = mbar_wait_warp(&bars->raw_full[rs], rph, nullptr, kDevTimeoutFull);
+        if (ok && 2 * it >= a.op_stages) ok = mbar_wait_warp(&bars->op_empty[os], oph, nullptr, kDevTimeoutEmpty);
         if (!ok) break;
-        const uint8_t* from = raw + rs * raw_bytes + 16 * c;
-        uint8_t* to = op + os * op_bytes;
-        for (int r0 = th >> 2; r0 < rows; r0 += 128) {
-          uint4 w[4];
+        const uint8_t* src = raw + rs * raw_bytes + from;
+        uint8_t* dst = op + os * op_bytes;
+        if (2 * p + group < nk) {
+          for (int r = row; r < rows; r += 128, src += 128 * 128, dst += 128 * 128) {
+            uint4 w[4];
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (r0 + 32 * i < rows) w[i] = *reinterpret_cast<const uint4*>(from + (r0 + 32 * i) * kK);
+            for (int i = 0; i < 4; ++i)
+              if (r + 32 * i < rows) w[i] = *reinterpret_cast<const uint4*>(src + 32 * 128 * i);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int r = r0 + 32 * i;
-            if (r >= rows) break;
-            uint4 x, y;
-            codes_to_half(w[i].x, x.x, x.y);
-            codes_to_half(w[i].y, x.z, x.w);
-            codes_to_half(w[i].z, y.x, y.y);
-            codes_to_half(w[i].w, y.z, y.w);
-            *reinterpret_cast<uint4*>(to + r * 128 + (((2 * c) ^ (r & 7)) << 4)) = x;
-            *reinterpret_cast<uint4*>(to + r * 128 + (((2 * c + 1) ^ (r & 7)) << 4)) = y;
+            for (int i = 0; i < 4; ++i) {
+              if (r + 32 * i >= rows) break;
+              uint4 x, y;
+              codes_to_half(w[i].x, x.x, x.y);
+              codes_to_half(w[i].y, x.z, x.w);
+              codes_to_half(w[i].z, y.x, y.y);
+              codes_to_half(w[i].w, y.z, y.w);
+              *reinterpret_cast<uint4*>(dst + to0 + 32 * 128 * i) = x;
+              *reinterpret_cast<uint4*>(dst + to1 + 32 * 128 * i) = y;
+            }
           }
+          fence_proxy_async_smem();
         }
-        fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) {
           mbar_arrive(&bars->raw_empty[rs]);
           if (CL > 1) mbar_arrive_at(cluster_addr(&bars->op_full[os], 0));
           else mbar_arrive(&bars->op_full[os]);
         }
+        if (++rs == a.raw_stages) {
+          rs = 0;
+          rph ^= 1;
+        }
+        os += 2;
+        if (os >= a.op_stages) {
+          os = group;
+          oph ^= 1;
+        }
       }
     }
+    it *= 2;
     // no commit of the leader may still be on its way to this CTA when it ends
     for (int i = it > a.op_stages ? it - a.op_stages : 0; ok && i < it; ++i)
       ok = mbar_wait_warp(&bars->op_empty[i % a.op_stages], (i / a.op_stages) & 1, nullptr, kDevTimeoutEmpty);
@@ -345,7 +360,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_i8_kernel(const __grid_const
       for (int g = 0; g < kMaxBN / 32; ++g)
 #pragma unroll
         for (int e = 0; e < 16; ++e) sum[g][e] = 0;
-      for (int k0 = kb0; k0 < kb1; k0 += kChunk, ++t) {
+      for (int k0 = 2 * p0; k0 < 2 * p1; k0 += kChunk, ++t) {
         const int b = t & 1;
         if (!(ok = mbar_wait_warp(&bars->accf[b], (t >> 1) & 1, nullptr, kDevTimeoutAccum))) break;
         tc_fence_after();
@@ -469,12 +484,12 @@ void device_room(int& sms, int& pairs) {
 
 template <int CL, bool kSplit>
 cudaError_t launch_i8(const CUtensorMap& mW, const CUtensorMap& mX, I8Args a, int grid, cudaStream_t s) {
-  const int raw = (128 + a.BN / CL) * kK, room = kSmem - 1024 - kBarBytes;
-  // even numbers: a slot belongs to one of the two converting groups, which sees each of its phases
-  a.op_stages = 8 * raw + 2 * raw > room ? 2 : 4;
-  a.raw_stages = (room - a.op_stages * 2 * raw) / raw / 2 * 2;
+  const int tile = (128 + a.BN / CL) * 128, room = kSmem - 1024 - kBarBytes;
+  // an even number of operand stages: a slot belongs to one of the two converting groups, which sees each of its phases
+  a.op_stages = 6 * tile > room ? 2 : 4;
+  a.raw_stages = room / tile - a.op_stages;
   if (a.raw_stages > kMaxStages) a.raw_stages = kMaxStages;
-  size_t smem = 1024 + static_cast<size_t>(a.op_stages) * 2 * raw + static_cast<size_t>(a.raw_stages) * raw + kBarBytes;
+  size_t smem = 1024 + static_cast<size_t>(a.op_stages + a.raw_stages) * tile + kBarBytes;
   if (smem < kLeast) smem = kLeast;
   cudaError_t e = allow_smem(gemm_i8_kernel<CL, kSplit>, kSmem);
   if (e != cudaSuccess) return e;
@@ -486,8 +501,8 @@ cudaError_t launch_i8(const CUtensorMap& mW, const CUtensorMap& mX, I8Args a, in
 bool code_map(CUtensorMap* m, const int8_t* base, int64_t ld, int K, int rows, int box_rows) {
   const cuuint64_t dims[3] = {static_cast<cuuint64_t>(K), static_cast<cuuint64_t>(rows), 1};
   const cuuint64_t strides[2] = {static_cast<cuuint64_t>(ld), static_cast<cuuint64_t>(ld)};   // the third dimension has one entry
-  const cuuint32_t box[3] = {kK, static_cast<cuuint32_t>(box_rows), 1};
-  return encode_map(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, base, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_NONE);
+  const cuuint32_t box[3] = {2 * kK, static_cast<cuuint32_t>(box_rows), 1};
+  return encode_map(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, base, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
 }  // namespace
@@ -544,7 +559,7 @@ oscars_status oscars_gemm_i8_nt(const int8_t* A, int64_t lda, const float* scale
       kb = kb > rows * kK / 45.0 ? kb : rows * kK / 45.0;
       // few tiles: the K-blocks of each over a cluster of `split` CTAs, whose sums meet in shared memory
       for (int split = 1; split <= (c == 1 ? 8 : 1); split *= 2) {
-        if (split > 1 && (units * split > (split == 8 ? sms * 3 / 4 : sms * 7 / 8) || nk < 2 * split || bn < 4 * split)) break;
+        if (split > 1 && (units * split > (split == 8 ? sms * 3 / 4 : sms * 7 / 8) || nk < 4 * split || bn < 4 * split)) break;
         const double waves = split > 1 ? 1.0 : static_cast<double>((units + room - 1) / room);
         const double cost = waves * ((nk + split - 1) / split * kb + 600.0) + 15.0 * bn + (c == 2 ? 1500.0 : 0.0) + (split > 1 ? 3000.0 : 0.0);
         if (best == 0.0 || cost < best) {
