@@ -107,27 +107,12 @@ __device__ __forceinline__ void umma_commit_pair(uint64_t* bar) {
       "h"(static_cast<uint16_t>(0x3))
       : "memory");
 }
+// An arrival on a barrier of the pair's leader.  What it is ordered behind lies in this SM: operands in its own shared
+// memory, which its own tensor core reads and a fence.proxy.async has shown to it, or reads of its tensor memory, which
+// tcgen05.wait::ld has waited for; so release at CTA scope (the default) is enough.  At cluster scope an arrival took
+// 1000 clocks (8192 x 4096 x 4096: a K-block 1200 clocks).
 __device__ __forceinline__ void mbar_arrive_at(uint32_t cluster_bar) {
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
-}
-// mbar_wait_keep for a barrier on which the peer CTA arrives after writing its shared memory
-__device__ __forceinline__ void mbar_wait_keep_cluster(uint32_t& limit, uint64_t* bar, uint32_t parity) {
-  uint32_t i = 0, ok = 0;
-  while (true) {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok)
-        : "r"(smem_u32(bar)), "r"(parity)
-        : "memory");
-    if (ok) break;
-    if (++i >= limit) {
-      limit = 1;
-      break;
-    }
-    if (i > 64) __nanosleep(64);
-  }
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
 template <int N>
 __device__ __forceinline__ void regs_down() {
@@ -256,8 +241,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_i8_kernel(const __grid_const
           tc_fence_after();
           const uint32_t acc = tmem + static_cast<uint32_t>(b * kMaxBN);
           for (int kb = k0; kb < k1; ++kb) {
-            if (CL > 1) mbar_wait_keep_cluster(limit, &bars->op_full[s], ph);
-            else mbar_wait_keep(limit, &bars->op_full[s], ph, nullptr, kDevTimeoutFull);
+            mbar_wait_keep(limit, &bars->op_full[s], ph, nullptr, kDevTimeoutFull);
             tc_fence_after();
             const uint64_t wd = smem_desc_k128(op0 + s * op_bytes), xd = smem_desc_k128(op0 + s * op_bytes + 128 * 128);
             if (elect_one() && limit > 1) {

@@ -89,8 +89,10 @@ __device__ __forceinline__ void umma_commit_pair(uint64_t* bar) {
       "h"(static_cast<uint16_t>(0x3))
       : "memory");
 }
+// An arrival on a barrier of the pair's leader: the accumulator has been read (tcgen05.wait::ld), and no write has to be
+// visible, so release at CTA scope (the default) is enough; at cluster scope an arrival takes 1000 clocks.
 __device__ __forceinline__ void mbar_arrive_at(uint32_t cluster_bar) {
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
 // fp16 operands (format 0), fp32 accumulator; bits 15 and 16: A, B MN-major
 __host__ __device__ constexpr uint32_t idesc_f16(int M, int N, int a_mn, int b_mn) {
