@@ -573,8 +573,8 @@ oscars_status oscars_quantize_i8(const void* x, int64_t ldx, int32_t dtype, int3
  *   C[m][n] = act(scale_a[m] scale_b[n] sum_k A[m][k] B[n][k] + bias[n]),
  * with the sum exact in 32-bit integers.  A: device int8, row m (a token) at
  * A + m lda; B: device int8, row n (an output channel) at B + n ldb; both
- * 16-byte aligned with lda and ldb multiples of 16 (bytes past column K are not
- * used).  scale_a [M], scale_b [N]: device fp32.  bias: device, N fp32, or NULL.
+ * 16-byte aligned with lda and ldb multiples of 16 (bytes behind column K up to a
+ * multiple of 16 may be read and are not used).  scale_a [M], scale_b [N]: device fp32.  bias: device, N fp32, or NULL.
  * relu != 0: act = max(0, .) (NaN stays), else none.  C: device, element (m, n) at
  * C[m ldc + n], of `dtype`, any alignment; scale, bias and act are fp32, rounded
  * once.  M = 0 (no tokens) does nothing; 1 <= N; 1 <= K <= 131071 (the sum of

@@ -27,6 +27,7 @@
 #include "../../include/oscars.h"
 #include "common.cuh"
 #include "internal.h"
+#include "rows.cuh"
 
 namespace oscars {
 
@@ -35,35 +36,87 @@ namespace {
 constexpr int kMaxK = 131071;   // 2^14 (2^17 - 1) < 2^31
 
 // ------------------------------------------------------------------ quantisation
-// one block a row: the maximum (NaN wins), then the codes
-template <typename T>
-__global__ void __launch_bounds__(256) quantize_i8_kernel(const T* __restrict__ x, int64_t ldx, int cols, int8_t* __restrict__ q,
-                                                          int64_t ldq, float* __restrict__ scale) {
-  __shared__ float part[8];
-  const T* row = x + blockIdx.x * ldx;
-  int8_t* out = q + blockIdx.x * ldq;
-  float mx = 0.f;
-  for (int j = threadIdx.x; j < cols; j += 256) {
-    const float v = fabsf(static_cast<float>(row[j]));
-    mx = v > mx || v != v ? v : mx;
+// A row on TPR threads, eight elements a thread and turn; up to kKeep turns stay in registers between the maximum and
+// the codes (a longer row is read again, from L2).  Bound by memory: a row is read and its codes are written once.
+constexpr int kQThreads = 256, kKeep = 4;
+
+__device__ __forceinline__ float nan_max(float a, float b) { return b > a || b != b ? b : a; }
+
+template <typename T, int TPR>
+__global__ void __launch_bounds__(kQThreads) quantize_i8_kernel(const T* __restrict__ x, int64_t ldx, int rows, int cols, int vec,
+                                                                int8_t* __restrict__ q, int64_t ldq, int qvec,
+                                                                float* __restrict__ scale) {
+  constexpr int kRows = kQThreads / TPR;
+  __shared__ float part[kQThreads / 32];
+  pdl_wait();
+  pdl_trigger();
+  const int64_t row = static_cast<int64_t>(blockIdx.x) * kRows + threadIdx.x / TPR;
+  const int t = threadIdx.x % TPR, turns = (cols + TPR * 8 - 1) / (TPR * 8);
+  if (TPR < kQThreads && row >= rows) return;   // a whole warp
+  const T* src = x + row * ldx;
+  float v[kKeep][8], mx = 0.f;
+#pragma unroll
+  for (int i = 0; i < kKeep; ++i)
+    load8(src + (i * TPR + t) * 8, cols - (i * TPR + t) * 8, vec != 0, v[i]);
+#pragma unroll
+  for (int i = 0; i < kKeep; ++i)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) mx = nan_max(mx, fabsf(v[i][e]));
+  for (int i = kKeep; i < turns; ++i) {
+    float w[8];
+    load8(src + (i * TPR + t) * 8, cols - (i * TPR + t) * 8, vec != 0, w);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) mx = nan_max(mx, fabsf(w[e]));
   }
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    const float v = __shfl_xor_sync(0xffffffffu, mx, o);
-    mx = v > mx || v != v ? v : mx;
-  }
-  if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = mx;
-  __syncthreads();
-  mx = part[0];
+  for (int o = 16; o > 0; o >>= 1) mx = nan_max(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+  if (TPR > 32) {
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = mx;
+    __syncthreads();
+    mx = part[0];
 #pragma unroll
-  for (int i = 1; i < 8; ++i) mx = part[i] > mx || part[i] != part[i] ? part[i] : mx;
+    for (int i = 1; i < TPR / 32; ++i) mx = nan_max(mx, part[i]);
+  }
   const float s = mx / 127.f;
-  if (threadIdx.x == 0) scale[blockIdx.x] = s;
-  const bool codes = s > 0.f && s <= 3.4e38f;
-  for (int j = threadIdx.x; j < cols; j += 256) {
-    const float v = codes ? fminf(fmaxf(rintf(static_cast<float>(row[j]) / s), -127.f), 127.f) : 0.f;
-    out[j] = static_cast<int8_t>(v);
+  if (t == 0) scale[row] = s;
+  const bool codes = s > 0.f && s < INFINITY;   // neither a row of zeros nor one with an infinity or NaN
+  int8_t* out = q + row * ldq;
+  auto store = [&](int at, const float (&w)[8]) {
+    uint32_t word[2] = {0u, 0u};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int c = codes ? __float2int_rn(fminf(fmaxf(w[e] / s, -127.f), 127.f)) : 0;
+      word[e >> 2] |= static_cast<uint32_t>(c & 255) << (8 * (e & 3));
+    }
+    if (qvec && at + 8 <= cols) {
+      *reinterpret_cast<uint2*>(out + at) = make_uint2(word[0], word[1]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (at + e < cols) out[at + e] = static_cast<int8_t>(word[e >> 2] >> (8 * (e & 3)));
+    }
+  };
+#pragma unroll
+  for (int i = 0; i < kKeep; ++i)
+    if ((i * TPR + t) * 8 < cols) store((i * TPR + t) * 8, v[i]);
+  for (int i = kKeep; i < turns; ++i) {
+    float w[8];
+    load8(src + (i * TPR + t) * 8, cols - (i * TPR + t) * 8, vec != 0, w);
+    if ((i * TPR + t) * 8 < cols) store((i * TPR + t) * 8, w);
   }
+}
+
+// Rows up to 1024 long on a warp each, longer ones on a block.
+template <typename T>
+cudaError_t quantize(const void* x, int64_t ldx, int rows, int cols, int8_t* q, int64_t ldq, float* scale, cudaStream_t s) {
+  const T* src = static_cast<const T*>(x);
+  const int vec = (reinterpret_cast<uintptr_t>(x) | static_cast<uintptr_t>(ldx) * sizeof(T)) % 16 == 0;
+  const int qvec = (reinterpret_cast<uintptr_t>(q) | static_cast<uintptr_t>(ldq)) % 8 == 0;
+  if (cols <= 32 * 8 * kKeep)
+    return launch_dependent(quantize_i8_kernel<T, 32>, dim3((rows + 7) / 8), kQThreads, 0, s, src, ldx, rows, cols, vec, q, ldq,
+                            qvec, scale);
+  return launch_dependent(quantize_i8_kernel<T, kQThreads>, dim3(rows), kQThreads, 0, s, src, ldx, rows, cols, vec, q, ldq, qvec,
+                          scale);
 }
 
 // ------------------------------------------------------------------ product
@@ -202,6 +255,8 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_i8_kernel(const __grid_const
   else __syncthreads();
   tc_fence_after();
   const uint32_t tmem = bars->tmem;
+  pdl_wait();
+  pdl_trigger();
 
   if (warp < 4) {
     regs_down<kLowRegs>();
@@ -422,6 +477,105 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_i8_kernel(const __grid_const
   }
 }
 
+// ------------------------------------------------------------------ few tokens
+// One or two tokens, or up to eight of few codes (tokens x K <= 8192): bound by the channels' bytes and by latency, so the
+// tensor core's set-up and the conversion do not pay.  A warp takes CH channels, each lane 16 codes of a row a turn; MT
+// tokens are multiplied with them by dp4a as they come, and the lanes' sums meet in log2(32) exchanges that halve the number
+// of values a lane holds.  Measured (us, this kernel / the tensor core's): 1 x 512 x 784 1.7 / 7.7; 1 x 4096 x 4096 4.3 / 10.2;
+// 2 x 300 x 8192 8.0 / 9.4; 8 x 1024 x 1024 4.8 / 6.2; beyond the rule 12 x 1024 x 1024 6.8 / 6.2, 8 x 4096 x 4096 15.4 / 10.4.
+constexpr int kFewThreads = 256;
+bool few_tokens(int M, int K) { return M <= 2 || (M <= 8 && static_cast<int64_t>(M) * K <= 8192); }
+
+template <int V>
+__device__ __forceinline__ void lanes_sum(int (&v)[V], int lane) {
+  // lane l ends with the sums of values l * V / 32 ... (V >= 32), or of value l * V / 32 (V < 32)
+#pragma unroll
+  for (int o = 16, n = V; o > 0; o >>= 1) {
+    if (n > 1) {
+      n >>= 1;
+      const bool up = lane & o;
+#pragma unroll
+      for (int i = 0; i < V / 2; ++i)
+        if (i < n) {
+          const int mine = up ? v[i + n] : v[i], other = up ? v[i] : v[i + n];
+          v[i] = mine + __shfl_xor_sync(0xffffffffu, other, o);
+        }
+    } else {
+      v[0] += __shfl_xor_sync(0xffffffffu, v[0], o);
+    }
+  }
+}
+
+// 16 codes from column k on, zero from column K on
+__device__ __forceinline__ int4 codes16(const int8_t* p, int left) {
+  int4 w = *reinterpret_cast<const int4*>(p);
+  if (left < 16) {
+    auto cut = [&](int v, int n) { return n >= 4 ? v : n <= 0 ? 0 : v & ((1 << (8 * n)) - 1); };
+    w.x = cut(w.x, left), w.y = cut(w.y, left - 4), w.z = cut(w.z, left - 8), w.w = cut(w.w, left - 12);
+  }
+  return w;
+}
+
+template <int MT, int CH>
+__global__ void __launch_bounds__(kFewThreads) gemm_i8_few_kernel(const int8_t* __restrict__ A, int64_t lda, const int8_t* __restrict__ B,
+                                                                  int64_t ldb, const __grid_constant__ I8Args a) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int64_t n0 = (static_cast<int64_t>(blockIdx.x) * (kFewThreads / 32) + warp) * CH;
+  pdl_wait();
+  pdl_trigger();
+  if (n0 >= a.N) return;
+  int sum[MT * CH];
+#pragma unroll
+  for (int i = 0; i < MT * CH; ++i) sum[i] = 0;
+  const int8_t* w = B + n0 * ldb;
+  constexpr int kAhead = CH == 1 ? 4 : CH == 2 ? 2 : 1;   // turns whose rows are requested together
+  for (int k0 = lane * 16; k0 < a.K; k0 += 512 * kAhead) {
+    int4 b[kAhead][CH];
+#pragma unroll
+    for (int h = 0; h < kAhead; ++h)
+#pragma unroll
+      for (int c = 0; c < CH; ++c)
+        b[h][c] = k0 + 512 * h < a.K && n0 + c < a.N ? *reinterpret_cast<const int4*>(w + c * ldb + k0 + 512 * h) : make_int4(0, 0, 0, 0);
+#pragma unroll
+    for (int h = 0; h < kAhead; ++h) {
+      const int k = k0 + 512 * h;
+      if (k >= a.K) break;
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+        if (m >= a.M) break;
+        const int4 x = codes16(A + m * lda + k, a.K - k);   // what lies behind column K of B meets zeros
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+          int s = sum[m * CH + c];
+          s = __dp4a(b[h][c].x, x.x, s);
+          s = __dp4a(b[h][c].y, x.y, s);
+          s = __dp4a(b[h][c].z, x.z, s);
+          sum[m * CH + c] = __dp4a(b[h][c].w, x.w, s);
+        }
+      }
+    }
+  }
+  constexpr int V = MT * CH, kEach = V < 32 ? 1 : V / 32;
+  lanes_sum<V>(sum, lane);
+  if (V < 32 && lane % (32 / (V < 32 ? V : 32)) != 0) return;
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    const int at = V < 32 ? lane / (32 / (V < 32 ? V : 32)) : lane * kEach + i;
+    const int m = at / CH;
+    const int64_t n = n0 + at % CH;
+    if (m >= a.M || n >= a.N) continue;
+    const float v = finish(a, sum[i], __ldg(a.sa + m), __ldg(a.sb + n), a.bias ? __ldg(a.bias + n) : 0.f);
+    if (a.bf16) static_cast<__nv_bfloat16*>(a.C)[m * a.ldc + n] = __float2bfloat16_rn(v);
+    else static_cast<float*>(a.C)[m * a.ldc + n] = v;
+  }
+}
+
+template <int MT, int CH>
+cudaError_t launch_few(const int8_t* A, int64_t lda, const int8_t* B, int64_t ldb, const I8Args& a, cudaStream_t s) {
+  const int per = kFewThreads / 32 * CH;
+  return launch_dependent(gemm_i8_few_kernel<MT, CH>, dim3((a.N + per - 1) / per), kFewThreads, 0, s, A, lda, B, ldb, a);
+}
+
 constexpr int kMaxDevices = 64;
 struct DevInfo {
   std::atomic<int> sms{0}, pairs{0};
@@ -477,8 +631,11 @@ cudaError_t launch_i8(const CUtensorMap& mW, const CUtensorMap& mX, I8Args a, in
   if (smem < kLeast) smem = kLeast;
   cudaError_t e = allow_smem(gemm_i8_kernel<CL, kSplit>, kSmem);
   if (e != cudaSuccess) return e;
-  cudaLaunchAttribute attr[1];
-  const cudaLaunchConfig_t cfg = config(attr, kSplit ? a.split : CL, grid, smem, s);
+  cudaLaunchAttribute attr[2];
+  cudaLaunchConfig_t cfg = config(attr, kSplit ? a.split : CL, grid, smem, s);
+  attr[cfg.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[cfg.numAttrs].val.programmaticStreamSerializationAllowed = 1;
+  ++cfg.numAttrs;
   return cudaLaunchKernelEx(&cfg, gemm_i8_kernel<CL, kSplit>, mW, mX, a);
 }
 
@@ -505,11 +662,9 @@ oscars_status oscars_quantize_i8(const void* x, int64_t ldx, int32_t dtype, int3
       (reinterpret_cast<uintptr_t>(x) & (dtype == OSCARS_F32 ? 3 : 1)))
     return OSCARS_EINVAL;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (dtype == OSCARS_F32)
-    quantize_i8_kernel<float><<<rows, 256, 0, s>>>(static_cast<const float*>(x), ldx, cols, q, ldq, scale);
-  else
-    quantize_i8_kernel<__nv_bfloat16><<<rows, 256, 0, s>>>(static_cast<const __nv_bfloat16*>(x), ldx, cols, q, ldq, scale);
-  return cudaGetLastError() == cudaSuccess ? OSCARS_OK : OSCARS_ECUDA;
+  const cudaError_t e = dtype == OSCARS_F32 ? quantize<float>(x, ldx, rows, cols, q, ldq, scale, s)
+                                            : quantize<__nv_bfloat16>(x, ldx, rows, cols, q, ldq, scale, s);
+  return e == cudaSuccess ? OSCARS_OK : OSCARS_ECUDA;
 }
 
 oscars_status oscars_gemm_i8_nt(const int8_t* A, int64_t lda, const float* scale_a, const int8_t* B, int64_t ldb,
@@ -525,6 +680,14 @@ oscars_status oscars_gemm_i8_nt(const int8_t* A, int64_t lda, const float* scale
     return OSCARS_EINVAL;
   if (reinterpret_cast<uintptr_t>(C) & (dtype == OSCARS_F32 ? 3 : 1)) return OSCARS_EINVAL;
   I8Args p{scale_a, scale_b, bias, C, ldc, M, N, K, relu, dtype == OSCARS_BF16, 0, 0, 0, 0, 1, 0, 0};
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (few_tokens(M, K)) {
+    const cudaError_t e = M == 1   ? launch_few<1, 1>(A, lda, B, ldb, p, s)
+                          : M == 2 ? launch_few<2, 1>(A, lda, B, ldb, p, s)
+                          : M <= 4 ? launch_few<4, 2>(A, lda, B, ldb, p, s)
+                                   : launch_few<8, 4>(A, lda, B, ldb, p, s);
+    return e == cudaSuccess ? OSCARS_OK : OSCARS_ECUDA;
+  }
   int sms, pairs;
   device_room(sms, pairs);
   // the shape with the least estimated time: waves of tiles times the longer of a K-block's products (2 BN
@@ -563,7 +726,6 @@ oscars_status oscars_gemm_i8_nt(const int8_t* A, int64_t lda, const float* scale
   CUtensorMap mW, mX;
   if (!code_map(&mW, B, ldb, K, N, 128) || !code_map(&mX, A, lda, K, M, p.BN / cl)) return OSCARS_ECUDA;
   const int room = cl == 2 ? pairs : sms, grid = (p.units < room ? p.units : room) * cl;
-  cudaStream_t s = static_cast<cudaStream_t>(stream);
   const cudaError_t e = p.split > 1 ? launch_i8<1, true>(mW, mX, p, p.units * p.split, s)
                         : cl == 2   ? launch_i8<2, false>(mW, mX, p, grid, s)
                                     : launch_i8<1, false>(mW, mX, p, grid, s);

@@ -19,6 +19,7 @@
 #include "../../include/oscars.h"
 #include "common.cuh"
 #include "internal.h"
+#include "rows.cuh"
 
 namespace oscars {
 
@@ -68,35 +69,6 @@ Shape make_shape(int batch, int rows, int cols, int dtype, bool with_u) {
 
 // ------------------------------------------------------------------ streaming passes
 
-template <typename T>
-__device__ __forceinline__ float to_f32(T v);
-template <>
-__device__ __forceinline__ float to_f32<float>(float v) { return v; }
-template <>
-__device__ __forceinline__ float to_f32<__nv_bfloat16>(__nv_bfloat16 v) { return __bfloat162float(v); }
-
-// 8 elements of a row; `vec`: 16-byte loads, all 8 inside
-template <typename T>
-__device__ __forceinline__ void load8(const T* p, int n, bool vec, float (&v)[8]) {
-  if (vec && n >= 8) {
-    if constexpr (sizeof(T) == 4) {
-      const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
-      v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
-    } else {
-      const uint4 a = *reinterpret_cast<const uint4*>(p);
-      const uint32_t w[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        v[2 * i] = __uint_as_float(w[i] << 16);
-        v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-      }
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < n ? to_f32(p[i]) : 0.f;
-  }
-}
-
 // Sum of 8 squares.  In fp32 where neither it nor a term that counts can leave
 // the range, else (magnitudes below 1e-10 or above 1e15) in fp64, so that no
 // update is too small or too large for its norm.
@@ -135,6 +107,8 @@ __device__ __forceinline__ double block_sum(double x) {
 template <typename T>
 __global__ void __launch_bounds__(kPasses) orth_norm_kernel(const T* __restrict__ G, int64_t ldg, int64_t bsg, int rows,
                                                             int cols, int vec, double* __restrict__ part) {
+  pdl_wait();
+  pdl_trigger();
   const T* g = G + blockIdx.y * bsg;
   const int per_row = (cols + 7) / 8;
   const int64_t n = static_cast<int64_t>(rows) * per_row, step = static_cast<int64_t>(gridDim.x) * kPasses;
@@ -154,6 +128,8 @@ template <int V>
 __global__ void __launch_bounds__(kPasses) orth_merge_kernel(const __grid_constant__ MergeArgs a, float* __restrict__ mom,
                                                              float mu, int nesterov, float* __restrict__ u, int64_t n,
                                                              double* __restrict__ part) {
+  pdl_wait();
+  pdl_trigger();
   const int64_t step = static_cast<int64_t>(gridDim.x) * kPasses * V;
   double sum = 0.0;
   for (int64_t i = (static_cast<int64_t>(blockIdx.x) * kPasses + threadIdx.x) * V; i < n; i += step) {
@@ -217,6 +193,8 @@ __global__ void __launch_bounds__(kPasses) orth_scale_kernel(const T* __restrict
                                                              int cols, int vec, const double* __restrict__ part, int parts,
                                                              float eps, __half* __restrict__ X, int64_t ldx) {
   __shared__ float inv_s[2];
+  pdl_wait();
+  pdl_trigger();
   double t = 0.0;
   for (int i = threadIdx.x; i < parts; i += kPasses) t += part[blockIdx.y * static_cast<int64_t>(parts) + i];
   t = block_sum(t);
@@ -287,9 +265,9 @@ cudaError_t steps_from(const Shape& p, uint8_t* ws, const T* G, int64_t ldg, int
   if (!half_maps(&mA, A, p.lds, p.s, p.s, p.batch, p.halves) || !half_maps(&mB, B, p.lds, p.s, p.s, p.batch, p.halves))
     return cudaErrorInvalidValue;
   const int vec = (reinterpret_cast<uintptr_t>(G) | (ldg * sizeof(T)) | (bsg * sizeof(T))) % 16 == 0;
-  orth_scale_kernel<T><<<dim3(pass_blocks(p.rows * (p.ldx / 8), 1024), p.batch), kPasses, 0, s>>>(
-      G, ldg, bsg, p.rows, p.cols, vec, reinterpret_cast<const double*>(ws + p.off_part), p.parts, eps, X[0], p.ldx);
-  cudaError_t e = cudaGetLastError();
+  cudaError_t e = launch_dependent(orth_scale_kernel<T>, dim3(pass_blocks(p.rows * (p.ldx / 8), 1024), p.batch), kPasses, 0, s,
+                                   G, ldg, bsg, p.rows, p.cols, vec, reinterpret_cast<const double*>(ws + p.off_part), p.parts,
+                                   eps, X[0], p.ldx);
   const bool tall = p.rows > p.cols;
   const bool cubic = co[2] == 0.f;
   const float sums = kNsScaleA / (kNsScaleX * kNsScaleX);
@@ -357,9 +335,9 @@ oscars_status orthogonalize(const Shape& p, const void* G, int64_t ldg, int64_t 
                             const float (&co)[3], float eps, const Target& to, cudaStream_t s) {
   const T* g = static_cast<const T*>(G);
   const int vec = (reinterpret_cast<uintptr_t>(g) | (ldg * sizeof(T)) | (bsg * sizeof(T))) % 16 == 0;
-  orth_norm_kernel<T><<<dim3(p.parts, p.batch), kPasses, 0, s>>>(g, ldg, bsg, p.rows, p.cols, vec,
-                                                                 reinterpret_cast<double*>(ws + p.off_part));
-  if (cudaGetLastError() != cudaSuccess) return OSCARS_ECUDA;
+  if (launch_dependent(orth_norm_kernel<T>, dim3(p.parts, p.batch), kPasses, 0, s, g, ldg, bsg, p.rows, p.cols, vec,
+                       reinterpret_cast<double*>(ws + p.off_part)) != cudaSuccess)
+    return OSCARS_ECUDA;
   return steps_from(p, ws, g, ldg, bsg, eps, steps, co, to, s) == cudaSuccess ? OSCARS_OK : OSCARS_ECUDA;
 }
 
@@ -430,9 +408,9 @@ oscars_status oscars_merge_orthogonal(float* x_g, const float* const* deltas, co
   double* part = reinterpret_cast<double*>(ws + p.off_part);
   const int64_t n = static_cast<int64_t>(rows) * cols;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if ((bits & 15) == 0) orth_merge_kernel<4><<<p.parts, kPasses, 0, s>>>(a, momentum, mu, nesterov != 0, u, n, part);
-  else orth_merge_kernel<1><<<p.parts, kPasses, 0, s>>>(a, momentum, mu, nesterov != 0, u, n, part);
-  if (cudaGetLastError() != cudaSuccess) return OSCARS_ECUDA;
+  if (launch_dependent((bits & 15) == 0 ? orth_merge_kernel<4> : orth_merge_kernel<1>, dim3(p.parts), kPasses, 0, s, a, momentum,
+                       mu, nesterov != 0 ? 1 : 0, u, n, part) != cudaSuccess)
+    return OSCARS_ECUDA;
   const Target to{x_g, cols, 0, kNsAdd, server_lr};
   return steps_from(p, ws, static_cast<const float*>(u), cols, 0, eps, steps, co, to, s) == cudaSuccess ? OSCARS_OK
                                                                                                        : OSCARS_ECUDA;
