@@ -238,10 +238,10 @@ struct NsArgs {
   void* out;                     // kNsLast
   int64_t ldo, zo;
   int out_type;                  // NsOut
-  int BN, stages, mt, nt, units; // set by the launcher, and the rows of a load's box:
-  int a_rows, b_rows;
+  int BN, stages, mt, nt, units, split;   // set by the launcher, and B's boxes of a half:
+  int b_rows, b_loads;
 };
-// maps of one tensor (inner, row, batch, half): loads in boxes of 64 x 64 and 64 x
+// maps of one tensor (inner, row, half x batch + z): loads in boxes of 64 x 64 and 64 x
 // 128 with 128-byte swizzle, stores in boxes of 32 x 32 with 64-byte swizzle
 struct NsMaps {
   CUtensorMap load64, load128, store;

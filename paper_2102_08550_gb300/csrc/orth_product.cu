@@ -64,12 +64,11 @@ struct Bars {
 static_assert(sizeof(Bars) <= kBarBytes, "barriers fit");
 
 constexpr uint32_t kLeaderMask = 0xFEFFFFFFu;   // a pair's barrier of the leader at the same offset
-__device__ __forceinline__ void tma_load_4d_pair(void* smem_dst, const CUtensorMap* map, int c0, int c1, int c2, int c3,
-                                                 uint64_t* bar) {
+__device__ __forceinline__ void tma_load_3d_pair(void* smem_dst, const CUtensorMap* map, int c0, int c1, int c2, uint64_t* bar) {
   asm volatile(
-      "cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
-      " [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(smem_u32(smem_dst)),
-      "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(smem_u32(bar) & kLeaderMask)
+      "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(smem_u32(smem_dst)),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(c2), "r"(smem_u32(bar) & kLeaderMask)
       : "memory");
 }
 // kind::f16 takes its operands' type from the instruction descriptor
@@ -124,7 +123,7 @@ __device__ __forceinline__ Tile tile_of(const NsArgs& a, int u) {
   return t;
 }
 
-template <int EPI, int CL, bool kSums>
+template <int EPI, int CL, bool kSums, bool kSplit>
 __global__ void __launch_bounds__(kThreads, 1) ns_product_kernel(const __grid_constant__ CUtensorMap mapA,
                                                                  const __grid_constant__ CUtensorMap mapB,
                                                                  const __grid_constant__ CUtensorMap mapD,
@@ -140,8 +139,11 @@ __global__ void __launch_bounds__(kThreads, 1) ns_product_kernel(const __grid_co
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const int rank = CL > 1 ? static_cast<int>(cluster_ctarank()) : 0;
   const int nk = (a.K + kK - 1) / kK;
+  // kSplit: the K-blocks of a tile over a cluster of a.split CTAs, whose sums meet in shared memory
+  const int part = kSplit ? static_cast<int>(cluster_ctarank()) : 0;
+  const int kb0 = kSplit ? nk * part / a.split : 0, kb1 = kSplit ? nk * (part + 1) / a.split : nk;
   const int chunk = kSums ? kChunk : nk;   // K-blocks of one accumulation
-  const int u0 = blockIdx.x / CL, ustep = gridDim.x / CL;
+  const int u0 = blockIdx.x / (kSplit ? a.split : CL), ustep = gridDim.x / (kSplit ? a.split : CL);
 
   if (threadIdx.x == 0) {
     prefetch_tmap(&mapA);
@@ -169,37 +171,142 @@ __global__ void __launch_bounds__(kThreads, 1) ns_product_kernel(const __grid_co
     }
   }
   tc_fence_before();
-  if (CL > 1) cluster_sync();   // the peer's barriers are initialised before anything arrives on them
+  if (CL > 1 || kSplit) cluster_sync();   // the peers run, and their barriers are initialised before anything arrives on them
   else __syncthreads();
   tc_fence_after();
   const uint32_t tmem = bars->tmem;
   pdl_wait();
   pdl_trigger();
 
-  if (warp == 0 && lane == 0) {
-    // ---- TMA producer
+  // ---- what the epilogue's warps do with 32 columns of their 32 rows (m0) of matrix z, from column n on
+  uint8_t* my = stg + (warp >= 4 ? warp - 4 : 0) * 2 * kStg;
+  int nst = 0;
+  auto finish = [&](int z, int m0, int n, bool mirrored, const float (&v)[32]) {
+    if constexpr (EPI != kNsLast) {
+      uint32_t hi[16], lo[16];
+      const int d = m0 + lane - n;   // the column on the diagonal
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        float x = v[2 * e] * a.factor, y = v[2 * e + 1] * a.factor;
+        if (kSym) {
+          x += d == 2 * e ? a.diag : 0.f;
+          y += d == 2 * e + 1 ? a.diag : 0.f;
+        }
+        const __half2 h = __floats2half2_rn(x, y);
+        const float2 f = __half22float2(h);
+        const __half2 l = __floats2half2_rn(x - f.x, y - f.y);
+        hi[e] = *reinterpret_cast<const uint32_t*>(&h);
+        lo[e] = *reinterpret_cast<const uint32_t*>(&l);
+      }
+      // one box of 32 x 32: rows as they are, or (kSym) the mirror image
+      auto store = [&](const uint32_t (&w)[16], int half, bool mirror) {
+        uint8_t* box = my + (nst & 1) * kStg;
+        if (lane == 0 && nst >= 2) bulk_wait_read_but_one();   // the store of two boxes ago has read this one
+        ++nst;
+        __syncwarp();
+        if (!mirror) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            *reinterpret_cast<uint4*>(box + lane * 64 + ((q ^ ((lane >> 1) & 3)) << 4)) =
+                make_uint4(w[4 * q], w[4 * q + 1], w[4 * q + 2], w[4 * q + 3]);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 32; ++e)
+            *reinterpret_cast<uint16_t*>(box + e * 64 + (((lane >> 3) ^ ((e >> 1) & 3)) << 4) + (lane & 7) * 2) =
+                static_cast<uint16_t>(w[e >> 1] >> (16 * (e & 1)));
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+          tma_store_3d(&mapD, box, mirror ? m0 : n, mirror ? n : m0, half * a.batch + z);
+          bulk_commit_group();
+        }
+      };
+      store(hi, 0, false);
+      if (a.d_halves == 2) store(lo, 1, false);
+      if (kSym && mirrored) {
+        store(hi, 0, true);
+        if (a.d_halves == 2) store(lo, 1, true);
+      }
+    } else {
+#pragma unroll
+      for (int q = 0; q < 8; ++q)
+        *reinterpret_cast<float4*>(my + lane * 128 + ((q ^ (lane & 7)) << 4)) =
+            make_float4(v[4 * q] * a.factor, v[4 * q + 1] * a.factor, v[4 * q + 2] * a.factor, v[4 * q + 3] * a.factor);
+      __syncwarp();
+      // rows of 32 columns, coalesced whatever the caller's alignment
+      const int col = n + lane;
+      const int64_t at0 = z * a.zo + col;
+      const int rows = a.M - m0 < 32 ? a.M - m0 : 32;
+      if (col < a.N) {
+        for (int i0 = 0; i0 < rows; i0 += 8) {
+          float x[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int rr = i0 + i;
+            x[i] = *reinterpret_cast<const float*>(my + rr * 128 + (((lane >> 2) ^ (rr & 7)) << 4) + (lane & 3) * 4);
+          }
+          if (a.out_type == kNsAdd) {
+            const float* o = static_cast<const float*>(a.out);
+            float old[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              old[i] = i0 + i < rows ? o[at0 + static_cast<int64_t>(m0 + i0 + i) * a.ldo] : 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] += old[i];
+          }
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            if (i0 + i >= rows) continue;
+            const int64_t at = at0 + static_cast<int64_t>(m0 + i0 + i) * a.ldo;
+            if (a.out_type == kNsBf16) static_cast<__nv_bfloat16*>(a.out)[at] = __float2bfloat16_rn(x[i]);
+            else static_cast<float*>(a.out)[at] = x[i];
+          }
+        }
+      }
+      __syncwarp();
+    }
+  };
+
+  if (warp == 0) {
+    // ---- TMA producer: the warp stays converged and one elected lane issues (a lane alone, with its box counts
+    // divided out of the arguments, took up to 700 clocks a K-block)
     int it = 0, s = 0, ph = 1, armed = 0;
-    bool ok = true;
-    for (int u = u0; ok && u < a.units; u += ustep) {
+    uint32_t limit = kSpinLimit;
+    for (int u = u0; u < a.units; u += ustep) {
       const Tile t = tile_of<CL, kSym>(a, u);
       const int m0 = (t.i * CL + rank) * 128, n0 = t.j * a.BN + rank * (a.BN / CL);
       const bool same = kSym && t.i == t.j && b_boxes == 2;   // a tile on the diagonal: B is A
-      for (int kb = 0; kb < nk; ++kb, ++it) {
-        if (it >= a.stages && !(ok = mbar_wait(&bars->empty[s], ph, nullptr, kDevTimeoutEmpty))) break;
-        uint8_t* at = ring + s * stage_bytes;
-        // a pair's bytes count on the leader's
-        if (rank == 0) mbar_arrive_expect_tx(&bars->full[s], CL * (same ? a_bytes : stage_bytes));
-        armed = it + 1;
-        auto load = [&](const CUtensorMap* map, int mn, int boxes, int rows, int row0, int half) {
-          for (int i = 0; i < boxes; ++i, row0 += rows, at += rows * 128) {
-            const int c0 = mn ? row0 : kb * kK, c1 = mn ? kb * kK : row0;
-            if (CL > 1) tma_load_4d_pair(at, map, c0, c1, t.z, half, &bars->full[s]);
-            else tma_load_4d(at, map, c0, c1, t.z, half, &bars->full[s]);
+      const uint32_t bytes = CL * (same ? a_bytes : stage_bytes);
+      for (int kb = kb0; kb < kb1; ++kb, ++it) {
+        if (it >= a.stages) mbar_wait_keep(limit, &bars->empty[s], ph, nullptr, kDevTimeoutEmpty);
+        if (elect_one() && limit > 1) {
+          uint8_t* at = ring + s * stage_bytes;
+          uint64_t* bar = &bars->full[s];
+          if (rank == 0) mbar_arrive_expect_tx(bar, bytes);   // a pair's bytes count on the leader's
+          auto load = [&](const CUtensorMap* map, int c0, int c1, int z) {
+            if (CL > 1) tma_load_3d_pair(at, map, c0, c1, z, bar);
+            else tma_load_3d(at, map, c0, c1, z, bar);
+          };
+          const int k = kb * kK;
+          for (int h = 0, z = t.z; h < a.a_halves; ++h, z += a.batch) {
+            if (a.a_mn) {
+              load(&mapA, m0, k, z);
+              at += kBox;
+              load(&mapA, m0 + 64, k, z);
+              at += kBox;
+            } else {
+              load(&mapA, k, m0, z);
+              at += 2 * kBox;
+            }
           }
-        };
-        for (int h = 0; h < a.a_halves; ++h) load(&mapA, a.a_mn, 128 / a.a_rows, a.a_rows, m0, h);
-        if (!same)
-          for (int h = 0; h < a.b_halves; ++h) load(&mapB, a.b_mn, 64 * b_boxes / a.b_rows, a.b_rows, n0, h);
+          if (!same)
+            for (int h = 0, z = t.z; h < a.b_halves; ++h, z += a.batch)
+              for (int i = 0; i < a.b_loads; ++i, at += a.b_rows * 128)
+                load(&mapB, a.b_mn ? n0 + a.b_rows * i : k, a.b_mn ? k : n0 + a.b_rows * i, z);
+          armed = it + 1;
+        }
+        __syncwarp();
         if (++s == a.stages) {
           s = 0;
           ph ^= 1;
@@ -207,9 +314,10 @@ __global__ void __launch_bounds__(kThreads, 1) ns_product_kernel(const __grid_co
       }
     }
     // no copy, and no commit of the leader, may still be on its way when this CTA ends
+    armed = __reduce_max_sync(0xffffffffu, armed);
     for (int i = armed > a.stages ? armed - a.stages : 0; i < armed; ++i) {
-      if (rank == 0) mbar_wait(&bars->full[i % a.stages], (i / a.stages) & 1, nullptr, kDevTimeoutFull);
-      if (!mbar_wait(&bars->empty[i % a.stages], (i / a.stages) & 1, nullptr, kDevTimeoutEmpty)) break;
+      if (rank == 0) mbar_wait_warp(&bars->full[i % a.stages], (i / a.stages) & 1, nullptr, kDevTimeoutFull);
+      if (!mbar_wait_warp(&bars->empty[i % a.stages], (i / a.stages) & 1, nullptr, kDevTimeoutEmpty)) break;
     }
   } else if (warp == 1 && rank == 0) {
     // ---- MMA issuer (the leader's, of a pair); the warp stays converged and one elected lane issues
@@ -226,8 +334,8 @@ __global__ void __launch_bounds__(kThreads, 1) ns_product_kernel(const __grid_co
         same = tl.i == tl.j && b_boxes == 2;
       }
       const int b_off = same ? 0 : a_bytes;
-      for (int k0 = 0; k0 < nk; k0 += chunk, ++t) {
-        const int b = t & 1, k1 = k0 + chunk < nk ? k0 + chunk : nk;
+      for (int k0 = kb0; k0 < kb1; k0 += chunk, ++t) {
+        const int b = t & 1, k1 = k0 + chunk < kb1 ? k0 + chunk : kb1;
         if (t >= 2) mbar_wait_keep(limit, &bars->acce[b], ((t >> 1) + 1) & 1, nullptr, kDevTimeoutAccum);
         tc_fence_after();
         const uint32_t acc = tmem + static_cast<uint32_t>(b * kMaxBN);
@@ -269,8 +377,7 @@ __global__ void __launch_bounds__(kThreads, 1) ns_product_kernel(const __grid_co
   } else if (warp >= 4) {
     // ---- epilogue: thread = one accumulator row and half of its columns
     const int quarter = warp & 3, span = a.BN / 2, cb = (warp >> 2) == 1 ? 0 : span;
-    uint8_t* my = stg + (warp - 4) * 2 * kStg;
-    int t = 0, nst = 0;
+    int t = 0;
     // the accumulator may be written again (by accumulation t + 2)
     auto release = [&](int b) {
       tc_fence_before();
@@ -280,98 +387,19 @@ __global__ void __launch_bounds__(kThreads, 1) ns_product_kernel(const __grid_co
         else mbar_arrive(&bars->acce[b]);
       }
     };
+    // partial sums [row][column], 16-byte chunks exchanged so that 32 rows of a column lie on different banks, where
+    // the operands were: the products have read them
+    auto keep = [&](int c, const float (&v)[32]) {
+      uint8_t* at = ring + (32 * quarter + lane) * a.BN * 4;
+#pragma unroll
+      for (int q = 0; q < 8; ++q)
+        *reinterpret_cast<float4*>(at + (((c / 4 + q) ^ (lane & 7)) << 4)) =
+            make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+    };
     for (int u = u0; u < a.units; u += ustep) {
       const Tile tl = tile_of<CL, kSym>(a, u);
       const int m0 = (tl.i * CL + rank) * 128 + 32 * quarter, n0 = tl.j * a.BN + cb;
-      const int r = m0 + lane;
       const uint32_t row0 = tmem + (static_cast<uint32_t>(32 * quarter) << 16) + cb;
-      // 32 columns from column c0 on
-      auto finish = [&](int c0, const float (&v)[32]) {
-        if constexpr (EPI != kNsLast) {
-          uint32_t hi[16], lo[16];
-          const int d = r - n0 - c0;   // the column on the diagonal
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            float x = v[2 * e] * a.factor, y = v[2 * e + 1] * a.factor;
-            if (kSym) {
-              x += d == 2 * e ? a.diag : 0.f;
-              y += d == 2 * e + 1 ? a.diag : 0.f;
-            }
-            const __half2 h = __floats2half2_rn(x, y);
-            const float2 f = __half22float2(h);
-            const __half2 l = __floats2half2_rn(x - f.x, y - f.y);
-            hi[e] = *reinterpret_cast<const uint32_t*>(&h);
-            lo[e] = *reinterpret_cast<const uint32_t*>(&l);
-          }
-          // one box of 32 x 32: rows as they are, or (kSym) the mirror image
-          auto store = [&](const uint32_t (&w)[16], int half, bool mirror) {
-            uint8_t* box = my + (nst & 1) * kStg;
-            if (lane == 0 && nst >= 2) bulk_wait_read_but_one();   // the store of two boxes ago has read this one
-            ++nst;
-            __syncwarp();
-            if (!mirror) {
-#pragma unroll
-              for (int q = 0; q < 4; ++q)
-                *reinterpret_cast<uint4*>(box + lane * 64 + ((q ^ ((lane >> 1) & 3)) << 4)) =
-                    make_uint4(w[4 * q], w[4 * q + 1], w[4 * q + 2], w[4 * q + 3]);
-            } else {
-#pragma unroll
-              for (int e = 0; e < 32; ++e)
-                *reinterpret_cast<uint16_t*>(box + e * 64 + (((lane >> 3) ^ ((e >> 1) & 3)) << 4) + (lane & 7) * 2) =
-                    static_cast<uint16_t>(w[e >> 1] >> (16 * (e & 1)));
-            }
-            fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) {
-              tma_store_4d(&mapD, box, mirror ? m0 : n0 + c0, mirror ? n0 + c0 : m0, tl.z, half);
-              bulk_commit_group();
-            }
-          };
-          store(hi, 0, false);
-          if (a.d_halves == 2) store(lo, 1, false);
-          if (kSym && tl.i != tl.j) {
-            store(hi, 0, true);
-            if (a.d_halves == 2) store(lo, 1, true);
-          }
-        } else {
-#pragma unroll
-          for (int q = 0; q < 8; ++q)
-            *reinterpret_cast<float4*>(my + lane * 128 + ((q ^ (lane & 7)) << 4)) =
-                make_float4(v[4 * q] * a.factor, v[4 * q + 1] * a.factor, v[4 * q + 2] * a.factor, v[4 * q + 3] * a.factor);
-          __syncwarp();
-          // rows of 32 columns, coalesced whatever the caller's alignment
-          const int col = n0 + c0 + lane;
-          const int64_t at0 = tl.z * a.zo + col;
-          const int rows = a.M - m0 < 32 ? a.M - m0 : 32;
-          if (col < a.N) {
-            for (int i0 = 0; i0 < rows; i0 += 8) {
-              float x[8];
-#pragma unroll
-              for (int i = 0; i < 8; ++i) {
-                const int rr = i0 + i;
-                x[i] = *reinterpret_cast<const float*>(my + rr * 128 + (((lane >> 2) ^ (rr & 7)) << 4) + (lane & 3) * 4);
-              }
-              if (a.out_type == kNsAdd) {
-                const float* o = static_cast<const float*>(a.out);
-                float old[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                  old[i] = i0 + i < rows ? o[at0 + static_cast<int64_t>(m0 + i0 + i) * a.ldo] : 0.f;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] += old[i];
-              }
-#pragma unroll
-              for (int i = 0; i < 8; ++i) {
-                if (i0 + i >= rows) continue;
-                const int64_t at = at0 + static_cast<int64_t>(m0 + i0 + i) * a.ldo;
-                if (a.out_type == kNsBf16) static_cast<__nv_bfloat16*>(a.out)[at] = __float2bfloat16_rn(x[i]);
-                else static_cast<float*>(a.out)[at] = x[i];
-              }
-            }
-          }
-          __syncwarp();
-        }
-      };
       if constexpr (kSums) {
         float sum[kMaxBN / 64][32];
 #pragma unroll
@@ -379,7 +407,7 @@ __global__ void __launch_bounds__(kThreads, 1) ns_product_kernel(const __grid_co
 #pragma unroll
           for (int e = 0; e < 32; ++e) sum[g][e] = 0.f;
         bool ok = true;
-        for (int k0 = 0; k0 < nk; k0 += chunk, ++t) {
+        for (int k0 = kb0; k0 < kb1; k0 += chunk, ++t) {
           const int b = t & 1;
           if (!(ok = mbar_wait_warp(&bars->accf[b], (t >> 1) & 1, nullptr, kDevTimeoutAccum))) break;
           tc_fence_after();
@@ -399,15 +427,19 @@ __global__ void __launch_bounds__(kThreads, 1) ns_product_kernel(const __grid_co
         if (!ok) break;
 #pragma unroll
         for (int g = 0; g < kMaxBN / 64; ++g)
-          if (32 * g < span && n0 + 32 * g < a.N && m0 < a.M) finish(32 * g, sum[g]);
+          if (kSplit ? 32 * g < span : 32 * g < span && n0 + 32 * g < a.N && m0 < a.M) {
+            if (kSplit) keep(cb + 32 * g, sum[g]);
+            else finish(tl.z, m0, n0 + 32 * g, tl.i != tl.j, sum[g]);
+          }
       } else {
         const int b = t & 1;
         if (!mbar_wait_warp(&bars->accf[b], (t >> 1) & 1, nullptr, kDevTimeoutAccum)) break;
         tc_fence_after();
-        for (int c0 = 0; c0 < span && n0 + c0 < a.N && m0 < a.M; c0 += 32) {
+        for (int c0 = 0; c0 < span && (kSplit || (n0 + c0 < a.N && m0 < a.M)); c0 += 32) {
           float v[32];
           tmem_ld_32x32b_x32(row0 + b * kMaxBN + c0, v);
-          finish(c0, v);
+          if (kSplit) keep(cb + c0, v);
+          else finish(tl.z, m0, n0 + c0, tl.i != tl.j, v);
         }
         release(b);
         ++t;
@@ -416,8 +448,31 @@ __global__ void __launch_bounds__(kThreads, 1) ns_product_kernel(const __grid_co
     if (lane == 0) bulk_wait_all();
   }
   tc_fence_before();
-  if (CL > 1) cluster_sync();   // the pair's products and arrivals are done in both CTAs
+  if (CL > 1 || kSplit) cluster_sync();   // the pair's products and arrivals are done in both CTAs; every part's sums are there
   else __syncthreads();
+  if constexpr (kSplit) {
+    // each CTA adds up its columns of the tile over the parts, in their order
+    const int quarter = warp & 3, span = a.BN / a.split;
+    const Tile tl = tile_of<CL, kSym>(a, u0);
+    const int m0 = tl.i * 128 + 32 * quarter;
+    for (int c0 = 32 * ((warp >> 2) - 1); warp >= 4 && c0 < span; c0 += 64) {
+      const int c = part * span + c0, n = tl.j * a.BN + c;
+      if (n >= a.N || m0 >= a.M) break;
+      const uint8_t* at = ring + (32 * quarter + lane) * a.BN * 4;
+      float v[32];
+#pragma unroll
+      for (int e = 0; e < 32; ++e) v[e] = 0.f;
+      for (int p = 0; p < a.split; ++p)
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+          const float4 f = ld_dsmem_f32x4(reinterpret_cast<const float*>(at + (((c / 4 + q) ^ (lane & 7)) << 4)), p);
+          v[4 * q] += f.x, v[4 * q + 1] += f.y, v[4 * q + 2] += f.z, v[4 * q + 3] += f.w;
+        }
+      finish(tl.z, m0, n, tl.i != tl.j, v);
+    }
+    if (warp >= 4 && lane == 0) bulk_wait_all();
+    cluster_sync();   // no CTA ends while a peer reads its sums
+  }
   if (warp == 2) {
     tc_fence_after();
     if (CL == 1) tmem_dealloc(tmem, 512);
@@ -432,15 +487,16 @@ struct DevInfo {
 DevInfo g_dev[kMaxDevices];
 
 int stage_bytes(const NsArgs& a, int BN, int cl) { return (a.a_halves * 2 + a.b_halves * (BN / cl / 64)) * kBox; }
-int stages_of(const NsArgs& a, int BN, int cl) {
-  const int nk = (a.K + kK - 1) / kK;
-  int st = kRing / stage_bytes(a, BN, cl);
+int stages_of(const NsArgs& a, int BN, int cl, int split) {
+  const int nk = ((a.K + kK - 1) / kK + split - 1) / split, bytes = stage_bytes(a, BN, cl);
+  int st = kRing / bytes;
   st = st > kMaxStages ? kMaxStages : st;
-  return st > nk ? (nk < 2 ? 2 : nk) : st;
+  int least = 2;
+  if (split > 1) least = (128 * BN * 4 + bytes - 1) / bytes > 2 ? (128 * BN * 4 + bytes - 1) / bytes : 2;   // the partial sums
+  return st > nk ? (nk < least ? least : nk) : st;
 }
 
-template <int CL>
-cudaLaunchConfig_t config(cudaLaunchAttribute* attr, int grid, size_t smem, cudaStream_t s) {
+cudaLaunchConfig_t config(cudaLaunchAttribute* attr, int cluster, int grid, size_t smem, cudaStream_t s) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(grid, 1, 1);
   cfg.blockDim = dim3(kThreads, 1, 1);
@@ -448,9 +504,9 @@ cudaLaunchConfig_t config(cudaLaunchAttribute* attr, int grid, size_t smem, cuda
   cfg.stream = s;
   cfg.attrs = attr;
   cfg.numAttrs = 0;
-  if (CL > 1) {
+  if (cluster > 1) {
     attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = CL;
+    attr[0].val.clusterDim.x = cluster;
     attr[0].val.clusterDim.y = 1;
     attr[0].val.clusterDim.z = 1;
     cfg.numAttrs = 1;
@@ -468,9 +524,9 @@ void device_room(int& sms, int& pairs) {
   if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || sms < 1) sms = 1;
   cudaLaunchAttribute attr[1];
   pairs = 0;
-  if (allow_smem(ns_product_kernel<kNsStep, 2, true>, kSmem) == cudaSuccess) {
-    cudaLaunchConfig_t cfg = config<2>(attr, 2, kSmem, nullptr);
-    if (cudaOccupancyMaxActiveClusters(&pairs, ns_product_kernel<kNsStep, 2, true>, &cfg) != cudaSuccess) pairs = 0;
+  if (allow_smem(ns_product_kernel<kNsStep, 2, true, false>, kSmem) == cudaSuccess) {
+    cudaLaunchConfig_t cfg = config(attr, 2, 2, kSmem, nullptr);
+    if (cudaOccupancyMaxActiveClusters(&pairs, ns_product_kernel<kNsStep, 2, true, false>, &cfg) != cudaSuccess) pairs = 0;
   }
   cudaGetLastError();
   if (pairs < 1) pairs = 1;
@@ -478,27 +534,34 @@ void device_room(int& sms, int& pairs) {
   g_dev[dev].pairs.store(pairs, std::memory_order_relaxed);
 }
 
-template <int EPI, int CL, bool kSums>
+template <int EPI, int CL, bool kSums, bool kSplit>
 cudaError_t launch_t(const CUtensorMap& mA, const CUtensorMap& mB, const CUtensorMap& mD, const NsArgs& a, int grid,
                      cudaStream_t s) {
   size_t smem = 1024 + kStgBytes + static_cast<size_t>(a.stages) * stage_bytes(a, a.BN, CL) + kBarBytes;
   if (smem < kLeast) smem = kLeast;
-  cudaError_t e = allow_smem(ns_product_kernel<EPI, CL, kSums>, kSmem);
+  cudaError_t e = allow_smem(ns_product_kernel<EPI, CL, kSums, kSplit>, kSmem);
   if (e != cudaSuccess) return e;
   cudaLaunchAttribute attr[2];
-  cudaLaunchConfig_t cfg = config<CL>(attr, grid, smem, s);
+  cudaLaunchConfig_t cfg = config(attr, kSplit ? a.split : CL, grid, smem, s);
   attr[cfg.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[cfg.numAttrs].val.programmaticStreamSerializationAllowed = 1;
   ++cfg.numAttrs;
-  return cudaLaunchKernelEx(&cfg, ns_product_kernel<EPI, CL, kSums>, mA, mB, mD, a);
+  return cudaLaunchKernelEx(&cfg, ns_product_kernel<EPI, CL, kSums, kSplit>, mA, mB, mD, a);
+}
+
+template <int EPI, bool kSums>
+cudaError_t launch_s(int cl, const CUtensorMap& mA, const CUtensorMap& mB, const CUtensorMap& mD, const NsArgs& a, int grid,
+                     cudaStream_t s) {
+  return a.split > 1 ? launch_t<EPI, 1, kSums, true>(mA, mB, mD, a, a.units * a.split, s)
+         : cl == 2   ? launch_t<EPI, 2, kSums, false>(mA, mB, mD, a, grid, s)
+                     : launch_t<EPI, 1, kSums, false>(mA, mB, mD, a, grid, s);
 }
 
 template <int EPI>
 cudaError_t launch_e(int cl, const CUtensorMap& mA, const CUtensorMap& mB, const CUtensorMap& mD, const NsArgs& a, int grid,
                      cudaStream_t s) {
-  if (a.a_halves + a.b_halves == 4)
-    return cl == 2 ? launch_t<EPI, 2, true>(mA, mB, mD, a, grid, s) : launch_t<EPI, 1, true>(mA, mB, mD, a, grid, s);
-  return cl == 2 ? launch_t<EPI, 2, false>(mA, mB, mD, a, grid, s) : launch_t<EPI, 1, false>(mA, mB, mD, a, grid, s);
+  return a.a_halves + a.b_halves == 4 ? launch_s<EPI, true>(cl, mA, mB, mD, a, grid, s)
+                                      : launch_s<EPI, false>(cl, mA, mB, mD, a, grid, s);
 }
 
 }  // namespace
@@ -520,24 +583,30 @@ cudaError_t launch_ns_product(int epi, const NsMaps& A, const NsMaps& B, const N
       const int nt = (a.N + bn - 1) / bn;
       const int64_t units = static_cast<int64_t>(a.batch) * (sym ? nt * static_cast<int64_t>(nt + 1) / 2 : static_cast<int64_t>(mt / c) * nt);
       const int room = c == 2 ? pairs : sms;
-      const double waves = static_cast<double>((units + room - 1) / room);
       const double mma = 2.0 * bn * products, load = stage_bytes(a, bn, c) / 45.0;
-      const double cost = waves * (nk * (load > mma ? load : mma) + 600.0) + 12.0 * bn + (c == 2 ? 1500.0 : 0.0);
-      if (best == 0.0 || cost < best) {
-        best = cost;
-        cl = c;
-        a.BN = bn;
-        a.mt = mt;
-        a.nt = nt;
-        a.units = static_cast<int>(units);   // far below 2^31: a tile is 16 KB of workspace at least
+      for (int split = 1; split <= (c == 1 ? 4 : 1); split *= 2) {
+        // a part has two K-blocks, a CTA 32 columns of the sums, and the clusters run at once
+        if (split > 1 && (units * split > sms * 7 / 8 || nk < 2 * split || bn < 32 * split)) break;
+        const double waves = split > 1 ? 1.0 : static_cast<double>((units + room - 1) / room);
+        const double cost = waves * ((nk + split - 1) / split * (load > mma ? load : mma) + 600.0) + 12.0 * bn +
+                            (c == 2 ? 1500.0 : 0.0) + (split > 1 ? 4000.0 : 0.0);
+        if (best == 0.0 || cost < best) {
+          best = cost;
+          cl = c;
+          a.BN = bn;
+          a.mt = mt;
+          a.nt = nt;
+          a.split = split;
+          a.units = static_cast<int>(units);   // far below 2^31: a tile is 16 KB of workspace at least
+        }
       }
     }
   }
-  a.stages = stages_of(a, a.BN, cl);
+  a.stages = stages_of(a, a.BN, cl, a.split);
   // K-major boxes of 128 rows where the tile has them: half as many copies
-  a.a_rows = a.a_mn ? 64 : 128;
   a.b_rows = a.b_mn || a.BN / cl % 128 ? 64 : 128;
-  const CUtensorMap &mA = a.a_rows == 64 ? A.load64 : A.load128, &mB = a.b_rows == 64 ? B.load64 : B.load128, &mD = D.store;
+  a.b_loads = a.BN / cl / a.b_rows;
+  const CUtensorMap &mA = a.a_mn ? A.load64 : A.load128, &mB = a.b_rows == 64 ? B.load64 : B.load128, &mD = D.store;
   const int room = cl == 2 ? pairs : sms, grid = (a.units < room ? a.units : room) * cl;
   switch (epi) {
     case kNsSym: return launch_e<kNsSym>(cl, mA, mB, mD, a, grid, s);

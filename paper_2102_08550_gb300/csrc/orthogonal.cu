@@ -238,15 +238,14 @@ struct Target {
 
 // fp16 [halves][batch][rows][ld]
 bool half_maps(NsMaps* m, const void* base, int64_t ld, int cols, int rows, int batch, int halves) {
-  const cuuint64_t dims[4] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows), static_cast<cuuint64_t>(batch),
-                              static_cast<cuuint64_t>(halves)};
-  const cuuint64_t strides[3] = {static_cast<cuuint64_t>(ld) * 2, static_cast<cuuint64_t>(ld) * rows * 2,
-                                 static_cast<cuuint64_t>(ld) * rows * batch * 2};
-  const cuuint32_t b64[4] = {64, 64, 1, 1}, b128[4] = {64, 128, 1, 1}, out[4] = {32, 32, 1, 1};
+  const cuuint64_t dims[3] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows),
+                              static_cast<cuuint64_t>(batch) * halves};
+  const cuuint64_t strides[2] = {static_cast<cuuint64_t>(ld) * 2, static_cast<cuuint64_t>(ld) * rows * 2};
+  const cuuint32_t b64[3] = {64, 64, 1}, b128[3] = {64, 128, 1}, out[3] = {32, 32, 1};
   const CUtensorMapDataType t = CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
-  return encode_map(&m->load64, t, 4, base, dims, strides, b64, CU_TENSOR_MAP_SWIZZLE_128B) &&
-         encode_map(&m->load128, t, 4, base, dims, strides, b128, CU_TENSOR_MAP_SWIZZLE_128B) &&
-         encode_map(&m->store, t, 4, base, dims, strides, out, CU_TENSOR_MAP_SWIZZLE_64B);
+  return encode_map(&m->load64, t, 3, base, dims, strides, b64, CU_TENSOR_MAP_SWIZZLE_128B) &&
+         encode_map(&m->load128, t, 3, base, dims, strides, b128, CU_TENSOR_MAP_SWIZZLE_128B) &&
+         encode_map(&m->store, t, 3, base, dims, strides, out, CU_TENSOR_MAP_SWIZZLE_64B);
 }
 
 int pass_blocks(int64_t units, int most) {
