@@ -93,6 +93,11 @@ __device__ __forceinline__ void umma_commit_pair(uint64_t* bar) {
 __device__ __forceinline__ void mbar_arrive_at(uint32_t cluster_bar) {
   asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
+// 16 bytes into a peer's shared memory (an address from cluster_addr)
+__device__ __forceinline__ void st_dsmem_at(uint32_t remote, float4 v) {
+  asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(remote), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w)
+               : "memory");
+}
 // fp16 operands (format 0), fp32 accumulator; bits 15 and 16: A, B MN-major
 __host__ __device__ constexpr uint32_t idesc_f16(int M, int N, int a_mn, int b_mn) {
   return (1u << 4) | (static_cast<uint32_t>(a_mn) << 15) | (static_cast<uint32_t>(b_mn) << 16) |
@@ -135,7 +140,9 @@ __global__ void __launch_bounds__(kThreads, 1) ns_product_kernel(const __grid_co
   uint8_t* ring = smem + kStgBytes;   // [stages][A: halves x 2 boxes | B: halves x BN / CL / 64 boxes]
   const int b_boxes = a.BN / CL / 64, b_half = b_boxes * kBox;
   const int a_bytes = a.a_halves * 2 * kBox, stage_bytes = a_bytes + a.b_halves * b_half;
-  Bars* bars = reinterpret_cast<Bars*>(ring + a.stages * stage_bytes);
+  // kSplit: the parts' sums of this CTA's columns [part][BN / split / 4][128 rows][4]
+  uint8_t* recv = ring + a.stages * stage_bytes;
+  Bars* bars = reinterpret_cast<Bars*>(recv + (kSplit ? 128 * a.BN * 4 : 0));
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const int rank = CL > 1 ? static_cast<int>(cluster_ctarank()) : 0;
   const int nk = (a.K + kK - 1) / kK;
@@ -387,14 +394,14 @@ __global__ void __launch_bounds__(kThreads, 1) ns_product_kernel(const __grid_co
         else mbar_arrive(&bars->acce[b]);
       }
     };
-    // partial sums [row][column], 16-byte chunks exchanged so that 32 rows of a column lie on different banks, where
-    // the operands were: the products have read them
+    // a part's sums go to the CTA that owns the columns, four columns of 32 rows (512 bytes in a row) a store.  Read by
+    // their owner from the peers, 32 loads a thread took 12000 clocks; stored 16 bytes a row, 4600.
     auto keep = [&](int c, const float (&v)[32]) {
-      uint8_t* at = ring + (32 * quarter + lane) * a.BN * 4;
+      const int owned = a.BN / a.split, owner = c / owned;
+      const uint32_t at = cluster_addr(recv + (((part * owned + c % owned) / 4) * 128 + 32 * quarter + lane) * 16, owner);
 #pragma unroll
       for (int q = 0; q < 8; ++q)
-        *reinterpret_cast<float4*>(at + (((c / 4 + q) ^ (lane & 7)) << 4)) =
-            make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+        st_dsmem_at(at + q * 128 * 16, make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]));
     };
     for (int u = u0; u < a.units; u += ustep) {
       const Tile tl = tile_of<CL, kSym>(a, u);
@@ -458,20 +465,20 @@ __global__ void __launch_bounds__(kThreads, 1) ns_product_kernel(const __grid_co
     for (int c0 = 32 * ((warp >> 2) - 1); warp >= 4 && c0 < span; c0 += 64) {
       const int c = part * span + c0, n = tl.j * a.BN + c;
       if (n >= a.N || m0 >= a.M) break;
-      const uint8_t* at = ring + (32 * quarter + lane) * a.BN * 4;
       float v[32];
 #pragma unroll
       for (int e = 0; e < 32; ++e) v[e] = 0.f;
-      for (int p = 0; p < a.split; ++p)
+      for (int p = 0; p < a.split; ++p) {
+        const uint8_t* at = recv + (((p * span + c0) / 4) * 128 + 32 * quarter + lane) * 16;
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
-          const float4 f = ld_dsmem_f32x4(reinterpret_cast<const float*>(at + (((c / 4 + q) ^ (lane & 7)) << 4)), p);
+          const float4 f = *reinterpret_cast<const float4*>(at + q * 128 * 16);
           v[4 * q] += f.x, v[4 * q + 1] += f.y, v[4 * q + 2] += f.z, v[4 * q + 3] += f.w;
         }
+      }
       finish(tl.z, m0, n, tl.i != tl.j, v);
     }
     if (warp >= 4 && lane == 0) bulk_wait_all();
-    cluster_sync();   // no CTA ends while a peer reads its sums
   }
   if (warp == 2) {
     tc_fence_after();
@@ -489,11 +496,9 @@ DevInfo g_dev[kMaxDevices];
 int stage_bytes(const NsArgs& a, int BN, int cl) { return (a.a_halves * 2 + a.b_halves * (BN / cl / 64)) * kBox; }
 int stages_of(const NsArgs& a, int BN, int cl, int split) {
   const int nk = ((a.K + kK - 1) / kK + split - 1) / split, bytes = stage_bytes(a, BN, cl);
-  int st = kRing / bytes;
+  int st = (kRing - (split > 1 ? 128 * BN * 4 : 0)) / bytes;   // beside the parts' sums
   st = st > kMaxStages ? kMaxStages : st;
-  int least = 2;
-  if (split > 1) least = (128 * BN * 4 + bytes - 1) / bytes > 2 ? (128 * BN * 4 + bytes - 1) / bytes : 2;   // the partial sums
-  return st > nk ? (nk < least ? least : nk) : st;
+  return st > nk ? (nk < 2 ? 2 : nk) : st;
 }
 
 cudaLaunchConfig_t config(cudaLaunchAttribute* attr, int cluster, int grid, size_t smem, cudaStream_t s) {
@@ -537,7 +542,7 @@ void device_room(int& sms, int& pairs) {
 template <int EPI, int CL, bool kSums, bool kSplit>
 cudaError_t launch_t(const CUtensorMap& mA, const CUtensorMap& mB, const CUtensorMap& mD, const NsArgs& a, int grid,
                      cudaStream_t s) {
-  size_t smem = 1024 + kStgBytes + static_cast<size_t>(a.stages) * stage_bytes(a, a.BN, CL) + kBarBytes;
+  size_t smem = 1024 + kStgBytes + static_cast<size_t>(a.stages) * stage_bytes(a, a.BN, CL) + (kSplit ? 128 * a.BN * 4 : 0) + kBarBytes;
   if (smem < kLeast) smem = kLeast;
   cudaError_t e = allow_smem(ns_product_kernel<EPI, CL, kSums, kSplit>, kSmem);
   if (e != cudaSuccess) return e;
@@ -572,7 +577,7 @@ cudaError_t launch_ns_product(int epi, const NsMaps& A, const NsMaps& B, const N
   const bool sym = epi == kNsSym;
   const int nk = (a.K + kK - 1) / kK, products = a.a_halves + a.b_halves - 1;
   // The shape with the least estimated time: waves of tiles times the longer of a
-  // tile's products (2 BN clocks a K-block and product) and loads (45 bytes a clock
+  // tile's products (2 BN clocks a K-block and product) and loads (52 bytes a clock
   // into an SM), plus a tile's and a launch's fixed part.  Triangles take square tiles.
   double best = 0.0;
   int cl = 1;
@@ -583,13 +588,13 @@ cudaError_t launch_ns_product(int epi, const NsMaps& A, const NsMaps& B, const N
       const int nt = (a.N + bn - 1) / bn;
       const int64_t units = static_cast<int64_t>(a.batch) * (sym ? nt * static_cast<int64_t>(nt + 1) / 2 : static_cast<int64_t>(mt / c) * nt);
       const int room = c == 2 ? pairs : sms;
-      const double mma = 2.0 * bn * products, load = stage_bytes(a, bn, c) / 45.0;
+      const double mma = 2.0 * bn * products, load = stage_bytes(a, bn, c) / 52.0;
       for (int split = 1; split <= (c == 1 ? 4 : 1); split *= 2) {
         // a part has two K-blocks, a CTA 32 columns of the sums, and the clusters run at once
-        if (split > 1 && (units * split > sms * 7 / 8 || nk < 2 * split || bn < 32 * split)) break;
+        if (split > 1 && (units * split > sms * 7 / 8 || nk < 2 * split || bn < 32 * split || stages_of(a, bn, c, split) < 2)) break;
         const double waves = split > 1 ? 1.0 : static_cast<double>((units + room - 1) / room);
         const double cost = waves * ((nk + split - 1) / split * (load > mma ? load : mma) + 600.0) + 12.0 * bn +
-                            (c == 2 ? 1500.0 : 0.0) + (split > 1 ? 4000.0 : 0.0);
+                            (c == 2 ? 1500.0 : 0.0) + (split > 1 ? 2500.0 : 0.0);
         if (best == 0.0 || cost < best) {
           best = cost;
           cl = c;
