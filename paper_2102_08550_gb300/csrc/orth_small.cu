@@ -1,0 +1,277 @@
+// Newton-Schulz steps of small matrices in one launch (see orthogonal.cu for the method).
+//
+// Where the shorter side s is at most 64, a launch for each of a step's products takes longer than its products: 15
+// launches of a 10 x 512 matrix took 68 us, their products less than one.  Here a matrix stays in shared memory for all
+// steps, the longer side over a cluster of up to 8 CTAs.  A step: each CTA's share of the Gram matrix (fp32, tiles of 4 x 4
+// a thread, the long sum over groups of threads); the shares are added in rank order, each CTA a part of the entries, and
+// the sums stored to every CTA; B = a I + b A + c A A in every CTA; X <- B X on its columns.  Everything in fp32.
+#include <atomic>
+
+#include "../../include/oscars.h"
+#include "common.cuh"
+#include "internal.h"
+#include "rows.cuh"
+
+namespace oscars {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kMaxS = 64, kMaxCluster = 8;
+constexpr size_t kMaxSmem = 200 * 1024;
+constexpr double kMaxWork = 600e3;               // multiply-adds of a CTA's Gram share: beyond, the tensor cores are faster
+
+struct SmallArgs {
+  const void* G;
+  int64_t ldg, zg;
+  void* out;
+  int64_t ldo, zo;
+  int out_type;                                  // NsOut
+  int rows, cols, s, len, share, cluster, steps; // share: columns (of the longer side) of a CTA, a multiple of 4
+  float a, b, c, eps, scale;
+};
+
+int up4(int x) { return (x + 3) / 4 * 4; }
+// floats of a row of X: 16-byte aligned, rows on different banks
+__host__ __device__ inline int row_floats(int share) { return share % 8 == 4 ? share : share + 4; }
+size_t smem_floats(int s, int share) {
+  const int s4 = up4(s);
+  return static_cast<size_t>(2) * s4 * row_floats(share) + 3 * static_cast<size_t>(s4) * (s4 + 4) + kThreads * 16;
+}
+
+__device__ __forceinline__ void st_peer(const void* local, int rank, float v) {
+  asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(cluster_addr(local, rank)), "f"(v) : "memory");
+}
+__device__ __forceinline__ void st_peer_f64(const void* local, int rank, double v) {
+  asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(cluster_addr(local, rank)), "d"(v) : "memory");
+}
+
+// Sum over the CTA in a fixed order, in every thread.
+__device__ __forceinline__ double cta_sum(double x, double* part) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+  if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = x;
+  __syncthreads();
+  double s = 0.0;
+  for (int i = 0; i < kThreads / 32; ++i) s += part[i];
+  return s;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kThreads) orth_small_kernel(const __grid_constant__ SmallArgs p) {
+  extern __shared__ __align__(16) float sm[];
+  __shared__ double norm_part[kThreads / 32], norm_peer[kMaxCluster];
+  const int s4 = (p.s + 3) / 4 * 4, lda = s4 + 4, ldx = row_floats(p.share), tid = threadIdx.x;
+  float* X = sm;                                 // [2][s4][ldx]
+  float* A = X + 2 * s4 * ldx;                   // [s4][lda]
+  float* B = A + s4 * lda;                       // [s4][lda]
+  float* P = B + s4 * lda;                       // [s4][lda]: this CTA's share of A
+  float* red = P + s4 * lda;                     // [groups][tiles][16]
+  const int rank = p.cluster > 1 ? static_cast<int>(cluster_ctarank()) : 0, z = blockIdx.x / p.cluster;
+  const int l0 = rank * p.share, n = p.len - l0 < p.share ? (p.len - l0 > 0 ? p.len - l0 : 0) : p.share;
+  const bool tall = p.rows > p.cols;
+  pdl_wait();
+  pdl_trigger();
+
+  // ---- X as it comes, and its norm.  Of a wide matrix a CTA holds columns, of a tall one rows (as columns)
+  const T* g = static_cast<const T*>(p.G) + z * p.zg;
+  for (int i = tid; i < 2 * s4 * ldx; i += kThreads) X[i] = 0.f;
+  __syncthreads();
+  double sum = 0.0;
+  const int fast = tall ? p.s : n;               // consecutive in memory
+  for (int64_t i = tid; i < static_cast<int64_t>(p.s) * n; i += kThreads) {
+    const int outer = static_cast<int>(i / fast), inner = static_cast<int>(i - static_cast<int64_t>(outer) * fast);
+    const int r = tall ? inner : outer, l = tall ? outer : inner;
+    const float v = to_f32(tall ? g[(l0 + l) * p.ldg + r] : g[r * p.ldg + l0 + l]);
+    X[r * ldx + l] = v;
+    const float one[1] = {v};
+    sum += squares(one);
+  }
+  sum = cta_sum(sum, norm_part);
+  if (p.cluster > 1) {
+    cluster_sync();                              // every CTA runs
+    if (tid < p.cluster) st_peer_f64(&norm_peer[rank], tid, sum);
+    cluster_sync();
+    sum = 0.0;
+    for (int i = 0; i < p.cluster; ++i) sum += norm_peer[i];
+  }
+  float power, factor;
+  inverse_norm(sum, p.eps, power, factor);
+  for (int i = tid; i < s4 * ldx; i += kThreads) X[i] = (X[i] * power) * factor;
+  __syncthreads();
+
+  const int side = s4 / 4, tiles = side * side;  // at most 256
+  int groups = 1;
+  while (groups * 2 * tiles <= kThreads) groups *= 2;
+  const int tile = tid % tiles, group = tid / tiles, ti = tile / side * 4, tj = tile % side * 4;
+  int cur = 0;
+  for (int step = 0; step < p.steps; ++step) {
+    const float* x = X + cur * s4 * ldx;
+    float* y = X + (cur ^ 1) * s4 * ldx;
+    // ---- this CTA's share of A = X X^T
+    if (group < groups) {
+      float acc[4][4] = {};
+      for (int l = group * 4; l < p.share; l += groups * 4) {
+        float4 u[4], v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          u[i] = *reinterpret_cast<const float4*>(x + (ti + i) * ldx + l);
+          v[i] = *reinterpret_cast<const float4*>(x + (tj + i) * ldx + l);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            acc[i][j] = fmaf(u[i].x, v[j].x, fmaf(u[i].y, v[j].y, fmaf(u[i].z, v[j].z, fmaf(u[i].w, v[j].w, acc[i][j]))));
+      }
+#pragma unroll
+      for (int e = 0; e < 16; ++e) red[(group * 16 + e) * tiles + tile] = acc[e / 4][e % 4];
+    }
+    __syncthreads();
+    for (int i = tid; i < tiles * 16; i += kThreads) {
+      float v = 0.f;
+      for (int q = 0; q < groups; ++q) v += red[q * tiles * 16 + i];
+      const int e = i / tiles, t = i - e * tiles;
+      P[(t / side * 4 + e / 4) * lda + t % side * 4 + e % 4] = v;
+    }
+    // ---- A in every CTA
+    const float* full = P;
+    if (p.cluster > 1) {
+      cluster_sync();                            // the shares are there, and no peer reads the last step's A any more
+      const int all = s4 * s4, per = (all + p.cluster - 1) / p.cluster;
+      for (int i = rank * per + tid; i < (rank + 1) * per && i < all; i += kThreads) {
+        const int at = i / s4 * lda + i % s4;
+        float v[kMaxCluster];
+#pragma unroll
+        for (int q = 0; q < kMaxCluster; ++q) v[q] = q < p.cluster ? ld_dsmem_f32(P + at, q) : 0.f;
+        float t = 0.f;
+#pragma unroll
+        for (int q = 0; q < kMaxCluster; ++q) t += v[q];
+        for (int q = 0; q < p.cluster; ++q) st_peer(A + at, q, t);
+      }
+      cluster_sync();
+      full = A;
+    } else {
+      __syncthreads();
+    }
+    // ---- B = a I + b A + c A A, a tile of four rows and columns a thread
+    for (int t = tid; t < tiles; t += kThreads) {
+      const int i0 = t / side * 4, j0 = t % side * 4;
+      float acc[4][4] = {};
+      for (int k = 0; k < s4; k += 4) {
+        float4 u[4], v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          u[i] = *reinterpret_cast<const float4*>(full + (i0 + i) * lda + k);
+          v[i] = *reinterpret_cast<const float4*>(full + (j0 + i) * lda + k);   // A is symmetric
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            acc[i][j] = fmaf(u[i].x, v[j].x, fmaf(u[i].y, v[j].y, fmaf(u[i].z, v[j].z, fmaf(u[i].w, v[j].w, acc[i][j]))));
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          B[(i0 + i) * lda + j0 + j] = fmaf(p.c, acc[i][j], fmaf(p.b, full[(i0 + i) * lda + j0 + j], i0 + i == j0 + j ? p.a : 0.f));
+    }
+    __syncthreads();
+    // ---- X <- B X, four rows and columns a thread
+    const int across = p.share / 4;
+    for (int t = tid; t < side * across; t += kThreads) {
+      const int i0 = t / across * 4, l = t % across * 4;
+      float4 acc[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int k = 0; k < s4; k += 4) {
+        float4 u[4], v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          u[i] = *reinterpret_cast<const float4*>(B + (i0 + i) * lda + k);
+          v[i] = *reinterpret_cast<const float4*>(x + (k + i) * ldx + l);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float w[4] = {u[i].x, u[i].y, u[i].z, u[i].w};
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            acc[i].x = fmaf(w[j], v[j].x, acc[i].x);
+            acc[i].y = fmaf(w[j], v[j].y, acc[i].y);
+            acc[i].z = fmaf(w[j], v[j].z, acc[i].z);
+            acc[i].w = fmaf(w[j], v[j].w, acc[i].w);
+          }
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) *reinterpret_cast<float4*>(y + (i0 + i) * ldx + l) = acc[i];
+    }
+    cur ^= 1;
+    __syncthreads();
+  }
+  // ---- the result
+  const float* x = X + cur * s4 * ldx;
+  for (int64_t i = tid; i < static_cast<int64_t>(p.s) * n; i += kThreads) {
+    const int outer = static_cast<int>(i / fast), inner = static_cast<int>(i - static_cast<int64_t>(outer) * fast);
+    const int r = tall ? inner : outer, l = tall ? outer : inner;
+    const int64_t at = z * p.zo + (tall ? (l0 + l) * p.ldo + r : r * p.ldo + l0 + l);
+    const float v = x[r * ldx + l] * p.scale;
+    if (p.out_type == kNsBf16) static_cast<__nv_bfloat16*>(p.out)[at] = __float2bfloat16_rn(v);
+    else if (p.out_type == kNsAdd) static_cast<float*>(p.out)[at] += v;
+    else static_cast<float*>(p.out)[at] = v;
+  }
+  if (p.cluster > 1) cluster_sync();             // no CTA ends while a peer may read its share
+}
+
+}  // namespace
+
+// CTAs a matrix, 0 where the products run on the tensor cores
+int ns_small_cluster(int rows, int cols) {
+  const int s = rows < cols ? rows : cols, len = rows < cols ? cols : rows;
+  if (s > kMaxS) return 0;
+  for (int c = 1; c <= kMaxCluster; c *= 2) {
+    const int share = up4((len + c - 1) / c);
+    const double work = static_cast<double>(s) * s * share;
+    // a cluster only where a CTA alone has more to do than the exchanges take
+    if (smem_floats(s, share) * 4 <= kMaxSmem && (work <= 100e3 || (c == kMaxCluster && work <= kMaxWork))) return c;
+  }
+  return 0;
+}
+
+cudaError_t launch_ns_small(const void* G, int64_t ldg, int64_t zg, bool bf16, void* out, int64_t ldo, int64_t zo, int out_type,
+                            int batch, int rows, int cols, int steps, const float (&co)[3], float eps, float scale,
+                            cudaStream_t s) {
+  SmallArgs a{};
+  a.G = G, a.ldg = ldg, a.zg = zg;
+  a.out = out, a.ldo = ldo, a.zo = zo, a.out_type = out_type;
+  a.rows = rows, a.cols = cols;
+  a.s = rows < cols ? rows : cols;
+  a.len = rows < cols ? cols : rows;
+  a.cluster = ns_small_cluster(rows, cols);
+  a.share = up4((a.len + a.cluster - 1) / a.cluster);
+  a.steps = steps;
+  a.a = co[0], a.b = co[1], a.c = co[2];
+  a.eps = eps, a.scale = scale;
+  const size_t smem = smem_floats(a.s, a.share) * 4;
+  void (*kernel)(SmallArgs) = bf16 ? orth_small_kernel<__nv_bfloat16> : orth_small_kernel<float>;
+  cudaError_t e = allow_smem(kernel, smem);
+  if (e != cudaSuccess) return e;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = a.cluster;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(batch * a.cluster, 1, 1);
+  cfg.blockDim = dim3(kThreads, 1, 1);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cfg.attrs = attr;
+  cfg.numAttrs = a.cluster > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kernel, a);
+}
+
+}  // namespace oscars

@@ -11,7 +11,7 @@
 // X <- X B (B is a polynomial in A, so both are the same step).  No transposed
 // copy is made of either.
 //
-// Launches: the sum of squares (with the merge of the deltas in the same pass),
+// Small matrices: one launch (orth_small.cu).  Others: the sum of squares (with the merge of the deltas in the same pass),
 // X = G / norm, then three products a step, two where c = 0 (orth_product.cu, where the precision
 // of X, A and B is explained).
 #include <cmath>
@@ -68,27 +68,6 @@ Shape make_shape(int batch, int rows, int cols, int dtype, bool with_u) {
 }
 
 // ------------------------------------------------------------------ streaming passes
-
-// Sum of 8 squares.  In fp32 where neither it nor a term that counts can leave
-// the range, else (magnitudes below 1e-10 or above 1e15) in fp64, so that no
-// update is too small or too large for its norm.
-template <int N>
-__device__ __forceinline__ double squares(const float (&v)[N]) {
-  float s = 0.f;
-  bool any = false;
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    s = fmaf(v[i], v[i], s);
-    any |= v[i] != 0.f;
-  }
-  if (any && !(s > 1e-20f && s < 1e30f)) {
-    double d = 0.0;
-#pragma unroll
-    for (int i = 0; i < N; ++i) d += static_cast<double>(v[i]) * static_cast<double>(v[i]);
-    return d;
-  }
-  return s;
-}
 
 // Sum over the block in a fixed order; the result is thread 0's.
 __device__ __forceinline__ double block_sum(double x) {
@@ -199,11 +178,7 @@ __global__ void __launch_bounds__(kPasses) orth_scale_kernel(const T* __restrict
   for (int i = threadIdx.x; i < parts; i += kPasses) t += part[blockIdx.y * static_cast<int64_t>(parts) + i];
   t = block_sum(t);
   if (threadIdx.x == 0) {
-    // 1 / (norm + eps) = power x factor, each a normal fp32 number
-    int e;
-    const double m = frexp(sqrt(t) + static_cast<double>(eps), &e);
-    inv_s[0] = static_cast<float>(1.0 / m);
-    inv_s[1] = isinf(t) ? 0.f : ldexpf(1.f, -e);
+    inverse_norm(t, eps, inv_s[1], inv_s[0]);
   }
   __syncthreads();
   const float f = inv_s[0], pw = inv_s[1];
@@ -333,6 +308,9 @@ template <typename T>
 oscars_status orthogonalize(const Shape& p, const void* G, int64_t ldg, int64_t bsg, uint8_t* ws, int steps,
                             const float (&co)[3], float eps, const Target& to, cudaStream_t s) {
   const T* g = static_cast<const T*>(G);
+  if (ns_small_cluster(p.rows, p.cols) > 0)
+    return launch_ns_small(G, ldg, bsg, sizeof(T) == 2, to.D, to.ldd, to.zd, to.type, p.batch, p.rows, p.cols, steps, co, eps,
+                           to.scale, s) == cudaSuccess ? OSCARS_OK : OSCARS_ECUDA;
   const int vec = (reinterpret_cast<uintptr_t>(g) | (ldg * sizeof(T)) | (bsg * sizeof(T))) % 16 == 0;
   if (launch_dependent(orth_norm_kernel<T>, dim3(p.parts, p.batch), kPasses, 0, s, g, ldg, bsg, p.rows, p.cols, vec,
                        reinterpret_cast<double*>(ws + p.off_part)) != cudaSuccess)
@@ -411,6 +389,9 @@ oscars_status oscars_merge_orthogonal(float* x_g, const float* const* deltas, co
                        mu, nesterov != 0 ? 1 : 0, u, n, part) != cudaSuccess)
     return OSCARS_ECUDA;
   const Target to{x_g, cols, 0, kNsAdd, server_lr};
+  if (ns_small_cluster(rows, cols) > 0)
+    return launch_ns_small(u, cols, 0, false, to.D, to.ldd, to.zd, to.type, 1, rows, cols, steps, co, eps, to.scale, s) ==
+                   cudaSuccess ? OSCARS_OK : OSCARS_ECUDA;
   return steps_from(p, ws, static_cast<const float*>(u), cols, 0, eps, steps, co, to, s) == cudaSuccess ? OSCARS_OK
                                                                                                        : OSCARS_ECUDA;
 }

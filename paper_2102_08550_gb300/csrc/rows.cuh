@@ -35,6 +35,35 @@ __device__ __forceinline__ void load8(const T* p, int n, bool vec, float (&v)[8]
   }
 }
 
+// Sum of squares.  In fp32 where neither it nor a term that counts can leave
+// the range, else (magnitudes below 1e-10 or above 1e15) in fp64, so that no
+// update is too small or too large for its norm.
+template <int N>
+__device__ __forceinline__ double squares(const float (&v)[N]) {
+  float s = 0.f;
+  bool any = false;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    s = fmaf(v[i], v[i], s);
+    any |= v[i] != 0.f;
+  }
+  if (any && !(s > 1e-20f && s < 1e30f)) {
+    double d = 0.0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) d += static_cast<double>(v[i]) * static_cast<double>(v[i]);
+    return d;
+  }
+  return s;
+}
+
+// 1 / (norm + eps) = power x factor, each a normal fp32 number (power: of two), of a sum of squares.
+__device__ __forceinline__ void inverse_norm(double squares, float eps, float& power, float& factor) {
+  int e;
+  const double m = frexp(sqrt(squares) + static_cast<double>(eps), &e);
+  factor = static_cast<float>(1.0 / m);
+  power = isinf(squares) ? 0.f : ldexpf(1.f, -e);
+}
+
 // A launch whose set-up may run while the previous kernel on the stream ends: the
 // kernel calls pdl_wait() before it touches global memory.
 template <typename... P, typename... A>
