@@ -248,10 +248,10 @@ struct NsMaps {
 };
 // All steps of small matrices in one launch (csrc/orth_small.cu): CTAs a matrix,
 // or 0 where the products run on the tensor cores
-int ns_small_cluster(int rows, int cols);
+int ns_small_cluster(int batch, int rows, int cols, bool f32);
 cudaError_t launch_ns_small(const void* G, int64_t ldg, int64_t zg, bool bf16, void* out, int64_t ldo, int64_t zo, int out_type,
-                            int batch, int rows, int cols, int steps, const float (&co)[3], float eps, float scale,
-                            cudaStream_t s);
+                            int batch, int rows, int cols, int cluster, int steps, const float (&co)[3], float eps,
+                            float scale, cudaStream_t s);
 cudaError_t launch_ns_product(int epi, const NsMaps& A, const NsMaps& B, const NsMaps& D, NsArgs a, cudaStream_t s);
 
 // Weight gradient + SGD of up to kDwMaxLayers hidden layers, persistent

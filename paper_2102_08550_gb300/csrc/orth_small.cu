@@ -16,10 +16,10 @@ namespace oscars {
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 512;
 constexpr int kMaxS = 64, kMaxCluster = 8;
 constexpr size_t kMaxSmem = 200 * 1024;
-constexpr double kMaxWork = 600e3;               // multiply-adds of a CTA's Gram share: beyond, the tensor cores are faster
+constexpr int kMaxGroups = 32;                   // of threads that share a tile's long sum
 
 struct SmallArgs {
   const void* G;
@@ -42,25 +42,11 @@ size_t smem_floats(int s, int share) {
 __device__ __forceinline__ void st_peer(const void* local, int rank, float v) {
   asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(cluster_addr(local, rank)), "f"(v) : "memory");
 }
-__device__ __forceinline__ void st_peer_f64(const void* local, int rank, double v) {
-  asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(cluster_addr(local, rank)), "d"(v) : "memory");
-}
-
-// Sum over the CTA in a fixed order, in every thread.
-__device__ __forceinline__ double cta_sum(double x, double* part) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-  if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = x;
-  __syncthreads();
-  double s = 0.0;
-  for (int i = 0; i < kThreads / 32; ++i) s += part[i];
-  return s;
-}
-
 template <typename T>
 __global__ void __launch_bounds__(kThreads) orth_small_kernel(const __grid_constant__ SmallArgs p) {
   extern __shared__ __align__(16) float sm[];
-  __shared__ double norm_part[kThreads / 32], norm_peer[kMaxCluster];
+  __shared__ Squares norm_part[kThreads / 32], norm_peer[kMaxCluster];
+  __shared__ float scale_s[2];
   const int s4 = (p.s + 3) / 4 * 4, lda = s4 + 4, ldx = row_floats(p.share), tid = threadIdx.x;
   float* X = sm;                                 // [2][s4][ldx]
   float* A = X + 2 * s4 * ldx;                   // [s4][lda]
@@ -75,35 +61,62 @@ __global__ void __launch_bounds__(kThreads) orth_small_kernel(const __grid_const
 
   // ---- X as it comes, and its norm.  Of a wide matrix a CTA holds columns, of a tall one rows (as columns)
   const T* g = static_cast<const T*>(p.G) + z * p.zg;
-  for (int i = tid; i < 2 * s4 * ldx; i += kThreads) X[i] = 0.f;
+  for (int i = tid * 4; i < s4 * ldx; i += kThreads * 4) *reinterpret_cast<float4*>(X + i) = make_float4(0.f, 0.f, 0.f, 0.f);
   __syncthreads();
-  double sum = 0.0;
-  const int fast = tall ? p.s : n;               // consecutive in memory
-  for (int64_t i = tid; i < static_cast<int64_t>(p.s) * n; i += kThreads) {
-    const int outer = static_cast<int>(i / fast), inner = static_cast<int>(i - static_cast<int64_t>(outer) * fast);
-    const int r = tall ? inner : outer, l = tall ? outer : inner;
-    const float v = to_f32(tall ? g[(l0 + l) * p.ldg + r] : g[r * p.ldg + l0 + l]);
-    X[r * ldx + l] = v;
-    const float one[1] = {v};
-    sum += squares(one);
+  Squares sum;
+  const uint32_t fast = tall ? p.s : n, count = static_cast<uint32_t>(p.s) * n;   // fast: consecutive in memory
+  for (uint32_t i0 = tid; i0 < count; i0 += kThreads * 8) {
+    float v[8];
+    int at[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {   // eight loads in flight
+      const uint32_t i = i0 + e * kThreads;
+      at[e] = -1;
+      v[e] = 0.f;
+      if (i < count) {
+        const uint32_t outer = i / fast, inner = i - outer * fast;
+        const int r = tall ? inner : outer, l = tall ? outer : inner;
+        v[e] = to_f32(tall ? g[(l0 + l) * p.ldg + r] : g[r * p.ldg + l0 + l]);
+        at[e] = r * ldx + l;
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (at[e] >= 0) X[at[e]] = v[e];
+    sum.add(v);
   }
-  sum = cta_sum(sum, norm_part);
+  sum.block_sum(norm_part);
   if (p.cluster > 1) {
     cluster_sync();                              // every CTA runs
-    if (tid < p.cluster) st_peer_f64(&norm_peer[rank], tid, sum);
+    if (tid == 0)
+      for (int q = 0; q < p.cluster; ++q) {
+        st_peer(&norm_peer[rank].mid, q, sum.mid);
+        st_peer(&norm_peer[rank].big, q, sum.big);
+        st_peer(&norm_peer[rank].small, q, sum.small);
+      }
     cluster_sync();
-    sum = 0.0;
-    for (int i = 0; i < p.cluster; ++i) sum += norm_peer[i];
+    if (tid == 0) {
+      sum = norm_peer[0];
+      for (int q = 1; q < p.cluster; ++q) sum.add(norm_peer[q]);
+    }
   }
-  float power, factor;
-  inverse_norm(sum, p.eps, power, factor);
-  for (int i = tid; i < s4 * ldx; i += kThreads) X[i] = (X[i] * power) * factor;
+  if (tid == 0) inverse_norm(sum.total(), p.eps, scale_s[0], scale_s[1]);   // fp64: one thread's, not 512
+  __syncthreads();
+  const float power = scale_s[0], factor = scale_s[1];
+  for (int i = tid * 4; i < s4 * ldx; i += kThreads * 4) {
+    float4 v = *reinterpret_cast<const float4*>(X + i);
+    v.x = (v.x * power) * factor, v.y = (v.y * power) * factor, v.z = (v.z * power) * factor, v.w = (v.w * power) * factor;
+    *reinterpret_cast<float4*>(X + i) = v;
+  }
   __syncthreads();
 
+  // a thread's tile: rows tr, tr + side, ... and columns tc, tc + side, ... (neighbours read neighbouring rows, which
+  // lie on different banks); the tiles' long sums over groups of threads
   const int side = s4 / 4, tiles = side * side;  // at most 256
   int groups = 1;
-  while (groups * 2 * tiles <= kThreads) groups *= 2;
-  const int tile = tid % tiles, group = tid / tiles, ti = tile / side * 4, tj = tile % side * 4;
+  while (groups < kMaxGroups && groups * 2 * tiles <= kThreads) groups *= 2;
+  const int tile = tid % tiles, group = tid / tiles, tr = tile / side, tc = tile % side;
+  const int across = p.share / 4;
   int cur = 0;
   for (int step = 0; step < p.steps; ++step) {
     const float* x = X + cur * s4 * ldx;
@@ -115,8 +128,8 @@ __global__ void __launch_bounds__(kThreads) orth_small_kernel(const __grid_const
         float4 u[4], v[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          u[i] = *reinterpret_cast<const float4*>(x + (ti + i) * ldx + l);
-          v[i] = *reinterpret_cast<const float4*>(x + (tj + i) * ldx + l);
+          u[i] = *reinterpret_cast<const float4*>(x + (tr + i * side) * ldx + l);
+          v[i] = *reinterpret_cast<const float4*>(x + (tc + i * side) * ldx + l);
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -128,12 +141,14 @@ __global__ void __launch_bounds__(kThreads) orth_small_kernel(const __grid_const
       for (int e = 0; e < 16; ++e) red[(group * 16 + e) * tiles + tile] = acc[e / 4][e % 4];
     }
     __syncthreads();
-    for (int i = tid; i < tiles * 16; i += kThreads) {
-      float v = 0.f;
-      for (int q = 0; q < groups; ++q) v += red[q * tiles * 16 + i];
-      const int e = i / tiles, t = i - e * tiles;
-      P[(t / side * 4 + e / 4) * lda + t % side * 4 + e % 4] = v;
-    }
+    // entry e of a tile is group e's, e + groups', ... thread of that tile
+    if (group < groups)
+      for (int e = group; e < 16; e += groups) {
+        float v = 0.f;
+#pragma unroll 8
+        for (int q = 0; q < groups; ++q) v += red[(q * 16 + e) * tiles + tile];
+        P[(tr + e / 4 * side) * lda + tc + e % 4 * side] = v;
+      }
     // ---- A in every CTA
     const float* full = P;
     if (p.cluster > 1) {
@@ -154,16 +169,25 @@ __global__ void __launch_bounds__(kThreads) orth_small_kernel(const __grid_const
     } else {
       __syncthreads();
     }
-    // ---- B = a I + b A + c A A, a tile of four rows and columns a thread
-    for (int t = tid; t < tiles; t += kThreads) {
-      const int i0 = t / side * 4, j0 = t % side * 4;
+    // ---- B = a I + b A + c A A: an entry a thread, or of more than 16 rows a tile
+    if (s4 <= 16) {
+      for (int i = tid; i < s4 * s4; i += kThreads) {
+        const int r = i / s4, c = i - r * s4;
+        float acc = 0.f;
+        for (int k = 0; k < s4; k += 4) {
+          const float4 u = *reinterpret_cast<const float4*>(full + r * lda + k), v = *reinterpret_cast<const float4*>(full + c * lda + k);
+          acc = fmaf(u.x, v.x, fmaf(u.y, v.y, fmaf(u.z, v.z, fmaf(u.w, v.w, acc))));   // A is symmetric
+        }
+        B[r * lda + c] = fmaf(p.c, acc, fmaf(p.b, full[r * lda + c], r == c ? p.a : 0.f));
+      }
+    } else if (tid < tiles) {
       float acc[4][4] = {};
       for (int k = 0; k < s4; k += 4) {
         float4 u[4], v[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          u[i] = *reinterpret_cast<const float4*>(full + (i0 + i) * lda + k);
-          v[i] = *reinterpret_cast<const float4*>(full + (j0 + i) * lda + k);   // A is symmetric
+          u[i] = *reinterpret_cast<const float4*>(full + (tr + i * side) * lda + k);
+          v[i] = *reinterpret_cast<const float4*>(full + (tc + i * side) * lda + k);
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -174,12 +198,13 @@ __global__ void __launch_bounds__(kThreads) orth_small_kernel(const __grid_const
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          B[(i0 + i) * lda + j0 + j] = fmaf(p.c, acc[i][j], fmaf(p.b, full[(i0 + i) * lda + j0 + j], i0 + i == j0 + j ? p.a : 0.f));
+        for (int j = 0; j < 4; ++j) {
+          const int r = tr + i * side, c = tc + j * side;
+          B[r * lda + c] = fmaf(p.c, acc[i][j], fmaf(p.b, full[r * lda + c], r == c ? p.a : 0.f));
+        }
     }
     __syncthreads();
     // ---- X <- B X, four rows and columns a thread
-    const int across = p.share / 4;
     for (int t = tid; t < side * across; t += kThreads) {
       const int i0 = t / across * 4, l = t % across * 4;
       float4 acc[4];
@@ -212,43 +237,67 @@ __global__ void __launch_bounds__(kThreads) orth_small_kernel(const __grid_const
   }
   // ---- the result
   const float* x = X + cur * s4 * ldx;
-  for (int64_t i = tid; i < static_cast<int64_t>(p.s) * n; i += kThreads) {
-    const int outer = static_cast<int>(i / fast), inner = static_cast<int>(i - static_cast<int64_t>(outer) * fast);
-    const int r = tall ? inner : outer, l = tall ? outer : inner;
-    const int64_t at = z * p.zo + (tall ? (l0 + l) * p.ldo + r : r * p.ldo + l0 + l);
-    const float v = x[r * ldx + l] * p.scale;
-    if (p.out_type == kNsBf16) static_cast<__nv_bfloat16*>(p.out)[at] = __float2bfloat16_rn(v);
-    else if (p.out_type == kNsAdd) static_cast<float*>(p.out)[at] += v;
-    else static_cast<float*>(p.out)[at] = v;
+  for (uint32_t i0 = tid; i0 < count; i0 += kThreads * 8) {
+    float v[8];
+    int64_t at[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t i = i0 + e * kThreads;
+      at[e] = -1;
+      if (i < count) {
+        const uint32_t outer = i / fast, inner = i - outer * fast;
+        const int r = tall ? inner : outer, l = tall ? outer : inner;
+        at[e] = z * p.zo + (tall ? (l0 + l) * p.ldo + r : r * p.ldo + l0 + l);
+        v[e] = x[r * ldx + l] * p.scale;
+        if (p.out_type == kNsAdd) v[e] += static_cast<const float*>(p.out)[at[e]];
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      if (at[e] < 0) continue;
+      if (p.out_type == kNsBf16) static_cast<__nv_bfloat16*>(p.out)[at[e]] = __float2bfloat16_rn(v[e]);
+      else static_cast<float*>(p.out)[at[e]] = v[e];
+    }
   }
   if (p.cluster > 1) cluster_sync();             // no CTA ends while a peer may read its share
 }
 
 }  // namespace
 
-// CTAs a matrix, 0 where the products run on the tensor cores
-int ns_small_cluster(int rows, int cols) {
+// CTAs a matrix, or 0 where the products run on the tensor cores: the shorter of two estimates of five steps in us, each
+// fitted to measurements (s x len x batch, fp32: this kernel / the tensor cores: 10 x 512 x 1 21 / 66, 32 x 1000 x 1 34 / 76,
+// 32 x 1000 x 16 67 / 90, 48 x 800 x 1 55 / 78, 64 x 784 x 1 74 / 78, 64 x 784 x 16 146 / 90; bf16: 24 x 1000 x 64 140 / 98).
+// A CTA takes 15 us for its barriers and the load, more for longer sides of A and for its share; one CTA runs on an SM.
+int ns_small_cluster(int batch, int rows, int cols, bool f32) {
   const int s = rows < cols ? rows : cols, len = rows < cols ? cols : rows;
   if (s > kMaxS) return 0;
+  const double per_len = batch <= 8 ? 0.01 : batch <= 32 ? 0.02 : 0.04;   // the tensor cores' Gram products
+  double best = 0.9 * ((f32 ? 55.0 : 43.0) + per_len * len);
+  int most = 0;
   for (int c = 1; c <= kMaxCluster; c *= 2) {
     const int share = up4((len + c - 1) / c);
-    const double work = static_cast<double>(s) * s * share;
-    // a cluster only where a CTA alone has more to do than the exchanges take
-    if (smem_floats(s, share) * 4 <= kMaxSmem && (work <= 100e3 || (c == kMaxCluster && work <= kMaxWork))) return c;
+    if (smem_floats(s, share) * 4 > kMaxSmem) continue;
+    const int room = c == 8 ? 15 * 8 : 144;      // CTAs at once: a GPC's SMs are no multiple of 8
+    const double waves = static_cast<double>((static_cast<int64_t>(batch) * c + room - 1) / room);
+    const double cost = waves * (15.0 + 0.35 * s + 8e-5 * s * s * share + (c > 1 ? 4.0 : 0.0));
+    if (cost < best) {
+      best = cost;
+      most = c;
+    }
   }
-  return 0;
+  return most;
 }
 
 cudaError_t launch_ns_small(const void* G, int64_t ldg, int64_t zg, bool bf16, void* out, int64_t ldo, int64_t zo, int out_type,
-                            int batch, int rows, int cols, int steps, const float (&co)[3], float eps, float scale,
-                            cudaStream_t s) {
+                            int batch, int rows, int cols, int cluster, int steps, const float (&co)[3], float eps,
+                            float scale, cudaStream_t s) {
   SmallArgs a{};
   a.G = G, a.ldg = ldg, a.zg = zg;
   a.out = out, a.ldo = ldo, a.zo = zo, a.out_type = out_type;
   a.rows = rows, a.cols = cols;
   a.s = rows < cols ? rows : cols;
   a.len = rows < cols ? cols : rows;
-  a.cluster = ns_small_cluster(rows, cols);
+  a.cluster = cluster;
   a.share = up4((a.len + a.cluster - 1) / a.cluster);
   a.steps = steps;
   a.a = co[0], a.b = co[1], a.c = co[2];

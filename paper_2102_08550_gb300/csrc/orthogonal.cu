@@ -58,7 +58,7 @@ Shape make_shape(int batch, int rows, int cols, int dtype, bool with_u) {
     at = up(at + bytes, 256);
     return o;
   };
-  p.off_part = take(static_cast<int64_t>(batch) * p.parts * 8);
+  p.off_part = take(static_cast<int64_t>(batch) * p.parts * sizeof(Squares));
   p.off_u = with_u ? take(elems * 4) : 0;
   for (int i = 0; i < 2; ++i) p.off_x[i] = take(static_cast<int64_t>(batch) * rows * p.ldx * 4);
   p.off_a = take(static_cast<int64_t>(batch) * p.s * p.lds * 2 * p.halves);
@@ -69,36 +69,24 @@ Shape make_shape(int batch, int rows, int cols, int dtype, bool with_u) {
 
 // ------------------------------------------------------------------ streaming passes
 
-// Sum over the block in a fixed order; the result is thread 0's.
-__device__ __forceinline__ double block_sum(double x) {
-  __shared__ double part[kPasses / 32];
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-  if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = x;
-  __syncthreads();
-  double s = 0.0;
-  if (threadIdx.x == 0)
-    for (int i = 0; i < kPasses / 32; ++i) s += part[i];
-  return s;
-}
-
 // part[z][block] = sum of squares of the block's share of matrix z
 template <typename T>
 __global__ void __launch_bounds__(kPasses) orth_norm_kernel(const T* __restrict__ G, int64_t ldg, int64_t bsg, int rows,
-                                                            int cols, int vec, double* __restrict__ part) {
+                                                            int cols, int vec, Squares* __restrict__ part) {
+  __shared__ Squares warps[kPasses / 32];
   pdl_wait();
   pdl_trigger();
   const T* g = G + blockIdx.y * bsg;
   const int per_row = (cols + 7) / 8;
   const int64_t n = static_cast<int64_t>(rows) * per_row, step = static_cast<int64_t>(gridDim.x) * kPasses;
-  double sum = 0.0;
+  Squares sum;
   for (int64_t i = static_cast<int64_t>(blockIdx.x) * kPasses + threadIdx.x; i < n; i += step) {
     const int r = static_cast<int>(i / per_row), c = static_cast<int>(i - static_cast<int64_t>(r) * per_row) * 8;
     float v[8];
     load8(g + r * ldg + c, cols - c, vec, v);
-    sum += squares(v);
+    sum.add(v);
   }
-  sum = block_sum(sum);
+  sum.block_sum(warps);
   if (threadIdx.x == 0) part[blockIdx.y * gridDim.x + blockIdx.x] = sum;
 }
 
@@ -106,11 +94,12 @@ __global__ void __launch_bounds__(kPasses) orth_norm_kernel(const T* __restrict_
 template <int V>
 __global__ void __launch_bounds__(kPasses) orth_merge_kernel(const __grid_constant__ MergeArgs a, float* __restrict__ mom,
                                                              float mu, int nesterov, float* __restrict__ u, int64_t n,
-                                                             double* __restrict__ part) {
+                                                             Squares* __restrict__ part) {
+  __shared__ Squares warps[kPasses / 32];
   pdl_wait();
   pdl_trigger();
   const int64_t step = static_cast<int64_t>(gridDim.x) * kPasses * V;
-  double sum = 0.0;
+  Squares sum;
   for (int64_t i = (static_cast<int64_t>(blockIdx.x) * kPasses + threadIdx.x) * V; i < n; i += step) {
     const bool full = i + V <= n;
     float d[V], x[V];
@@ -160,25 +149,26 @@ __global__ void __launch_bounds__(kPasses) orth_merge_kernel(const __grid_consta
 #pragma unroll
     for (int j = 0; j < V; ++j)
       if (i + j < n) u[i + j] = d[j];
-    sum += squares(d);
+    sum.add(d);
   }
-  sum = block_sum(sum);
+  sum.block_sum(warps);
   if (threadIdx.x == 0) part[blockIdx.x] = sum;
 }
 
 // X = G / (norm + eps) as two fp16 halves, [half][z][rows][ldx], the row padding zero
 template <typename T>
 __global__ void __launch_bounds__(kPasses) orth_scale_kernel(const T* __restrict__ G, int64_t ldg, int64_t bsg, int rows,
-                                                             int cols, int vec, const double* __restrict__ part, int parts,
+                                                             int cols, int vec, const Squares* __restrict__ part, int parts,
                                                              float eps, __half* __restrict__ X, int64_t ldx) {
   __shared__ float inv_s[2];
   pdl_wait();
   pdl_trigger();
-  double t = 0.0;
-  for (int i = threadIdx.x; i < parts; i += kPasses) t += part[blockIdx.y * static_cast<int64_t>(parts) + i];
-  t = block_sum(t);
-  if (threadIdx.x == 0) {
-    inverse_norm(t, eps, inv_s[1], inv_s[0]);
+  if (threadIdx.x < 32) {   // one warp adds up the parts: blocks' sums may leave fp32's range together, so in fp64
+    double t = 0.0;
+    for (int i = threadIdx.x; i < parts; i += 32) t += part[blockIdx.y * static_cast<int64_t>(parts) + i].total();
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
+    if (threadIdx.x == 0) inverse_norm(t, eps, inv_s[1], inv_s[0]);
   }
   __syncthreads();
   const float f = inv_s[0], pw = inv_s[1];
@@ -240,7 +230,7 @@ cudaError_t steps_from(const Shape& p, uint8_t* ws, const T* G, int64_t ldg, int
     return cudaErrorInvalidValue;
   const int vec = (reinterpret_cast<uintptr_t>(G) | (ldg * sizeof(T)) | (bsg * sizeof(T))) % 16 == 0;
   cudaError_t e = launch_dependent(orth_scale_kernel<T>, dim3(pass_blocks(p.rows * (p.ldx / 8), 1024), p.batch), kPasses, 0, s,
-                                   G, ldg, bsg, p.rows, p.cols, vec, reinterpret_cast<const double*>(ws + p.off_part), p.parts,
+                                   G, ldg, bsg, p.rows, p.cols, vec, reinterpret_cast<const Squares*>(ws + p.off_part), p.parts,
                                    eps, X[0], p.ldx);
   const bool tall = p.rows > p.cols;
   const bool cubic = co[2] == 0.f;
@@ -308,12 +298,12 @@ template <typename T>
 oscars_status orthogonalize(const Shape& p, const void* G, int64_t ldg, int64_t bsg, uint8_t* ws, int steps,
                             const float (&co)[3], float eps, const Target& to, cudaStream_t s) {
   const T* g = static_cast<const T*>(G);
-  if (ns_small_cluster(p.rows, p.cols) > 0)
-    return launch_ns_small(G, ldg, bsg, sizeof(T) == 2, to.D, to.ldd, to.zd, to.type, p.batch, p.rows, p.cols, steps, co, eps,
+  if (const int c = ns_small_cluster(p.batch, p.rows, p.cols, sizeof(T) == 4))
+    return launch_ns_small(G, ldg, bsg, sizeof(T) == 2, to.D, to.ldd, to.zd, to.type, p.batch, p.rows, p.cols, c, steps, co, eps,
                            to.scale, s) == cudaSuccess ? OSCARS_OK : OSCARS_ECUDA;
   const int vec = (reinterpret_cast<uintptr_t>(g) | (ldg * sizeof(T)) | (bsg * sizeof(T))) % 16 == 0;
   if (launch_dependent(orth_norm_kernel<T>, dim3(p.parts, p.batch), kPasses, 0, s, g, ldg, bsg, p.rows, p.cols, vec,
-                       reinterpret_cast<double*>(ws + p.off_part)) != cudaSuccess)
+                       reinterpret_cast<Squares*>(ws + p.off_part)) != cudaSuccess)
     return OSCARS_ECUDA;
   return steps_from(p, ws, g, ldg, bsg, eps, steps, co, to, s) == cudaSuccess ? OSCARS_OK : OSCARS_ECUDA;
 }
@@ -382,15 +372,15 @@ oscars_status oscars_merge_orthogonal(float* x_g, const float* const* deltas, co
   if (!workspace_ok(workspace, workspace_bytes, p.bytes)) return OSCARS_EINVAL;
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   float* u = reinterpret_cast<float*>(ws + p.off_u);
-  double* part = reinterpret_cast<double*>(ws + p.off_part);
+  Squares* part = reinterpret_cast<Squares*>(ws + p.off_part);
   const int64_t n = static_cast<int64_t>(rows) * cols;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   if (launch_dependent((bits & 15) == 0 ? orth_merge_kernel<4> : orth_merge_kernel<1>, dim3(p.parts), kPasses, 0, s, a, momentum,
                        mu, nesterov != 0 ? 1 : 0, u, n, part) != cudaSuccess)
     return OSCARS_ECUDA;
   const Target to{x_g, cols, 0, kNsAdd, server_lr};
-  if (ns_small_cluster(rows, cols) > 0)
-    return launch_ns_small(u, cols, 0, false, to.D, to.ldd, to.zd, to.type, 1, rows, cols, steps, co, eps, to.scale, s) ==
+  if (const int c = ns_small_cluster(1, rows, cols, true))
+    return launch_ns_small(u, cols, 0, false, to.D, to.ldd, to.zd, to.type, 1, rows, cols, c, steps, co, eps, to.scale, s) ==
                    cudaSuccess ? OSCARS_OK : OSCARS_ECUDA;
   return steps_from(p, ws, static_cast<const float*>(u), cols, 0, eps, steps, co, to, s) == cudaSuccess ? OSCARS_OK
                                                                                                        : OSCARS_ECUDA;

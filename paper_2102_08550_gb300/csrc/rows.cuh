@@ -35,26 +35,50 @@ __device__ __forceinline__ void load8(const T* p, int n, bool vec, float (&v)[8]
   }
 }
 
-// Sum of squares.  In fp32 where neither it nor a term that counts can leave
-// the range, else (magnitudes below 1e-10 or above 1e15) in fp64, so that no
-// update is too small or too large for its norm.
-template <int N>
-__device__ __forceinline__ double squares(const float (&v)[N]) {
-  float s = 0.f;
-  bool any = false;
+// Sums of squares over the whole range of fp32, in fp32 (the card's fp64 rate is 1/64 of it): of values whose squares
+// neither overflow nor underflow, of larger ones times 2^-80 and of smaller ones times 2^80.
+struct Squares {
+  float mid = 0.f, big = 0.f, small = 0.f;
+
+  template <int N>
+  __device__ __forceinline__ void add(const float (&v)[N]) {
+    float s = 0.f, m = 0.f;
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    s = fmaf(v[i], v[i], s);
-    any |= v[i] != 0.f;
-  }
-  if (any && !(s > 1e-20f && s < 1e30f)) {
-    double d = 0.0;
+    for (int i = 0; i < N; ++i) {
+      s = fmaf(v[i], v[i], s);
+      m = fmaxf(m, fabsf(v[i]));
+    }
+    if ((s > 1e-20f && s < 1e25f) || m == 0.f) {   // m is 0 for zeros, and for NaN alone, which s carries on
+      mid += s;
+    } else {
+      const float by = m > 1.f ? 0x1p-80f : 0x1p80f;
+      float t = 0.f;
 #pragma unroll
-    for (int i = 0; i < N; ++i) d += static_cast<double>(v[i]) * static_cast<double>(v[i]);
-    return d;
+      for (int i = 0; i < N; ++i) t = fmaf(v[i] * by, v[i] * by, t);
+      (m > 1.f ? big : small) += t;
+    }
   }
-  return s;
-}
+  __device__ __forceinline__ void add(const Squares& o) { mid += o.mid, big += o.big, small += o.small; }
+  __device__ __forceinline__ void warp_sum() {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      mid += __shfl_xor_sync(0xffffffffu, mid, o);
+      big += __shfl_xor_sync(0xffffffffu, big, o);
+      small += __shfl_xor_sync(0xffffffffu, small, o);
+    }
+  }
+  // sum over the block in a fixed order, in thread 0 (`part`: one entry a warp)
+  __device__ __forceinline__ void block_sum(Squares* part) {
+    warp_sum();
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = *this;
+    __syncthreads();
+    if (threadIdx.x == 0)
+      for (int i = 1; i < static_cast<int>(blockDim.x) / 32; ++i) add(part[i]);
+  }
+  __device__ __forceinline__ double total() const {
+    return static_cast<double>(mid) + static_cast<double>(big) * 0x1p160 + static_cast<double>(small) * 0x1p-160;
+  }
+};
 
 // 1 / (norm + eps) = power x factor, each a normal fp32 number (power: of two), of a sum of squares.
 __device__ __forceinline__ void inverse_norm(double squares, float eps, float& power, float& factor) {
