@@ -200,6 +200,41 @@ __device__ __forceinline__ float finish(const I8Args& a, int sum, float sa, floa
   return a.relu && v < 0.f ? 0.f : v;
 }
 
+// A thread's channel n of tokens m0 ... m0 + span: 16 values at a time without a branch between them (with the type and
+// the edges tested at each, a token took a warp 120 clocks, and a tile of 256 x 256 longer than its products)
+template <typename T>
+__device__ __forceinline__ void store_tokens(const I8Args& a, T* C, int m0, int n, int span, const int (&sum)[kMaxBN / 32][16],
+                                             const float (&sa)[kMaxBN / 64], float sb, float bias) {
+  T* at = C + m0 * a.ldc + n;
+  const int rows = n < a.N ? a.M - m0 : 0;
+#pragma unroll
+  for (int g = 0; g < kMaxBN / 32; ++g)
+    if (16 * g < span) {
+      float v[16];
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        v[e] = static_cast<float>(sum[g][e]) * __shfl_sync(0xffffffffu, sa[g / 2], (g & 1) * 16 + e) * sb;
+      if (a.bias) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) v[e] += bias;
+      }
+      if (a.relu) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) v[e] = v[e] < 0.f ? 0.f : v[e];
+      }
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        if (16 * g + e < rows) *at = static_cast<T>(v[e]);
+        at += a.ldc;
+      }
+    }
+}
+
+// four bytes into a peer's shared memory
+__device__ __forceinline__ void st_peer(const void* local, int rank, int v) {
+  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(cluster_addr(local, rank)), "r"(v) : "memory");
+}
+
 template <int CL, bool kSplit>
 __global__ void __launch_bounds__(kThreads, 1) gemm_i8_kernel(const __grid_constant__ CUtensorMap mapW,
                                                               const __grid_constant__ CUtensorMap mapX,
@@ -210,7 +245,8 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_i8_kernel(const __grid_const
   const int raw_bytes = rows * 128, op_bytes = rows * 128;   // 128 codes, or 64 in fp16
   uint8_t* op = smem;                              // [op stages][128 channels | bn tokens][128 bytes]
   uint8_t* raw = smem + a.op_stages * op_bytes;    // [raw stages][128 channels | bn tokens][128 bytes]
-  Bars* bars = reinterpret_cast<Bars*>(raw + a.raw_stages * raw_bytes);
+  uint8_t* recv = raw + a.raw_stages * raw_bytes;  // kSplit: the parts' sums of this CTA's tokens [part][BN / split][128]
+  Bars* bars = reinterpret_cast<Bars*>(recv + (kSplit ? a.BN * 512 : 0));
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const int part = kSplit ? static_cast<int>(cluster_ctarank()) : 0;
   const int rank = CL > 1 ? static_cast<int>(cluster_ctarank()) : 0;
@@ -419,29 +455,21 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_i8_kernel(const __grid_const
         }
       }
       if (!ok) break;
-      if constexpr (kSplit) {   // partial sums [token][channel] where the operands were: the products have read them
-        int* out = reinterpret_cast<int*>(op) + cb * 128 + 32 * quarter + lane;
-#pragma unroll
-        for (int g = 0; g < kMaxBN / 32; ++g)
-          if (16 * g < span) {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) out[(16 * g + e) * 128] = sum[g][e];
-          }
-      } else {
+      if constexpr (kSplit) {   // a part's sums [token][channel] go to the CTA that adds up the token
+        const int owned = a.BN / a.split;
 #pragma unroll
         for (int g = 0; g < kMaxBN / 32; ++g)
           if (16 * g < span) {
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-              const float s = __shfl_sync(0xffffffffu, sa[g / 2], (g & 1) * 16 + e);
-              const int m = m0 + 16 * g + e;
-              if (m < a.M && n < a.N) {
-                const float v = finish(a, sum[g][e], s, sb, bias);
-                if (a.bf16) static_cast<__nv_bfloat16*>(a.C)[m * a.ldc + n] = __float2bfloat16_rn(v);
-                else static_cast<float*>(a.C)[m * a.ldc + n] = v;
-              }
+              const int tok = cb + 16 * g + e;
+              st_peer(recv + ((part * owned + tok % owned) * 128 + 32 * quarter + lane) * 4, tok / owned, sum[g][e]);
             }
           }
+      } else if (a.bf16) {
+        store_tokens(a, static_cast<__nv_bfloat16*>(a.C), m0, n, span, sum, sa, sb, bias);
+      } else {
+        store_tokens(a, static_cast<float*>(a.C), m0, n, span, sum, sa, sb, bias);
       }
     }
   }
@@ -449,26 +477,18 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_i8_kernel(const __grid_const
   if (CL > 1 || kSplit) cluster_sync();   // the pair's products and arrivals are done in both CTAs; every part's sums are there
   else __syncthreads();
   if constexpr (kSplit) {
-    // each CTA adds up its tokens of the tile over the parts, four channels a thread
-    const int n0 = (u0 % mu) * 128, m0 = (u0 / mu) * a.BN, tokens = a.BN / a.split;
-    for (int i = threadIdx.x; i < tokens * 32; i += kThreads) {
-      const int tok = part * tokens + i / 32, ch = (i % 32) * 4, m = m0 + tok;
-      int4 s = make_int4(0, 0, 0, 0);
-      for (int p = 0; p < a.split; ++p) {
-        const float4 f = ld_dsmem_f32x4(reinterpret_cast<const float*>(op) + tok * 128 + ch, p);
-        s.x += __float_as_int(f.x), s.y += __float_as_int(f.y), s.z += __float_as_int(f.z), s.w += __float_as_int(f.w);
-      }
-      const int v[4] = {s.x, s.y, s.z, s.w};
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int n = n0 + ch + e;
-        if (m >= a.M || n >= a.N) continue;
-        const float y = finish(a, v[e], __ldg(a.sa + m), __ldg(a.sb + n), a.bias ? __ldg(a.bias + n) : 0.f);
-        if (a.bf16) static_cast<__nv_bfloat16*>(a.C)[m * a.ldc + n] = __float2bfloat16_rn(y);
-        else static_cast<float*>(a.C)[m * a.ldc + n] = y;
-      }
+    // each CTA adds up its tokens of the tile over the parts
+    const int n0 = (u0 % mu) * 128, tokens = a.BN / a.split, m0 = (u0 / mu) * a.BN + part * tokens;
+    const int* sums = reinterpret_cast<const int*>(recv);
+    for (int i = threadIdx.x; i < tokens * 128; i += kThreads) {
+      const int m = m0 + i / 128, n = n0 + i % 128;
+      if (m >= a.M || n >= a.N) continue;
+      int t = 0;
+      for (int p = 0; p < a.split; ++p) t += sums[p * tokens * 128 + i];
+      const float y = finish(a, t, __ldg(a.sa + m), __ldg(a.sb + n), a.bias ? __ldg(a.bias + n) : 0.f);
+      if (a.bf16) static_cast<__nv_bfloat16*>(a.C)[m * a.ldc + n] = __float2bfloat16_rn(y);
+      else static_cast<float*>(a.C)[m * a.ldc + n] = y;
     }
-    cluster_sync();   // no CTA ends while a peer reads its sums
   }
   if (warp == 2) {
     tc_fence_after();
@@ -622,12 +642,12 @@ void device_room(int& sms, int& pairs) {
 
 template <int CL, bool kSplit>
 cudaError_t launch_i8(const CUtensorMap& mW, const CUtensorMap& mX, I8Args a, int grid, cudaStream_t s) {
-  const int tile = (128 + a.BN / CL) * 128, room = kSmem - 1024 - kBarBytes;
+  const int tile = (128 + a.BN / CL) * 128, sums = kSplit ? a.BN * 512 : 0, room = kSmem - 1024 - kBarBytes - sums;
   // an even number of operand stages: a slot belongs to one of the two converting groups, which sees each of its phases
   a.op_stages = 6 * tile > room ? 2 : 4;
   a.raw_stages = room / tile - a.op_stages;
   if (a.raw_stages > kMaxStages) a.raw_stages = kMaxStages;
-  size_t smem = 1024 + static_cast<size_t>(a.op_stages + a.raw_stages) * tile + kBarBytes;
+  size_t smem = 1024 + static_cast<size_t>(a.op_stages + a.raw_stages) * tile + sums + kBarBytes;
   if (smem < kLeast) smem = kLeast;
   cudaError_t e = allow_smem(gemm_i8_kernel<CL, kSplit>, kSmem);
   if (e != cudaSuccess) return e;
@@ -706,7 +726,7 @@ oscars_status oscars_gemm_i8_nt(const int8_t* A, int64_t lda, const float* scale
       kb = kb > rows * kK / 45.0 ? kb : rows * kK / 45.0;
       // few tiles: the K-blocks of each over a cluster of `split` CTAs, whose sums meet in shared memory
       for (int split = 1; split <= (c == 1 ? 8 : 1); split *= 2) {
-        if (split > 1 && (units * split > (split == 8 ? sms * 3 / 4 : sms * 7 / 8) || nk < 4 * split || bn < 4 * split)) break;
+        if (split > 1 && (units * split > (split == 8 ? sms * 3 / 4 : sms * 7 / 8) || nk < 4 * split || bn < 4 * split || bn > 128)) break;
         const double waves = split > 1 ? 1.0 : static_cast<double>((units + room - 1) / room);
         const double cost = waves * ((nk + split - 1) / split * kb + 600.0) + 15.0 * bn + (c == 2 ? 1500.0 : 0.0) + (split > 1 ? 3000.0 : 0.0);
         if (best == 0.0 || cost < best) {

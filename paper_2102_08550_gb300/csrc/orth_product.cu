@@ -36,6 +36,7 @@
 // (half of a tile's columns each group of four) run the epilogue of a tile, or the
 // sum of a chunk, under the products of the next.
 #include <atomic>
+#include <type_traits>
 
 #include "common.cuh"
 #include "internal.h"
@@ -241,36 +242,31 @@ __global__ void __launch_bounds__(kThreads, 1) ns_product_kernel(const __grid_co
         *reinterpret_cast<float4*>(my + lane * 128 + ((q ^ (lane & 7)) << 4)) =
             make_float4(v[4 * q] * a.factor, v[4 * q + 1] * a.factor, v[4 * q + 2] * a.factor, v[4 * q + 3] * a.factor);
       __syncwarp();
-      // rows of 32 columns, coalesced whatever the caller's alignment
-      const int col = n + lane;
-      const int64_t at0 = z * a.zo + col;
-      const int rows = a.M - m0 < 32 ? a.M - m0 : 32;
-      if (col < a.N) {
-        for (int i0 = 0; i0 < rows; i0 += 8) {
-          float x[8];
+      // rows of 32 columns, coalesced whatever the caller's alignment, 16 at a time without a branch between them
+      const int col = n + lane, rows = col < a.N ? (a.M - m0 < 32 ? a.M - m0 : 32) : 0;
+      const int64_t at0 = z * a.zo + col + static_cast<int64_t>(m0) * a.ldo;
+      auto store = [&](auto* out, bool add) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
+        for (int i0 = 0; i0 < 32; i0 += 16) {
+          float x[16], old[16];
+          auto* at = out + at0 + i0 * a.ldo;
+          if (add) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) old[i] = i0 + i < rows ? static_cast<float>(at[i * a.ldo]) : 0.f;
+          }
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
             const int rr = i0 + i;
             x[i] = *reinterpret_cast<const float*>(my + rr * 128 + (((lane >> 2) ^ (rr & 7)) << 4) + (lane & 3) * 4);
-          }
-          if (a.out_type == kNsAdd) {
-            const float* o = static_cast<const float*>(a.out);
-            float old[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-              old[i] = i0 + i < rows ? o[at0 + static_cast<int64_t>(m0 + i0 + i) * a.ldo] : 0.f;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] += old[i];
+            if (add) x[i] += old[i];
           }
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            if (i0 + i >= rows) continue;
-            const int64_t at = at0 + static_cast<int64_t>(m0 + i0 + i) * a.ldo;
-            if (a.out_type == kNsBf16) static_cast<__nv_bfloat16*>(a.out)[at] = __float2bfloat16_rn(x[i]);
-            else static_cast<float*>(a.out)[at] = x[i];
-          }
+          for (int i = 0; i < 16; ++i)
+            if (i0 + i < rows) at[i * a.ldo] = static_cast<std::remove_reference_t<decltype(*at)>>(x[i]);
         }
-      }
+      };
+      if (a.out_type == kNsBf16) store(static_cast<__nv_bfloat16*>(a.out), false);
+      else store(static_cast<float*>(a.out), a.out_type == kNsAdd);
       __syncwarp();
     }
   };
