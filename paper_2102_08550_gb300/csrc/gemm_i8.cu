@@ -498,17 +498,17 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_i8_kernel(const __grid_const
 }
 
 // ------------------------------------------------------------------ few tokens
-// One or two tokens, or up to eight of few codes (tokens x K <= 8192): bound by the channels' bytes and by latency, so the
-// tensor core's set-up and the conversion do not pay.  A warp takes CH channels, each lane 16 codes of a row a turn; MT
-// tokens are multiplied with them by dp4a as they come, and the lanes' sums meet in log2(32) exchanges that halve the number
-// of values a lane holds.  Measured (us, this kernel / the tensor core's): 1 x 512 x 784 1.7 / 7.7; 1 x 4096 x 4096 4.3 / 10.2;
-// 2 x 300 x 8192 8.0 / 9.4; 8 x 1024 x 1024 4.8 / 6.2; beyond the rule 12 x 1024 x 1024 6.8 / 6.2, 8 x 4096 x 4096 15.4 / 10.4.
+// One token, or two of few channels: bound by the channels' bytes and by latency, so neither the tensor core's set-up nor a
+// conversion pays.  A warp takes one channel, each lane 16 codes of a row a turn; the tokens are multiplied with them by dp4a
+// as they come, and the lanes' sums meet in log2(32) exchanges that halve the number of values a lane holds.  Measured (us,
+// this kernel / the one for up to 32 tokens): 1 x 512 x 784 1.7 / 2.3; 1 x 4096 x 4096 4.3 / 5.6 (3.9 TB/s of codes); 2 x 300 x
+// 8192 8.0 / 8.9; 2 x 1024 x 1024 2.3 / 2.4; beyond the rule 2 x 4096 x 4096 6.5 / 5.9, 4 x 512 x 784 2.9 / 2.4.
 constexpr int kFewThreads = 256;
-bool few_tokens(int M, int K) { return M <= 2 || (M <= 8 && static_cast<int64_t>(M) * K <= 8192); }
+bool few_tokens(int M, int N) { return M == 1 || (M == 2 && N <= 1024); }
 
+// the sums over the lanes of V (a power of two) values: lane l ends with that of value l V / 32
 template <int V>
 __device__ __forceinline__ void lanes_sum(int (&v)[V], int lane) {
-  // lane l ends with the sums of values l * V / 32 ... (V >= 32), or of value l * V / 32 (V < 32)
 #pragma unroll
   for (int o = 16, n = V; o > 0; o >>= 1) {
     if (n > 1) {
@@ -536,64 +536,151 @@ __device__ __forceinline__ int4 codes16(const int8_t* p, int left) {
   return w;
 }
 
-template <int MT, int CH>
+template <int MT>
 __global__ void __launch_bounds__(kFewThreads) gemm_i8_few_kernel(const int8_t* __restrict__ A, int64_t lda, const int8_t* __restrict__ B,
                                                                   int64_t ldb, const __grid_constant__ I8Args a) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int64_t n0 = (static_cast<int64_t>(blockIdx.x) * (kFewThreads / 32) + warp) * CH;
+  const int n = blockIdx.x * (kFewThreads / 32) + warp;
   pdl_wait();
   pdl_trigger();
-  if (n0 >= a.N) return;
-  int sum[MT * CH];
-#pragma unroll
-  for (int i = 0; i < MT * CH; ++i) sum[i] = 0;
-  const int8_t* w = B + n0 * ldb;
-  constexpr int kAhead = CH == 1 ? 4 : CH == 2 ? 2 : 1;   // turns whose rows are requested together
+  if (n >= a.N) return;
+  int sum[MT] = {};
+  const int8_t* w = B + n * ldb;
+  constexpr int kAhead = 4;   // turns whose codes are requested together
   for (int k0 = lane * 16; k0 < a.K; k0 += 512 * kAhead) {
-    int4 b[kAhead][CH];
+    int4 b[kAhead];
 #pragma unroll
     for (int h = 0; h < kAhead; ++h)
-#pragma unroll
-      for (int c = 0; c < CH; ++c)
-        b[h][c] = k0 + 512 * h < a.K && n0 + c < a.N ? *reinterpret_cast<const int4*>(w + c * ldb + k0 + 512 * h) : make_int4(0, 0, 0, 0);
+      b[h] = k0 + 512 * h < a.K ? *reinterpret_cast<const int4*>(w + k0 + 512 * h) : make_int4(0, 0, 0, 0);
 #pragma unroll
     for (int h = 0; h < kAhead; ++h) {
       const int k = k0 + 512 * h;
       if (k >= a.K) break;
 #pragma unroll
       for (int m = 0; m < MT; ++m) {
-        if (m >= a.M) break;
         const int4 x = codes16(A + m * lda + k, a.K - k);   // what lies behind column K of B meets zeros
-#pragma unroll
-        for (int c = 0; c < CH; ++c) {
-          int s = sum[m * CH + c];
-          s = __dp4a(b[h][c].x, x.x, s);
-          s = __dp4a(b[h][c].y, x.y, s);
-          s = __dp4a(b[h][c].z, x.z, s);
-          sum[m * CH + c] = __dp4a(b[h][c].w, x.w, s);
-        }
+        sum[m] = __dp4a(b[h].x, x.x, sum[m]);
+        sum[m] = __dp4a(b[h].y, x.y, sum[m]);
+        sum[m] = __dp4a(b[h].z, x.z, sum[m]);
+        sum[m] = __dp4a(b[h].w, x.w, sum[m]);
       }
     }
   }
-  constexpr int V = MT * CH, kEach = V < 32 ? 1 : V / 32;
-  lanes_sum<V>(sum, lane);
-  if (V < 32 && lane % (32 / (V < 32 ? V : 32)) != 0) return;
+  lanes_sum<MT>(sum, lane);
+  if (lane % (32 / MT) != 0) return;
+  const int m = lane / (32 / MT);
+  const float v = finish(a, sum[0], __ldg(a.sa + m), __ldg(a.sb + n), a.bias ? __ldg(a.bias + n) : 0.f);
+  if (a.bf16) static_cast<__nv_bfloat16*>(a.C)[m * a.ldc + n] = __float2bfloat16_rn(v);
+  else static_cast<float*>(a.C)[m * a.ldc + n] = v;
+}
+
+template <int MT>
+cudaError_t launch_few(const int8_t* A, int64_t lda, const int8_t* B, int64_t ldb, const I8Args& a, cudaStream_t s) {
+  constexpr int kPer = kFewThreads / 32;
+  return launch_dependent(gemm_i8_few_kernel<MT>, dim3((a.N + kPer - 1) / kPer), kFewThreads, 0, s, A, lda, B, ldb, a);
+}
+
+// ------------------------------------------------------------------ up to 32 tokens
+// Bound by the channels' bytes: they go from global memory to registers, become fp16 there and meet the tokens in mma.sync
+// (m16n8k16), whose operands need no shared memory; in the tcgen05 kernel a K-block's 128 channels pass it four times.  The
+// order of K within a lane's 16 codes is the same for both operands, so a lane's 16-byte load holds its share of four
+// products as it comes.  A CTA takes 32 channels, its eight warps K-blocks of 128 in turn; sums move to int32 every 1024 of
+// K, and the warps' sums meet in shared memory.
+constexpr int kNarrowThreads = 256, kNarrowK = 128, kNarrowCh = 32;
+
+__device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+template <int NT>   // groups of 8 tokens
+__global__ void __launch_bounds__(kNarrowThreads, NT == 4 ? 1 : 2) gemm_i8_narrow_kernel(const int8_t* __restrict__ A, int64_t lda,
+                                                                        const int8_t* __restrict__ B, int64_t ldb,
+                                                                        const __grid_constant__ I8Args a) {
+  __shared__ int sums[kNarrowThreads / 32][NT * 8][kNarrowCh];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  const int n0 = blockIdx.x * kNarrowCh;
+  pdl_wait();
+  pdl_trigger();
+  const int8_t* w[4];        // rows g, g + 8, g + 16, g + 24 of the channels; the last one again past the end
 #pragma unroll
-  for (int i = 0; i < kEach; ++i) {
-    const int at = V < 32 ? lane / (32 / (V < 32 ? V : 32)) : lane * kEach + i;
-    const int m = at / CH;
-    const int64_t n = n0 + at % CH;
-    if (m >= a.M || n >= a.N) continue;
-    const float v = finish(a, sum[i], __ldg(a.sa + m), __ldg(a.sb + n), a.bias ? __ldg(a.bias + n) : 0.f);
-    if (a.bf16) static_cast<__nv_bfloat16*>(a.C)[m * a.ldc + n] = __float2bfloat16_rn(v);
-    else static_cast<float*>(a.C)[m * a.ldc + n] = v;
+  for (int i = 0; i < 4; ++i) w[i] = B + static_cast<int64_t>(n0 + g + 8 * i < a.N ? n0 + g + 8 * i : a.N - 1) * ldb + 16 * t;
+  float acc[2][NT][4] = {};
+  int sum[2][NT][4] = {};
+  int turn = 0;
+  for (int k0 = warp * kNarrowK; k0 < a.K; k0 += kNarrowThreads / 32 * kNarrowK) {
+    int4 c[2][4];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        c[h][i] = k0 + 64 * h + 16 * t < a.K ? __ldcs(reinterpret_cast<const int4*>(w[i] + k0 + 64 * h)) : make_int4(0, 0, 0, 0);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int k = k0 + 64 * h + 16 * t;
+      int4 x[NT];
+#pragma unroll
+      for (int j = 0; j < NT; ++j)   // codes behind column K, and tokens behind the last, are zeros
+        x[j] = k < a.K && 8 * j + g < a.M ? codes16(A + (8 * j + g) * lda + k, a.K - k) : make_int4(0, 0, 0, 0);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        uint32_t lo[4], hi[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) codes_to_half(q == 0 ? c[h][i].x : q == 1 ? c[h][i].y : q == 2 ? c[h][i].z : c[h][i].w, lo[i], hi[i]);
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+          uint32_t b0, b1;
+          codes_to_half(q == 0 ? x[j].x : q == 1 ? x[j].y : q == 2 ? x[j].z : x[j].w, b0, b1);
+          mma_f16(acc[0][j], lo[0], lo[1], hi[0], hi[1], b0, b1);
+          mma_f16(acc[1][j], lo[2], lo[3], hi[2], hi[3], b0, b1);
+        }
+      }
+    }
+    if (++turn == 1024 / kNarrowK) {
+      turn = 0;
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            sum[i][j][e] += __float2int_rn(acc[i][j][e]);
+            acc[i][j][e] = 0.f;
+          }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)   // channel 16 i + g (+ 8), token 8 j + 2 t (+ 1)
+        sums[warp][8 * j + 2 * t + (e & 1)][16 * i + g + 8 * (e >> 1)] = sum[i][j][e] + __float2int_rn(acc[i][j][e]);
+  __syncthreads();
+  const int n = n0 + lane;
+  if (n >= a.N) return;
+  const float sb = __ldg(a.sb + n), bias = a.bias ? __ldg(a.bias + n) : 0.f;
+  for (int m = warp; m < a.M; m += kNarrowThreads / 32) {
+    int v = 0;
+#pragma unroll
+    for (int p = 0; p < kNarrowThreads / 32; ++p) v += sums[p][m][lane];
+    const float y = finish(a, v, __ldg(a.sa + m), sb, bias);
+    if (a.bf16) static_cast<__nv_bfloat16*>(a.C)[m * a.ldc + n] = __float2bfloat16_rn(y);
+    else static_cast<float*>(a.C)[m * a.ldc + n] = y;
   }
 }
 
-template <int MT, int CH>
-cudaError_t launch_few(const int8_t* A, int64_t lda, const int8_t* B, int64_t ldb, const I8Args& a, cudaStream_t s) {
-  const int per = kFewThreads / 32 * CH;
-  return launch_dependent(gemm_i8_few_kernel<MT, CH>, dim3((a.N + per - 1) / per), kFewThreads, 0, s, A, lda, B, ldb, a);
+// Measured (us, this kernel / the tcgen05 kernel): 8 x 512 x 784 2.3 / 7.5, 16 x 512 x 784 3.2 / 7.5, 32 x 1024 x 1024 4.7 / 6.4,
+// 8 x 4096 x 4096 6.0 / 10.4 (2.8 TB/s of codes), 16 x 4096 x 4096 8.0 / 10.3; beyond the rule 32 x 4096 x 4096 13.2 / 10.6, 32 x
+// 16384 x 512 11.8 / 6.4, 16 x 300 x 8192 12.8 / 9.4.
+bool narrow(int M, int N, int K) {
+  return M <= 8 || (M <= 16 && K <= 4096) || (M <= 32 && static_cast<int64_t>(N) * K <= (2 << 20));
+}
+
+template <int NT>
+cudaError_t launch_narrow(const int8_t* A, int64_t lda, const int8_t* B, int64_t ldb, const I8Args& a, cudaStream_t s) {
+  return launch_dependent(gemm_i8_narrow_kernel<NT>, dim3((a.N + kNarrowCh - 1) / kNarrowCh), kNarrowThreads, 0, s, A, lda, B, ldb, a);
 }
 
 constexpr int kMaxDevices = 64;
@@ -701,11 +788,14 @@ oscars_status oscars_gemm_i8_nt(const int8_t* A, int64_t lda, const float* scale
   if (reinterpret_cast<uintptr_t>(C) & (dtype == OSCARS_F32 ? 3 : 1)) return OSCARS_EINVAL;
   I8Args p{scale_a, scale_b, bias, C, ldc, M, N, K, relu, dtype == OSCARS_BF16, 0, 0, 0, 0, 1, 0, 0};
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (few_tokens(M, K)) {
-    const cudaError_t e = M == 1   ? launch_few<1, 1>(A, lda, B, ldb, p, s)
-                          : M == 2 ? launch_few<2, 1>(A, lda, B, ldb, p, s)
-                          : M <= 4 ? launch_few<4, 2>(A, lda, B, ldb, p, s)
-                                   : launch_few<8, 4>(A, lda, B, ldb, p, s);
+  if (few_tokens(M, N)) {
+    const cudaError_t e = M == 1 ? launch_few<1>(A, lda, B, ldb, p, s) : launch_few<2>(A, lda, B, ldb, p, s);
+    return e == cudaSuccess ? OSCARS_OK : OSCARS_ECUDA;
+  }
+  if (narrow(M, N, K)) {
+    const cudaError_t e = M <= 8    ? launch_narrow<1>(A, lda, B, ldb, p, s)
+                          : M <= 16 ? launch_narrow<2>(A, lda, B, ldb, p, s)
+                                    : launch_narrow<4>(A, lda, B, ldb, p, s);
     return e == cudaSuccess ? OSCARS_OK : OSCARS_ECUDA;
   }
   int sms, pairs;
