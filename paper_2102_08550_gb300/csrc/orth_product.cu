@@ -18,7 +18,7 @@
 // everything.  bf16 results take two halves of X and one of A and B: what X's
 // rounding leaves in the directions in which the update is near zero is
 // multiplied by a at every step (485 over five), while the roundings of A and B
-// multiply X and stay relative to it.  fp16 rather than bf16: three more bits at
+// multiply X and stay relative to it (the last step's X takes one half as well).  fp16 rather than bf16: three more bits at
 // the same rate, and the values are bounded (singular values below 2).
 //
 // The tensor core cuts what an addition to its accumulator leaves below fp32's last

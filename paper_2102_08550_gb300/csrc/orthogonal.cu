@@ -258,7 +258,13 @@ cudaError_t steps_from(const Shape& p, uint8_t* ws, const T* G, int64_t ldg, int
   u.b_mn = !tall;
   u.d_halves = 2;
   u.factor = 1.f / kNsScaleA;
-  NsArgs last = u;
+  // The step before a bf16 result's last one leaves X in one half, and the last step takes that: its rounding is multiplied
+  // by a once (3.4 x 2^-12), where an earlier one would be by a to the number of steps left.
+  NsArgs before = u, last = u;
+  if (p.halves == 1) {
+    before.d_halves = 1;
+    last.a_halves = last.b_halves = 1;
+  }
   last.factor = to.scale / (kNsScaleA * kNsScaleX);
   last.out = to.D;
   last.ldo = to.ldd;
@@ -270,7 +276,7 @@ cudaError_t steps_from(const Shape& p, uint8_t* ws, const T* G, int64_t ldg, int
     e = launch_ns_product(kNsSym, x, x, cubic ? mB : mA, g, s);
     if (e == cudaSuccess && !cubic) e = launch_ns_product(kNsSym, mA, mA, mB, q, s);
     if (e == cudaSuccess)
-      e = launch_ns_product(end ? kNsLast : kNsStep, tall ? x : mB, tall ? mB : x, mX[(k + 1) & 1], end ? last : u, s);
+      e = launch_ns_product(end ? kNsLast : kNsStep, tall ? x : mB, tall ? mB : x, mX[(k + 1) & 1], end ? last : k + 2 == steps ? before : u, s);
   }
   return e;
 }

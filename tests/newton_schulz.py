@@ -39,14 +39,14 @@ def newton_schulz(G, steps, coeff=MUON, eps=1e-7, gen=None, dtype=torch.float32)
         return R
 
     f = FACTOR[dtype]
-    for _ in range(steps):
+    for k in range(steps):
         A = product(_rel(X, f, gen), _rel(X, f, gen).T)
         if gen is not None and c != 0:   # as it is computed: c (A + b / 2c)^2 + (a - b^2 / 4c), A + b / 2c stored
             A = _rel(A + b / (2 * c) * eye, f, gen)
             B = _rel((a - b * b / (4 * c)) * eye + c * product(A, A), f, gen)
         else:
             B = _rel(a * eye + b * A + c * product(A, A), f, gen)
-        X = _rel(product(B, X), STORE, gen)
+        X = _rel(product(B, _rel(X, f, gen) if k + 1 == steps else X), STORE, gen)   # the last step's X as the factors
     return X.T if tall else X
 
 
