@@ -485,7 +485,7 @@ __global__ void __launch_bounds__(kThreads, 1) ns_product_kernel(const __grid_co
 
 constexpr int kMaxDevices = 64;
 struct DevInfo {
-  std::atomic<int> sms{0}, pairs{0};
+  std::atomic<int> sms{0}, pairs{0}, fours{0};
 };
 DevInfo g_dev[kMaxDevices];
 
@@ -515,24 +515,30 @@ cudaLaunchConfig_t config(cudaLaunchAttribute* attr, int cluster, int grid, size
   return cfg;
 }
 
-// {SMs, resident clusters of two} of the current device, queried once
-void device_room(int& sms, int& pairs) {
+// {SMs, clusters of two and of four that run at once} of the current device, queried once
+void device_room(int& sms, int& pairs, int& fours) {
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) dev = 0;
   sms = g_dev[dev].sms.load(std::memory_order_relaxed);
   pairs = g_dev[dev].pairs.load(std::memory_order_relaxed);
-  if (sms > 0 && pairs > 0) return;
+  fours = g_dev[dev].fours.load(std::memory_order_relaxed);
+  if (sms > 0 && pairs > 0 && fours > 0) return;
   if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || sms < 1) sms = 1;
-  cudaLaunchAttribute attr[1];
-  pairs = 0;
-  if (allow_smem(ns_product_kernel<kNsStep, 2, true, false>, kSmem) == cudaSuccess) {
-    cudaLaunchConfig_t cfg = config(attr, 2, 2, kSmem, nullptr);
-    if (cudaOccupancyMaxActiveClusters(&pairs, ns_product_kernel<kNsStep, 2, true, false>, &cfg) != cudaSuccess) pairs = 0;
-  }
-  cudaGetLastError();
-  if (pairs < 1) pairs = 1;
+  auto clusters = [](int size) {
+    int n = 0;
+    cudaLaunchAttribute attr[1];
+    if (allow_smem(ns_product_kernel<kNsStep, 1, true, true>, kSmem) == cudaSuccess) {
+      cudaLaunchConfig_t cfg = config(attr, size, size, kSmem, nullptr);
+      if (cudaOccupancyMaxActiveClusters(&n, ns_product_kernel<kNsStep, 1, true, true>, &cfg) != cudaSuccess) n = 0;
+    }
+    cudaGetLastError();
+    return n < 1 ? 1 : n;
+  };
+  pairs = clusters(2);
+  fours = clusters(4);
   g_dev[dev].sms.store(sms, std::memory_order_relaxed);
   g_dev[dev].pairs.store(pairs, std::memory_order_relaxed);
+  g_dev[dev].fours.store(fours, std::memory_order_relaxed);
 }
 
 template <int EPI, int CL, bool kSums, bool kSplit>
@@ -568,8 +574,8 @@ cudaError_t launch_e(int cl, const CUtensorMap& mA, const CUtensorMap& mB, const
 }  // namespace
 
 cudaError_t launch_ns_product(int epi, const NsMaps& A, const NsMaps& B, const NsMaps& D, NsArgs a, cudaStream_t s) {
-  int sms, pairs;
-  device_room(sms, pairs);
+  int sms, pairs, fours;
+  device_room(sms, pairs, fours);
   const bool sym = epi == kNsSym;
   const int nk = (a.K + kK - 1) / kK, products = a.a_halves + a.b_halves - 1;
   // The shape with the least estimated time: waves of tiles times the longer of a
@@ -587,7 +593,7 @@ cudaError_t launch_ns_product(int epi, const NsMaps& A, const NsMaps& B, const N
       const double mma = 2.0 * bn * products, load = stage_bytes(a, bn, c) / 52.0;
       for (int split = 1; split <= (c == 1 ? 4 : 1); split *= 2) {
         // a part has two K-blocks, a CTA 32 columns of the sums, and the clusters run at once
-        if (split > 1 && (units * split > sms * 7 / 8 || nk < 2 * split || bn < 32 * split || stages_of(a, bn, c, split) < 2)) break;
+        if (split > 1 && (units > (split == 2 ? pairs : fours) || nk < 2 * split || bn < 32 * split || stages_of(a, bn, c, split) < 2)) break;
         const double waves = split > 1 ? 1.0 : static_cast<double>((units + room - 1) / room);
         const double cost = waves * ((nk + split - 1) / split * (load > mma ? load : mma) + 600.0) + 12.0 * bn +
                             (c == 2 ? 1500.0 : 0.0) + (split > 1 ? 2500.0 : 0.0);

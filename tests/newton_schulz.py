@@ -10,9 +10,9 @@ MUON = (3.4445, -4.7750, 2.0315)
 # a bf16 result rounds A and the factor to fp16 (2^-11)
 STORE = 2.0 ** -22
 FACTOR = {torch.float32: 2.0 ** -22, torch.bfloat16: 2.0 ** -11}
-# fp32 accumulation in the tensor core of up to 4096 products: each addition of 16
-# products may cut up to 2^-23 of the running sum, so 256 of them 2^-15 at the
-# very most where all terms have one sign; a tenth of that where they have not
+# accumulation: the tensor core cuts up to 2^-23 of the running sum at each addition
+# of 16 products, four to twelve of them (64 of K, one to three products) before the
+# sum moves to fp32 registers, or K / 16 for bf16 results, whose factors are coarser
 ACC = 2.0 ** -21
 
 
