@@ -40,54 +40,65 @@ constexpr int kMaxK = 131071;   // 2^14 (2^17 - 1) < 2^31
 // the codes (a longer row is read again, from L2).  Bound by memory: a row is read and its codes are written once.
 constexpr int kQThreads = 256, kKeep = 4;
 
-__device__ __forceinline__ float nan_max(float a, float b) { return b > a || b != b ? b : a; }
+// Four codes.  The quotient's integer is that of x times the reciprocal wherever the product, which is within 3e-5 of the
+// quotient, is further than that from a half; the division (about 20 instructions, and most of the kernel's time when every
+// value took one: 8192 x 4096 fp32 48 us) is left for the others.  Adding 1.5 x 2^23 rounds to an integer in the low byte.
+__device__ __forceinline__ uint32_t four_codes(const float (&w)[8], int at, float s, float r) {
+  uint32_t bits[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float q = w[at + e] * r, t = q + 12582912.f;
+    bits[e] = __float_as_uint(t);
+    if (!(fabsf(q - (t - 12582912.f)) < 0.4999f && fabsf(q) < 127.4f))
+      bits[e] = __float_as_uint(fminf(fmaxf(w[at + e] / s, -127.f), 127.f) + 12582912.f);
+  }
+  return __byte_perm(__byte_perm(bits[0], bits[1], 0x0040), __byte_perm(bits[2], bits[3], 0x0040), 0x5410);
+}
 
 template <typename T, int TPR>
 __global__ void __launch_bounds__(kQThreads) quantize_i8_kernel(const T* __restrict__ x, int64_t ldx, int rows, int cols, int vec,
                                                                 int8_t* __restrict__ q, int64_t ldq, int qvec,
                                                                 float* __restrict__ scale) {
   constexpr int kRows = kQThreads / TPR;
-  __shared__ float part[kQThreads / 32];
+  __shared__ uint32_t part[kQThreads / 32];
   pdl_wait();
   pdl_trigger();
   const int64_t row = static_cast<int64_t>(blockIdx.x) * kRows + threadIdx.x / TPR;
   const int t = threadIdx.x % TPR, turns = (cols + TPR * 8 - 1) / (TPR * 8);
-  if (TPR < kQThreads && row >= rows) return;   // a whole warp
-  const T* src = x + row * ldx;
-  float v[kKeep][8], mx = 0.f;
+  if (TPR == 32 && row >= rows) return;          // a whole warp
+  const bool live = row < rows;
+  const T* src = x + (live ? row : 0) * ldx;
+  // magnitudes as integers: in order, infinity above every number and NaN above it
+  float v[kKeep][8];
+  uint32_t mx = 0;
+  auto take = [&](const float (&w)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) mx = max(mx, __float_as_uint(w[e]) & 0x7FFFFFFFu);
+  };
 #pragma unroll
   for (int i = 0; i < kKeep; ++i)
     load8(src + (i * TPR + t) * 8, cols - (i * TPR + t) * 8, vec != 0, v[i]);
 #pragma unroll
-  for (int i = 0; i < kKeep; ++i)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) mx = nan_max(mx, fabsf(v[i][e]));
+  for (int i = 0; i < kKeep; ++i) take(v[i]);
   for (int i = kKeep; i < turns; ++i) {
     float w[8];
     load8(src + (i * TPR + t) * 8, cols - (i * TPR + t) * 8, vec != 0, w);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) mx = nan_max(mx, fabsf(w[e]));
+    take(w);
   }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) mx = nan_max(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+  mx = __reduce_max_sync(0xffffffffu, mx);
   if (TPR > 32) {
     if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = mx;
     __syncthreads();
-    mx = part[0];
 #pragma unroll
-    for (int i = 1; i < TPR / 32; ++i) mx = nan_max(mx, part[i]);
+    for (int i = 0; i < TPR / 32; ++i) mx = max(mx, part[threadIdx.x / TPR * (TPR / 32) + i]);
+    if (!live) return;
   }
-  const float s = mx / 127.f;
+  const float s = __uint_as_float(mx) / 127.f, r = 1.f / s;
   if (t == 0) scale[row] = s;
   const bool codes = s > 0.f && s < INFINITY;   // neither a row of zeros nor one with an infinity or NaN
   int8_t* out = q + row * ldq;
   auto store = [&](int at, const float (&w)[8]) {
-    uint32_t word[2] = {0u, 0u};
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int c = codes ? __float2int_rn(fminf(fmaxf(w[e] / s, -127.f), 127.f)) : 0;
-      word[e >> 2] |= static_cast<uint32_t>(c & 255) << (8 * (e & 3));
-    }
+    const uint32_t word[2] = {codes ? four_codes(w, 0, s, r) : 0u, codes ? four_codes(w, 4, s, r) : 0u};
     if (qvec && at + 8 <= cols) {
       *reinterpret_cast<uint2*>(out + at) = make_uint2(word[0], word[1]);
     } else {
@@ -106,7 +117,8 @@ __global__ void __launch_bounds__(kQThreads) quantize_i8_kernel(const T* __restr
   }
 }
 
-// Rows up to 1024 long on a warp each, longer ones on a block.
+// Rows up to 1024 long on a warp each, up to 4096 on four, longer ones on a block: as few threads as keep the row in
+// registers, so that more rows' loads are in flight (8192 x 4096 bf16 on a block each 40 us).
 template <typename T>
 cudaError_t quantize(const void* x, int64_t ldx, int rows, int cols, int8_t* q, int64_t ldq, float* scale, cudaStream_t s) {
   const T* src = static_cast<const T*>(x);
@@ -114,6 +126,9 @@ cudaError_t quantize(const void* x, int64_t ldx, int rows, int cols, int8_t* q, 
   const int qvec = (reinterpret_cast<uintptr_t>(q) | static_cast<uintptr_t>(ldq)) % 8 == 0;
   if (cols <= 32 * 8 * kKeep)
     return launch_dependent(quantize_i8_kernel<T, 32>, dim3((rows + 7) / 8), kQThreads, 0, s, src, ldx, rows, cols, vec, q, ldq,
+                            qvec, scale);
+  if (cols <= 128 * 8 * kKeep)
+    return launch_dependent(quantize_i8_kernel<T, 128>, dim3((rows + 1) / 2), kQThreads, 0, s, src, ldx, rows, cols, vec, q, ldq,
                             qvec, scale);
   return launch_dependent(quantize_i8_kernel<T, kQThreads>, dim3(rows), kQThreads, 0, s, src, ldx, rows, cols, vec, q, ldq, qvec,
                           scale);
@@ -584,9 +599,9 @@ cudaError_t launch_few(const int8_t* A, int64_t lda, const int8_t* B, int64_t ld
 // Bound by the channels' bytes: they go from global memory to registers, become fp16 there and meet the tokens in mma.sync
 // (m16n8k16), whose operands need no shared memory; in the tcgen05 kernel a K-block's 128 channels pass it four times.  The
 // order of K within a lane's 16 codes is the same for both operands, so a lane's 16-byte load holds its share of four
-// products as it comes.  A CTA takes 32 channels, its eight warps K-blocks of 128 in turn; sums move to int32 every 1024 of
+// products as it comes.  A CTA takes 32 channels, its warps K-blocks of 128 in turn; sums move to int32 every 1024 of
 // K, and the warps' sums meet in shared memory.
-constexpr int kNarrowThreads = 256, kNarrowK = 128, kNarrowCh = 32;
+constexpr int kNarrowK = 128, kNarrowCh = 32;
 
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -594,11 +609,11 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1,
                : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-template <int NT>   // groups of 8 tokens
-__global__ void __launch_bounds__(kNarrowThreads, NT == 4 ? 1 : 2) gemm_i8_narrow_kernel(const int8_t* __restrict__ A, int64_t lda,
+template <int NT, int kWarps>   // groups of 8 tokens
+__global__ void __launch_bounds__(32 * kWarps, NT == 4 ? 1 : 16 / kWarps) gemm_i8_narrow_kernel(const int8_t* __restrict__ A, int64_t lda,
                                                                         const int8_t* __restrict__ B, int64_t ldb,
                                                                         const __grid_constant__ I8Args a) {
-  __shared__ int sums[kNarrowThreads / 32][NT * 8][kNarrowCh];
+  __shared__ int sums[kWarps][NT * 8][kNarrowCh];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int n0 = blockIdx.x * kNarrowCh;
   pdl_wait();
@@ -609,7 +624,7 @@ __global__ void __launch_bounds__(kNarrowThreads, NT == 4 ? 1 : 2) gemm_i8_narro
   float acc[2][NT][4] = {};
   int sum[2][NT][4] = {};
   int turn = 0;
-  for (int k0 = warp * kNarrowK; k0 < a.K; k0 += kNarrowThreads / 32 * kNarrowK) {
+  for (int k0 = warp * kNarrowK; k0 < a.K; k0 += kWarps * kNarrowK) {
     int4 c[2][4];
 #pragma unroll
     for (int h = 0; h < 2; ++h)
@@ -661,10 +676,10 @@ __global__ void __launch_bounds__(kNarrowThreads, NT == 4 ? 1 : 2) gemm_i8_narro
   const int n = n0 + lane;
   if (n >= a.N) return;
   const float sb = __ldg(a.sb + n), bias = a.bias ? __ldg(a.bias + n) : 0.f;
-  for (int m = warp; m < a.M; m += kNarrowThreads / 32) {
+  for (int m = warp; m < a.M; m += kWarps) {
     int v = 0;
 #pragma unroll
-    for (int p = 0; p < kNarrowThreads / 32; ++p) v += sums[p][m][lane];
+    for (int p = 0; p < kWarps; ++p) v += sums[p][m][lane];
     const float y = finish(a, v, __ldg(a.sa + m), sb, bias);
     if (a.bf16) static_cast<__nv_bfloat16*>(a.C)[m * a.ldc + n] = __float2bfloat16_rn(y);
     else static_cast<float*>(a.C)[m * a.ldc + n] = y;
@@ -672,15 +687,16 @@ __global__ void __launch_bounds__(kNarrowThreads, NT == 4 ? 1 : 2) gemm_i8_narro
 }
 
 // Measured (us, this kernel / the tcgen05 kernel): 8 x 512 x 784 2.3 / 7.5, 16 x 512 x 784 3.2 / 7.5, 32 x 1024 x 1024 4.7 / 6.4,
-// 8 x 4096 x 4096 6.0 / 10.4 (2.8 TB/s of codes), 16 x 4096 x 4096 8.0 / 10.3; beyond the rule 32 x 4096 x 4096 13.2 / 10.6, 32 x
-// 16384 x 512 11.8 / 6.4, 16 x 300 x 8192 12.8 / 9.4.
+// 8 x 4096 x 4096 4.7 / 10.4 (3.6 TB/s of codes), 16 x 4096 x 4096 6.5 / 10.3; 16 x 300 x 8192 9.2 / 9.4; beyond the rule 32 x 4096
+// x 4096 13.2 / 10.6, 32 x 16384 x 512 11.8 / 6.4.
 bool narrow(int M, int N, int K) {
-  return M <= 8 || (M <= 16 && K <= 4096) || (M <= 32 && static_cast<int64_t>(N) * K <= (2 << 20));
+  return M <= 16 || (M <= 32 && static_cast<int64_t>(N) * K <= (2 << 20));
 }
 
-template <int NT>
+template <int NT, int kWarps>
 cudaError_t launch_narrow(const int8_t* A, int64_t lda, const int8_t* B, int64_t ldb, const I8Args& a, cudaStream_t s) {
-  return launch_dependent(gemm_i8_narrow_kernel<NT>, dim3((a.N + kNarrowCh - 1) / kNarrowCh), kNarrowThreads, 0, s, A, lda, B, ldb, a);
+  return launch_dependent(gemm_i8_narrow_kernel<NT, kWarps>, dim3((a.N + kNarrowCh - 1) / kNarrowCh), 32 * kWarps, 0, s, A, lda, B,
+                          ldb, a);
 }
 
 constexpr int kMaxDevices = 64;
@@ -793,9 +809,12 @@ oscars_status oscars_gemm_i8_nt(const int8_t* A, int64_t lda, const float* scale
     return e == cudaSuccess ? OSCARS_OK : OSCARS_ECUDA;
   }
   if (narrow(M, N, K)) {
-    const cudaError_t e = M <= 8    ? launch_narrow<1>(A, lda, B, ldb, p, s)
-                          : M <= 16 ? launch_narrow<2>(A, lda, B, ldb, p, s)
-                                    : launch_narrow<4>(A, lda, B, ldb, p, s);
+    // 16 warps where each has two K-blocks or more, so that the codes' latency is waited for less often (8 x 4096 x 4096 6.0 ->
+    // 4.7 us), else 8 and two CTAs an SM (8 x 8192 x 2048 4.7, 5.5 with 16)
+    const bool many = K > 2048;
+    const cudaError_t e = M > 16  ? launch_narrow<4, 8>(A, lda, B, ldb, p, s)
+                          : M > 8 ? (many ? launch_narrow<2, 16>(A, lda, B, ldb, p, s) : launch_narrow<2, 8>(A, lda, B, ldb, p, s))
+                                  : (many ? launch_narrow<1, 16>(A, lda, B, ldb, p, s) : launch_narrow<1, 8>(A, lda, B, ldb, p, s));
     return e == cudaSuccess ? OSCARS_OK : OSCARS_ECUDA;
   }
   int sms, pairs;

@@ -166,7 +166,7 @@ def quantize(x, ldq=None, q=None):
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("rows,cols,pad,shift", [(1, 1, 0, 0), (1, 784, 0, 0), (3, 5, 11, 1), (7, 33, 0, 3), (64, 512, 0, 0), (5, 1000, 8, 0),
                                                  (2, 4096, 16, 0), (1000, 130, 2, 0), (4, 8192, 0, 0), (3, 20001, 7, 5), (2, 70000, 0, 0),
-                                                 (8192, 784, 0, 0)])
+                                                 (8192, 784, 0, 0), (3, 1025, 0, 0), (7, 4096, 3, 1), (1, 3001, 0, 0), (5, 4097, 0, 2)])
 def test_codes_equal_fp32_division(cuda_device, rows, cols, pad, shift, dtype):
     g = torch.Generator(device=cuda_device).manual_seed(rows + cols)
     buf = torch.randn(shift + rows * (cols + pad), device=cuda_device, generator=g).to(dtype)
