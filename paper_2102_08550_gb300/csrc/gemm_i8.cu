@@ -56,7 +56,7 @@ __device__ __forceinline__ uint32_t four_codes(const float (&w)[8], int at, floa
 }
 
 template <typename T, int TPR>
-__global__ void __launch_bounds__(kQThreads) quantize_i8_kernel(const T* __restrict__ x, int64_t ldx, int rows, int cols, int vec,
+__global__ void __launch_bounds__(kQThreads, sizeof(T) == 2 ? 6 : 4) quantize_i8_kernel(const T* __restrict__ x, int64_t ldx, int rows, int cols, int vec,
                                                                 int8_t* __restrict__ q, int64_t ldq, int qvec,
                                                                 float* __restrict__ scale) {
   constexpr int kRows = kQThreads / TPR;
@@ -69,7 +69,7 @@ __global__ void __launch_bounds__(kQThreads) quantize_i8_kernel(const T* __restr
   const bool live = row < rows;
   const T* src = x + (live ? row : 0) * ldx;
   // magnitudes as integers: in order, infinity above every number and NaN above it
-  float v[kKeep][8];
+  Held8<T> v[kKeep];
   uint32_t mx = 0;
   auto take = [&](const float (&w)[8]) {
 #pragma unroll
@@ -77,9 +77,13 @@ __global__ void __launch_bounds__(kQThreads) quantize_i8_kernel(const T* __restr
   };
 #pragma unroll
   for (int i = 0; i < kKeep; ++i)
-    load8(src + (i * TPR + t) * 8, cols - (i * TPR + t) * 8, vec != 0, v[i]);
+    v[i].load(src + (i * TPR + t) * 8, cols - (i * TPR + t) * 8, vec != 0);
 #pragma unroll
-  for (int i = 0; i < kKeep; ++i) take(v[i]);
+  for (int i = 0; i < kKeep; ++i) {
+    float w[8];
+    v[i].get(w);
+    take(w);
+  }
   for (int i = kKeep; i < turns; ++i) {
     float w[8];
     load8(src + (i * TPR + t) * 8, cols - (i * TPR + t) * 8, vec != 0, w);
@@ -109,7 +113,11 @@ __global__ void __launch_bounds__(kQThreads) quantize_i8_kernel(const T* __restr
   };
 #pragma unroll
   for (int i = 0; i < kKeep; ++i)
-    if ((i * TPR + t) * 8 < cols) store((i * TPR + t) * 8, v[i]);
+    if ((i * TPR + t) * 8 < cols) {
+      float w[8];
+      v[i].get(w);
+      store((i * TPR + t) * 8, w);
+    }
   for (int i = kKeep; i < turns; ++i) {
     float w[8];
     load8(src + (i * TPR + t) * 8, cols - (i * TPR + t) * 8, vec != 0, w);

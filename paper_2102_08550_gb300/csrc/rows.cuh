@@ -35,6 +35,38 @@ __device__ __forceinline__ void load8(const T* p, int n, bool vec, float (&v)[8]
   }
 }
 
+// Eight elements of a row held as they were read (bf16 in half the registers).
+template <typename T>
+struct Held8 {
+  float v[8];
+  __device__ __forceinline__ void load(const T* p, int n, bool vec) { load8(p, n, vec, v); }
+  __device__ __forceinline__ void get(float (&to)[8]) const {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) to[i] = v[i];
+  }
+};
+template <>
+struct Held8<__nv_bfloat16> {
+  uint32_t w[4];
+  __device__ __forceinline__ void load(const __nv_bfloat16* p, int n, bool vec) {
+    if (vec && n >= 8) {
+      const uint4 a = *reinterpret_cast<const uint4*>(p);
+      w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w;
+    } else {
+      const unsigned short* u = reinterpret_cast<const unsigned short*>(p);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = (2 * i < n ? u[2 * i] : 0u) | (2 * i + 1 < n ? static_cast<uint32_t>(u[2 * i + 1]) << 16 : 0u);
+    }
+  }
+  __device__ __forceinline__ void get(float (&to)[8]) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      to[2 * i] = __uint_as_float(w[i] << 16);
+      to[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    }
+  }
+};
+
 // Sums of squares over the whole range of fp32, in fp32 (the card's fp64 rate is 1/64 of it): of values whose squares
 // neither overflow nor underflow, of larger ones times 2^-80 and of smaller ones times 2^80.
 struct Squares {
