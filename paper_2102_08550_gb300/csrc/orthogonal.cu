@@ -26,7 +26,8 @@ namespace oscars {
 namespace {
 
 constexpr int kPasses = 256;        // threads of the streaming passes
-constexpr int kMaxParts = 304;      // partial sums of squares of one matrix
+constexpr int kMaxParts = 608;      // partial sums of squares of one matrix
+constexpr int kAhead = 4;           // groups of eight elements that a thread of a pass requests together
 constexpr int kMaxDim = 65536, kMaxBatch = 65535, kMaxSteps = 64;
 constexpr float kMaxCoeff = 8.f;
 
@@ -50,7 +51,7 @@ Shape make_shape(int batch, int rows, int cols, int dtype, bool with_u) {
   p.ldx = up(cols, 8);
   p.lds = up(p.s, 8);
   const int64_t elems = static_cast<int64_t>(rows) * cols;
-  const int64_t parts = (elems + 8 * kPasses - 1) / (8 * kPasses);
+  const int64_t each = (with_u ? 4 : 8 * kAhead) * kPasses, parts = (elems + each - 1) / each;   // a block's share, at least
   p.parts = static_cast<int>(parts < kMaxParts ? parts : kMaxParts);
   int64_t at = 0;
   auto take = [&](int64_t bytes) {
@@ -77,14 +78,22 @@ __global__ void __launch_bounds__(kPasses) orth_norm_kernel(const T* __restrict_
   pdl_wait();
   pdl_trigger();
   const T* g = G + blockIdx.y * bsg;
-  const int per_row = (cols + 7) / 8;
-  const int64_t n = static_cast<int64_t>(rows) * per_row, step = static_cast<int64_t>(gridDim.x) * kPasses;
+  // groups of eight: at most 2^29 (a 64-bit division for each took longer than its bytes)
+  const uint32_t per_row = (cols + 7) / 8, n = rows * per_row, step = gridDim.x * kPasses;
   Squares sum;
-  for (int64_t i = static_cast<int64_t>(blockIdx.x) * kPasses + threadIdx.x; i < n; i += step) {
-    const int r = static_cast<int>(i / per_row), c = static_cast<int>(i - static_cast<int64_t>(r) * per_row) * 8;
-    float v[8];
-    load8(g + r * ldg + c, cols - c, vec, v);
-    sum.add(v);
+  for (uint32_t i0 = blockIdx.x * kPasses + threadIdx.x; i0 < n; i0 += kAhead * step) {
+    Held8<T> h[kAhead];
+#pragma unroll
+    for (int e = 0; e < kAhead; ++e) {
+      const uint32_t i = i0 + e * step, r = i / per_row, c = (i - r * per_row) * 8;
+      h[e].load(g + static_cast<int64_t>(r) * ldg + c, i < n ? cols - static_cast<int>(c) : 0, vec);
+    }
+#pragma unroll
+    for (int e = 0; e < kAhead; ++e) {
+      float v[8];
+      h[e].get(v);
+      sum.add(v);
+    }
   }
   sum.block_sum(warps);
   if (threadIdx.x == 0) part[blockIdx.y * gridDim.x + blockIdx.x] = sum;
@@ -175,21 +184,31 @@ __global__ void __launch_bounds__(kPasses) orth_scale_kernel(const T* __restrict
   const T* g = G + blockIdx.y * bsg;
   __half* x = X + blockIdx.y * rows * ldx;
   const int64_t second = static_cast<int64_t>(gridDim.y) * rows * ldx;
-  const int per_row = static_cast<int>(ldx / 8);
-  const int64_t n = static_cast<int64_t>(rows) * per_row, step = static_cast<int64_t>(gridDim.x) * kPasses;
-  for (int64_t i = static_cast<int64_t>(blockIdx.x) * kPasses + threadIdx.x; i < n; i += step) {
-    const int r = static_cast<int>(i / per_row), c = static_cast<int>(i - static_cast<int64_t>(r) * per_row) * 8;
-    float v[8];
-    load8(g + r * ldg + c, cols - c, vec, v);
-    __align__(16) __half hi[8], lo[8];
+  const uint32_t per_row = static_cast<uint32_t>(ldx / 8), n = rows * per_row, step = gridDim.x * kPasses;
+  for (uint32_t i0 = blockIdx.x * kPasses + threadIdx.x; i0 < n; i0 += kAhead * step) {
+    Held8<T> held[kAhead];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float y = ((v[j] * pw) * f) * kNsScaleX;
-      hi[j] = __float2half_rn(y);
-      lo[j] = __float2half_rn(y - __half2float(hi[j]));
+    for (int e = 0; e < kAhead; ++e) {
+      const uint32_t i = i0 + e * step, r = i / per_row, c = (i - r * per_row) * 8;
+      held[e].load(g + static_cast<int64_t>(r) * ldg + c, i < n ? cols - static_cast<int>(c) : 0, vec);
     }
-    *reinterpret_cast<uint4*>(x + r * ldx + c) = *reinterpret_cast<const uint4*>(hi);
-    *reinterpret_cast<uint4*>(x + second + r * ldx + c) = *reinterpret_cast<const uint4*>(lo);
+#pragma unroll
+    for (int e = 0; e < kAhead; ++e) {
+      const uint32_t i = i0 + e * step;
+      if (i >= n) break;
+      float v[8];
+      held[e].get(v);
+      __align__(16) __half hi[8], lo[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float y = ((v[j] * pw) * f) * kNsScaleX;
+        hi[j] = __float2half_rn(y);
+        lo[j] = __float2half_rn(y - __half2float(hi[j]));
+      }
+      // rows of X are as long as their groups, so group i lies at 8 i
+      *reinterpret_cast<uint4*>(x + 8 * static_cast<int64_t>(i)) = *reinterpret_cast<const uint4*>(hi);
+      *reinterpret_cast<uint4*>(x + second + 8 * static_cast<int64_t>(i)) = *reinterpret_cast<const uint4*>(lo);
+    }
   }
 }
 
@@ -229,7 +248,7 @@ cudaError_t steps_from(const Shape& p, uint8_t* ws, const T* G, int64_t ldg, int
   if (!half_maps(&mA, A, p.lds, p.s, p.s, p.batch, p.halves) || !half_maps(&mB, B, p.lds, p.s, p.s, p.batch, p.halves))
     return cudaErrorInvalidValue;
   const int vec = (reinterpret_cast<uintptr_t>(G) | (ldg * sizeof(T)) | (bsg * sizeof(T))) % 16 == 0;
-  cudaError_t e = launch_dependent(orth_scale_kernel<T>, dim3(pass_blocks(p.rows * (p.ldx / 8), 1024), p.batch), kPasses, 0, s,
+  cudaError_t e = launch_dependent(orth_scale_kernel<T>, dim3(pass_blocks((p.rows * (p.ldx / 8) + kAhead - 1) / kAhead, 608), p.batch), kPasses, 0, s,
                                    G, ldg, bsg, p.rows, p.cols, vec, reinterpret_cast<const Squares*>(ws + p.off_part), p.parts,
                                    eps, X[0], p.ldx);
   const bool tall = p.rows > p.cols;
