@@ -513,12 +513,14 @@ oscars_status oscars_softreg_steps_noalloc(const float* params_in, float* params
  * NaN gives NaN throughout.  The norm neither overflows nor underflows.
  * Accuracy: fp32 results keep X and the factors in 22 bits and add in fp32; bf16
  * results round the factors to 11 bits, about 1e-3 of a result's size.
- * The arithmetic is fixed: equal inputs give equal bits.
+ * The arithmetic of a call is fixed: equal calls give equal bits (a matrix alone
+ * and in a batch may differ in the last ones).
  * workspace: device, 256-byte aligned, at least the bytes that
  * oscars_orthogonalize_workspace gives for the same sizes; the call leaves
  * nothing in it that a later call needs, and calls (or captured graphs) that
  * may run at the same time need one each.  The call allocates nothing and can
- * be captured.  Ordered on `stream`.  batch = 0 does nothing.
+ * be captured (after a first call on the device, which loads the kernels).
+ * Ordered on `stream`.  batch = 0 does nothing.
  * Errors: EINVAL (NULL or misaligned pointers, batch outside [0, 65535], rows
  * or cols outside [1, 65536], ldg or ldo < cols, a negative batch_stride_g, a
  * batch_stride_o below a matrix's extent with batch > 1, steps outside [1, 64],
@@ -563,7 +565,7 @@ oscars_status oscars_merge_orthogonal(float* x_g, const float* const* deltas, co
  * row that holds an infinity or NaN has that (NaN first) for its scale and codes
  * 0, so that its products are NaN.  rows = 0 does nothing.  Ordered on `stream`.
  * Errors: EINVAL (NULL pointers, x or scale not aligned to its elements, rows
- * < 0, cols < 1, ldx or ldq < cols), ECUDA.
+ * outside [0, 2^30], cols outside [1, 2^30], ldx or ldq < cols), ECUDA.
  */
 oscars_status oscars_quantize_i8(const void* x, int64_t ldx, int32_t dtype, int32_t rows, int32_t cols, int8_t* q,
                                  int64_t ldq, float* scale, void* stream);
@@ -577,9 +579,9 @@ oscars_status oscars_quantize_i8(const void* x, int64_t ldx, int32_t dtype, int3
  * multiple of 16 may be read and are not used).  scale_a [M], scale_b [N]: device fp32.  bias: device, N fp32, or NULL.
  * relu != 0: act = max(0, .) (NaN stays), else none.  C: device, element (m, n) at
  * C[m ldc + n], of `dtype`, any alignment; scale, bias and act are fp32, rounded
- * once.  M = 0 (no tokens) does nothing; 1 <= N; 1 <= K <= 131071 (the sum of
- * products of -128 stays within 32 bits).  Ordered on `stream`; allocates
- * nothing.
+ * once.  M = 0 (no tokens) does nothing; M, N <= 2^30, N >= 1; 1 <= K <= 131071
+ * (the sum of products of -128 stays within 32 bits).  Ordered on `stream`;
+ * allocates nothing and can be captured.
  * Errors: EINVAL (NULL or misaligned pointers, sizes or strides out of range),
  * ECUDA.
  */

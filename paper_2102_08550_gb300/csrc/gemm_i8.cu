@@ -34,6 +34,7 @@ namespace oscars {
 namespace {
 
 constexpr int kMaxK = 131071;   // 2^14 (2^17 - 1) < 2^31
+constexpr int kMaxSide = 1 << 30;   // rows, columns, tokens, channels: what is counted beyond them by a tile stays an int
 
 // ------------------------------------------------------------------ quantisation
 // A row on TPR threads, eight elements a thread and turn; up to kKeep turns stay in registers between the maximum and
@@ -786,7 +787,7 @@ extern "C" {
 
 oscars_status oscars_quantize_i8(const void* x, int64_t ldx, int32_t dtype, int32_t rows, int32_t cols, int8_t* q,
                                  int64_t ldq, float* scale, void* stream) {
-  if (rows < 0 || cols < 1 || ldx < cols || ldq < cols || (dtype != OSCARS_F32 && dtype != OSCARS_BF16))
+  if (rows < 0 || rows > kMaxSide || cols < 1 || cols > kMaxSide || ldx < cols || ldq < cols || (dtype != OSCARS_F32 && dtype != OSCARS_BF16))
     return OSCARS_EINVAL;
   if (rows == 0) return OSCARS_OK;
   if (!x || !q || !scale || (reinterpret_cast<uintptr_t>(scale) & 3) ||
@@ -801,7 +802,7 @@ oscars_status oscars_quantize_i8(const void* x, int64_t ldx, int32_t dtype, int3
 oscars_status oscars_gemm_i8_nt(const int8_t* A, int64_t lda, const float* scale_a, const int8_t* B, int64_t ldb,
                                 const float* scale_b, const float* bias, int32_t relu, void* C, int64_t ldc,
                                 int32_t dtype, int32_t M, int32_t N, int32_t K, void* stream) {
-  if (M < 0 || N < 1 || K < 1 || K > kMaxK || lda < K || ldb < K || lda % 16 || ldb % 16 || ldc < N ||
+  if (M < 0 || M > kMaxSide || N < 1 || N > kMaxSide || K < 1 || K > kMaxK || lda < K || ldb < K || lda % 16 || ldb % 16 || ldc < N ||
       (dtype != OSCARS_F32 && dtype != OSCARS_BF16))
     return OSCARS_EINVAL;
   if (M == 0) return OSCARS_OK;

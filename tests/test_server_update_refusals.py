@@ -75,7 +75,8 @@ def quant(x=A, ldx=8, dtype=0, rows=4, cols=8, q=A, ldq=8, s=A):
 
 
 @pytest.mark.parametrize("kw", [dict(x=0), dict(q=0), dict(s=0), dict(x=A + 2), dict(x=A + 1, dtype=1), dict(s=A + 2), dict(ldx=7), dict(ldq=7),
-                                dict(rows=-1), dict(cols=0), dict(dtype=2), dict(dtype=-1)])
+                                dict(rows=-1), dict(cols=0), dict(dtype=2), dict(dtype=-1), dict(rows=(1 << 30) + 1),
+                                dict(cols=(1 << 30) + 1, ldx=1 << 31, ldq=1 << 31)])
 def test_quantize(oscars_lib, kw):
     refused(quant, **kw)
 
@@ -87,7 +88,7 @@ def product(a=A, lda=16, sa=A, b=A, ldb=16, sb=A, c=A, ldc=8, dtype=0, M=4, N=8,
 @pytest.mark.parametrize("kw", [
     dict(a=0), dict(b=0), dict(c=0), dict(sa=0), dict(sb=0), dict(a=A + 8), dict(b=A + 1), dict(sa=A + 1), dict(sb=A + 2), dict(bias_ptr=A + 2),
     dict(c=A + 2), dict(c=A + 1, dtype=1), dict(lda=15), dict(lda=24), dict(ldb=40), dict(lda=0), dict(K=17), dict(ldc=7), dict(M=-1), dict(N=0), dict(K=0),
-    dict(K=131072, lda=131072, ldb=131072), dict(dtype=2),
+    dict(K=131072, lda=131072, ldb=131072), dict(dtype=2), dict(M=(1 << 30) + 1), dict(N=(1 << 30) + 1, ldc=1 << 31),
 ])
 def test_gemm_i8(oscars_lib, kw):
     refused(product, **kw)
