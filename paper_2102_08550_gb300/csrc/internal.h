@@ -222,7 +222,7 @@ cudaError_t launch_gemm_rows(int epi, const RowsPlan& p, const CUtensorMap& mA, 
 // The products of a Newton-Schulz step (csrc/orth_product.cu).  Operands are fp16,
 // [half][batch][rows][ld]: one half, or two whose sum is the value.
 enum NsEpi {
-  kNsSym,      // D = factor A B + diag I, symmetric: the tiles of one triangle and their mirror images
+  kNsSym,      // D = factor A B + diag I, symmetric
   kNsStep,     // D = the next X, two halves
   kNsLast      // the last step's X, times factor, to `out`
 };
@@ -238,7 +238,7 @@ struct NsArgs {
   void* out;                     // kNsLast
   int64_t ldo, zo;
   int out_type;                  // NsOut
-  int BN, stages, mt, nt, units, split;   // set by the launcher, and B's boxes of a half:
+  int BN, stages, mt, nt, units, split, full;   // set by the launcher, and B's boxes of a half:
   int b_rows, b_loads;
 };
 // maps of one tensor (inner, row, half x batch + z): loads in boxes of 64 x 64 and 64 x

@@ -18,20 +18,22 @@
 // everything.  bf16 results take two halves of X and one of A and B: what X's
 // rounding leaves in the directions in which the update is near zero is
 // multiplied by a at every step (485 over five), while the roundings of A and B
-// multiply X and stay relative to it (the last step's X takes one half as well).  fp16 rather than bf16: three more bits at
-// the same rate, and the values are bounded (singular values below 2).
+// multiply X and stay relative to it (the last step's X takes one half as well).
+// fp16 rather than bf16: three more bits at the same rate, and the values are bounded
+// (singular values below 2).
 //
 // The tensor core cuts what an addition to its accumulator leaves below fp32's last
 // bit.  Over 4096 products in three passes of 256 additions each that is a loss of
 // 1e-5 of a sum of squares, so for fp32 results the accumulator takes kChunk K-blocks
 // at a time, and the epilogue adds it, rounded to nearest, to a sum in registers.
 //
-// A and B are symmetric: only tiles on and above the diagonal are computed, and
-// the epilogue writes each tile and its mirror image, half the work of two of the
-// three products.
+// A and B are symmetric: where there is work for more than a wave of tiles, only
+// those on and above the diagonal are computed, and the epilogue writes each tile and
+// its mirror image, half the work of two of the three products.
 //
 // Structure: persistent, one CTA per SM or a cluster of two (cta_group::2, a tile
-// of 256 x BN) striding over tiles; warp 0 lane 0 streams K-blocks of 64 by TMA
+// of 256 x BN) striding over tiles, or a cluster of two or four on the K-blocks of one
+// tile; warp 0 streams K-blocks of 64 by TMA
 // (128-byte swizzle), warp 1 issues into one of two TMEM accumulators, warps 4-11
 // (half of a tile's columns each group of four) run the epilogue of a tile, or the
 // sum of a chunk, under the products of the next.
@@ -109,10 +111,10 @@ __host__ __device__ constexpr uint32_t idesc_f16(int M, int N, int a_mn, int b_m
 struct Tile {
   int z, i, j;
 };
-template <int CL, bool kSym>
+template <int CL, bool kSym, bool kSplit>
 __device__ __forceinline__ Tile tile_of(const NsArgs& a, int u) {
   Tile t;
-  if (kSym) {
+  if (kSym && (kSplit || !a.full)) {
     const int per = a.nt * (a.nt + 1) / 2;
     t.z = u / per;
     int r = u - t.z * per;
@@ -277,7 +279,7 @@ __global__ void __launch_bounds__(kThreads, 1) ns_product_kernel(const __grid_co
     int it = 0, s = 0, ph = 1, armed = 0;
     uint32_t limit = kSpinLimit;
     for (int u = u0; u < a.units; u += ustep) {
-      const Tile t = tile_of<CL, kSym>(a, u);
+      const Tile t = tile_of<CL, kSym, kSplit>(a, u);
       const int m0 = (t.i * CL + rank) * 128, n0 = t.j * a.BN + rank * (a.BN / CL);
       const bool same = kSym && t.i == t.j && b_boxes == 2;   // a tile on the diagonal: B is A
       const uint32_t bytes = CL * (same ? a_bytes : stage_bytes);
@@ -333,7 +335,7 @@ __global__ void __launch_bounds__(kThreads, 1) ns_product_kernel(const __grid_co
     for (int u = u0; u < a.units; u += ustep) {
       bool same = false;
       if (kSym) {
-        const Tile tl = tile_of<CL, kSym>(a, u);
+        const Tile tl = tile_of<CL, kSym, kSplit>(a, u);
         same = tl.i == tl.j && b_boxes == 2;
       }
       const int b_off = same ? 0 : a_bytes;
@@ -400,7 +402,7 @@ __global__ void __launch_bounds__(kThreads, 1) ns_product_kernel(const __grid_co
         st_dsmem_at(at + q * 128 * 16, make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]));
     };
     for (int u = u0; u < a.units; u += ustep) {
-      const Tile tl = tile_of<CL, kSym>(a, u);
+      const Tile tl = tile_of<CL, kSym, kSplit>(a, u);
       const int m0 = (tl.i * CL + rank) * 128 + 32 * quarter, n0 = tl.j * a.BN + cb;
       const uint32_t row0 = tmem + (static_cast<uint32_t>(32 * quarter) << 16) + cb;
       if constexpr (kSums) {
@@ -432,7 +434,7 @@ __global__ void __launch_bounds__(kThreads, 1) ns_product_kernel(const __grid_co
         for (int g = 0; g < kMaxBN / 64; ++g)
           if (kSplit ? 32 * g < span : 32 * g < span && n0 + 32 * g < a.N && m0 < a.M) {
             if (kSplit) keep(cb + 32 * g, sum[g]);
-            else finish(tl.z, m0, n0 + 32 * g, tl.i != tl.j, sum[g]);
+            else finish(tl.z, m0, n0 + 32 * g, tl.i != tl.j && (kSplit || !a.full), sum[g]);
           }
       } else {
         const int b = t & 1;
@@ -442,7 +444,7 @@ __global__ void __launch_bounds__(kThreads, 1) ns_product_kernel(const __grid_co
           float v[32];
           tmem_ld_32x32b_x32(row0 + b * kMaxBN + c0, v);
           if (kSplit) keep(cb + c0, v);
-          else finish(tl.z, m0, n0 + c0, tl.i != tl.j, v);
+          else finish(tl.z, m0, n0 + c0, tl.i != tl.j && (kSplit || !a.full), v);
         }
         release(b);
         ++t;
@@ -456,7 +458,7 @@ __global__ void __launch_bounds__(kThreads, 1) ns_product_kernel(const __grid_co
   if constexpr (kSplit) {
     // each CTA adds up its columns of the tile over the parts, in their order
     const int quarter = warp & 3, span = a.BN / a.split;
-    const Tile tl = tile_of<CL, kSym>(a, u0);
+    const Tile tl = tile_of<CL, kSym, kSplit>(a, u0);
     const int m0 = tl.i * 128 + 32 * quarter;
     for (int c0 = 32 * ((warp >> 2) - 1); warp >= 4 && c0 < span; c0 += 64) {
       const int c = part * span + c0, n = tl.j * a.BN + c;
@@ -472,7 +474,7 @@ __global__ void __launch_bounds__(kThreads, 1) ns_product_kernel(const __grid_co
           v[4 * q] += f.x, v[4 * q + 1] += f.y, v[4 * q + 2] += f.z, v[4 * q + 3] += f.w;
         }
       }
-      finish(tl.z, m0, n, tl.i != tl.j, v);
+      finish(tl.z, m0, n, tl.i != tl.j && (kSplit || !a.full), v);
     }
     if (warp >= 4 && lane == 0) bulk_wait_all();
   }
@@ -580,7 +582,11 @@ cudaError_t launch_ns_product(int epi, const NsMaps& A, const NsMaps& B, const N
   const int nk = (a.K + kK - 1) / kK, products = a.a_halves + a.b_halves - 1;
   // The shape with the least estimated time: waves of tiles times the longer of a
   // tile's products (2 BN clocks a K-block and product) and loads (52 bytes a clock
-  // into an SM), plus a tile's and a launch's fixed part.  Triangles take square tiles.
+  // into an SM), plus a tile's and a launch's fixed part, a split's exchange and a
+  // triangle's second write.  Symmetric products take square
+  // tiles: a triangle of them and their mirror images, or all of them where a wave has
+  // room (us a call, a triangle / all: 16 x 512 x 784 bf16 183 / 173, 4 x 768 x 768 bf16 124 /
+  // 119; with the K-blocks split, 512 x 784 fp32, 122 / 124).
   double best = 0.0;
   int cl = 1;
   for (int c = 1; c <= 2; ++c) {
@@ -588,15 +594,17 @@ cudaError_t launch_ns_product(int epi, const NsMaps& A, const NsMaps& B, const N
     for (int bn = 64; bn <= kMaxBN; bn += 64) {
       if ((c == 2 && bn % 128) || (sym && bn != 128 * c)) continue;
       const int nt = (a.N + bn - 1) / bn;
-      const int64_t units = static_cast<int64_t>(a.batch) * (sym ? nt * static_cast<int64_t>(nt + 1) / 2 : static_cast<int64_t>(mt / c) * nt);
       const int room = c == 2 ? pairs : sms;
       const double mma = 2.0 * bn * products, load = stage_bytes(a, bn, c) / 52.0;
-      for (int split = 1; split <= (c == 1 ? 4 : 1); split *= 2) {
+      for (int split = 1, full = 0; split <= (c == 1 ? 4 : 1); full ^= 1, split *= full ? 1 : 2) {
+        if (full && (!sym || split > 1)) continue;
+        const int64_t tiles = sym && !full ? nt * static_cast<int64_t>(nt + 1) / 2 : static_cast<int64_t>(mt / c) * nt;
+        const int64_t units = a.batch * tiles;
         // a part has two K-blocks, a CTA 32 columns of the sums, and the clusters run at once
-        if (split > 1 && (units > (split == 2 ? pairs : fours) || nk < 2 * split || bn < 32 * split || stages_of(a, bn, c, split) < 2)) break;
+        if (split > 1 && (units > (split == 2 ? pairs : fours) || nk < 2 * split || bn < 32 * split || stages_of(a, bn, c, split) < 2)) continue;
         const double waves = split > 1 ? 1.0 : static_cast<double>((units + room - 1) / room);
         const double cost = waves * ((nk + split - 1) / split * (load > mma ? load : mma) + 600.0) + 12.0 * bn +
-                            (c == 2 ? 1500.0 : 0.0) + (split > 1 ? 2500.0 : 0.0);
+                            (c == 2 ? 1500.0 : 0.0) + (split > 1 ? 2500.0 : sym && !full && nt > 1 ? 6.0 * bn : 0.0);
         if (best == 0.0 || cost < best) {
           best = cost;
           cl = c;
@@ -604,6 +612,7 @@ cudaError_t launch_ns_product(int epi, const NsMaps& A, const NsMaps& B, const N
           a.mt = mt;
           a.nt = nt;
           a.split = split;
+          a.full = full;
           a.units = static_cast<int>(units);   // far below 2^31: a tile is 16 KB of workspace at least
         }
       }
