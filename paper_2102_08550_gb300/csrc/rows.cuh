@@ -112,12 +112,15 @@ struct Squares {
   }
 };
 
-// 1 / (norm + eps) = power x factor, each a normal fp32 number (power: of two), of a sum of squares.
+// 1 / (norm + eps) = power x factor of a sum of squares, each a normal fp32 number: norm + eps lies between 2^-149 and 2^145,
+// further from 1 than the reciprocal of a power of two can follow it, so `power` stops at 2^125 and 2^-126 and `factor` has the
+// rest.  (With all of it in `power`, zeros under an eps of 2^-129 came out as 0 x infinity.)
 __device__ __forceinline__ void inverse_norm(double squares, float eps, float& power, float& factor) {
   int e;
   const double m = frexp(sqrt(squares) + static_cast<double>(eps), &e);
-  factor = static_cast<float>(1.0 / m);
-  power = isinf(squares) ? 0.f : ldexpf(1.f, -e);
+  const int in_power = min(max(e, -125), 126);
+  factor = static_cast<float>(ldexp(1.0 / m, in_power - e));
+  power = isinf(squares) ? 0.f : ldexpf(1.f, -in_power);
 }
 
 // A launch whose set-up may run while the previous kernel on the stream ends: the
