@@ -220,15 +220,21 @@ cudaError_t launch_gemm_rows(int epi, const RowsPlan& p, const CUtensorMap& mA, 
                              const CUtensorMap& mD, RowsArgs a, cudaStream_t s);
 
 // The products of a Newton-Schulz step (csrc/orth_product.cu).  Operands are fp16,
-// [half][batch][rows][ld]: one half, or two whose sum is the value.
+// [half][batch][rows][ld]: one half, or two whose sum is the value (of an fp32
+// result's operands, the first plus 2^-kNsShift times the second).
 enum NsEpi {
   kNsSym,      // D = factor A B + diag I, symmetric
   kNsStep,     // D = the next X, two halves
   kNsLast      // the last step's X, times factor, to `out`
 };
 enum NsOut { kNsF32, kNsBf16, kNsAdd };   // kNsAdd: out += factor X, fp32
-// values are stored times these, which keeps the second half out of fp16's subnormal range
-constexpr float kNsScaleX = 1024.f, kNsScaleA = 256.f;
+// Values are stored times these: X below 16 and A, B below 256 stay within fp16's range.  A half's rounding is off by at
+// most 2^-11 of it or, among fp16's subnormal numbers, by 2^-25; so two halves are off by 2^-22 of X or 2^-37, whichever is
+// more (A, B: 2^-33).  For an fp32 result that is not enough: of an update with one row a million times larger than the
+// others, which are small all over then, 12 steps came out 5e-4 off.  There the second half is stored 2^11 times larger, as
+// large as the first, which takes the floors to 2^-48 of X and 2^-44 of A and B.
+constexpr float kNsScaleX = 4096.f, kNsScaleA = 256.f;
+constexpr int kNsShift = 11;
 struct NsArgs {
   int batch, M, N, K;
   int a_halves, b_halves;        // of the operands

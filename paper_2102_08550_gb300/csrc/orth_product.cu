@@ -15,7 +15,9 @@
 // bits) or as two whose sum has 22, and a product of values in two halves takes
 // three products, high x high, high x low and low x high (the fourth is below
 // fp32's last bit), into one fp32 accumulator.  fp32 results take two halves of
-// everything.  bf16 results take two halves of X and one of A and B: what X's
+// everything, the second stored 2^11 times larger (internal.h): the accumulator takes the
+// two mixed products of a K-block first, and the first instruction of high x high scales
+// what is there by 2^-11 (scale-input-d), which costs nothing.  bf16 results take two halves of X and one of A and B: what X's
 // rounding leaves in the directions in which the update is near zero is
 // multiplied by a at every step (485 over five), while the roundings of A and B
 // multiply X and stay relative to it (the last step's X takes one half as well).
@@ -49,6 +51,7 @@ namespace {
 
 constexpr int kK = 64, kThreads = 384, kMaxBN = 256, kMaxStages = 8;
 constexpr int kChunk = 1;                          // K-blocks of one accumulation of an fp32 result
+static_assert(kChunk == 1, "an accumulation's mixed products come before its others, which scale them once");
 constexpr int kEpiWarps = 8;
 constexpr int kBox = 64 * 128;                     // one operand box: 64 rows of 128 bytes
 constexpr int kStg = 2048;                         // one staging box: 32 rows x 64 bytes
@@ -83,6 +86,24 @@ __device__ __forceinline__ void umma_f16_pair(uint32_t d_tmem, uint64_t a_desc, 
       "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
       "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
       : "memory");
+}
+// the same (or a CTA's alone) with what the accumulator holds times 2^-kNsShift
+template <int CL>
+__device__ __forceinline__ void umma_f16_scaled(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc) {
+  if (CL > 1)
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.eq.b32 p, 0, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p, %4;\n\t}" ::"r"(d_tmem),
+        "l"(a_desc), "l"(b_desc), "r"(idesc), "n"(kNsShift)
+        : "memory");
+  else
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.eq.b32 p, 0, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p, %4;\n\t}" ::"r"(d_tmem),
+        "l"(a_desc), "l"(b_desc), "r"(idesc), "n"(kNsShift)
+        : "memory");
 }
 __device__ __forceinline__ void umma_commit_pair(uint64_t* bar) {
   asm volatile(
@@ -137,6 +158,7 @@ __global__ void __launch_bounds__(kThreads, 1) ns_product_kernel(const __grid_co
                                                                  const __grid_constant__ CUtensorMap mapD,
                                                                  const __grid_constant__ NsArgs a) {
   constexpr bool kSym = EPI == kNsSym;
+  constexpr float kSecond = kSums ? static_cast<float>(1 << kNsShift) : 1.f;   // an fp32 result's second halves
   extern __shared__ uint8_t ns_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(ns_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* stg = smem;
@@ -204,7 +226,7 @@ __global__ void __launch_bounds__(kThreads, 1) ns_product_kernel(const __grid_co
         }
         const __half2 h = __floats2half2_rn(x, y);
         const float2 f = __half22float2(h);
-        const __half2 l = __floats2half2_rn(x - f.x, y - f.y);
+        const __half2 l = __floats2half2_rn((x - f.x) * kSecond, (y - f.y) * kSecond);
         hi[e] = *reinterpret_cast<const uint32_t*>(&h);
         lo[e] = *reinterpret_cast<const uint32_t*>(&l);
       }
@@ -352,17 +374,23 @@ __global__ void __launch_bounds__(kThreads, 1) ns_product_kernel(const __grid_co
           const uint64_t bd = a.b_mn ? smem_desc_mn128(at + b_off, kBox) : smem_desc_k128(at + b_off);
           if (elect_one() && limit > 1) {
             uint32_t more = kb == k0 ? 0u : 1u;
-            auto issue = [&](uint64_t x, uint64_t y) {
+            auto issue = [&](uint64_t x, uint64_t y, int n = kK / 16) {
 #pragma unroll
               for (int j = 0; j < kK / 16; ++j) {
+                if (j >= n) break;
                 if (CL > 1) umma_f16_pair(acc, x + j * astep, y + j * bstep, idesc, more);
                 else umma_bf16(acc, x + j * astep, y + j * bstep, idesc, more);
                 more = 1u;
               }
             };
-            if (a.b_halves == 2) issue(ad, bd + blo);
-            if (a.a_halves == 2) issue(ad + alo, bd);
-            issue(ad, bd);
+            if (kSums || a.b_halves == 2) issue(ad, bd + blo);
+            if (kSums || a.a_halves == 2) issue(ad + alo, bd);
+            if (kSums) {   // kChunk is 1: the accumulator holds these two products alone
+              umma_f16_scaled<CL>(acc, ad, bd, idesc);
+              issue(ad + astep, bd + bstep, kK / 16 - 1);
+            } else {
+              issue(ad, bd);
+            }
             if (CL > 1) umma_commit_pair(&bars->empty[s]);
             else umma_commit(&bars->empty[s]);
           }

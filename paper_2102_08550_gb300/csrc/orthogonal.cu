@@ -169,7 +169,7 @@ __global__ void __launch_bounds__(kPasses) orth_merge_kernel(const __grid_consta
 template <typename T>
 __global__ void __launch_bounds__(kPasses) orth_scale_kernel(const T* __restrict__ G, int64_t ldg, int64_t bsg, int rows,
                                                              int cols, int vec, const Squares* __restrict__ part, int parts,
-                                                             float eps, __half* __restrict__ X, int64_t ldx) {
+                                                             float eps, float second_scale, __half* __restrict__ X, int64_t ldx) {
   __shared__ float inv_s[2];
   pdl_wait();
   pdl_trigger();
@@ -204,7 +204,7 @@ __global__ void __launch_bounds__(kPasses) orth_scale_kernel(const T* __restrict
       for (int j = 0; j < 8; ++j) {
         const float y = ((v[j] * pw) * f) * kNsScaleX;
         hi[j] = __float2half_rn(y);
-        lo[j] = __float2half_rn(y - __half2float(hi[j]));
+        lo[j] = __float2half_rn((y - __half2float(hi[j])) * second_scale);
       }
       // rows of X are as long as their groups, so group i lies at 8 i
       *reinterpret_cast<uint4*>(x + 8 * static_cast<int64_t>(i)) = *reinterpret_cast<const uint4*>(hi);
@@ -251,7 +251,7 @@ cudaError_t steps_from(const Shape& p, uint8_t* ws, const T* G, int64_t ldg, int
   const int vec = (reinterpret_cast<uintptr_t>(G) | (ldg * sizeof(T)) | (bsg * sizeof(T))) % 16 == 0;
   cudaError_t e = launch_dependent(orth_scale_kernel<T>, dim3(pass_blocks((p.rows * (p.ldx / 8) + kAhead - 1) / kAhead, 608), p.batch), kPasses, 0, s,
                                    G, ldg, bsg, p.rows, p.cols, vec, reinterpret_cast<const Squares*>(ws + p.off_part), p.parts,
-                                   eps, X[0], p.ldx);
+                                   eps, p.halves == 2 ? static_cast<float>(1 << kNsShift) : 1.f, X[0], p.ldx);
   const bool tall = p.rows > p.cols;
   const bool cubic = co[2] == 0.f;
   const float sums = kNsScaleA / (kNsScaleX * kNsScaleX);
