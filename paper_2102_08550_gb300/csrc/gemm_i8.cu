@@ -221,15 +221,22 @@ __host__ __device__ constexpr uint32_t idesc_f16(int M, int N) {
   return (1u << 4) | (static_cast<uint32_t>(N >> 3) << 17) | (static_cast<uint32_t>(M >> 4) << 24);
 }
 
+// sum x sa x sb for any scales.  The sum is below 2^31, so its product with a scale in [2^-126, 2^96], or with zero, stays
+// among fp32's normal numbers, and only the result can leave them.  With other scales it may where the result does not
+// (tokens of 1e37 against channels of 1e-3); then sa is taken 2^64 nearer to 1, and the result times `back` afterwards.
+__device__ __forceinline__ float near_one(float s) { return fabsf(s) > 0x1p96f ? s * 0x1p-64f : fabsf(s) < 0x1p-126f ? s * 0x1p64f : s; }
+__device__ __forceinline__ float back(float s) { return fabsf(s) > 0x1p96f ? 0x1p64f : fabsf(s) < 0x1p-126f ? 0x1p-64f : 1.f; }
+
 __device__ __forceinline__ float finish(const I8Args& a, int sum, float sa, float sb, float bias) {
-  float v = static_cast<float>(sum) * sa * sb;
+  float v = static_cast<float>(sum) * near_one(sa) * sb * back(sa);
   if (a.bias) v += bias;
   return a.relu && v < 0.f ? 0.f : v;
 }
 
 // A thread's channel n of tokens m0 ... m0 + span: 16 values at a time without a branch between them (with the type and
 // the edges tested at each, a token took a warp 120 clocks, and a tile of 256 x 256 longer than its products)
-template <typename T>
+// (kFar: some of sa are near_one's, a copy of its own, since a branch more a group took 8192 x 512 x 784 from 24.7 to 25.4 us)
+template <bool kFar, typename T>
 __device__ __forceinline__ void store_tokens(const I8Args& a, T* C, int m0, int n, int span, const int (&sum)[kMaxBN / 32][16],
                                              const float (&sa)[kMaxBN / 64], float sb, float bias) {
   T* at = C + m0 * a.ldc + n;
@@ -241,6 +248,12 @@ __device__ __forceinline__ void store_tokens(const I8Args& a, T* C, int m0, int 
 #pragma unroll
       for (int e = 0; e < 16; ++e)
         v[e] = static_cast<float>(sum[g][e]) * __shfl_sync(0xffffffffu, sa[g / 2], (g & 1) * 16 + e) * sb;
+      if constexpr (kFar) {
+        const int m = m0 + 16 * g + (threadIdx.x & 15);
+        const float to = m < a.M ? back(__ldg(a.sa + m)) : 1.f;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) v[e] *= __shfl_sync(0xffffffffu, to, e);
+      }
       if (a.bias) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) v[e] += bias;
@@ -457,6 +470,15 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_i8_kernel(const __grid_const
       float sa[kMaxBN / 64];   // lane l: tokens l, 32 + l, ...
 #pragma unroll
       for (int i = 0; i < kMaxBN / 64; ++i) sa[i] = m0 + 32 * i + lane < a.M && 32 * i < span ? __ldg(a.sa + m0 + 32 * i + lane) : 0.f;
+      bool far = false;        // of any of the tile's tokens
+      if (!kSplit) {
+#pragma unroll
+        for (int i = 0; i < kMaxBN / 64; ++i) {
+          far |= sa[i] != 0.f && back(sa[i]) != 1.f;
+          sa[i] = near_one(sa[i]);
+        }
+        far = __any_sync(0xffffffffu, far);
+      }
       int sum[kMaxBN / 32][16];
 #pragma unroll
       for (int g = 0; g < kMaxBN / 32; ++g)
@@ -493,10 +515,13 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_i8_kernel(const __grid_const
               st_peer(recv + ((part * owned + tok % owned) * 128 + 32 * quarter + lane) * 4, tok / owned, sum[g][e]);
             }
           }
+      } else if (far) {
+        if (a.bf16) store_tokens<true>(a, static_cast<__nv_bfloat16*>(a.C), m0, n, span, sum, sa, sb, bias);
+        else store_tokens<true>(a, static_cast<float*>(a.C), m0, n, span, sum, sa, sb, bias);
       } else if (a.bf16) {
-        store_tokens(a, static_cast<__nv_bfloat16*>(a.C), m0, n, span, sum, sa, sb, bias);
+        store_tokens<false>(a, static_cast<__nv_bfloat16*>(a.C), m0, n, span, sum, sa, sb, bias);
       } else {
-        store_tokens(a, static_cast<float*>(a.C), m0, n, span, sum, sa, sb, bias);
+        store_tokens<false>(a, static_cast<float*>(a.C), m0, n, span, sum, sa, sb, bias);
       }
     }
   }
