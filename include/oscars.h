@@ -513,8 +513,9 @@ oscars_status oscars_softreg_steps_noalloc(const float* params_in, float* params
  * NaN gives NaN throughout.  The norm neither overflows nor underflows.
  * Accuracy: fp32 results keep X (whose norm is 1 at first) in 22 bits or to 2^-48
  * and the factors in 22 bits or to 2^-44, whichever is coarser, and add in
- * fp32, where a sum is cut and not rounded; so rows 2^-20 of the update's norm
- * come up in later steps like others, and what is 2^-40 of it may be lost.
+ * fp32: about as near to the definition as products in fp32 come.  Rows 2^-20
+ * of the update's norm come up in later steps like others; what is 2^-40 of it
+ * may be lost.
  * Where the shorter side is at most 64, matrices may take fp32 throughout.
  * bf16 results round the factors to 11 bits, which moves a step's result by at
  * most about (|a| + b^2 / 2|c|) 2^-11 of X (after five steps with the default

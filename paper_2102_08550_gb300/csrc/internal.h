@@ -235,6 +235,8 @@ enum NsOut { kNsF32, kNsBf16, kNsAdd };   // kNsAdd: out += factor X, fp32
 // large as the first, which takes the floors to 2^-48 of X and 2^-44 of A and B.
 constexpr float kNsScaleX = 4096.f, kNsScaleA = 256.f;
 constexpr int kNsShift = 11;
+// An fp32 result's sums times this: what the accumulator cuts off them on average (csrc/orth_product.cu)
+constexpr float kNsWhole = 1.f + 0x1p-22f;
 struct NsArgs {
   int batch, M, N, K;
   int a_halves, b_halves;        // of the operands

@@ -254,7 +254,8 @@ cudaError_t steps_from(const Shape& p, uint8_t* ws, const T* G, int64_t ldg, int
                                    eps, p.halves == 2 ? static_cast<float>(1 << kNsShift) : 1.f, X[0], p.ldx);
   const bool tall = p.rows > p.cols;
   const bool cubic = co[2] == 0.f;
-  const float sums = kNsScaleA / (kNsScaleX * kNsScaleX);
+  const float whole = p.halves == 2 ? kNsWhole : 1.f;   // what the accumulator cuts off (orth_product.cu)
+  const float sums = whole * (kNsScaleA / (kNsScaleX * kNsScaleX));
   NsArgs g{};   // A + beta I, or B itself where c = 0
   g.batch = p.batch;
   g.M = g.N = p.s;
@@ -266,7 +267,7 @@ cudaError_t steps_from(const Shape& p, uint8_t* ws, const T* G, int64_t ldg, int
   NsArgs q = g;   // B = c (A + beta I)^2 + gamma I
   q.K = p.s;
   q.a_mn = q.b_mn = 0;
-  q.factor = co[2] / kNsScaleA;
+  q.factor = whole * (co[2] / kNsScaleA);
   q.diag = static_cast<float>(co[0] - 0.25 * co[1] * co[1] / co[2]) * kNsScaleA;
   NsArgs u{};   // X <- B X or X B
   u.batch = p.batch;
@@ -277,7 +278,7 @@ cudaError_t steps_from(const Shape& p, uint8_t* ws, const T* G, int64_t ldg, int
   u.b_halves = tall ? p.halves : 2;
   u.b_mn = !tall;
   u.d_halves = 2;
-  u.factor = 1.f / kNsScaleA;
+  u.factor = whole / kNsScaleA;
   // The step before a bf16 result's last one leaves X in one half, and the last step takes that: its rounding is multiplied
   // by a once (3.4 x 2^-12), where an earlier one would be by a to the number of steps left.
   NsArgs before = u, last = u;
@@ -285,7 +286,7 @@ cudaError_t steps_from(const Shape& p, uint8_t* ws, const T* G, int64_t ldg, int
     before.d_halves = 1;
     last.a_halves = last.b_halves = 1;
   }
-  last.factor = to.scale / (kNsScaleA * kNsScaleX);
+  last.factor = whole * (to.scale / (kNsScaleA * kNsScaleX));
   last.out = to.D;
   last.ldo = to.ldd;
   last.zo = to.zd;
