@@ -49,21 +49,17 @@
 
 #include "common.cuh"
 #include "internal.h"
+#include "orth_shape.h"
 
 namespace oscars {
 
 namespace {
 
-constexpr int kK = 64, kThreads = 384, kMaxBN = 256, kMaxStages = 8;
+constexpr int kK = kNsK, kThreads = 384, kMaxBN = kNsMaxBN, kMaxStages = kNsMaxStages;
 constexpr int kChunk = 1;                          // K-blocks of one accumulation of an fp32 result
 static_assert(kChunk == 1, "an accumulation's mixed products come before its others, which scale them once");
-constexpr int kEpiWarps = 8;
-constexpr int kBox = 64 * 128;                     // one operand box: 64 rows of 128 bytes
-constexpr int kStg = 2048;                         // one staging box: 32 rows x 64 bytes
-constexpr int kStgBytes = kEpiWarps * 2 * kStg;    // two per epilogue warp
-constexpr int kBarBytes = 256;
-constexpr int kSmem = 227 * 1024;
-constexpr int kRing = kSmem - 1024 - kBarBytes - kStgBytes;
+constexpr int kEpiWarps = kNsEpiWarps, kBox = kNsBox, kStg = kNsStg, kStgBytes = kNsStgBytes, kBarBytes = kNsBarBytes;
+constexpr int kSmem = kNsSmem;
 // at least: one CTA an SM, and no other kernel's cluster beside it (tensor memory)
 constexpr size_t kLeast = 164 * 1024;
 static_assert(no_cluster_beside(kLeast), "no other cluster's CTA beside this kernel's");
@@ -524,14 +520,6 @@ struct DevInfo {
 };
 DevInfo g_dev[kMaxDevices];
 
-int stage_bytes(const NsArgs& a, int BN, int cl) { return (a.a_halves * 2 + a.b_halves * (BN / cl / 64)) * kBox; }
-int stages_of(const NsArgs& a, int BN, int cl, int split) {
-  const int nk = ((a.K + kK - 1) / kK + split - 1) / split, bytes = stage_bytes(a, BN, cl);
-  int st = (kRing - (split > 1 ? 128 * BN * 4 : 0)) / bytes;   // beside the parts' sums
-  st = st > kMaxStages ? kMaxStages : st;
-  return st > nk ? (nk < 2 ? 2 : nk) : st;
-}
-
 cudaLaunchConfig_t config(cudaLaunchAttribute* attr, int cluster, int grid, size_t smem, cudaStream_t s) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(grid, 1, 1);
@@ -579,7 +567,7 @@ void device_room(int& sms, int& pairs, int& fours) {
 template <int EPI, int CL, bool kSums, bool kSplit>
 cudaError_t launch_t(const CUtensorMap& mA, const CUtensorMap& mB, const CUtensorMap& mD, const NsArgs& a, int grid,
                      cudaStream_t s) {
-  size_t smem = 1024 + kStgBytes + static_cast<size_t>(a.stages) * stage_bytes(a, a.BN, CL) + (kSplit ? 128 * a.BN * 4 : 0) + kBarBytes;
+  size_t smem = 1024 + kStgBytes + static_cast<size_t>(a.stages) * ((a.a_halves * 2 + a.b_halves * (a.BN / CL / 64)) * kBox) + (kSplit ? 128 * a.BN * 4 : 0) + kBarBytes;
   if (smem < kLeast) smem = kLeast;
   cudaError_t e = allow_smem(ns_product_kernel<EPI, CL, kSums, kSplit>, kSmem);
   if (e != cudaSuccess) return e;
@@ -609,54 +597,17 @@ cudaError_t launch_e(int cl, const CUtensorMap& mA, const CUtensorMap& mB, const
 }  // namespace
 
 cudaError_t launch_ns_product(int epi, const NsMaps& A, const NsMaps& B, const NsMaps& D, NsArgs a, cudaStream_t s) {
-  int sms, pairs, fours;
-  device_room(sms, pairs, fours);
-  const bool sym = epi == kNsSym;
-  const int nk = (a.K + kK - 1) / kK, products = a.a_halves + a.b_halves - 1;
-  // The shape with the least estimated time: waves of tiles times the longer of a
-  // tile's products (2 BN clocks a K-block and product) and loads (52 bytes a clock
-  // into an SM), plus a tile's and a launch's fixed part, a split's exchange and a
-  // triangle's second write.  Symmetric products take square
-  // tiles: a triangle of them and their mirror images, or all of them where a wave has
-  // room (us a call, a triangle / all: 16 x 512 x 784 bf16 183 / 173, 4 x 768 x 768 bf16 124 /
-  // 119; with the K-blocks split, 512 x 784 fp32, 122 / 124).
-  double best = 0.0;
-  int cl = 1;
-  for (int c = 1; c <= 2; ++c) {
-    const int mt = ((a.M + 127) / 128 + c - 1) / c * c;
-    for (int bn = 64; bn <= kMaxBN; bn += 64) {
-      if ((c == 2 && bn % 128) || (sym && bn != 128 * c)) continue;
-      const int nt = (a.N + bn - 1) / bn;
-      const int room = c == 2 ? pairs : sms;
-      const double mma = 2.0 * bn * products, load = stage_bytes(a, bn, c) / 52.0;
-      for (int split = 1, full = 0; split <= (c == 1 ? 4 : 1); full ^= 1, split *= full ? 1 : 2) {
-        if (full && (!sym || split > 1)) continue;
-        const int64_t tiles = sym && !full ? nt * static_cast<int64_t>(nt + 1) / 2 : static_cast<int64_t>(mt / c) * nt;
-        const int64_t units = a.batch * tiles;
-        // a part has two K-blocks, a CTA 32 columns of the sums, and the clusters run at once
-        if (split > 1 && (units > (split == 2 ? pairs : fours) || nk < 2 * split || bn < 32 * split || stages_of(a, bn, c, split) < 2)) continue;
-        const double waves = split > 1 ? 1.0 : static_cast<double>((units + room - 1) / room);
-        const double cost = waves * ((nk + split - 1) / split * (load > mma ? load : mma) + 600.0) + 12.0 * bn +
-                            (c == 2 ? 1500.0 : 0.0) + (split > 1 ? 2500.0 : sym && !full && nt > 1 ? 6.0 * bn : 0.0);
-        if (best == 0.0 || cost < best) {
-          best = cost;
-          cl = c;
-          a.BN = bn;
-          a.mt = mt;
-          a.nt = nt;
-          a.split = split;
-          a.full = full;
-          a.units = static_cast<int>(units);   // far below 2^31: a tile is 16 KB of workspace at least
-        }
-      }
-    }
-  }
-  a.stages = stages_of(a, a.BN, cl, a.split);
+  NsRoom has;
+  device_room(has.sms, has.pairs, has.fours);
+  const NsShape sh = ns_shape({epi == kNsSym, a.batch, a.M, a.N, a.K, a.a_halves, a.b_halves}, has);
+  const int cl = sh.cl;
+  a.BN = sh.BN, a.mt = sh.mt, a.nt = sh.nt, a.split = sh.split, a.full = sh.full, a.stages = sh.stages;
+  a.units = static_cast<int>(sh.units);
   // K-major boxes of 128 rows where the tile has them: half as many copies
   a.b_rows = a.b_mn || a.BN / cl % 128 ? 64 : 128;
   a.b_loads = a.BN / cl / a.b_rows;
   const CUtensorMap &mA = a.a_mn ? A.load64 : A.load128, &mB = a.b_rows == 64 ? B.load64 : B.load128, &mD = D.store;
-  const int room = cl == 2 ? pairs : sms, grid = (a.units < room ? a.units : room) * cl;
+  const int room = cl == 2 ? has.pairs : has.sms, grid = (a.units < room ? a.units : room) * cl;
   switch (epi) {
     case kNsSym: return launch_e<kNsSym>(cl, mA, mB, mD, a, grid, s);
     case kNsStep: return launch_e<kNsStep>(cl, mA, mB, mD, a, grid, s);
