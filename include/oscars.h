@@ -529,7 +529,8 @@ oscars_status oscars_softreg_steps_noalloc(const float* params_in, float* params
  * be captured (after a first call on the device, which loads the kernels).
  * Ordered on `stream`.  batch = 0 does nothing.
  * Errors: EINVAL (NULL or misaligned pointers, batch outside [0, 65535], rows
- * or cols outside [1, 65536], ldg or ldo < cols, a negative batch_stride_g, a
+ * or cols outside [1, 65536], 2^29 tiles of 128 x 64 or more in all, which
+ * no device holds, ldg or ldo < cols, a negative batch_stride_g, a
  * batch_stride_o below a matrix's extent with batch > 1, steps outside [1, 64],
  * coefficients or eps out of range, a workspace that is too small), ECUDA.
  */

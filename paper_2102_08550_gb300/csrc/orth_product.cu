@@ -600,6 +600,7 @@ cudaError_t launch_ns_product(int epi, const NsMaps& A, const NsMaps& B, const N
   NsRoom has;
   device_room(has.sms, has.pairs, has.fours);
   const NsShape sh = ns_shape({epi == kNsSym, a.batch, a.M, a.N, a.K, a.a_halves, a.b_halves}, has);
+  if (sh.units > INT32_MAX / 4) return cudaErrorInvalidValue;   // refused by the entries
   const int cl = sh.cl;
   a.BN = sh.BN, a.mt = sh.mt, a.nt = sh.nt, a.split = sh.split, a.full = sh.full, a.stages = sh.stages;
   a.units = static_cast<int>(sh.units);

@@ -303,7 +303,9 @@ cudaError_t steps_from(const Shape& p, uint8_t* ws, const T* G, int64_t ldg, int
 }
 
 bool sizes_ok(int32_t batch, int32_t rows, int32_t cols) {
-  return batch >= 0 && batch <= kMaxBatch && rows >= 1 && rows <= kMaxDim && cols >= 1 && cols <= kMaxDim;
+  if (batch < 0 || batch > kMaxBatch || rows < 1 || rows > kMaxDim || cols < 1 || cols > kMaxDim) return false;
+  // tiles of 128 x 64 (the smallest) in clusters of four are counted in 32 bits; more take some 2^44 bytes of workspace
+  return static_cast<int64_t>(batch) * ((rows + 127) / 128) * ((cols + 63) / 64) <= INT32_MAX / 4;
 }
 
 bool settings_ok(int32_t steps, const float* coeff, float eps, float scale, float (&co)[3]) {

@@ -7,6 +7,9 @@ import subprocess
 
 import pytest
 
+import paper_2102_08550_gb300 as P
+from tests.test_server_update_refusals import orth, refused
+
 CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2102_08550_gb300", "csrc")
 
 DRIVER = r"""
@@ -67,3 +70,16 @@ def test_every_shape_is_one_the_kernel_can_run(tmp_path):
     r = subprocess.run([str(exe)], capture_output=True, text=True)
     assert r.returncode == 0, r.stdout
     assert "fits(192, 4) 0" in r.stdout and "split 0 " not in r.stdout, r.stdout
+
+
+@pytest.mark.parametrize("batch,rows,cols", [(65535, 65536, 65536), (65535, 8200, 8200), (65535, 1100, 65536), (16384, 65536, 4096)])
+def test_more_tiles_than_are_counted(oscars_lib, batch, rows, cols):
+    """The numbers of such tiles leave 32 bits; no workspace of that size exists, but the call only sees what it is told."""
+    for dtype in (P.F32, P.BF16):
+        refused(P.oscars_orthogonalize_workspace, batch, rows, cols, dtype)
+        refused(orth, batch=batch, rows=rows, cols=cols, ldg=cols, ldo=cols, bsg=rows * cols, bso=rows * cols, dtype=dtype, n=1 << 62)
+
+
+def test_the_largest_that_are(oscars_lib):
+    for batch, rows, cols in [(1, 65536, 65536), (512, 65536, 65536), (65535, 1, 65536), (65535, 65536, 1), (65535, 1000, 4000)]:
+        assert P.oscars_orthogonalize_workspace(batch, rows, cols, P.F32) > 0
