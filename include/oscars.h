@@ -527,6 +527,9 @@ oscars_status oscars_softreg_steps_noalloc(const float* params_in, float* params
  * nothing in it that a later call needs, and calls (or captured graphs) that
  * may run at the same time need one each.  The call allocates nothing and can
  * be captured (after a first call on the device, which loads the kernels).
+ * The workspace's first 4 bytes are a status, an int32 that is 0 once the work is
+ * done.  Not 0: a wait inside a kernel ran out (none is known to), and O is not
+ * to be used; elements of it may be as they were before the call.
  * Ordered on `stream`.  batch = 0 does nothing.
  * Errors: EINVAL (NULL or misaligned pointers, batch outside [0, 65535], rows
  * or cols outside [1, 65536], 2^29 tiles of 128 x 64 or more in all, which
@@ -552,7 +555,9 @@ oscars_status oscars_orthogonalize(const void* G, int64_t ldg, int64_t batch_str
  * x_g and momentum are updated in place.  momentum == NULL: u = d (mu is not
  * read, nesterov must be 0).  deltas: host array of W device pointers, w: host,
  * W floats, W <= 256.  Everything in fp32.  Workspace, coeff, eps, determinism
- * and capture as for oscars_orthogonalize.
+ * and capture as for oscars_orthogonalize, and so the status: if it is not 0,
+ * momentum is updated and x_g is not, unless the wait was one of the last kernel's,
+ * which may have updated some elements by then.
  * Errors: EINVAL, ECUDA.
  */
 oscars_status oscars_merge_orthogonal_workspace(int32_t rows, int32_t cols, int64_t* bytes);
@@ -589,7 +594,9 @@ oscars_status oscars_quantize_i8(const void* x, int64_t ldx, int32_t dtype, int3
  * C[m ldc + n], of `dtype`, any alignment; scale, bias and act are fp32, rounded
  * once.  M = 0 (no tokens) does nothing; M, N <= 2^30, N >= 1; 1 <= K <= 131071
  * (the sum of products of -128 stays within 32 bits).  Ordered on `stream`;
- * allocates nothing and can be captured.
+ * allocates nothing and can be captured.  A wait inside the kernel that runs
+ * out (none is known to) is not reported, as in oscars_gemm_bf16_nt; it leaves
+ * elements of C as they were, and never part of a sum in them.
  * Errors: EINVAL (NULL or misaligned pointers, sizes or strides out of range),
  * ECUDA.
  */

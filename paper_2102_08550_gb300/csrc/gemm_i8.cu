@@ -168,6 +168,7 @@ static_assert(kChunk * kK * 128 * 128 <= 1 << 24, "a chunk's sums are exact in f
 struct Bars {
   uint64_t raw_full[kMaxStages], raw_empty[kMaxStages], op_full[kMaxStages], op_empty[kMaxStages], accf[2], acce[2];
   uint32_t tmem;
+  int failed;   // kSplit: a part's sums are not all there
 };
 static_assert(sizeof(Bars) <= kBarBytes, "barriers fit");
 
@@ -313,6 +314,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_i8_kernel(const __grid_const
       mbar_init(&bars->accf[i], 1);
       mbar_init(&bars->acce[i], kEpiWarps * CL);
     }
+    bars->failed = 0;
     fence_barrier_init();
     fence_proxy_async_smem();
   }
@@ -503,7 +505,10 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_i8_kernel(const __grid_const
           else mbar_arrive(&bars->acce[b]);
         }
       }
-      if (!ok) break;
+      if (!ok) {   // every wait that runs out in this CTA ends in one of the accumulator's; its peers then leave the tile alone too
+        if (kSplit && lane < a.split) st_peer(&bars->failed, lane, 1);
+        break;
+      }
       if constexpr (kSplit) {   // a part's sums [token][channel] go to the CTA that adds up the token
         const int owned = a.BN / a.split;
 #pragma unroll
@@ -530,9 +535,10 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_i8_kernel(const __grid_const
   else __syncthreads();
   if constexpr (kSplit) {
     // each CTA adds up its tokens of the tile over the parts
+    const int missing = bars->failed;
     const int n0 = (u0 % mu) * 128, tokens = a.BN / a.split, m0 = (u0 / mu) * a.BN + part * tokens;
     const int* sums = reinterpret_cast<const int*>(recv);
-    for (int i = threadIdx.x; i < tokens * 128; i += kThreads) {
+    for (int i = threadIdx.x; missing == 0 && i < tokens * 128; i += kThreads) {
       const int m = m0 + i / 128, n = n0 + i % 128;
       if (m >= a.M || n >= a.N) continue;
       int t = 0;

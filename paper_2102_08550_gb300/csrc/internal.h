@@ -246,6 +246,7 @@ struct NsArgs {
   void* out;                     // kNsLast
   int64_t ldo, zo;
   int out_type;                  // NsOut
+  int* status;                   // the call's: a DevErr once a wait has run out, then kNsLast writes nothing more
   int BN, stages, mt, nt, units, split, full;   // set by the launcher, and B's boxes of a half:
   int b_rows, b_loads;
 };
@@ -259,7 +260,7 @@ struct NsMaps {
 int ns_small_cluster(int batch, int rows, int cols, bool f32);
 cudaError_t launch_ns_small(const void* G, int64_t ldg, int64_t zg, bool bf16, void* out, int64_t ldo, int64_t zo, int out_type,
                             int batch, int rows, int cols, int cluster, int steps, const float (&co)[3], float eps,
-                            float scale, cudaStream_t s);
+                            float scale, int* status, cudaStream_t s);
 cudaError_t launch_ns_product(int epi, const NsMaps& A, const NsMaps& B, const NsMaps& D, NsArgs a, cudaStream_t s);
 
 // Weight gradient + SGD of up to kDwMaxLayers hidden layers, persistent

@@ -67,6 +67,7 @@ static_assert(no_cluster_beside(kLeast), "no other cluster's CTA beside this ker
 struct Bars {
   uint64_t full[kMaxStages], empty[kMaxStages], accf[2], acce[2];
   uint32_t tmem;
+  uint32_t failed;   // kSplit: a part's sums are not all there
 };
 static_assert(sizeof(Bars) <= kBarBytes, "barriers fit");
 
@@ -122,6 +123,9 @@ __device__ __forceinline__ void mbar_arrive_at(uint32_t cluster_bar) {
 __device__ __forceinline__ void st_dsmem_at(uint32_t remote, float4 v) {
   asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(remote), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w)
                : "memory");
+}
+__device__ __forceinline__ void st_dsmem_at(uint32_t remote, uint32_t v) {
+  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(remote), "r"(v) : "memory");
 }
 // fp16 operands (format 0), fp32 accumulator; bits 15 and 16: A, B MN-major
 __host__ __device__ constexpr uint32_t idesc_f16(int M, int N, int a_mn, int b_mn) {
@@ -190,6 +194,7 @@ __global__ void __launch_bounds__(kThreads, 1) ns_product_kernel(const __grid_co
       mbar_init(&bars->accf[i], 1);
       mbar_init(&bars->acce[i], kEpiWarps * CL);
     }
+    bars->failed = 0;
     fence_barrier_init();
     fence_proxy_async_smem();
   }
@@ -210,6 +215,8 @@ __global__ void __launch_bounds__(kThreads, 1) ns_product_kernel(const __grid_co
   const uint32_t tmem = bars->tmem;
   pdl_wait();
   pdl_trigger();
+  // A launch before this one that gave up a wait has left a matrix unfinished: the caller's is not touched then.
+  const int before = EPI == kNsLast && warp >= 4 ? *static_cast<const volatile int*>(a.status) : 0;
 
   // ---- what the epilogue's warps do with 32 columns of their 32 rows (m0) of matrix z, from column n on
   uint8_t* my = stg + (warp >= 4 ? warp - 4 : 0) * 2 * kStg;
@@ -268,7 +275,7 @@ __global__ void __launch_bounds__(kThreads, 1) ns_product_kernel(const __grid_co
             make_float4(v[4 * q] * a.factor, v[4 * q + 1] * a.factor, v[4 * q + 2] * a.factor, v[4 * q + 3] * a.factor);
       __syncwarp();
       // rows of 32 columns, coalesced whatever the caller's alignment, 16 at a time without a branch between them
-      const int col = n + lane, rows = col < a.N ? (a.M - m0 < 32 ? a.M - m0 : 32) : 0;
+      const int col = n + lane, rows = col < a.N && before == 0 ? (a.M - m0 < 32 ? a.M - m0 : 32) : 0;
       const int64_t at0 = z * a.zo + col + static_cast<int64_t>(m0) * a.ldo;
       auto store = [&](auto* out, bool add) {
 #pragma unroll
@@ -430,6 +437,12 @@ __global__ void __launch_bounds__(kThreads, 1) ns_product_kernel(const __grid_co
       for (int q = 0; q < 8; ++q)
         st_dsmem_at(at + q * 128 * 16, make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]));
     };
+    // Every wait of this CTA that runs out ends in one of the accumulator's, so those are recorded; its peers leave the tile
+    // alone then too.
+    auto give_up = [&] {
+      if (lane == 0) atomicCAS(a.status, kDevOk, kDevTimeoutAccum);
+      if (kSplit && lane < a.split) st_dsmem_at(cluster_addr(&bars->failed, lane), 1u);
+    };
     for (int u = u0; u < a.units; u += ustep) {
       const Tile tl = tile_of<CL, kSym, kSplit>(a, u);
       const int m0 = (tl.i * CL + rank) * 128 + 32 * quarter, n0 = tl.j * a.BN + cb;
@@ -458,7 +471,10 @@ __global__ void __launch_bounds__(kThreads, 1) ns_product_kernel(const __grid_co
             }
           release(b);
         }
-        if (!ok) break;
+        if (!ok) {
+          give_up();
+          break;
+        }
 #pragma unroll
         for (int g = 0; g < kMaxBN / 64; ++g)
           if (kSplit ? 32 * g < span : 32 * g < span && n0 + 32 * g < a.N && m0 < a.M) {
@@ -467,7 +483,10 @@ __global__ void __launch_bounds__(kThreads, 1) ns_product_kernel(const __grid_co
           }
       } else {
         const int b = t & 1;
-        if (!mbar_wait_warp(&bars->accf[b], (t >> 1) & 1, nullptr, kDevTimeoutAccum)) break;
+        if (!mbar_wait_warp(&bars->accf[b], (t >> 1) & 1, nullptr, kDevTimeoutAccum)) {
+          give_up();
+          break;
+        }
         tc_fence_after();
         for (int c0 = 0; c0 < span && (kSplit || (n0 + c0 < a.N && m0 < a.M)); c0 += 32) {
           float v[32];
@@ -486,10 +505,11 @@ __global__ void __launch_bounds__(kThreads, 1) ns_product_kernel(const __grid_co
   else __syncthreads();
   if constexpr (kSplit) {
     // each CTA adds up its columns of the tile over the parts, in their order
+    const uint32_t missing = bars->failed;   // (read at each turn it took 1024 x 1024 fp32 from 162.4 to 163.0 us)
     const int quarter = warp & 3, span = a.BN / a.split;
     const Tile tl = tile_of<CL, kSym, kSplit>(a, u0);
     const int m0 = tl.i * 128 + 32 * quarter;
-    for (int c0 = 32 * ((warp >> 2) - 1); warp >= 4 && c0 < span; c0 += 64) {
+    for (int c0 = 32 * ((warp >> 2) - 1); warp >= 4 && missing == 0 && c0 < span; c0 += 64) {
       const int c = part * span + c0, n = tl.j * a.BN + c;
       if (n >= a.N || m0 >= a.M) break;
       float v[32];

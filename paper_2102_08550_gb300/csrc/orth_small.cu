@@ -29,6 +29,7 @@ struct SmallArgs {
   int out_type;                                  // NsOut
   int rows, cols, s, len, share, cluster, steps; // share: columns (of the longer side) of a CTA, a multiple of 4
   float a, b, c, eps, scale;
+  int* status;                                   // set to zero (no wait of this kernel can run out), or NULL
 };
 
 int up4(int x) { return (x + 3) / 4 * 4; }
@@ -58,6 +59,7 @@ __global__ void __launch_bounds__(kThreads) orth_small_kernel(const __grid_const
   const bool tall = p.rows > p.cols;
   pdl_wait();
   pdl_trigger();
+  if (p.status && blockIdx.x == 0 && tid == 0) *p.status = kDevOk;
 
   // ---- X as it comes, and its norm.  Of a wide matrix a CTA holds columns, of a tall one rows (as columns)
   const T* g = static_cast<const T*>(p.G) + z * p.zg;
@@ -290,7 +292,7 @@ int ns_small_cluster(int batch, int rows, int cols, bool f32) {
 
 cudaError_t launch_ns_small(const void* G, int64_t ldg, int64_t zg, bool bf16, void* out, int64_t ldo, int64_t zo, int out_type,
                             int batch, int rows, int cols, int cluster, int steps, const float (&co)[3], float eps,
-                            float scale, cudaStream_t s) {
+                            float scale, int* status, cudaStream_t s) {
   SmallArgs a{};
   a.G = G, a.ldg = ldg, a.zg = zg;
   a.out = out, a.ldo = ldo, a.zo = zo, a.out_type = out_type;
@@ -302,6 +304,7 @@ cudaError_t launch_ns_small(const void* G, int64_t ldg, int64_t zg, bool bf16, v
   a.steps = steps;
   a.a = co[0], a.b = co[1], a.c = co[2];
   a.eps = eps, a.scale = scale;
+  a.status = status;
   const size_t smem = smem_floats(a.s, a.share) * 4;
   void (*kernel)(SmallArgs) = bf16 ? orth_small_kernel<__nv_bfloat16> : orth_small_kernel<float>;
   cudaError_t e = allow_smem(kernel, smem);

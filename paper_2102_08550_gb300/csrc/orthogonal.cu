@@ -36,7 +36,7 @@ struct Shape {
   int halves;                       // fp16 halves of A and B (X has two)
   int64_t ldx, lds;                 // rows of X and of A, B in the workspace, in elements
   int parts;                        // partial sums a matrix
-  int64_t off_part, off_u, off_x[2], off_a, off_b, bytes;
+  int64_t off_status, off_part, off_u, off_x[2], off_a, off_b, bytes;
 };
 
 int64_t up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
@@ -60,6 +60,7 @@ Shape make_shape(int batch, int rows, int cols, int dtype, bool with_u) {
     at = up(at + bytes, 256);
     return o;
   };
+  p.off_status = take(sizeof(int));   // first, where the caller finds it
   p.off_part = take(static_cast<int64_t>(batch) * p.parts * sizeof(Squares));
   p.off_u = with_u ? take(elems * 4) : 0;
   for (int i = 0; i < 2; ++i) p.off_x[i] = take(static_cast<int64_t>(batch) * rows * p.ldx * 4);
@@ -74,10 +75,11 @@ Shape make_shape(int batch, int rows, int cols, int dtype, bool with_u) {
 // part[z][block] = sum of squares of the block's share of matrix z
 template <typename T>
 __global__ void __launch_bounds__(kPasses) orth_norm_kernel(const T* __restrict__ G, int64_t ldg, int64_t bsg, int rows,
-                                                            int cols, int vec, Squares* __restrict__ part) {
+                                                            int cols, int vec, Squares* __restrict__ part, int* __restrict__ status) {
   __shared__ Squares warps[kPasses / 32];
   pdl_wait();
   pdl_trigger();
+  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *status = kDevOk;
   const T* g = G + blockIdx.y * bsg;
   // groups of eight: at most 2^29 (a 64-bit division for each took longer than its bytes)
   const uint32_t per_row = (cols + 7) / 8, n = rows * per_row, step = gridDim.x * kPasses;
@@ -104,10 +106,11 @@ __global__ void __launch_bounds__(kPasses) orth_norm_kernel(const T* __restrict_
 template <int V>
 __global__ void __launch_bounds__(kPasses) orth_merge_kernel(const __grid_constant__ MergeArgs a, float* __restrict__ mom,
                                                              float mu, int nesterov, float* __restrict__ u, int64_t n,
-                                                             Squares* __restrict__ part) {
+                                                             Squares* __restrict__ part, int* __restrict__ status) {
   __shared__ Squares warps[kPasses / 32];
   pdl_wait();
   pdl_trigger();
+  if (blockIdx.x == 0 && threadIdx.x == 0) *status = kDevOk;
   const int64_t step = static_cast<int64_t>(gridDim.x) * kPasses * V;
   Squares sum;
   for (int64_t i = (static_cast<int64_t>(blockIdx.x) * kPasses + threadIdx.x) * V; i < n; i += step) {
@@ -257,6 +260,7 @@ cudaError_t steps_from(const Shape& p, uint8_t* ws, const T* G, int64_t ldg, int
   const float whole = p.halves == 2 ? kNsWhole : 1.f;   // what the accumulator cuts off (orth_product.cu)
   const float sums = whole * (kNsScaleA / (kNsScaleX * kNsScaleX));
   NsArgs g{};   // A + beta I, or B itself where c = 0
+  g.status = reinterpret_cast<int*>(ws + p.off_status);
   g.batch = p.batch;
   g.M = g.N = p.s;
   g.K = tall ? p.rows : p.cols;
@@ -270,6 +274,7 @@ cudaError_t steps_from(const Shape& p, uint8_t* ws, const T* G, int64_t ldg, int
   q.factor = whole * (co[2] / kNsScaleA);
   q.diag = static_cast<float>(co[0] - 0.25 * co[1] * co[1] / co[2]) * kNsScaleA;
   NsArgs u{};   // X <- B X or X B
+  u.status = g.status;
   u.batch = p.batch;
   u.M = p.rows;
   u.N = p.cols;
@@ -329,10 +334,10 @@ oscars_status orthogonalize(const Shape& p, const void* G, int64_t ldg, int64_t 
   const T* g = static_cast<const T*>(G);
   if (const int c = ns_small_cluster(p.batch, p.rows, p.cols, sizeof(T) == 4))
     return launch_ns_small(G, ldg, bsg, sizeof(T) == 2, to.D, to.ldd, to.zd, to.type, p.batch, p.rows, p.cols, c, steps, co, eps,
-                           to.scale, s) == cudaSuccess ? OSCARS_OK : OSCARS_ECUDA;
+                           to.scale, reinterpret_cast<int*>(ws + p.off_status), s) == cudaSuccess ? OSCARS_OK : OSCARS_ECUDA;
   const int vec = (reinterpret_cast<uintptr_t>(g) | (ldg * sizeof(T)) | (bsg * sizeof(T))) % 16 == 0;
   if (launch_dependent(orth_norm_kernel<T>, dim3(p.parts, p.batch), kPasses, 0, s, g, ldg, bsg, p.rows, p.cols, vec,
-                       reinterpret_cast<Squares*>(ws + p.off_part)) != cudaSuccess)
+                       reinterpret_cast<Squares*>(ws + p.off_part), reinterpret_cast<int*>(ws + p.off_status)) != cudaSuccess)
     return OSCARS_ECUDA;
   return steps_from(p, ws, g, ldg, bsg, eps, steps, co, to, s) == cudaSuccess ? OSCARS_OK : OSCARS_ECUDA;
 }
@@ -405,12 +410,12 @@ oscars_status oscars_merge_orthogonal(float* x_g, const float* const* deltas, co
   const int64_t n = static_cast<int64_t>(rows) * cols;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   if (launch_dependent((bits & 15) == 0 ? orth_merge_kernel<4> : orth_merge_kernel<1>, dim3(p.parts), kPasses, 0, s, a, momentum,
-                       mu, nesterov != 0 ? 1 : 0, u, n, part) != cudaSuccess)
+                       mu, nesterov != 0 ? 1 : 0, u, n, part, reinterpret_cast<int*>(ws + p.off_status)) != cudaSuccess)
     return OSCARS_ECUDA;
   const Target to{x_g, cols, 0, kNsAdd, server_lr};
   if (const int c = ns_small_cluster(1, rows, cols, true))
-    return launch_ns_small(u, cols, 0, false, to.D, to.ldd, to.zd, to.type, 1, rows, cols, c, steps, co, eps, to.scale, s) ==
-                   cudaSuccess ? OSCARS_OK : OSCARS_ECUDA;
+    return launch_ns_small(u, cols, 0, false, to.D, to.ldd, to.zd, to.type, 1, rows, cols, c, steps, co, eps, to.scale, nullptr,
+                           s) == cudaSuccess ? OSCARS_OK : OSCARS_ECUDA;
   return steps_from(p, ws, static_cast<const float*>(u), cols, 0, eps, steps, co, to, s) == cudaSuccess ? OSCARS_OK
                                                                                                        : OSCARS_ECUDA;
 }
