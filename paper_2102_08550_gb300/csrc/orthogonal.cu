@@ -33,6 +33,7 @@ constexpr float kMaxCoeff = 8.f;
 
 struct Shape {
   int batch, rows, cols, s;         // s: the shorter side
+  int small;                        // CTAs a matrix of the one launch, or 0: products on the tensor cores
   int halves;                       // fp16 halves of A and B (X has two)
   int64_t ldx, lds;                 // rows of X and of A, B in the workspace, in elements
   int parts;                        // partial sums a matrix
@@ -42,11 +43,12 @@ struct Shape {
 int64_t up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 
 Shape make_shape(int batch, int rows, int cols, int dtype, bool with_u) {
-  Shape p;
+  Shape p{};
   p.batch = batch;
   p.rows = rows;
   p.cols = cols;
   p.s = rows < cols ? rows : cols;
+  p.small = ns_small_cluster(batch, rows, cols, dtype == OSCARS_F32);
   p.halves = dtype == OSCARS_F32 ? 2 : 1;
   // rows on 128-byte lines: a box's row of 128 bytes is one line then, not two (server step on 1537 x 385: 156 -> 146 us)
   p.ldx = up(cols, 64);
@@ -61,11 +63,13 @@ Shape make_shape(int batch, int rows, int cols, int dtype, bool with_u) {
     return o;
   };
   p.off_status = take(sizeof(int));   // first, where the caller finds it
-  p.off_part = take(static_cast<int64_t>(batch) * p.parts * sizeof(Squares));
+  if (!p.small || with_u) p.off_part = take(static_cast<int64_t>(batch) * p.parts * sizeof(Squares));
   p.off_u = with_u ? take(elems * 4) : 0;
-  for (int i = 0; i < 2; ++i) p.off_x[i] = take(static_cast<int64_t>(batch) * rows * p.ldx * 4);
-  p.off_a = take(static_cast<int64_t>(batch) * p.s * p.lds * 2 * p.halves);
-  p.off_b = take(static_cast<int64_t>(batch) * p.s * p.lds * 2 * p.halves);
+  if (!p.small) {   // one launch keeps a matrix in shared memory
+    for (int i = 0; i < 2; ++i) p.off_x[i] = take(static_cast<int64_t>(batch) * rows * p.ldx * 4);
+    p.off_a = take(static_cast<int64_t>(batch) * p.s * p.lds * 2 * p.halves);
+    p.off_b = take(static_cast<int64_t>(batch) * p.s * p.lds * 2 * p.halves);
+  }
   p.bytes = at;
   return p;
 }
@@ -332,8 +336,8 @@ template <typename T>
 oscars_status orthogonalize(const Shape& p, const void* G, int64_t ldg, int64_t bsg, uint8_t* ws, int steps,
                             const float (&co)[3], float eps, const Target& to, cudaStream_t s) {
   const T* g = static_cast<const T*>(G);
-  if (const int c = ns_small_cluster(p.batch, p.rows, p.cols, sizeof(T) == 4))
-    return launch_ns_small(G, ldg, bsg, sizeof(T) == 2, to.D, to.ldd, to.zd, to.type, p.batch, p.rows, p.cols, c, steps, co, eps,
+  if (p.small)
+    return launch_ns_small(G, ldg, bsg, sizeof(T) == 2, to.D, to.ldd, to.zd, to.type, p.batch, p.rows, p.cols, p.small, steps, co, eps,
                            to.scale, reinterpret_cast<int*>(ws + p.off_status), s) == cudaSuccess ? OSCARS_OK : OSCARS_ECUDA;
   const int vec = (reinterpret_cast<uintptr_t>(g) | (ldg * sizeof(T)) | (bsg * sizeof(T))) % 16 == 0;
   if (launch_dependent(orth_norm_kernel<T>, dim3(p.parts, p.batch), kPasses, 0, s, g, ldg, bsg, p.rows, p.cols, vec,
@@ -413,8 +417,8 @@ oscars_status oscars_merge_orthogonal(float* x_g, const float* const* deltas, co
                        mu, nesterov != 0 ? 1 : 0, u, n, part, reinterpret_cast<int*>(ws + p.off_status)) != cudaSuccess)
     return OSCARS_ECUDA;
   const Target to{x_g, cols, 0, kNsAdd, server_lr};
-  if (const int c = ns_small_cluster(1, rows, cols, true))
-    return launch_ns_small(u, cols, 0, false, to.D, to.ldd, to.zd, to.type, 1, rows, cols, c, steps, co, eps, to.scale, nullptr,
+  if (p.small)
+    return launch_ns_small(u, cols, 0, false, to.D, to.ldd, to.zd, to.type, 1, rows, cols, p.small, steps, co, eps, to.scale, nullptr,
                            s) == cudaSuccess ? OSCARS_OK : OSCARS_ECUDA;
   return steps_from(p, ws, static_cast<const float*>(u), cols, 0, eps, steps, co, to, s) == cudaSuccess ? OSCARS_OK
                                                                                                        : OSCARS_ECUDA;
