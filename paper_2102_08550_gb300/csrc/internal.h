@@ -243,6 +243,7 @@ struct NsArgs {
   int a_mn, b_mn;                // read MN-major (the transposed tensor)
   int d_halves;                  // of D
   float factor, diag;            // factor includes the operands' and D's scales, diag D's
+  float scale;                   // kNsLast: the caller's, by itself, as its product with factor may be subnormal
   void* out;                     // kNsLast
   int64_t ldo, zo;
   int out_type;                  // NsOut

@@ -272,7 +272,8 @@ __global__ void __launch_bounds__(kThreads, 1) ns_product_kernel(const __grid_co
 #pragma unroll
       for (int q = 0; q < 8; ++q)
         *reinterpret_cast<float4*>(my + lane * 128 + ((q ^ (lane & 7)) << 4)) =
-            make_float4(v[4 * q] * a.factor, v[4 * q + 1] * a.factor, v[4 * q + 2] * a.factor, v[4 * q + 3] * a.factor);
+            make_float4(v[4 * q] * a.factor * a.scale, v[4 * q + 1] * a.factor * a.scale, v[4 * q + 2] * a.factor * a.scale,
+                        v[4 * q + 3] * a.factor * a.scale);
       __syncwarp();
       // rows of 32 columns, coalesced whatever the caller's alignment, 16 at a time without a branch between them
       const int col = n + lane, rows = col < a.N && before == 0 ? (a.M - m0 < 32 ? a.M - m0 : 32) : 0;

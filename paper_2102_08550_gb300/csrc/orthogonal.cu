@@ -295,7 +295,8 @@ cudaError_t steps_from(const Shape& p, uint8_t* ws, const T* G, int64_t ldg, int
     before.d_halves = 1;
     last.a_halves = last.b_halves = 1;
   }
-  last.factor = whole * (to.scale / (kNsScaleA * kNsScaleX));
+  last.factor = whole / (kNsScaleA * kNsScaleX);
+  last.scale = to.scale;
   last.out = to.D;
   last.ldo = to.ldd;
   last.zo = to.zd;

@@ -49,3 +49,18 @@ def test_updates_of_huge_numbers(cuda_device, rows, cols, dtype, size):
     G = (G / G.abs().max() * size * 8).to(dtype)
     assert torch.isfinite(G).all()
     check(orth(G[None])[0], G, 5)
+
+
+@pytest.mark.parametrize("scale", [0.0, 1.0, -3.0, 1e38, 1e-30, 2.0 ** -110, 1e-35, -1e-36, 2.0 ** -130])
+@pytest.mark.parametrize("rows,cols", SIZES)
+def test_every_scale(cuda_device, rows, cols, scale):
+    """The result with a scale is that of one times it: four roundings of 2^-24, or 2^-150 each where it is subnormal."""
+    G = update(rows, cols, 6, cuda_device)
+    one, got = orth(G[None])[0].double(), orth(G[None], scale=scale)[0].double()
+    want = one * torch.tensor(scale, dtype=torch.float32).double()
+    assert torch.isfinite(got).all() and ((got - want).abs() <= 4 * (2.0 ** -24 * want.abs() + 2.0 ** -150)).all()
+    H = G.bfloat16()
+    one, got = orth(H[None])[0].double(), orth(H[None], scale=scale)[0].double()
+    want = one * torch.tensor(scale, dtype=torch.float32).double()
+    # both rounded to bf16, whose 8 bits are off by up to 2^-8 of a value (half a step of 2^-7 in [1, 2)), or 2^-134
+    assert ((got - want).abs() <= 2.02 * 2.0 ** -8 * want.abs() + 2.0 ** -133).all()
