@@ -511,15 +511,15 @@ oscars_status oscars_softreg_steps_noalloc(const float* params_in, float* params
  * Others have to keep them below 2 in every step, or the result may overflow.
  * eps > 0: a matrix of zeros gives zeros.  A matrix that holds an infinity or
  * NaN gives NaN throughout.  The norm neither overflows nor underflows.
- * Accuracy: fp32 results keep X (whose norm is 1 at first) in 22 bits or to 2^-48
- * and the factors in 22 bits or to 2^-44, whichever is coarser, and add in
- * fp32: about as near to the definition as products in fp32 come.  Rows 2^-20
- * of the update's norm come up in later steps like others; what is 2^-40 of it
- * may be lost.
- * Where the shorter side is at most 64, matrices may take fp32 throughout.
- * bf16 results round the factors to 11 bits, which moves a step's result by at
- * most about (|a| + b^2 / 2|c|) 2^-11 of X (after five steps with the default
- * coefficients by about 1e-3), and keep X to 2^-37 and the factors to 2^-33.
+ * Accuracy: fp32 results keep X (whose norm is 1 at first, or less where eps
+ * counts) in 22 bits or to 2^-48, whichever is coarser, and the factors in 22
+ * bits or to 2^-44, and add in fp32: about as near to the definition as products
+ * in fp32 come.  Rows 2^-20 of the update's norm come up in later steps like
+ * others; what is 2^-40 of it may be lost.  Where the shorter side is at most
+ * 64, matrices may take fp32 throughout.  bf16 results round the factors to 11
+ * bits, which moves a step's result by at most about (|a| + b^2 / 2|c|) 2^-11 of
+ * X (after five steps with the default coefficients by about 1e-3), and keep X
+ * to 2^-37 and the factors to 2^-33.
  * The arithmetic of a call is fixed: equal calls give equal bits (a matrix alone
  * and in a batch may differ in the last ones).
  * workspace: device, 256-byte aligned, at least the bytes that

@@ -188,10 +188,12 @@ __device__ __forceinline__ void umma_commit_pair(uint64_t* bar) {
       "h"(static_cast<uint16_t>(0x3))
       : "memory");
 }
-// An arrival on a barrier of the pair's leader.  What it is ordered behind lies in this SM: operands in its own shared
-// memory, which its own tensor core reads and a fence.proxy.async has shown to it, or reads of its tensor memory, which
-// tcgen05.wait::ld has waited for; so release at CTA scope (the default) is enough.  At cluster scope an arrival took
-// 1000 clocks (8192 x 4096 x 4096: a K-block 1200 clocks).
+// An arrival on a barrier of the pair's leader, released at CTA scope (the default).  By PTX's memory model that does not
+// synchronise with the leader, a thread of another CTA; this relies on the hardware instead: all that the arrival has to come
+// after has happened in this SM before it is issued.  That is operands in its own shared memory, which its own tensor core
+// reads and a fence.proxy.async of each writing lane has shown to it (the lanes then meet in __syncwarp), or reads of its tensor
+// memory, which tcgen05.wait::ld has seen finished.  At cluster scope an arrival took 1000 clocks (8192 x 4096 x 4096: a K-block
+// 1200 clocks).
 __device__ __forceinline__ void mbar_arrive_at(uint32_t cluster_bar) {
   asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }

@@ -114,8 +114,10 @@ __device__ __forceinline__ void umma_commit_pair(uint64_t* bar) {
       "h"(static_cast<uint16_t>(0x3))
       : "memory");
 }
-// An arrival on a barrier of the pair's leader: the accumulator has been read (tcgen05.wait::ld), and no write has to be
-// visible, so release at CTA scope (the default) is enough; at cluster scope an arrival takes 1000 clocks.
+// An arrival on a barrier of the pair's leader, released at CTA scope (the default).  By PTX's memory model that does not
+// synchronise with the leader, a thread of another CTA; this relies on the hardware instead: all that the arrival has to come
+// after is reads of this SM's own tensor memory, which tcgen05.wait::ld has seen finished before the arrival is issued, and
+// no write has to be visible.  At cluster scope an arrival takes 1000 clocks.
 __device__ __forceinline__ void mbar_arrive_at(uint32_t cluster_bar) {
   asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }

@@ -270,6 +270,8 @@ __global__ void __launch_bounds__(kThreads) orth_small_kernel(const __grid_const
 // fitted to measurements (s x len x batch, fp32: this kernel / the tensor cores: 10 x 512 x 1 21 / 66, 32 x 1000 x 1 34 / 76,
 // 32 x 1000 x 16 67 / 90, 48 x 800 x 1 55 / 78, 64 x 784 x 1 74 / 78, 64 x 784 x 16 146 / 90; bf16: 24 x 1000 x 64 140 / 98).
 // A CTA takes 15 us for its barriers and the load, more for longer sides of A and for its share; one CTA runs on an SM.
+// The fit is of up to 64 matrices and five steps: the tensor cores' estimate has no waves of its own, so a batch of some hundreds
+// goes there sooner than it should (10 x 512 fp32 from 433 matrices on), and other numbers of steps choose as five do.
 int ns_small_cluster(int batch, int rows, int cols, bool f32) {
   const int s = rows < cols ? rows : cols, len = rows < cols ? cols : rows;
   if (s > kMaxS) return 0;
