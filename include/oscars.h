@@ -517,9 +517,10 @@ oscars_status oscars_softreg_steps_noalloc(const float* params_in, float* params
  * in fp32 come.  Rows 2^-20 of the update's norm come up in later steps like
  * others; what is 2^-40 of it may be lost.  Where the shorter side is at most
  * 64, matrices may take fp32 throughout.  bf16 results round the factors to 11
- * bits, which moves a step's result by at most about (|a| + b^2 / 2|c|) 2^-11 of
- * X (after five steps with the default coefficients by about 1e-3), and keep X
- * to 2^-37 and the factors to 2^-33.
+ * bits in up to five steps, or the last three of more, each of which moves them
+ * by at most about (|a| + b^2 / 2|c|) 2^-11 of X (five with the default
+ * coefficients by about 1e-3 in all), and keep X to 2^-37 and the factors to
+ * 2^-33 there.
  * The arithmetic of a call is fixed: equal calls give equal bits (a matrix alone
  * and in a batch may differ in the last ones).
  * workspace: device, 256-byte aligned, at least the bytes that

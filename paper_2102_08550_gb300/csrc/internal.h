@@ -220,8 +220,8 @@ cudaError_t launch_gemm_rows(int epi, const RowsPlan& p, const CUtensorMap& mA, 
                              const CUtensorMap& mD, RowsArgs a, cudaStream_t s);
 
 // The products of a Newton-Schulz step (csrc/orth_product.cu).  Operands are fp16,
-// [half][batch][rows][ld]: one half, or two whose sum is the value (of an fp32
-// result's operands, the first plus 2^-kNsShift times the second).
+// [half][batch][rows][ld]: one half, or two whose sum is the value (where both operands
+// of a product have two, the first plus 2^-kNsShift times the second).
 enum NsEpi {
   kNsSym,      // D = factor A B + diag I, symmetric
   kNsStep,     // D = the next X, two halves
@@ -242,6 +242,9 @@ struct NsArgs {
   int a_halves, b_halves;        // of the operands
   int a_mn, b_mn;                // read MN-major (the transposed tensor)
   int d_halves;                  // of D
+  float d_second;                // kNsStep: D's second half is stored times this, 2^kNsShift or 1
+  float* cut;                    // [batch][M], or NULL: 2 x what the rounding to one half took off D's diagonal x the diagonal
+  const float* add;              // such a vector of the operands', or NULL: times factor it belongs on D's diagonal
   float factor, diag;            // factor includes the operands' and D's scales, diag D's
   float scale;                   // kNsLast: the caller's, by itself, as its product with factor may be subnormal
   void* out;                     // kNsLast

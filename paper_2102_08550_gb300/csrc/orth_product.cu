@@ -17,10 +17,17 @@
 // fp32's last bit), into one fp32 accumulator.  fp32 results take two halves of
 // everything, the second stored 2^11 times larger (internal.h): the accumulator takes the
 // two mixed products of a K-block first, and the first instruction of high x high scales
-// what is there by 2^-11 (scale-input-d), which costs nothing.  bf16 results take two halves of X and one of A and B: what X's
-// rounding leaves in the directions in which the update is near zero is
-// multiplied by a at every step (485 over five), while the roundings of A and B
-// multiply X and stay relative to it (the last step's X takes one half as well).
+// what is there by 2^-11 (scale-input-d), which costs nothing.  bf16 results take
+// two halves of X and one of A and B: what X's rounding leaves in the directions in which
+// the update is near zero is multiplied by a at every step (485 over five), while the
+// roundings of A and B multiply X and stay relative to it (in the Gram product and the last
+// step X takes one half as well).  The largest of them is that of A's diagonal, about beta, which
+// all of a row is multiplied by: the Gram product keeps it (cut), and the next adds what it
+// is worth to B's diagonal (error beside the result's own rounding, which is 1.66e-3,
+// after five steps: 512 x 784 1.05 -> 0.81e-3, 100 x 2000 1.75 -> 1.18e-3).  Later steps multiply
+// what earlier ones lost, so of more than five steps all but the last three take two halves of A
+// and B too (error of 400 x 4096 after eight, in roundings of the result: 1.92 in one half throughout, 1.81 with two in
+// all but the last five, 1.14 in all but three, 1.07 in all; 4096 x 4096 2.01 ms, 2.59, 2.98, 3.81).
 // fp16 rather than bf16: three more bits at the same rate, and the values are bounded
 // (singular values below 2).
 //
@@ -129,6 +136,10 @@ __device__ __forceinline__ void st_dsmem_at(uint32_t remote, float4 v) {
 __device__ __forceinline__ void st_dsmem_at(uint32_t remote, uint32_t v) {
   asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(remote), "r"(v) : "memory");
 }
+// to = v where a == b, as a select: an array element chosen by lane would go through local memory (16 x 512 x 784 bf16 210 us)
+__device__ __forceinline__ void take_if(float& to, float v, int a, int b) {
+  asm("{\n\t.reg .pred p;\n\tsetp.eq.s32 p, %2, %3;\n\tselp.f32 %0, %1, %0, p;\n\t}" : "+f"(to) : "f"(v), "r"(a), "r"(b));
+}
 // fp16 operands (format 0), fp32 accumulator; bits 15 and 16: A, B MN-major
 __host__ __device__ constexpr uint32_t idesc_f16(int M, int N, int a_mn, int b_mn) {
   return (1u << 4) | (static_cast<uint32_t>(a_mn) << 15) | (static_cast<uint32_t>(b_mn) << 16) |
@@ -165,7 +176,6 @@ __global__ void __launch_bounds__(kThreads, 1) ns_product_kernel(const __grid_co
                                                                  const __grid_constant__ CUtensorMap mapD,
                                                                  const __grid_constant__ NsArgs a) {
   constexpr bool kSym = EPI == kNsSym;
-  constexpr float kSecond = kSums ? static_cast<float>(1 << kNsShift) : 1.f;   // an fp32 result's second halves
   extern __shared__ uint8_t ns_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(ns_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* stg = smem;
@@ -223,22 +233,30 @@ __global__ void __launch_bounds__(kThreads, 1) ns_product_kernel(const __grid_co
   // ---- what the epilogue's warps do with 32 columns of their 32 rows (m0) of matrix z, from column n on
   uint8_t* my = stg + (warp >= 4 ? warp - 4 : 0) * 2 * kStg;
   int nst = 0;
+  float extra = 0.f;   // of this lane's row, on D's diagonal; read before the tile's products are there
   auto finish = [&](int z, int m0, int n, bool mirrored, const float (&v)[32]) {
     if constexpr (EPI != kNsLast) {
       uint32_t hi[16], lo[16];
       const int d = m0 + lane - n;   // the column on the diagonal
+      constexpr bool kCut = kSym && !kSums;
+      const float on = kCut ? a.diag + extra : a.diag;
+      const float larger = kSym ? static_cast<float>(1 << kNsShift) : a.d_second;   // (two halves of A and B always meet two)
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        float x = v[2 * e] * a.factor, y = v[2 * e + 1] * a.factor;
-        if (kSym) {
-          x += d == 2 * e ? a.diag : 0.f;
-          y += d == 2 * e + 1 ? a.diag : 0.f;
-        }
+        const float x = fmaf(v[2 * e], a.factor, kSym && d == 2 * e ? on : 0.f);
+        const float y = fmaf(v[2 * e + 1], a.factor, kSym && d == 2 * e + 1 ? on : 0.f);
         const __half2 h = __floats2half2_rn(x, y);
         const float2 f = __half22float2(h);
-        const __half2 l = __floats2half2_rn((x - f.x) * kSecond, (y - f.y) * kSecond);
+        const __half2 l = __floats2half2_rn((x - f.x) * larger, (y - f.y) * larger);
         hi[e] = *reinterpret_cast<const uint32_t*>(&h);
         lo[e] = *reinterpret_cast<const uint32_t*>(&l);
+      }
+      if (kCut && m0 == n && a.cut) {   // a box on the diagonal, whose elements are each lane's own
+        float mine = 0.f;
+#pragma unroll
+        for (int e = 0; e < 32; ++e) take_if(mine, v[e], lane, e);
+        const float x = fmaf(mine, a.factor, on), kept = __half2float(__float2half_rn(x));
+        if (m0 + lane < a.M) a.cut[z * static_cast<int64_t>(a.M) + m0 + lane] = 2.f * kept * (x - kept);
       }
       // one box of 32 x 32: rows as they are, or (kSym) the mirror image
       auto store = [&](const uint32_t (&w)[16], int half, bool mirror) {
@@ -450,6 +468,8 @@ __global__ void __launch_bounds__(kThreads, 1) ns_product_kernel(const __grid_co
       const Tile tl = tile_of<CL, kSym, kSplit>(a, u);
       const int m0 = (tl.i * CL + rank) * 128 + 32 * quarter, n0 = tl.j * a.BN + cb;
       const uint32_t row0 = tmem + (static_cast<uint32_t>(32 * quarter) << 16) + cb;
+      if (kSym && !kSums && a.add)
+        extra = tl.i == tl.j && m0 + lane < a.M ? a.factor * a.add[tl.z * static_cast<int64_t>(a.M) + m0 + lane] : 0.f;
       if constexpr (kSums) {
         float sum[kMaxBN / 64][32];
 #pragma unroll

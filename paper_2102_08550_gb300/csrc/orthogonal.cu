@@ -29,15 +29,15 @@ constexpr int kPasses = 256;        // threads of the streaming passes
 constexpr int kMaxParts = 608;      // partial sums of squares of one matrix
 constexpr int kAhead = 4;           // groups of eight elements that a thread of a pass requests together
 constexpr int kMaxDim = 65536, kMaxBatch = 65535, kMaxSteps = 64;
+constexpr int kFewSteps = 5, kCoarse = 3;   // a bf16 result's steps that take one half of A and B (orth_product.cu)
 constexpr float kMaxCoeff = 8.f;
 
 struct Shape {
   int batch, rows, cols, s;         // s: the shorter side
   int small;                        // CTAs a matrix of the one launch, or 0: products on the tensor cores
-  int halves;                       // fp16 halves of A and B (X has two)
   int64_t ldx, lds;                 // rows of X and of A, B in the workspace, in elements
   int parts;                        // partial sums a matrix
-  int64_t off_status, off_part, off_u, off_x[2], off_a, off_b, bytes;
+  int64_t off_status, off_part, off_u, off_cut, off_x[2], off_a, off_b, bytes;
 };
 
 int64_t up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
@@ -49,7 +49,6 @@ Shape make_shape(int batch, int rows, int cols, int dtype, bool with_u) {
   p.cols = cols;
   p.s = rows < cols ? rows : cols;
   p.small = ns_small_cluster(batch, rows, cols, dtype == OSCARS_F32);
-  p.halves = dtype == OSCARS_F32 ? 2 : 1;
   // rows on 128-byte lines: a box's row of 128 bytes is one line then, not two (server step on 1537 x 385: 156 -> 146 us)
   p.ldx = up(cols, 64);
   p.lds = up(p.s, 64);
@@ -66,9 +65,11 @@ Shape make_shape(int batch, int rows, int cols, int dtype, bool with_u) {
   if (!p.small || with_u) p.off_part = take(static_cast<int64_t>(batch) * p.parts * sizeof(Squares));
   p.off_u = with_u ? take(elems * 4) : 0;
   if (!p.small) {   // one launch keeps a matrix in shared memory
+    // X, A and B in two fp16 halves each
     for (int i = 0; i < 2; ++i) p.off_x[i] = take(static_cast<int64_t>(batch) * rows * p.ldx * 4);
-    p.off_a = take(static_cast<int64_t>(batch) * p.s * p.lds * 2 * p.halves);
-    p.off_b = take(static_cast<int64_t>(batch) * p.s * p.lds * 2 * p.halves);
+    if (dtype != OSCARS_F32) p.off_cut = take(static_cast<int64_t>(batch) * p.s * sizeof(float));
+    p.off_a = take(static_cast<int64_t>(batch) * p.s * p.lds * 4);
+    p.off_b = take(static_cast<int64_t>(batch) * p.s * p.lds * 4);
   }
   p.bytes = at;
   return p;
@@ -253,29 +254,29 @@ cudaError_t steps_from(const Shape& p, uint8_t* ws, const T* G, int64_t ldg, int
   NsMaps mX[2], mA, mB;
   for (int i = 0; i < 2; ++i)
     if (!half_maps(&mX[i], X[i], p.ldx, p.cols, p.rows, p.batch, 2)) return cudaErrorInvalidValue;
-  if (!half_maps(&mA, A, p.lds, p.s, p.s, p.batch, p.halves) || !half_maps(&mB, B, p.lds, p.s, p.s, p.batch, p.halves))
+  if (!half_maps(&mA, A, p.lds, p.s, p.s, p.batch, 2) || !half_maps(&mB, B, p.lds, p.s, p.s, p.batch, 2))
     return cudaErrorInvalidValue;
   const int vec = (reinterpret_cast<uintptr_t>(G) | (ldg * sizeof(T)) | (bsg * sizeof(T))) % 16 == 0;
+  constexpr bool kF32 = sizeof(T) == 4;
+  auto halves = [&](int k) { return kF32 || (steps > kFewSteps && steps - k > kCoarse) ? 2 : 1; };   // of A and B in step k
+  auto second = [&](int k) { return halves(k) == 2 ? static_cast<float>(1 << kNsShift) : 1.f; };
   cudaError_t e = launch_dependent(orth_scale_kernel<T>, dim3(pass_blocks((p.rows * (p.ldx / 8) + kAhead - 1) / kAhead, 608), p.batch), kPasses, 0, s,
                                    G, ldg, bsg, p.rows, p.cols, vec, reinterpret_cast<const Squares*>(ws + p.off_part), p.parts,
-                                   eps, p.halves == 2 ? static_cast<float>(1 << kNsShift) : 1.f, X[0], p.ldx);
+                                   eps, second(0), X[0], p.ldx);
   const bool tall = p.rows > p.cols;
   const bool cubic = co[2] == 0.f;
-  const float whole = p.halves == 2 ? kNsWhole : 1.f;   // what the accumulator cuts off (orth_product.cu)
-  const float sums = whole * (kNsScaleA / (kNsScaleX * kNsScaleX));
   NsArgs g{};   // A + beta I, or B itself where c = 0
   g.status = reinterpret_cast<int*>(ws + p.off_status);
   g.batch = p.batch;
   g.M = g.N = p.s;
   g.K = tall ? p.rows : p.cols;
-  g.a_halves = g.b_halves = g.d_halves = p.halves;
+  g.a_halves = g.b_halves = kF32 ? 2 : 1;
   g.a_mn = g.b_mn = tall;
-  g.factor = cubic ? co[1] * sums : sums;
+  g.factor = (kF32 ? kNsWhole : 1.f) * (kNsScaleA / (kNsScaleX * kNsScaleX)) * (cubic ? co[1] : 1.f);
   g.diag = (cubic ? co[0] : static_cast<float>(0.5 * co[1] / co[2])) * kNsScaleA;
   NsArgs q = g;   // B = c (A + beta I)^2 + gamma I
   q.K = p.s;
   q.a_mn = q.b_mn = 0;
-  q.factor = whole * (co[2] / kNsScaleA);
   q.diag = static_cast<float>(co[0] - 0.25 * co[1] * co[1] / co[2]) * kNsScaleA;
   NsArgs u{};   // X <- B X or X B
   u.status = g.status;
@@ -283,31 +284,32 @@ cudaError_t steps_from(const Shape& p, uint8_t* ws, const T* G, int64_t ldg, int
   u.M = p.rows;
   u.N = p.cols;
   u.K = p.s;
-  u.a_halves = tall ? 2 : p.halves;
-  u.b_halves = tall ? p.halves : 2;
   u.b_mn = !tall;
-  u.d_halves = 2;
-  u.factor = whole / kNsScaleA;
-  // The step before a bf16 result's last one leaves X in one half, and the last step takes that: its rounding is multiplied
-  // by a once (3.4 x 2^-12), where an earlier one would be by a to the number of steps left.
-  NsArgs before = u, last = u;
-  if (p.halves == 1) {
-    before.d_halves = 1;
-    last.a_halves = last.b_halves = 1;
-  }
-  last.factor = whole / (kNsScaleA * kNsScaleX);
-  last.scale = to.scale;
-  last.out = to.D;
-  last.ldo = to.ldd;
-  last.zo = to.zd;
-  last.out_type = to.type;
+  u.scale = to.scale;
+  u.out = to.D;
+  u.ldo = to.ldd;
+  u.zo = to.zd;
+  u.out_type = to.type;
   for (int k = 0; k < steps && e == cudaSuccess; ++k) {
     const NsMaps& x = mX[k & 1];
     const bool end = k + 1 == steps;
+    const int h = halves(k);
+    const float whole = h == 2 ? kNsWhole : 1.f;   // what the accumulator cuts off (orth_product.cu)
+    g.d_halves = q.d_halves = q.a_halves = q.b_halves = h;
+    g.cut = h == 1 && !cubic ? reinterpret_cast<float*>(ws + p.off_cut) : nullptr;
+    q.add = g.cut;
+    q.factor = whole * (co[2] / kNsScaleA);
+    // The step before a bf16 result's last one leaves X in one half, and the last step takes that: its rounding is multiplied
+    // by a once (3.4 x 2^-12), where an earlier one would be by a to the number of steps left.
+    const int xh = end && !kF32 ? 1 : 2;
+    u.a_halves = tall ? xh : h;
+    u.b_halves = tall ? h : xh;
+    u.d_halves = k + 2 == steps && !kF32 ? 1 : 2;
+    u.d_second = second(k + 1);
+    u.factor = whole / kNsScaleA * (end ? 1.f / kNsScaleX : 1.f);
     e = launch_ns_product(kNsSym, x, x, cubic ? mB : mA, g, s);
     if (e == cudaSuccess && !cubic) e = launch_ns_product(kNsSym, mA, mA, mB, q, s);
-    if (e == cudaSuccess)
-      e = launch_ns_product(end ? kNsLast : kNsStep, tall ? x : mB, tall ? mB : x, mX[(k + 1) & 1], end ? last : k + 2 == steps ? before : u, s);
+    if (e == cudaSuccess) e = launch_ns_product(end ? kNsLast : kNsStep, tall ? x : mB, tall ? mB : x, mX[(k + 1) & 1], u, s);
   }
   return e;
 }

@@ -17,9 +17,10 @@ def test_a_server_step_on_one_wants_its_update(oscars_lib):
 
 
 def test_others_want_two_x_and_both_factors(oscars_lib):
-    for dtype, halves in ((P.F32, 2), (P.BF16, 1)):
+    """In two halves of 16 bits each, rows on 128-byte lines; a bf16 result the rounding of A's diagonal too."""
+    for dtype, more in ((P.F32, 0), (P.BF16, 3 * 512 * 4)):
         n = P.oscars_orthogonalize_workspace(3, 512, 784, dtype)
-        want = 3 * (2 * 512 * 832 * 4 + 2 * 512 * 512 * 2 * halves)   # rows on 128-byte lines
+        want = 3 * (2 * 512 * 832 * 4 + 2 * 512 * 512 * 4) + more
         assert want < n <= want + 3 * 608 * 12 + 2048
 
 
