@@ -81,6 +81,12 @@ typedef enum {
   OSCARS_BF16 = 1
 } oscars_dtype;
 
+/* How 4-bit codes are scaled (oscars_quantize_fp4). */
+typedef enum {
+  OSCARS_MXFP4 = 0, /* blocks of 32 values, a power of two each                       */
+  OSCARS_NVFP4 = 1  /* blocks of 16 values, an 8-bit scale each, and fp32 row scales  */
+} oscars_fp4_format;
+
 typedef enum {
   OSCARS_W_UNIFORM = 0,    /* w_k = 1/N: the average of Eq. 4 (first branch)        */
   OSCARS_W_LOCALSTEPS = 1, /* w_k = tau_k / sum_j tau_j: NOT in the paper            */
@@ -604,6 +610,118 @@ oscars_status oscars_quantize_i8(const void* x, int64_t ldx, int32_t dtype, int3
 oscars_status oscars_gemm_i8_nt(const int8_t* A, int64_t lda, const float* scale_a, const int8_t* B, int64_t ldb,
                                 const float* scale_b, const float* bias, int32_t relu, void* C, int64_t ldc,
                                 int32_t dtype, int32_t M, int32_t N, int32_t K, void* stream);
+
+/*
+ * Rows in 4 bits.  A value is a code c (e2m1: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their
+ * negatives, the sign in bit 3) times its block's scale, times its row's if there
+ * are row scales.  A row's blocks start at column 0; the last may be cut short by the
+ * row's end.
+ *   Codes: column j of row i in byte i ldq + j / 2, in its low half for even j; 16-byte
+ * aligned, ldq a multiple of 16 and at least ceil(cols / 32) 16.
+ *   Block scales: one byte each, OSCARS_MXFP4 2^(byte - 127), 255 a NaN;
+ * OSCARS_NVFP4 an e4m3 number without a sign (bit 7 is 0), 127 a NaN.  They lie in tiles
+ * of 128 rows x 4 blocks (512 bytes), as the tensor cores take them: block j of row i,
+ * of rows with n blocks, at
+ *   ((i / 128) ceil(n / 4) + j / 4) 512 + (i % 32) 16 + (i % 128) / 32 4 + j % 4,
+ * 16-byte aligned; oscars_fp4_scale_bytes gives the size, whole tiles.
+ *   Row scales: fp32, one a row.
+ *
+ * oscars_quantize_fp4 - rows of x in 4 bits.  With |block| the largest magnitude of a
+ * block and |row| of a row, each operation rounded to fp32:
+ *   OSCARS_MXFP4: e = max(floor(log2 |block|) - 2, -127), byte e + 127, 0 for zeros;
+ *     c = x / 2^e to the nearest code, ties to even codes, magnitudes over 6 to 6.
+ *     A block with an infinity or NaN has byte 255 and codes 0.  row_scale is NULL.
+ *   OSCARS_NVFP4: t = max(|row| / 2688, 2^-110), 0 for zeros; b = |block| times
+ *     1 / (6 t), at most 448, to the nearest e4m3 (ties to even); c = x times
+ *     1 / (b t) to the nearest code as above, 0 where b is.  row_scale[i] = t.  A
+ *     row with an infinity or NaN has that (NaN first) for t, and bytes and codes 0.
+ * x: device, element (i, j) at x[i ldx + j], of `dtype`, any alignment.  Codes are
+ * written, and behind a row's end zeros, up to a multiple of 32 columns, bytes behind
+ * that stay; scales up to a multiple of 4 blocks (0 behind the last); rows of the last
+ * tile behind the last row stay as they were.  rows = 0 does nothing.
+ * oscars_dequantize_fp4 - the values again: x[i ldx + j] = c scale, exact or one
+ * rounding to fp32, times row_scale[i] (if not NULL, either format; another
+ * rounding), rounded to `dtype`.
+ * Both allocate nothing and can be captured.  Ordered on `stream`.
+ * Errors: EINVAL (NULL or misaligned pointers, unknown format or dtype, rows outside
+ * [0, 2^30], cols outside [1, 2^30], ldx < cols, ldq, row_scale NULL with
+ * OSCARS_NVFP4 in oscars_quantize_fp4 or not NULL with OSCARS_MXFP4), ECUDA.
+ */
+oscars_status oscars_fp4_scale_bytes(int32_t rows, int32_t cols, int32_t format, int64_t* bytes);
+oscars_status oscars_quantize_fp4(const void* x, int64_t ldx, int32_t dtype, int32_t rows, int32_t cols, int32_t format, uint8_t* q,
+                                  int64_t ldq, uint8_t* scales, float* row_scale, void* stream);
+oscars_status oscars_dequantize_fp4(const uint8_t* q, int64_t ldq, const uint8_t* scales, const float* row_scale, int32_t format,
+                                    int32_t rows, int32_t cols, void* x, int64_t ldx, int32_t dtype, void* stream);
+
+/*
+ * oscars_gemm_fp4_nt - the product of a dense layer kept in 4 bits,
+ *   C[m][n] = act(row_a[m] row_b[n] sum_k A[m][k] B[n][k] + bias[n]),
+ * A (tokens, M rows of K) and B (output channels, N rows) as oscars_quantize_fp4
+ * writes them, both of `format`: the codes behind column K up to a multiple of 32
+ * and the scales behind the last block up to a multiple of 4 have to be zeros.  row_a
+ * and row_b: device fp32, or NULL for ones (either format).  Products are exact; their
+ * sum is kept in fp32 (a block's sum is exact; where block scales' products leave
+ * fp32's normal numbers, so does the sum).  bias: device, N fp32, or NULL.  relu != 0:
+ * act = max(0, .) (NaN stays).  C: device, element (m, n) at C[m ldc + n], of `dtype`,
+ * any alignment; row scales, bias and act are fp32, rounded once to `dtype`.  M = 0 does
+ * nothing.  Equal calls give equal bits.  Allocates nothing and can be captured
+ * (after a first call on the device, which loads the kernels).  Ordered on `stream`.
+ * A wait inside the kernel that runs out (none is known to) is not reported, as in
+ * oscars_gemm_i8_nt; it leaves elements of C as they were.
+ * Errors: EINVAL (NULL or misaligned pointers, unknown format or dtype, M outside
+ * [0, 2^30], N or K outside [1, 2^30], strides out of range), ECUDA.
+ */
+oscars_status oscars_gemm_fp4_nt(const uint8_t* A, int64_t lda, const uint8_t* scales_a, const float* row_a, const uint8_t* B,
+                                 int64_t ldb, const uint8_t* scales_b, const float* row_b, int32_t format, const float* bias,
+                                 int32_t relu, void* C, int64_t ldc, int32_t dtype, int32_t M, int32_t N, int32_t K, void* stream);
+
+/*
+ * oscars_layer_norm - the norm in front of a dense layer, of `groups` groups of
+ * `rows` rows each (the mini-batches of W workers in one launch, or one group):
+ *   mean = sum_j x[j] / cols;  rstd = 1 / sqrt(sum_j (x[j] - mean)^2 / cols + eps);
+ *   y[j] = (x[j] - mean) rstd gamma[j] + beta[j].
+ * x, y: device, element (i, j) at x[i ldx + j], of `dtype`, i counting the rows of
+ * all groups; any alignment (16-byte aligned rows take the vector path).  y may be x
+ * itself with ldy = ldx, else they must not overlap.  gamma, beta: device fp32, group
+ * g's at gamma[g param_stride + j] (a stride of 0: all groups read one); NULL for
+ * ones and for zeros.  mean, rstd: device fp32, one a row of all groups, or NULL:
+ * what the backward pass wants.  Sums are kept in fp32, the squares' over its whole
+ * range; values up to 2^126 in magnitude.  A row with an infinity or NaN gives NaN.
+ * eps > 0.  Allocates nothing and can be captured.  Ordered on `stream`.
+ * rows = 0 or groups = 0 does nothing.
+ * Errors: EINVAL (NULL or misaligned pointers, unknown dtype, groups outside [0,
+ * 65535], rows or groups x rows outside [0, 2^30], cols outside [1, 2^30], ldx or
+ * ldy < cols, a negative param_stride, eps not a positive finite number), ECUDA.
+ */
+oscars_status oscars_layer_norm(const void* x, int64_t ldx, const float* gamma, const float* beta, int64_t param_stride, void* y,
+                                int64_t ldy, float* mean, float* rstd, int32_t dtype, int32_t groups, int32_t rows, int32_t cols,
+                                float eps, void* stream);
+
+/*
+ * oscars_layer_norm_backward - its backward pass.  With xh = (x - mean) rstd and
+ * h = dy gamma, of a row:
+ *   dx[j] = rstd (h[j] - sum h / cols - xh[j] sum(h xh) / cols),
+ * and of each group: dgamma[j] = sum over its rows of dy xh, dbeta[j] = that of dy.
+ * dy, x, dx: as x in oscars_layer_norm; dx may be dy or x itself with the same
+ * stride, else it must not overlap them.  mean, rstd: as the forward pass left them.
+ * gamma: as there, or NULL for ones.  dgamma, dbeta: device fp32, group g's at
+ * dgamma[g dparam_stride + j], overwritten (rows = 0: zeros).  dx, dgamma and dbeta
+ * may each be NULL: not wanted.  All sums are in fp32 and in a fixed order: equal calls
+ * give equal bits.  (Where xh leaves a row no freedom, as with two columns, dx is
+ * what fp32 leaves of terms that cancel.)
+ * workspace: device, 16-byte aligned, at least the bytes that
+ * oscars_layer_norm_backward_workspace gives for the same sizes (it may be 0, then
+ * NULL will do); nothing in it is kept from call to call, and calls (or captured
+ * graphs) that may run at the same time need one each.  Allocates nothing and can be
+ * captured.  Ordered on `stream`.  groups = 0 does nothing.
+ * Errors: EINVAL (those of oscars_layer_norm, a dparam_stride < cols with
+ * groups > 1, a workspace that is too small), ECUDA.
+ */
+oscars_status oscars_layer_norm_backward_workspace(int32_t groups, int32_t rows, int32_t cols, int64_t* bytes);
+oscars_status oscars_layer_norm_backward(const void* dy, int64_t lddy, const void* x, int64_t ldx, const float* gamma,
+                                         int64_t param_stride, const float* mean, const float* rstd, void* dx, int64_t lddx,
+                                         float* dgamma, float* dbeta, int64_t dparam_stride, int32_t dtype, int32_t groups,
+                                         int32_t rows, int32_t cols, void* workspace, int64_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

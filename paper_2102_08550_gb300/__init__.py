@@ -18,6 +18,7 @@ LIB_PATH = os.path.join(HERE, "_lib", "liboscars.so")
 OSCARS_OK, OSCARS_EINVAL, OSCARS_ENOMEM, OSCARS_ECUDA, OSCARS_ESTATE, OSCARS_ETIMEOUT, OSCARS_ENOTSUP = range(7)
 MODEL_FLAT, MODEL_MLP, MODEL_CNN = 0, 1, 2
 F32, BF16 = 0, 1
+MXFP4, NVFP4 = 0, 1
 W_UNIFORM, W_LOCALSTEPS, W_EXPLICIT = 0, 1, 2
 SEARCH_CAPPED, SEARCH_LITERAL = 0, 1
 POLICY_OSCARS, POLICY_BSP, POLICY_LOCAL_SGD = 0, 1, 2
@@ -99,6 +100,19 @@ _SIGS = {
                                      c_void_p]),
     "oscars_gemm_i8_nt": (c_int32, [c_void_p, c_int64, c_void_p, c_void_p, c_int64, c_void_p, c_void_p, c_int32, c_void_p,
                                     c_int64, c_int32, c_int32, c_int32, c_int32, c_void_p]),
+    "oscars_fp4_scale_bytes": (c_int32, [c_int32, c_int32, c_int32, POINTER(c_int64)]),
+    "oscars_quantize_fp4": (c_int32, [c_void_p, c_int64, c_int32, c_int32, c_int32, c_int32, c_void_p, c_int64, c_void_p,
+                                      c_void_p, c_void_p]),
+    "oscars_dequantize_fp4": (c_int32, [c_void_p, c_int64, c_void_p, c_void_p, c_int32, c_int32, c_int32, c_void_p, c_int64,
+                                        c_int32, c_void_p]),
+    "oscars_gemm_fp4_nt": (c_int32, [c_void_p, c_int64, c_void_p, c_void_p, c_void_p, c_int64, c_void_p, c_void_p, c_int32,
+                                     c_void_p, c_int32, c_void_p, c_int64, c_int32, c_int32, c_int32, c_int32, c_void_p]),
+    "oscars_layer_norm": (c_int32, [c_void_p, c_int64, c_void_p, c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_void_p,
+                                    c_int32, c_int32, c_int32, c_int32, c_float, c_void_p]),
+    "oscars_layer_norm_backward_workspace": (c_int32, [c_int32, c_int32, c_int32, POINTER(c_int64)]),
+    "oscars_layer_norm_backward": (c_int32, [c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_void_p,
+                                             c_void_p, c_int64, c_void_p, c_void_p, c_int64, c_int32, c_int32, c_int32,
+                                             c_int32, c_void_p, c_int64, c_void_p]),
     "oscars_merge": (c_int32, [c_void_p, POINTER(c_void_p), POINTER(c_float), c_int32, c_int64, c_float, c_void_p]),
 }
 
@@ -361,6 +375,59 @@ def oscars_gemm_i8_nt(a_ptr: int, lda: int, scale_a_ptr: int, b_ptr: int, ldb: i
     """8-bit product with scales, bias and ReLU (strides in elements)."""
     _check(lib().oscars_gemm_i8_nt(a_ptr, lda, scale_a_ptr, b_ptr, ldb, scale_b_ptr, bias_ptr, int(relu), c_ptr, ldc, dtype,
                                    M, N, K, stream))
+
+
+def oscars_fp4_scale_bytes(rows: int, cols: int, fmt: int) -> int:
+    """Bytes of the block scales of a matrix in 4 bits."""
+    out = c_int64()
+    _check(lib().oscars_fp4_scale_bytes(rows, cols, fmt, ctypes.byref(out)))
+    return out.value
+
+
+def oscars_quantize_fp4(x_ptr: int, ldx: int, dtype: int, rows: int, cols: int, fmt: int, q_ptr: int, ldq: int, scales_ptr: int,
+                        row_scale_ptr: Optional[int] = None, stream: Optional[int] = None):
+    """Rows in 4 bits with a scale for each block (ldx in elements, ldq in bytes)."""
+    _check(lib().oscars_quantize_fp4(x_ptr, ldx, dtype, rows, cols, fmt, q_ptr, ldq, scales_ptr, row_scale_ptr, stream))
+
+
+def oscars_dequantize_fp4(q_ptr: int, ldq: int, scales_ptr: int, row_scale_ptr: Optional[int], fmt: int, rows: int, cols: int,
+                          x_ptr: int, ldx: int, dtype: int, stream: Optional[int] = None):
+    """The values of rows in 4 bits (ldq in bytes, ldx in elements)."""
+    _check(lib().oscars_dequantize_fp4(q_ptr, ldq, scales_ptr, row_scale_ptr, fmt, rows, cols, x_ptr, ldx, dtype, stream))
+
+
+def oscars_gemm_fp4_nt(a_ptr: int, lda: int, scales_a_ptr: int, b_ptr: int, ldb: int, scales_b_ptr: int, fmt: int, c_ptr: int,
+                       ldc: int, dtype: int, M: int, N: int, K: int, row_scale_a_ptr: Optional[int] = None,
+                       row_scale_b_ptr: Optional[int] = None, bias_ptr: Optional[int] = None, relu: bool = False,
+                       stream: Optional[int] = None):
+    """4-bit product with scales, bias and ReLU (lda, ldb in bytes, ldc in elements)."""
+    _check(lib().oscars_gemm_fp4_nt(a_ptr, lda, scales_a_ptr, row_scale_a_ptr, b_ptr, ldb, scales_b_ptr, row_scale_b_ptr, fmt,
+                                    bias_ptr, int(relu), c_ptr, ldc, dtype, M, N, K, stream))
+
+
+def oscars_layer_norm(x_ptr: int, ldx: int, gamma_ptr: Optional[int], beta_ptr: Optional[int], param_stride: int, y_ptr: int,
+                      ldy: int, dtype: int, groups: int, rows: int, cols: int, eps: float, mean_ptr: Optional[int] = None,
+                      rstd_ptr: Optional[int] = None, stream: Optional[int] = None):
+    """Layer norm of `groups` groups of rows with parameters of their own (strides in elements)."""
+    _check(lib().oscars_layer_norm(x_ptr, ldx, gamma_ptr, beta_ptr, param_stride, y_ptr, ldy, mean_ptr, rstd_ptr, dtype, groups,
+                                   rows, cols, eps, stream))
+
+
+def oscars_layer_norm_backward_workspace(groups: int, rows: int, cols: int) -> int:
+    """Bytes of workspace that oscars_layer_norm_backward wants for these sizes."""
+    out = c_int64()
+    _check(lib().oscars_layer_norm_backward_workspace(groups, rows, cols, ctypes.byref(out)))
+    return out.value
+
+
+def oscars_layer_norm_backward(dy_ptr: int, lddy: int, x_ptr: int, ldx: int, gamma_ptr: Optional[int], param_stride: int,
+                               mean_ptr: int, rstd_ptr: int, dx_ptr: Optional[int], lddx: int, dgamma_ptr: Optional[int],
+                               dbeta_ptr: Optional[int], dparam_stride: int, dtype: int, groups: int, rows: int, cols: int,
+                               workspace_ptr: Optional[int], workspace_bytes: int, stream: Optional[int] = None):
+    """Layer norm's backward pass with the gradients of its parameters (strides in elements)."""
+    _check(lib().oscars_layer_norm_backward(dy_ptr, lddy, x_ptr, ldx, gamma_ptr, param_stride, mean_ptr, rstd_ptr, dx_ptr, lddx,
+                                            dgamma_ptr, dbeta_ptr, dparam_stride, dtype, groups, rows, cols, workspace_ptr,
+                                            workspace_bytes, stream))
 
 
 def oscars_profile_read(ctx: int):

@@ -67,6 +67,23 @@ struct Held8<__nv_bfloat16> {
   }
 };
 
+// 8 values of a row; `vec`: 16-byte stores
+template <typename T>
+__device__ __forceinline__ void store8(T* p, int n, bool vec, const float (&v)[8]) {
+  if (vec && n >= 8) {
+    if constexpr (sizeof(T) == 4) {
+      reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+      reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+    } else {
+      *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < n) p[i] = static_cast<T>(v[i]);
+  }
+}
+
 // Sums of squares over the whole range of fp32, in fp32 (the card's fp64 rate is 1/64 of it): of values whose squares
 // neither overflow nor underflow, of larger ones times 2^-80 and of smaller ones times 2^80.
 struct Squares {
