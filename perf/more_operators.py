@@ -153,7 +153,7 @@ def _pack(codes, byte, rows):
     q = flat[:, 0::2] | (flat[:, 1::2] << 4)
     tiles = torch.nn.functional.pad(byte, (0, -byte.shape[1] % 4, 0, -rows % 128))
     s = tiles.reshape(tiles.shape[0] // 128, 4, 32, -1, 4).permute(0, 3, 2, 1, 4).contiguous()
-    return q.contiguous(), s.reshape(-1)
+    return q.to(torch.uint8).contiguous(), s.reshape(-1)   # bytes, as the calls take them
 
 
 def _unpack(q, s, rows, cols, fmt):
