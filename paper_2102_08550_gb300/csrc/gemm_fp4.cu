@@ -3,6 +3,17 @@
 //   C[m][n] = act(ra[m] rb[n] sum_k A[m][k] B[n][k] + bias[n]),  A and B codes times their blocks' scales
 //
 // A product of two codes is a multiple of 1/4 up to 36, so a block's sum is exact in fp32.
+//
+// The product is computed as rows = channels (B), columns = tokens (A): the accumulator's lanes then run along a row of C,
+// so that a store of a token's 32 channels is coalesced as it leaves the registers, whatever C's alignment.
+//
+// gemm_fp4_kernel: tcgen05 (kind::mxf4nvf4), persistent, one CTA per SM or a pair (cta_group::2), 20 warps:
+//   0       TMA of codes (128 channels and BN tokens, 256 of K) and of their scales into a ring
+//   1       copies a stage's scales to tensor memory and issues its products
+//   4-19    accumulators -> C, under the products of the next tile
+// gemm_fp4_few_kernel for one or two tokens.
+#include <atomic>
+
 #include "common.cuh"
 #include "fp4.cuh"
 #include "internal.h"
@@ -44,7 +55,8 @@ __global__ void __launch_bounds__(kFewThreads) gemm_fp4_few_kernel(const __grid_
   const int n = blockIdx.x * (kFewThreads / 32) + warp;
   if (n >= a.N) return;
   const int groups = (a.K + 31) / 32;
-  for (int m0 = blockIdx.y * MT; m0 < a.M; m0 += gridDim.y * MT) {
+  {
+    constexpr int m0 = 0;
     float sum[MT] = {};
     for (int g = lane; g < groups; g += 32) {
       const uint4 w = *reinterpret_cast<const uint4*>(a.B + n * a.ldb + g * 16);
@@ -94,6 +106,468 @@ __global__ void __launch_bounds__(kFewThreads) gemm_fp4_few_kernel(const __grid_
   }
 }
 
+// ------------------------------------------------------------------ tensor cores
+constexpr int kThreads = 640, kMaxBN = 256, kMaxStages = 8, kEpiWarps = 16, kSpan = kMaxBN / 4;
+constexpr int kK = 256;                          // K-block: 128 bytes of a row
+constexpr int kBarBytes = 512, kSmem = 227 * 1024;
+constexpr size_t kLeast = 164 * 1024;            // one CTA an SM, and no other kernel's cluster beside it (tensor memory)
+static_assert(no_cluster_beside(kLeast), "no other cluster's CTA beside this kernel's");
+constexpr int kScaleCol = 256;                   // tensor memory: accumulators in front of it, scales of the stages behind
+
+struct Tile {
+  int BN, nt, mt, units, split, stages, accs, chunk;   // chunk: K-blocks that one accumulation takes
+};
+
+struct Bars {
+  uint64_t full[kMaxStages], empty[kMaxStages], accf[2], acce[2];
+  uint32_t tmem;
+  int failed;   // kSplit: a part's sums are not all there
+};
+static_assert(sizeof(Bars) <= kBarBytes, "barriers fit");
+
+constexpr uint32_t kLeaderMask = 0xFEFFFFFFu;    // a pair's barrier of the leader at the same offset
+__device__ __forceinline__ void tma_load_3d_pair(void* smem_dst, const CUtensorMap* map, int c0, int c1, int c2, uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(smem_u32(smem_dst)),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(c2), "r"(smem_u32(bar) & kLeaderMask)
+      : "memory");
+}
+// D (+)= A B^T of codes with block scales in tensor memory, 64 of K
+template <int CL, bool kMx>
+__device__ __forceinline__ void umma_fp4(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb, uint32_t accumulate) {
+#define OSCARS_UMMA_FP4(group, vec)                                                                                       \
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"                                                          \
+               "tcgen05.mma.cta_group::" group ".kind::mxf4nvf4.block_scale.scale_vec::" vec " [%0], %1, %2, %3, [%4], [%5], p;\n\t}" \
+               ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate)                                      \
+               : "memory")
+  if constexpr (CL == 2 && kMx) OSCARS_UMMA_FP4("2", "2X");
+  else if constexpr (CL == 2) OSCARS_UMMA_FP4("2", "4X");
+  else if constexpr (kMx) OSCARS_UMMA_FP4("1", "2X");
+  else OSCARS_UMMA_FP4("1", "4X");
+#undef OSCARS_UMMA_FP4
+}
+// 512 bytes of scales (a tile of 128 rows x 4 blocks) to four columns of tensor memory
+template <int CL>
+__device__ __forceinline__ void copy_scales(uint32_t taddr, uint64_t desc) {
+  if constexpr (CL == 2) asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+  else asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+}
+// such a tile in shared memory: 32 rows of 16 bytes, groups of 8 rows 128 bytes apart, no swizzle
+__device__ __forceinline__ uint64_t scale_desc(uint32_t saddr) {
+  return static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4) | static_cast<uint64_t>(128 >> 4) << 32 | static_cast<uint64_t>(1) << 46;
+}
+__device__ __forceinline__ void umma_commit_pair(uint64_t* bar) {
+  asm volatile(
+      "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(
+          smem_u32(bar)),
+      "h"(static_cast<uint16_t>(0x3))
+      : "memory");
+}
+// An arrival on a barrier of the pair's leader, released at CTA scope: all that it has to come after are reads of this SM's
+// tensor memory, which tcgen05.wait::ld has seen finished (gemm_i8.cu).
+__device__ __forceinline__ void mbar_arrive_at(uint32_t cluster_bar) {
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+}
+__device__ __forceinline__ void st_peer(const void* local, int rank, uint32_t v) {
+  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(cluster_addr(local, rank)), "r"(v) : "memory");
+}
+
+// e2m1 operands (1), both K-major; scales e8m0 or e4m3
+__host__ __device__ constexpr uint32_t idesc_fp4(int M, int N, bool mx) {
+  return (1u << 7) | (1u << 10) | (static_cast<uint32_t>(N >> 3) << 17) | (mx ? 1u << 23 : 0u) | (static_cast<uint32_t>(M >> 7) << 27);
+}
+// which of a tile's four scales a product takes (0, 2), of both operands
+__host__ __device__ constexpr uint32_t scale_id(int id) { return static_cast<uint32_t>(id) << 4 | static_cast<uint32_t>(id) << 29; }
+
+// A thread's channel n of tokens m0 ... m0 + span (kFar: some of the tokens' row scales are near_one's)
+template <bool kFar, typename T>
+__device__ __forceinline__ void store_tokens(const Fp4Args& a, T* C, int m0, int n, int span, const float (&sum)[kSpan / 16][16],
+                                             const float (&ra)[kSpan / 32], float rb, float bias) {
+  T* at = C + m0 * a.ldc + n;
+  const int rows = n < a.N ? a.M - m0 : 0;
+#pragma unroll
+  for (int g = 0; g < kSpan / 16; ++g)
+    if (16 * g < span) {
+      float v[16];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) v[e] = sum[g][e] * __shfl_sync(0xffffffffu, ra[g / 2], (g & 1) * 16 + e) * rb;
+      if constexpr (kFar) {
+        const int m = m0 + 16 * g + (threadIdx.x & 15);
+        const float to = m < a.M && a.ra ? back(__ldg(a.ra + m)) : 1.f;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) v[e] *= __shfl_sync(0xffffffffu, to, e);
+      }
+      if (a.bias) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) v[e] += bias;
+      }
+      if (a.relu) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) v[e] = v[e] < 0.f ? 0.f : v[e];
+      }
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        if (16 * g + e < rows) *at = static_cast<T>(v[e]);
+        at += a.ldc;
+      }
+    }
+}
+
+template <int CL, bool kSplit, bool kMx>
+__global__ void __launch_bounds__(kThreads, 1) gemm_fp4_kernel(const __grid_constant__ CUtensorMap mapW, const __grid_constant__ CUtensorMap mapX,
+                                                               const __grid_constant__ CUtensorMap mapSW, const __grid_constant__ CUtensorMap mapSX,
+                                                               const __grid_constant__ Fp4Args a, const __grid_constant__ Tile p) {
+  extern __shared__ uint8_t fp4_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(fp4_raw) + 1023) & ~uintptr_t(1023));
+  constexpr int kTk = kMx ? 2 : 4;                 // scale tiles of a row tile in a K-block
+  const int bn = p.BN / CL, xt = p.BN > 128 ? 2 : 1;   // this CTA's tokens of a tile; row tiles of the tokens' scales
+  const int x_at = 128 * 128, sw_at = x_at + bn * 128, sx_at = sw_at + kTk * 512, stage_bytes = (sx_at + xt * kTk * 512 + 1023) & ~1023;
+  const int copied = sx_at + xt * kTk * 512;
+  uint8_t* ring = smem;
+  uint8_t* recv = smem + p.stages * stage_bytes;   // kSplit: the parts' sums of this CTA's tokens [part][BN / split][128]
+  Bars* bars = reinterpret_cast<Bars*>(recv + (kSplit ? p.BN * 512 : 0));
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+  const int part = kSplit ? static_cast<int>(cluster_ctarank()) : 0;
+  const int rank = CL > 1 ? static_cast<int>(cluster_ctarank()) : 0;
+  const int nk = (a.K + kK - 1) / kK;
+  const int k0 = kSplit ? static_cast<int>(static_cast<int64_t>(nk) * part / p.split) : 0;
+  const int k1 = kSplit ? static_cast<int>(static_cast<int64_t>(nk) * (part + 1) / p.split) : nk;
+  const int per = kSplit ? p.split : CL;           // CTAs of a tile
+  const int u0 = blockIdx.x / per, ustep = gridDim.x / per;
+  const int mu = p.mt / CL;                        // row tiles (of channels); rows fastest
+
+  if (threadIdx.x == 0) {
+    prefetch_tmap(&mapW);
+    prefetch_tmap(&mapX);
+    prefetch_tmap(&mapSW);
+    prefetch_tmap(&mapSX);
+    for (int i = 0; i < p.stages; ++i) {
+      mbar_init(&bars->full[i], 1);
+      mbar_init(&bars->empty[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&bars->accf[i], 1);
+      mbar_init(&bars->acce[i], kEpiWarps * CL);
+    }
+    bars->failed = 0;
+    fence_barrier_init();
+    fence_proxy_async_smem();
+  }
+  if (warp == 2) {
+    if (CL == 1) {
+      tmem_alloc(&bars->tmem, 512);
+      tmem_relinquish();
+    } else {
+      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars->tmem)), "r"(512)
+                   : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+  }
+  tc_fence_before();
+  if (CL > 1 || kSplit) cluster_sync();   // the peers run, and their barriers are initialised
+  else __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = bars->tmem;
+  pdl_wait();
+  pdl_trigger();
+
+  if (warp == 0) {
+    // ---- TMA
+    int it = 0, s = 0, ph = 1;
+    uint32_t limit = kSpinLimit;
+    for (int u = u0; u < p.units; u += ustep) {
+      const int n0 = ((u % mu) * CL + rank) * 128, m0 = (u / mu) * p.BN;
+      for (int kb = k0; kb < k1; ++kb, ++it) {
+        if (it >= p.stages) mbar_wait_keep(limit, &bars->empty[s], ph, nullptr, kDevTimeoutEmpty);
+        if (elect_one() && limit > 1) {
+          uint8_t* at = ring + s * stage_bytes;
+          uint64_t* bar = &bars->full[s];
+          if (rank == 0) mbar_arrive_expect_tx(bar, CL * copied);   // a pair's bytes count on the leader's
+          auto load = [&](int to, const CUtensorMap* map, int c0, int c1, int c2) {
+            if (CL > 1) tma_load_3d_pair(at + to, map, c0, c1, c2, bar);
+            else tma_load_3d(at + to, map, c0, c1, c2, bar);
+          };
+          load(0, &mapW, kb * 128, n0, 0);
+          load(x_at, &mapX, kb * 128, m0 + rank * bn, 0);
+          load(sw_at, &mapSW, 0, kb * kTk, n0 >> 7);
+          load(sx_at, &mapSX, 0, kb * kTk, m0 >> 7);
+        }
+        __syncwarp();
+        if (++s == p.stages) {
+          s = 0;
+          ph ^= 1;
+        }
+      }
+    }
+    // the copies have landed before this CTA ends (a pair's end together)
+    if (rank == 0)
+      for (int i = it > p.stages ? it - p.stages : 0; i < it; ++i)
+        mbar_wait_keep(limit, &bars->full[i % p.stages], (i / p.stages) & 1, nullptr, kDevTimeoutFull);
+  } else if (warp == 1 && rank == 0) {
+    // ---- scales to tensor memory, products (the leader's, of a pair); the warp stays converged and one elected lane issues
+    const uint32_t idesc = idesc_fp4(128 * CL, p.BN, kMx), ring0 = smem_u32(ring);
+    const int cols = (1 + xt) * kTk * 4;           // of a stage's scales
+    int s = 0, ph = 0, t = 0;                      // t: accumulations begun
+    uint32_t limit = kSpinLimit;
+    for (int u = u0; u < p.units; u += ustep) {
+      for (int c0 = k0; c0 < k1; c0 += p.chunk, ++t) {
+        const int b = t % p.accs, c1 = c0 + p.chunk < k1 ? c0 + p.chunk : k1;
+        if (t >= p.accs) mbar_wait_keep(limit, &bars->acce[b], (t / p.accs + 1) & 1, nullptr, kDevTimeoutAccum);
+        tc_fence_after();
+        const uint32_t acc = tmem + b * 128;
+        for (int kb = c0; kb < c1; ++kb) {
+          mbar_wait_keep(limit, &bars->full[s], ph, nullptr, kDevTimeoutFull);
+          tc_fence_after();
+          if (elect_one() && limit > 1) {
+            const uint32_t at = ring0 + s * stage_bytes, sw = tmem + kScaleCol + s * cols, sx = sw + 4 * kTk;
+            const uint64_t wd = smem_desc_k128(at), xd = smem_desc_k128(at + x_at);
+            const uint64_t swd = scale_desc(at + sw_at), sxd = scale_desc(at + sx_at);
+            const int left = a.K - kb * kK, n = left >= kK ? 4 : (left + 63) / 64;
+            // a stage's columns were last read by products that have ended: its copies have been waited for
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              if (j < n) {
+                const int tile = kMx ? j / 2 : j;
+                if (!kMx || j % 2 == 0) {
+                  copy_scales<CL>(sw + 4 * tile, swd + tile * 32);
+                  for (int i = 0; i < xt; ++i) copy_scales<CL>(sx + 4 * (tile * xt + i), sxd + (i * kTk + tile) * 32);
+                }
+                umma_fp4<CL, kMx>(acc, wd + 2 * j, xd + 2 * j, idesc | (kMx ? scale_id(j % 2 * 2) : 0), sw + 4 * tile, sx + 4 * tile * xt, (kb > c0) | (j > 0));
+              }
+            if (CL > 1) umma_commit_pair(&bars->empty[s]);
+            else umma_commit(&bars->empty[s]);
+          }
+          __syncwarp();
+          if (++s == p.stages) {
+            s = 0;
+            ph ^= 1;
+          }
+        }
+        if (elect_one() && limit > 1) {
+          if (CL > 1) umma_commit_pair(&bars->accf[b]);
+          else umma_commit(&bars->accf[b]);
+        }
+        __syncwarp();
+      }
+    }
+  } else if (warp >= 4) {
+    // ---- C: thread = one channel and a quarter of the tile's tokens (16 of fewer than 64)
+    const int quarter = warp & 3, span = p.BN > 64 ? p.BN / 4 : 16, cb = (warp / 4 - 1) * span;
+    const bool works = cb < p.BN;
+    int t = 0;
+    bool ok = true;
+    for (int u = u0; ok && u < p.units; u += ustep) {
+      const int n = ((u % mu) * CL + rank) * 128 + 32 * quarter + lane, m0 = (u / mu) * p.BN + cb;
+      const uint32_t row0 = tmem + (static_cast<uint32_t>(32 * quarter) << 16) + cb;
+      float rb = 1.f, bias = 0.f, ra[kSpan / 32];   // lane l: tokens l, 32 + l, ...
+      bool far = false;
+      if (!kSplit) {
+        if (a.rb && n < a.N) rb = __ldg(a.rb + n);
+        if (a.bias && n < a.N) bias = __ldg(a.bias + n);
+#pragma unroll
+        for (int i = 0; i < kSpan / 32; ++i) {
+          ra[i] = a.ra && m0 + 32 * i + lane < a.M && 32 * i < span ? __ldg(a.ra + m0 + 32 * i + lane) : 1.f;
+          far |= ra[i] != 0.f && back(ra[i]) != 1.f;
+          ra[i] = near_one(ra[i]);
+        }
+        far = __any_sync(0xffffffffu, far);
+      }
+      float sum[kSpan / 16][16];
+#pragma unroll
+      for (int g = 0; g < kSpan / 16; ++g)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sum[g][e] = 0.f;
+      for (int c0 = k0; c0 < k1; c0 += p.chunk, ++t) {
+        const int b = t % p.accs;
+        if (!(ok = mbar_wait_warp(&bars->accf[b], (t / p.accs) & 1, nullptr, kDevTimeoutAccum))) break;
+        tc_fence_after();
+#pragma unroll
+        for (int g = 0; g < kSpan / 16; ++g)
+          if (works && 16 * g < span) {
+            float v[16];
+            tmem_ld_32x32b_x16(row0 + b * 128 + 16 * g, v);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) sum[g][e] += v[e];
+          }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          if (CL > 1) mbar_arrive_at(cluster_addr(&bars->acce[b], 0));
+          else mbar_arrive(&bars->acce[b]);
+        }
+      }
+      if (!ok) {   // every wait that runs out in this CTA ends in one of the accumulator's; its peers then leave the tile alone too
+        if (kSplit && lane < p.split) st_peer(&bars->failed, lane, 1);
+        break;
+      }
+      if (!works) continue;
+      if constexpr (kSplit) {   // a part's sums [token][channel] go to the CTA that adds up the token
+        const int owned = p.BN / p.split;
+#pragma unroll
+        for (int g = 0; g < kSpan / 16; ++g)
+          if (16 * g < span) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const int tok = cb + 16 * g + e;
+              st_peer(recv + ((part * owned + tok % owned) * 128 + 32 * quarter + lane) * 4, tok / owned, __float_as_uint(sum[g][e]));
+            }
+          }
+      } else if (far) {
+        if (a.bf16) store_tokens<true>(a, static_cast<__nv_bfloat16*>(a.C), m0, n, span, sum, ra, rb, bias);
+        else store_tokens<true>(a, static_cast<float*>(a.C), m0, n, span, sum, ra, rb, bias);
+      } else if (a.bf16) {
+        store_tokens<false>(a, static_cast<__nv_bfloat16*>(a.C), m0, n, span, sum, ra, rb, bias);
+      } else {
+        store_tokens<false>(a, static_cast<float*>(a.C), m0, n, span, sum, ra, rb, bias);
+      }
+    }
+  }
+  tc_fence_before();
+  if (CL > 1 || kSplit) cluster_sync();   // the pair's products and arrivals are done in both CTAs; every part's sums are there
+  else __syncthreads();
+  if constexpr (kSplit) {
+    // each CTA adds up its tokens of the tile over the parts
+    const int missing = bars->failed;
+    const int n0 = (u0 % mu) * 128, tokens = p.BN / p.split, m0 = (u0 / mu) * p.BN + part * tokens;
+    const float* sums = reinterpret_cast<const float*>(recv);
+    for (int i = threadIdx.x; missing == 0 && i < tokens * 128; i += kThreads) {
+      const int m = m0 + i / 128, n = n0 + i % 128;
+      if (m >= a.M || n >= a.N) continue;
+      float t = 0.f;
+      for (int q = 0; q < p.split; ++q) t += sums[q * tokens * 128 + i];
+      const float y = finish(a, t, a.ra ? __ldg(a.ra + m) : 1.f, a.rb ? __ldg(a.rb + n) : 1.f, a.bias ? __ldg(a.bias + n) : 0.f);
+      if (a.bf16) static_cast<__nv_bfloat16*>(a.C)[m * a.ldc + n] = __float2bfloat16_rn(y);
+      else static_cast<float*>(a.C)[m * a.ldc + n] = y;
+    }
+  }
+  if (warp == 2) {
+    tc_fence_after();
+    if (CL == 1) tmem_dealloc(tmem, 512);
+    else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+  }
+}
+
+constexpr int kMaxDevices = 64;
+struct DevInfo {
+  std::atomic<int> sms{0}, pairs{0};
+};
+DevInfo g_dev[kMaxDevices];
+
+cudaLaunchConfig_t config(cudaLaunchAttribute* attr, int cluster, int grid, size_t smem, cudaStream_t s) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid, 1, 1);
+  cfg.blockDim = dim3(kThreads, 1, 1);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cfg.attrs = attr;
+  cfg.numAttrs = 0;
+  if (cluster > 1) {
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = cluster;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cfg.numAttrs = 1;
+  }
+  return cfg;
+}
+
+// {SMs, resident clusters of two} of the current device, queried once
+void device_room(int& sms, int& pairs) {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) dev = 0;
+  sms = g_dev[dev].sms.load(std::memory_order_relaxed);
+  pairs = g_dev[dev].pairs.load(std::memory_order_relaxed);
+  if (sms > 0 && pairs > 0) return;
+  if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || sms < 1) sms = 1;
+  cudaLaunchAttribute attr[1];
+  pairs = 0;
+  if (allow_smem(gemm_fp4_kernel<2, false, false>, kSmem) == cudaSuccess) {
+    cudaLaunchConfig_t cfg = config(attr, 2, 2, kSmem, nullptr);
+    if (cudaOccupancyMaxActiveClusters(&pairs, gemm_fp4_kernel<2, false, false>, &cfg) != cudaSuccess) pairs = 0;
+  }
+  cudaGetLastError();
+  if (pairs < 1) pairs = 1;
+  g_dev[dev].sms.store(sms, std::memory_order_relaxed);
+  g_dev[dev].pairs.store(pairs, std::memory_order_relaxed);
+}
+
+template <int CL, bool kSplit, bool kMx>
+cudaError_t launch_fp4(const CUtensorMap (&m)[4], const Fp4Args& a, Tile p, int grid, cudaStream_t s) {
+  const int tk = kMx ? 2 : 4, xt = p.BN > 128 ? 2 : 1;
+  const int stage = (128 * 128 + p.BN / CL * 128 + (1 + xt) * tk * 512 + 1023) & ~1023, sums = kSplit ? p.BN * 512 : 0;
+  p.stages = (kSmem - 1024 - kBarBytes - sums) / stage;
+  if (p.stages > kMaxStages) p.stages = kMaxStages;
+  const int cols = (1 + xt) * tk * 4;
+  if (p.stages > (512 - kScaleCol) / cols) p.stages = (512 - kScaleCol) / cols;
+  size_t smem = 1024 + static_cast<size_t>(p.stages) * stage + sums + kBarBytes;
+  if (smem < kLeast) smem = kLeast;
+  cudaError_t e = allow_smem(gemm_fp4_kernel<CL, kSplit, kMx>, kSmem);
+  if (e != cudaSuccess) return e;
+  cudaLaunchAttribute attr[2];
+  cudaLaunchConfig_t cfg = config(attr, kSplit ? p.split : CL, grid, smem, s);
+  attr[cfg.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[cfg.numAttrs].val.programmaticStreamSerializationAllowed = 1;
+  ++cfg.numAttrs;
+  return cudaLaunchKernelEx(&cfg, gemm_fp4_kernel<CL, kSplit, kMx>, m[0], m[1], m[2], m[3], a, p);
+}
+
+bool code_map(CUtensorMap* m, const uint8_t* base, int64_t ld, int K, int rows, int box_rows) {
+  const cuuint64_t dims[3] = {static_cast<cuuint64_t>(fp4_row_bytes(K)), static_cast<cuuint64_t>(rows), 1};
+  const cuuint64_t strides[2] = {static_cast<cuuint64_t>(ld), static_cast<cuuint64_t>(ld)};   // the third dimension has one entry
+  const cuuint32_t box[3] = {128, static_cast<cuuint32_t>(box_rows), 1};
+  return encode_map(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, base, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B);
+}
+// scale tiles, 128 words each; tiles past the last are zeros
+bool scale_map(CUtensorMap* m, const uint8_t* base, int tiles, int rows, int box_tiles, int box_rows) {
+  const cuuint64_t dims[3] = {128, static_cast<cuuint64_t>(tiles), static_cast<cuuint64_t>((static_cast<int64_t>(rows) + 127) / 128)};
+  const cuuint64_t strides[2] = {512, static_cast<cuuint64_t>(tiles) * 512};
+  const cuuint32_t box[3] = {128, static_cast<cuuint32_t>(box_tiles), static_cast<cuuint32_t>(box_rows)};
+  return encode_map(m, CU_TENSOR_MAP_DATA_TYPE_UINT32, 3, base, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_NONE);
+}
+
+// The shape with the least estimated time: waves of tiles times the longer of a K-block's products (2 BN clocks, or 130 for
+// the channels' reads) and its loads (45 bytes a clock), plus fixed parts
+void choose(const Fp4Args& a, int sms, int pairs, Tile& p, int& cl) {
+  const int nk = (a.K + kK - 1) / kK;
+  double best = 0.0;
+  for (int c = 1; c <= 2; ++c) {
+    const int mt = ((a.N + 127) / 128 + c - 1) / c * c;
+    for (int bn = c == 1 ? 16 : 64; bn <= kMaxBN; bn *= 2) {
+      if (bn < 128 && a.M > bn) continue;   // a product takes a scale tile from its first row on
+      const int64_t nt = (static_cast<int64_t>(a.M) + bn - 1) / bn, units = mt / c * nt;
+      const int room = c == 2 ? pairs : sms;
+      const double bytes = (128 + bn / c) * 128 + 512 * (a.mx ? 2 : 4) * (bn > 128 ? 3 : 2);
+      double kb = 2.0 * bn;
+      kb = kb > 130.0 ? kb : 130.0;
+      kb = kb > bytes / 45.0 ? kb : bytes / 45.0;
+      for (int split = 1; split <= (c == 1 ? 8 : 1); split *= 2) {
+        if (split > 1 && (units * split > sms * 7 / 8 || nk < 2 * split || bn < 2 * split || bn > 128)) break;
+        const double waves = split > 1 ? 1.0 : static_cast<double>((units + room - 1) / room);
+        const double cost = waves * ((nk + split - 1) / split * kb + 600.0) + 15.0 * bn + (c == 2 ? 1500.0 : 0.0) + (split > 1 ? 3000.0 : 0.0);
+        if (best == 0.0 || cost < best) {
+          best = cost;
+          cl = c;
+          p.BN = bn;
+          p.mt = mt;
+          p.nt = static_cast<int>(nt);
+          p.split = split;
+        }
+      }
+    }
+  }
+  p.accs = p.BN > 128 ? 1 : 2;
+  p.chunk = nk;
+}
+
+template <bool kMx>
+cudaError_t launch_tile(const CUtensorMap (&m)[4], const Fp4Args& a, const Tile& p, int cl, int room, cudaStream_t s) {
+  const int grid = (p.units < room ? p.units : room) * cl;
+  return p.split > 1 ? launch_fp4<1, true, kMx>(m, a, p, p.units * p.split, s)
+         : cl == 2   ? launch_fp4<2, false, kMx>(m, a, p, grid, s)
+                     : launch_fp4<1, false, kMx>(m, a, p, grid, s);
+}
+
 bool at_bytes(const void* p, int n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 
 }  // namespace
@@ -116,9 +590,27 @@ oscars_status oscars_gemm_fp4_nt(const uint8_t* A, int64_t lda, const uint8_t* s
   Fp4Args a{A, scales_a, B, scales_b, row_a, row_b, bias, C, lda, ldb, ldc, M, N, K, format == OSCARS_MXFP4, fp4_tiles(K, format), relu,
             dtype == OSCARS_BF16};
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  constexpr int kPer = kFewThreads / 32;
-  const dim3 grid((N + kPer - 1) / kPer, (M + 3) / 4 < 65535 ? (M + 3) / 4 : 65535);
-  const cudaError_t e = launch_dependent(gemm_fp4_few_kernel<4>, grid, kFewThreads, 0, s, a);
+  if (M <= 2) {
+    constexpr int kPer = kFewThreads / 32;
+    const dim3 grid((N + kPer - 1) / kPer);
+    const cudaError_t e = M == 1 ? launch_dependent(gemm_fp4_few_kernel<1>, grid, kFewThreads, 0, s, a)
+                                 : launch_dependent(gemm_fp4_few_kernel<2>, grid, kFewThreads, 0, s, a);
+    return e == cudaSuccess ? OSCARS_OK : OSCARS_ECUDA;
+  }
+  int sms, pairs, cl = 1;
+  device_room(sms, pairs);
+  Tile p{};
+  choose(a, sms, pairs, p, cl);
+  const int64_t units = static_cast<int64_t>(p.mt / cl) * p.nt;
+  if (units > INT32_MAX / 2) return OSCARS_EINVAL;
+  p.units = static_cast<int>(units);
+  const int tk = a.mx ? 2 : 4;
+  CUtensorMap m[4];
+  if (!code_map(&m[0], B, ldb, K, N, 128) || !code_map(&m[1], A, lda, K, M, p.BN / cl) || !scale_map(&m[2], scales_b, a.tiles, N, tk, 1) ||
+      !scale_map(&m[3], scales_a, a.tiles, M, tk, p.BN > 128 ? 2 : 1))
+    return OSCARS_ECUDA;
+  const int room = cl == 2 ? pairs : sms;
+  const cudaError_t e = a.mx ? launch_tile<true>(m, a, p, cl, room, s) : launch_tile<false>(m, a, p, cl, room, s);
   return e == cudaSuccess ? OSCARS_OK : OSCARS_ECUDA;
 }
 
