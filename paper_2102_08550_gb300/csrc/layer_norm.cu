@@ -5,6 +5,8 @@
 //   dgamma = sum over the group's rows of dy xh,  dbeta = sum of dy
 //
 // Bound by memory: forward reads x and writes y, backward reads dy and x and writes dx.
+#include <type_traits>
+
 #include "../../include/oscars.h"
 #include "common.cuh"
 #include "internal.h"
@@ -15,7 +17,7 @@ namespace oscars {
 namespace {
 
 constexpr int kMaxSide = 1 << 30, kMaxGroups = 65535;
-constexpr int kThreads = 256, kKeep = 4;
+constexpr int kThreads = 256;
 
 // the sum of a value over the TPR threads of a row, in each of them, in a fixed order (a barrier of the row's threads
 // alone: rows of one block may differ in how many sums they take)
@@ -45,6 +47,131 @@ __device__ __forceinline__ void params8(const float* p, int at, int cols, bool v
   }
 }
 
+// ------------------------------------------------------------------ rows through shared memory
+// Up to 8192 columns: TPR threads take a row, a block 512 / TPR rows at a time; a thread owns 8 kTurns columns.  kMats matrices'
+// rows come through a ring in shared memory in which each thread reads what it has copied itself (cp.async, no barrier).
+// Where rows are not 16-byte aligned, neighbouring threads take neighbouring columns and load them when they are due.
+constexpr int kBlock = 512;
+
+__device__ __forceinline__ void copy16(void* to, const void* from, int bytes) {   // zeros behind the first `bytes`
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(to)), "l"(from), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copy16(void* to, const void* from) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(to)), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copies_done() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+
+template <typename T, int TPR, int kTurns, bool kVec, int kMats>
+struct Rows {
+  static constexpr int kLanes = kBlock / TPR, kCap = TPR * kTurns * 8;
+  static constexpr int kPieces = kTurns * static_cast<int>(sizeof(T)) / 2;          // of 16 bytes, of a thread's columns of one matrix
+  static constexpr int kStage = kMats * kPieces * kBlock * 16;
+  static constexpr int kDepth = kVec ? (196608 / kStage < 6 ? 196608 / kStage : 6) : 1;
+  static constexpr int kBytes = kVec ? kDepth * kStage : 0;
+
+  __device__ __forceinline__ static int column(int i, int e) {
+    const int t = threadIdx.x % TPR;
+    return kVec ? (i * TPR + t) * 8 + e : (i * 8 + e) * TPR + t;
+  }
+  // whether all of this thread's columns are inside the row
+  __device__ __forceinline__ static bool inside(int cols) { return column(kTurns - 1, 7) < cols; }
+  // begin the copy of row `row` of matrix m to a stage
+  __device__ __forceinline__ static void request(uint8_t* ring, int stage, int m, const T* row, int cols) {
+    constexpr int kPer = 16 / sizeof(T);                   // columns of a piece
+    uint8_t* to = ring + stage * kStage + (m * kPieces * kBlock + threadIdx.x) * 16;
+    if (inside(cols)) {
+#pragma unroll
+      for (int p = 0; p < kPieces; ++p) copy16(to + p * kBlock * 16, row + column(p * kPer / 8, p * kPer % 8));
+      return;
+    }
+#pragma unroll
+    for (int p = 0; p < kPieces; ++p) {
+      const int at = column(p * kPer / 8, p * kPer % 8), left = (cols - at) * static_cast<int>(sizeof(T));
+      copy16(to + p * kBlock * 16, row + (left > 0 ? at : 0), left >= 16 ? 16 : left > 0 ? left : 0);
+    }
+  }
+  // this thread's columns of it (zeros behind the row's end)
+  __device__ __forceinline__ static void take(const uint8_t* ring, int stage, int m, const T* row, int cols, float (&v)[kTurns][8]) {
+    if constexpr (kVec) {
+#pragma unroll
+      for (int p = 0; p < kPieces; ++p) {
+        const uint4 w = *reinterpret_cast<const uint4*>(ring + stage * kStage + ((m * kPieces + p) * kBlock + threadIdx.x) * 16);
+        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if constexpr (sizeof(T) == 4) {
+            v[p / 2][p % 2 * 4 + i] = __uint_as_float(u[i]);
+          } else {
+            v[p][2 * i] = __uint_as_float(u[i] << 16);
+            v[p][2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
+          }
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < kTurns; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[i][e] = column(i, e) < cols ? to_f32(row[column(i, e)]) : 0.f;
+    }
+  }
+  __device__ __forceinline__ static void put(T* row, int cols, float (&v)[kTurns][8]) {
+    if (kVec && inside(cols)) {
+#pragma unroll
+      for (int i = 0; i < kTurns; ++i) store8(row + column(i, 0), 8, true, v[i]);
+      return;
+    }
+#pragma unroll
+    for (int i = 0; i < kTurns; ++i) {
+      if constexpr (kVec) {
+        store8(row + column(i, 0), cols - column(i, 0), true, v[i]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (column(i, e) < cols) row[column(i, e)] = static_cast<T>(v[i][e]);
+      }
+    }
+  }
+  // a group's parameters, or `none` if there are none
+  __device__ __forceinline__ static void params(const float* p, int cols, bool vec, float none, float (&v)[kTurns][8]) {
+#pragma unroll
+    for (int i = 0; i < kTurns; ++i) {
+      if constexpr (kVec) {
+        params8(p, column(i, 0), cols, vec, none, v[i]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[i][e] = p && column(i, e) < cols ? p[column(i, e)] : none;
+      }
+    }
+  }
+};
+
+// Sums of N values over a row's threads, in each of them, in a fixed order.  `parts` alternates between two places, so that one
+// barrier is enough: a sum's parts are read before those of the one after the next are written.
+template <int TPR, int N>
+__device__ __forceinline__ void row_sums(float (&v)[N], float (*parts)[2]) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+    for (int n = 0; n < N; ++n) v[n] += __shfl_xor_sync(0xffffffffu, v[n], o);
+  if (TPR > 32) {
+    const int lane = threadIdx.x / TPR, t = threadIdx.x % TPR;
+    float(*part)[2] = parts + lane * (TPR / 32);
+    if ((t & 31) == 0)
+#pragma unroll
+      for (int n = 0; n < N; ++n) part[t >> 5][n] = v[n];
+    bar_named(1 + lane, TPR);
+#pragma unroll
+    for (int n = 0; n < N; ++n) v[n] = part[0][n];
+#pragma unroll
+    for (int i = 1; i < TPR / 32; ++i)
+#pragma unroll
+      for (int n = 0; n < N; ++n) v[n] += part[i][n];
+  }
+}
+
 // ------------------------------------------------------------------ forward
 struct FwdArgs {
   const void* x;
@@ -55,54 +182,139 @@ struct FwdArgs {
   int rows, cols;
   float eps;
   int xvec, yvec, pvec;
+  int groups, chunks, per;            // per: rows of a chunk
 };
+
+// 1 / sqrt(v) of a normal number: the approximation (2 steps off) and one Newton step
+__device__ __forceinline__ float inverse_sqrt(float v) {
+  const float r = rsqrtf(v);
+  return fmaf(r * 0.5f, fmaf(-v * r, r, 1.f), r);
+}
 
 // Sum of squares in the whole range of fp32 only where the plain one left it.
 __device__ __forceinline__ float inverse_std(const Squares& s, int cols, float eps) {
-  if (s.big == 0.f && s.small == 0.f) return 1.f / sqrtf(s.mid / cols + eps);
+  if (s.big == 0.f && s.small == 0.f && eps >= 0x1p-120f) return 1.f / sqrtf(s.mid / cols + eps);
   return static_cast<float>(1.0 / sqrt(s.total() / cols + eps));
 }
 
-template <typename T, int TPR>
-__global__ void __launch_bounds__(kThreads) layer_norm_kernel(const __grid_constant__ FwdArgs a) {
+template <typename T, int TPR, int kTurns, bool kVec>
+__global__ void __launch_bounds__(kBlock, 1) layer_norm_kernel(const __grid_constant__ FwdArgs a) {
+  using R = Rows<T, TPR, kTurns, kVec, 1>;
+  constexpr int kD = R::kDepth;
+  extern __shared__ __align__(16) uint8_t fwd_smem[];
+  __shared__ float parts[2][kBlock / 32][2];
+  const int t = threadIdx.x % TPR, lane = threadIdx.x / TPR;
+  const int group = blockIdx.x / a.chunks, chunk = blockIdx.x % a.chunks;
+  const int r1 = min((chunk + 1) * a.per, a.rows);
+  const int64_t first = static_cast<int64_t>(group) * a.rows;
+  pdl_wait();
+  pdl_trigger();
+  const T* x = static_cast<const T*>(a.x) + first * a.ldx;
+  auto request = [&](int r, int stage) {
+    if constexpr (kVec) {
+      if (r < r1) R::request(fwd_smem, stage, 0, x + r * a.ldx, a.cols);
+      copies_done();
+    }
+  };
+  int r = chunk * a.per + lane;
+#pragma unroll
+  for (int i = 0; i < kD - 1; ++i) request(r + i * R::kLanes, i);
+  float g[kTurns][8], b[kTurns][8];
+  R::params(a.gamma ? a.gamma + group * a.pstride : nullptr, a.cols, a.pvec, 1.f, g);
+  R::params(a.beta ? a.beta + group * a.pstride : nullptr, a.cols, a.pvec, 0.f, b);
+  const float each = 1.f / a.cols;
+  const bool full = R::inside(a.cols);
+  for (int stage = 0; r < r1; r += R::kLanes) {
+    if constexpr (kVec) {
+      request(r + (kD - 1) * R::kLanes, stage == 0 ? kD - 1 : stage - 1);
+      copies_wait<kD - 1>();
+    }
+    float v[kTurns][8];
+    R::take(fwd_smem, stage, 0, x + r * a.ldx, a.cols, v);
+    float sum[1] = {0.f}, none[1] = {0.f};
+#pragma unroll
+    for (int i = 0; i < kTurns; ++i) sum[0] += ((v[i][0] + v[i][1]) + (v[i][2] + v[i][3])) + ((v[i][4] + v[i][5]) + (v[i][6] + v[i][7]));
+    row_sums<TPR>(sum, parts[0]);
+    float mean = sum[0] * each;
+    mean = fmaf(fmaf(-mean, static_cast<float>(a.cols), sum[0]), each, mean);   // the quotient, whatever 1 / cols was rounded to
+    if (!(fabsf(sum[0]) < 0x1p127f)) {   // the sum may have left fp32 where the mean does not; all of the row's threads come here
+      sum[0] = 0.f;
+#pragma unroll
+      for (int i = 0; i < kTurns; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum[0] += v[i][e] * 0x1p-32f;
+      row_sums<TPR>(sum, parts[1]);
+      mean = sum[0] / a.cols * 0x1p32f;
+      row_sums<TPR>(none, parts[0]);   // keeps the two places in turn
+    }
+    Squares sq;
+#pragma unroll
+    for (int i = 0; i < kTurns; ++i) {
+      if (full) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[i][e] -= mean;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[i][e] = R::column(i, e) < a.cols ? v[i][e] - mean : 0.f;
+      }
+      float s = 0.f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s = fmaf(v[i][e], v[i][e], s);
+      if (s > 1e-20f && s < 1e25f) sq.mid += s;
+      else sq.add(v[i]);
+    }
+    float two[2] = {sq.mid, sq.big != 0.f || sq.small != 0.f ? 1.f : 0.f};
+    row_sums<TPR>(two, parts[1]);
+    float rstd = inverse_sqrt(fmaf(two[0], each, a.eps));
+    if (two[1] != 0.f || !(a.eps >= 0x1p-120f)) {
+      float far[2] = {sq.big, sq.small};
+      row_sums<TPR>(far, parts[0]);
+      row_sums<TPR>(none, parts[1]);
+      sq.mid = two[0], sq.big = far[0], sq.small = far[1];
+      rstd = inverse_std(sq, a.cols, a.eps);
+    }
+    if (t == 0) {
+      if (a.mean) a.mean[first + r] = mean;
+      if (a.rstd) a.rstd[first + r] = rstd;
+    }
+#pragma unroll
+    for (int i = 0; i < kTurns; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[i][e] = fmaf(v[i][e] * rstd, g[i][e], b[i][e]);
+    R::put(static_cast<T*>(a.y) + (first + r) * a.ldy, a.cols, v);
+    if (++stage >= kD) stage = 0;
+  }
+}
+
+// Wide rows: a block each, read again from L2 for the squares and for the result.
+template <typename T>
+__global__ void __launch_bounds__(kThreads) wide_norm_kernel(const __grid_constant__ FwdArgs a) {
   __shared__ float part[kThreads / 32];
   pdl_wait();
   pdl_trigger();
-  const int64_t row = static_cast<int64_t>(blockIdx.x) * (kThreads / TPR) + threadIdx.x / TPR;
-  const int t = threadIdx.x % TPR, turns = (a.cols + TPR * 8 - 1) / (TPR * 8);
-  if (TPR == 32 && row >= a.total) return;
-  const bool live = row < a.total;
-  const T* x = static_cast<const T*>(a.x) + (live ? row : 0) * a.ldx;
-  Held8<T> held[kKeep];
-  float sum = 0.f;
-#pragma unroll
-  for (int i = 0; i < kKeep; ++i) held[i].load(x + (i * TPR + t) * 8, a.cols - (i * TPR + t) * 8, a.xvec);
+  const int64_t row = blockIdx.x;
+  const T* x = static_cast<const T*>(a.x) + row * a.ldx;
+  T* y = static_cast<T*>(a.y) + row * a.ldy;
+  const int64_t group = row / a.rows;
+  const float *gamma = a.gamma ? a.gamma + group * a.pstride : nullptr, *beta = a.beta ? a.beta + group * a.pstride : nullptr;
   auto each = [&](auto&& f) {   // f(first column, its 8 values), zeros behind the row's end
-#pragma unroll
-    for (int i = 0; i < kKeep; ++i)
-      if ((i * TPR + t) * 8 < a.cols) {
-        float v[8];
-        held[i].get(v);
-        f((i * TPR + t) * 8, v);
-      }
-    for (int i = kKeep; i < turns; ++i) {
-      const int at = (i * TPR + t) * 8;
-      if (at >= a.cols) break;
+    for (int64_t at = threadIdx.x * 8; at < a.cols; at += kThreads * 8) {
       float v[8];
-      load8(x + at, a.cols - at, a.xvec, v);
-      f(at, v);
+      load8(x + at, a.cols - static_cast<int>(at), a.xvec, v);
+      f(static_cast<int>(at), v);
     }
   };
+  float sum = 0.f;
   each([&](int, float (&v)[8]) { sum += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7])); });
-  sum = row_sum<TPR>(sum, part);
+  sum = row_sum<kThreads>(sum, part);
   float mean = sum / a.cols;
-  if (!(fabsf(sum) < INFINITY)) {   // the sum may have left fp32 where the mean does not
+  if (!(fabsf(sum) < INFINITY)) {
     sum = 0.f;
     each([&](int, float (&v)[8]) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) sum += v[e] * 0x1p-32f;
     });
-    sum = row_sum<TPR>(sum, part);
+    sum = row_sum<kThreads>(sum, part);
     mean = sum / a.cols * 0x1p32f;
   }
   Squares sq;
@@ -111,18 +323,14 @@ __global__ void __launch_bounds__(kThreads) layer_norm_kernel(const __grid_const
     for (int e = 0; e < 8; ++e) v[e] = at + e < a.cols ? v[e] - mean : 0.f;
     sq.add(v);
   });
-  sq.mid = row_sum<TPR>(sq.mid, part);
-  sq.big = row_sum<TPR>(sq.big, part);
-  sq.small = row_sum<TPR>(sq.small, part);
-  if (!live) return;
+  sq.mid = row_sum<kThreads>(sq.mid, part);
+  sq.big = row_sum<kThreads>(sq.big, part);
+  sq.small = row_sum<kThreads>(sq.small, part);
   const float rstd = inverse_std(sq, a.cols, a.eps);
-  if (t == 0) {
+  if (threadIdx.x == 0) {
     if (a.mean) a.mean[row] = mean;
     if (a.rstd) a.rstd[row] = rstd;
   }
-  const int64_t group = row / a.rows;
-  const float *gamma = a.gamma ? a.gamma + group * a.pstride : nullptr, *beta = a.beta ? a.beta + group * a.pstride : nullptr;
-  T* y = static_cast<T*>(a.y) + row * a.ldy;
   each([&](int at, float (&v)[8]) {
     float g[8], b[8];
     params8(gamma, at, a.cols, a.pvec, 1.f, g);
@@ -133,16 +341,58 @@ __global__ void __launch_bounds__(kThreads) layer_norm_kernel(const __grid_const
   });
 }
 
-template <typename T>
-cudaError_t forward(const FwdArgs& a, cudaStream_t s) {
-  if (a.cols <= 32 * 8 * kKeep)
-    return launch_dependent(layer_norm_kernel<T, 32>, dim3(static_cast<unsigned>((a.total + 7) / 8)), kThreads, 0, s, a);
-  if (a.cols <= 128 * 8 * kKeep)
-    return launch_dependent(layer_norm_kernel<T, 128>, dim3(static_cast<unsigned>((a.total + 1) / 2)), kThreads, 0, s, a);
-  return launch_dependent(layer_norm_kernel<T, kThreads>, dim3(static_cast<unsigned>(a.total)), kThreads, 0, s, a);
+constexpr int kWide = 8192;       // columns that one pass takes
+
+// Calls f with a row's threads and each one's turns as types.  What a row costs beside its values (sums over the threads, the
+// copies' addresses) is as much as about 16 values a thread: the forward pass has 32 a thread, the backward pass, which
+// keeps more of each in registers, 16.
+template <int kTurns, typename F>
+cudaError_t by_width(int cols, F&& f) {
+  using std::integral_constant;
+  if (cols <= 256) return f(integral_constant<int, 32>(), integral_constant<int, 1>());
+  if (cols <= 512) return f(integral_constant<int, 32>(), integral_constant<int, 2>());
+  if (cols <= 1024) return f(integral_constant<int, 128 / kTurns>(), integral_constant<int, kTurns>());
+  if (cols <= 2048) return f(integral_constant<int, 256 / kTurns>(), integral_constant<int, kTurns>());
+  if (cols <= 4096) return f(integral_constant<int, 512 / kTurns>(), integral_constant<int, kTurns>());
+  return f(integral_constant<int, 1024 / kTurns>(), integral_constant<int, kTurns>());
+}
+// rows that a block takes at a time
+template <int kTurns>
+int lanes_of(int cols) {
+  int lanes = 1;
+  by_width<kTurns>(cols, [&](auto tpr, auto) {
+    lanes = kBlock / tpr();
+    return cudaSuccess;
+  });
+  return lanes;
+}
+constexpr int kForward = 4, kBackward = 2;
+
+template <typename T, bool kVec>
+cudaError_t forward_rows(const FwdArgs& a, cudaStream_t s) {
+  return by_width<kForward>(a.cols, [&](auto tpr, auto turns) {
+    constexpr int kBytes = Rows<T, tpr(), turns(), kVec, 1>::kBytes;
+    auto kernel = layer_norm_kernel<T, tpr(), turns(), kVec>;
+    const cudaError_t e = allow_smem(kernel, kBytes);
+    return e != cudaSuccess ? e : launch_dependent(kernel, dim3(static_cast<unsigned>(a.groups) * a.chunks), kBlock, kBytes, s, a);
+  });
 }
 
-// ------------------------------------------------------------------ backward
+template <typename T>
+cudaError_t forward(FwdArgs a, cudaStream_t s) {
+  if (a.cols > kWide) return launch_dependent(wide_norm_kernel<T>, dim3(static_cast<unsigned>(a.total)), kThreads, 0, s, a);
+  // a block an SM, each with a row for all of its lanes at least
+  const int lanes = lanes_of<kForward>(a.cols);
+  int64_t chunks = 152 / a.groups;
+  const int64_t most = (static_cast<int64_t>(a.rows) + lanes - 1) / lanes;
+  chunks = chunks < most ? chunks : most;
+  if (chunks < 1) chunks = 1;
+  a.per = static_cast<int>((a.rows + chunks - 1) / chunks);
+  a.chunks = (a.rows + a.per - 1) / a.per;
+  return a.xvec && a.yvec ? forward_rows<T, true>(a, s) : forward_rows<T, false>(a, s);
+}
+
+// ------------------------------------------------------------------ backward, any number of columns
 struct BwdArgs {
   const void *dy, *x;
   void* dx;
@@ -150,7 +400,7 @@ struct BwdArgs {
   float *dgamma, *dbeta, *part;       // part: [group][chunk][2][cols]
   int64_t lddy, ldx, lddx, pstride, dstride, total;
   int groups, rows, cols, chunks, per;   // per: rows of a chunk
-  int dyvec, xvec, dxvec, pvec;
+  int dyvec, xvec, dxvec, pvec, clustered;
 };
 
 template <typename T>
@@ -229,47 +479,237 @@ __global__ void __launch_bounds__(kThreads) norm_columns_kernel(const __grid_con
   }
 }
 
+// The chunks' sums of a column, eight threads a column, in a fixed order.
 __global__ void __launch_bounds__(kThreads) norm_join_kernel(const __grid_constant__ BwdArgs a) {
+  __shared__ float sums[kRowLanes][kColTile];
   pdl_wait();
   pdl_trigger();
-  const int64_t col = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
-  if (col >= a.cols) return;
+  const int c = threadIdx.x % kColTile, lane = threadIdx.x / kColTile;
+  const int64_t col = static_cast<int64_t>(blockIdx.x) * kColTile + c;
   const int group = blockIdx.z, which = blockIdx.y;
   float* to = which == 0 ? a.dgamma : a.dbeta;
   if (!to) return;
-  const float* from = a.part + (static_cast<int64_t>(group) * a.chunks * 2 + which) * a.cols + col;
   float s = 0.f;
-  for (int i = 0; i < a.chunks; ++i) s += from[static_cast<int64_t>(i) * 2 * a.cols];
-  to[group * a.dstride + col] = s;
+  if (col < a.cols) {
+    const float* from = a.part + (static_cast<int64_t>(group) * a.chunks * 2 + which) * a.cols + col;
+#pragma unroll 8
+    for (int i = lane; i < a.chunks; i += kRowLanes) s += from[static_cast<int64_t>(i) * 2 * a.cols];
+  }
+  sums[lane][c] = s;
+  __syncthreads();
+  if (lane == 0 && col < a.cols) {
+    s = 0.f;
+#pragma unroll
+    for (int i = 0; i < kRowLanes; ++i) s += sums[i][c];
+    to[group * a.dstride + col] = s;
+  }
 }
 
-// Rows of a chunk: chunks enough to fill the card, each of 64 rows or more.
-void split_rows(int groups, int rows, int cols, int& chunks, int& per) {
-  const int64_t tiles = (static_cast<int64_t>(cols) + kColTile - 1) / kColTile * groups;
-  int64_t want = (1216 + tiles - 1) / tiles;
-  const int64_t most = (static_cast<int64_t>(rows) + 63) / 64;
+// ------------------------------------------------------------------ backward, up to 8192 columns
+// One pass: a CTA takes a chunk of a group's rows, and a thread's columns' sums over them stay in its registers.
+// A group's chunks meet in a cluster of up to eight CTAs, or, of a large call, in the workspace and a second kernel.
+template <typename T, int TPR, int kTurns, bool kVec>
+constexpr int backward_smem() {
+  using R = Rows<T, TPR, kTurns, kVec, 2>;
+  constexpr int sums = 2 * R::kLanes * R::kCap * 4;   // at the end
+  return R::kBytes > sums ? R::kBytes : sums;
+}
+
+template <typename T, int TPR, int kTurns, bool kVec>
+__global__ void __launch_bounds__(kBlock, 1) norm_backward_kernel(const __grid_constant__ BwdArgs a) {
+  using R = Rows<T, TPR, kTurns, kVec, 2>;
+  constexpr int kLanes = R::kLanes, kD = R::kDepth, kCap = R::kCap;
+  extern __shared__ __align__(16) uint8_t bwd_smem[];
+  __shared__ float parts[2][kBlock / 32][2];
+  const int lane = threadIdx.x / TPR;
+  const int group = blockIdx.x / a.chunks, chunk = blockIdx.x % a.chunks;
+  const int r1 = min((chunk + 1) * a.per, a.rows);
+  const int64_t first = static_cast<int64_t>(group) * a.rows;
+  if (a.clustered) cluster_arrive();   // waited for before the sums of the peers are read
+  pdl_wait();
+  pdl_trigger();
+  const T *dy = static_cast<const T*>(a.dy) + first * a.lddy, *x = static_cast<const T*>(a.x) + first * a.ldx;
+  auto request = [&](int r, int stage) {
+    if constexpr (kVec) {
+      if (r < r1) {
+        R::request(bwd_smem, stage, 0, dy + r * a.lddy, a.cols);
+        R::request(bwd_smem, stage, 1, x + r * a.ldx, a.cols);
+      }
+      copies_done();
+    }
+  };
+  float dg[kTurns][8] = {}, db[kTurns][8] = {};
+  int r = chunk * a.per + lane;
+#pragma unroll
+  for (int i = 0; i < kD - 1; ++i) request(r + i * kLanes, i);
+  float g[kTurns][8];
+  R::params(a.gamma ? a.gamma + group * a.pstride : nullptr, a.cols, a.pvec, 1.f, g);
+  float mean = r < r1 ? a.mean[first + r] : 0.f, rstd = r < r1 ? a.rstd[first + r] : 0.f;
+  const float each = 1.f / a.cols;
+  for (int it = 0, stage = 0; r < r1; r += kLanes, ++it) {
+    if constexpr (kVec) {
+      request(r + (kD - 1) * kLanes, stage == 0 ? kD - 1 : stage - 1);
+      copies_wait<kD - 1>();
+    }
+    float h[kTurns][8], xh[kTurns][8];
+    R::take(bwd_smem, stage, 0, dy + r * a.lddy, a.cols, h);
+    R::take(bwd_smem, stage, 1, x + r * a.ldx, a.cols, xh);
+    const float mu = mean, rs = rstd;
+    if (r + kLanes < r1) {
+      mean = a.mean[first + r + kLanes];
+      rstd = a.rstd[first + r + kLanes];
+    }
+    float sh = 0.f, shx = 0.f;
+#pragma unroll
+    for (int i = 0; i < kTurns; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        xh[i][e] = (xh[i][e] - mu) * rs;
+        dg[i][e] = fmaf(h[i][e], xh[i][e], dg[i][e]);
+        db[i][e] += h[i][e];
+        h[i][e] *= g[i][e];
+        sh += h[i][e];
+        shx = fmaf(h[i][e], xh[i][e], shx);
+      }
+    if (a.dx) {
+      float mean_of[2] = {sh, shx};
+      row_sums<TPR>(mean_of, parts[it & 1]);
+      sh = mean_of[0] * each;
+      shx = mean_of[1] * each;
+#pragma unroll
+      for (int i = 0; i < kTurns; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) h[i][e] = rs * (h[i][e] - sh - xh[i][e] * shx);
+      R::put(static_cast<T*>(a.dx) + (first + r) * a.lddx, a.cols, h);
+    }
+    if (++stage >= kD) stage = 0;
+  }
+  if (!a.dgamma && !a.dbeta) {
+    if (a.clustered) cluster_wait();
+    return;
+  }
+
+  // the rows' lanes, then the chunks
+  if constexpr (kVec) copies_wait<0>();
+  __syncthreads();
+  float* sums = reinterpret_cast<float*>(bwd_smem);   // [2][kLanes][kCap]
+#pragma unroll
+  for (int i = 0; i < kTurns; ++i)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      sums[lane * kCap + R::column(i, e)] = dg[i][e];
+      sums[(kLanes + lane) * kCap + R::column(i, e)] = db[i][e];
+    }
+  __syncthreads();
+  for (int i = threadIdx.x; i < 2 * kCap; i += kBlock) {
+    const int which = i / kCap, c = i % kCap;
+    if (c >= a.cols) continue;
+    float* at = sums + which * kLanes * kCap + c;
+    float s = 0.f;
+#pragma unroll
+    for (int l = 0; l < kLanes; ++l) s += at[l * kCap];
+    if (a.clustered) {
+      *at = s;
+    } else {
+      float* to = a.chunks > 1 ? a.part + ((static_cast<int64_t>(group) * a.chunks + chunk) * 2 + which) * a.cols
+                               : (which == 0 ? a.dgamma : a.dbeta);
+      if (to) to[(a.chunks > 1 ? 0 : group * a.dstride) + c] = s;
+    }
+  }
+  if (a.clustered) {
+    cluster_wait();    // every CTA of the cluster runs
+    cluster_sync();    // and has its sums
+    for (int i = chunk * kBlock + threadIdx.x; i < 2 * a.cols; i += a.chunks * kBlock) {
+      const int which = i >= a.cols, c = i - which * a.cols;
+      float s = 0.f;
+      for (int k = 0; k < a.chunks; ++k) s += ld_dsmem_f32(sums + which * kLanes * kCap + c, k);
+      float* to = which == 0 ? a.dgamma : a.dbeta;
+      if (to) to[group * a.dstride + c] = s;
+    }
+    cluster_sync();    // no CTA ends while its sums are read
+  }
+}
+
+// ------------------------------------------------------------------ backward, how it is split
+constexpr int kCtas = 152;        // chunks of all groups: one CTA an SM
+constexpr int kCluster = 8;
+
+struct Split {
+  int chunks, per, clustered;
+};
+// One pass: a chunk for each SM, each with a row for all of its lanes at least.  Up to 16 chunks of a group are made eight, which
+// meet in a cluster: no second launch.
+// Wide rows: chunks of columns' tiles enough to fill the card, each of 64 rows or more.
+Split split_rows(int groups, int rows, int cols) {
+  int64_t want, most;
+  if (cols <= kWide) {
+    const int lanes = lanes_of<kBackward>(cols);
+    want = kCtas / groups;
+    most = (static_cast<int64_t>(rows) + lanes - 1) / lanes;
+  } else {
+    const int64_t tiles = (static_cast<int64_t>(cols) + kColTile - 1) / kColTile * groups;
+    want = (1216 + tiles - 1) / tiles;
+    most = (static_cast<int64_t>(rows) + 63) / 64;
+  }
   want = want < most ? want : most;
   if (want < 1) want = 1;
-  per = static_cast<int>((rows + want - 1) / want);
-  if (per < 1) per = 1;
-  chunks = rows > 0 ? (rows + per - 1) / per : 1;
+  if (cols <= kWide && want > kCluster && want <= 2 * kCluster) want = kCluster;
+  Split s;
+  s.per = static_cast<int>((rows + want - 1) / want);
+  if (s.per < 1) s.per = 1;
+  s.chunks = rows > 0 ? (rows + s.per - 1) / s.per : 1;
+  s.clustered = cols <= kWide && s.chunks > 1 && s.chunks <= kCluster;
+  return s;
 }
 
 int64_t workspace_bytes_of(int groups, int rows, int cols) {
-  int chunks, per;
-  split_rows(groups, rows, cols, chunks, per);
-  return chunks > 1 ? static_cast<int64_t>(groups) * chunks * 2 * cols * 4 : 0;
+  const Split s = split_rows(groups, rows, cols);
+  return s.chunks > 1 && !s.clustered ? static_cast<int64_t>(groups) * s.chunks * 2 * cols * 4 : 0;
+}
+
+template <typename T, bool kVec>
+cudaError_t one_pass(const BwdArgs& a, cudaStream_t s) {
+  return by_width<kBackward>(a.cols, [&](auto tpr, auto turns) {
+    constexpr int kBytes = backward_smem<T, tpr(), turns(), kVec>();
+    auto kernel = norm_backward_kernel<T, tpr(), turns(), kVec>;
+    const cudaError_t e = allow_smem(kernel, kBytes);
+    if (e != cudaSuccess) return e;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = a.chunks;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(a.groups) * a.chunks);
+    cfg.blockDim = dim3(kBlock);
+    cfg.dynamicSmemBytes = kBytes;
+    cfg.stream = s;
+    cfg.attrs = attr;
+    cfg.numAttrs = a.clustered ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kernel, a);
+  });
 }
 
 template <typename T>
 cudaError_t backward(BwdArgs a, cudaStream_t s) {
-  cudaError_t e = cudaSuccess;
-  if (a.dgamma || a.dbeta) {
-    split_rows(a.groups, a.rows, a.cols, a.chunks, a.per);
-    const dim3 grid((a.cols + kColTile - 1) / kColTile, a.chunks, a.groups);
-    e = launch_dependent(norm_columns_kernel<T>, grid, kThreads, 0, s, a);
-    if (e == cudaSuccess && a.chunks > 1)
-      e = launch_dependent(norm_join_kernel, dim3((a.cols + kThreads - 1) / kThreads, 2, a.groups), kThreads, 0, s, a);
+  const Split split = split_rows(a.groups, a.rows, a.cols);
+  a.chunks = split.chunks;
+  a.per = split.per;
+  a.clustered = split.clustered;
+  const bool params = a.dgamma || a.dbeta;
+  const dim3 join((a.cols + kColTile - 1) / kColTile, 2, a.groups);
+  cudaError_t e;
+  if (a.cols <= kWide) {
+    e = a.dyvec && a.xvec && (!a.dx || a.dxvec) ? one_pass<T, true>(a, s) : one_pass<T, false>(a, s);
+    if (e == cudaSuccess && params && a.chunks > 1 && !a.clustered) e = launch_dependent(norm_join_kernel, join, kThreads, 0, s, a);
+    return e;
+  }
+  e = cudaSuccess;
+  if (params) {
+    e = launch_dependent(norm_columns_kernel<T>, dim3((a.cols + kColTile - 1) / kColTile, a.chunks, a.groups), kThreads, 0, s, a);
+    if (e == cudaSuccess && a.chunks > 1) e = launch_dependent(norm_join_kernel, join, kThreads, 0, s, a);
   }
   if (e == cudaSuccess && a.dx && a.total > 0)
     e = launch_dependent(norm_dx_kernel<T>, dim3(static_cast<unsigned>(a.total)), kThreads, 0, s, a);
@@ -301,7 +741,7 @@ oscars_status oscars_layer_norm(const void* x, int64_t ldx, const float* gamma, 
       !at_bytes(rstd, 4) || (x == y && ldx != ldy))
     return OSCARS_EINVAL;
   FwdArgs a{x, y, gamma, beta, mean, rstd, ldx, ldy, param_stride, static_cast<int64_t>(groups) * rows, rows, cols, eps,
-            rows_16(x, ldx, size), rows_16(y, ldy, size), rows_16(gamma, param_stride, 4) && at_bytes(beta, 16)};
+            rows_16(x, ldx, size), rows_16(y, ldy, size), rows_16(gamma, param_stride, 4) && at_bytes(beta, 16), groups, 0, 0};
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const cudaError_t e = dtype == OSCARS_F32 ? forward<float>(a, s) : forward<__nv_bfloat16>(a, s);
   return e == cudaSuccess ? OSCARS_OK : OSCARS_ECUDA;
