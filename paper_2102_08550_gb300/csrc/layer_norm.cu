@@ -94,59 +94,61 @@ struct Rows {
     }
   }
   // this thread's columns of it (zeros behind the row's end)
-  __device__ __forceinline__ static void take(const uint8_t* ring, int stage, int m, const T* row, int cols, float (&v)[kTurns][8]) {
+  __device__ __forceinline__ static void take(const uint8_t* ring, int stage, int m, const T* row, int cols, float2 (&v)[kTurns][4]) {
     if constexpr (kVec) {
 #pragma unroll
       for (int p = 0; p < kPieces; ++p) {
         const uint4 w = *reinterpret_cast<const uint4*>(ring + stage * kStage + ((m * kPieces + p) * kBlock + threadIdx.x) * 16);
         const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+        if constexpr (sizeof(T) == 4) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if constexpr (sizeof(T) == 4) {
-            v[p / 2][p % 2 * 4 + i] = __uint_as_float(u[i]);
-          } else {
-            v[p][2 * i] = __uint_as_float(u[i] << 16);
-            v[p][2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
-          }
+          for (int i = 0; i < 2; ++i) v[p / 2][p % 2 * 2 + i] = make_float2(__uint_as_float(u[2 * i]), __uint_as_float(u[2 * i + 1]));
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v[p][i] = make_float2(__uint_as_float(u[i] << 16), __uint_as_float(u[i] & 0xFFFF0000u));
         }
       }
     } else {
 #pragma unroll
       for (int i = 0; i < kTurns; ++i)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[i][e] = column(i, e) < cols ? to_f32(row[column(i, e)]) : 0.f;
+        for (int e = 0; e < 4; ++e)
+          v[i][e] = make_float2(column(i, 2 * e) < cols ? to_f32(row[column(i, 2 * e)]) : 0.f,
+                                column(i, 2 * e + 1) < cols ? to_f32(row[column(i, 2 * e + 1)]) : 0.f);
     }
   }
-  __device__ __forceinline__ static void put(T* row, int cols, float (&v)[kTurns][8]) {
-    if (kVec && inside(cols)) {
-#pragma unroll
-      for (int i = 0; i < kTurns; ++i) store8(row + column(i, 0), 8, true, v[i]);
-      return;
-    }
+  __device__ __forceinline__ static void put(T* row, int cols, const float2 (&v)[kTurns][4]) {
+    const bool all = inside(cols);
 #pragma unroll
     for (int i = 0; i < kTurns; ++i) {
+      const float w[8] = {v[i][0].x, v[i][0].y, v[i][1].x, v[i][1].y, v[i][2].x, v[i][2].y, v[i][3].x, v[i][3].y};
       if constexpr (kVec) {
-        store8(row + column(i, 0), cols - column(i, 0), true, v[i]);
+        store8(row + column(i, 0), all ? 8 : cols - column(i, 0), true, w);
       } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-          if (column(i, e) < cols) row[column(i, e)] = static_cast<T>(v[i][e]);
+          if (column(i, e) < cols) row[column(i, e)] = static_cast<T>(w[e]);
       }
     }
   }
   // a group's parameters, or `none` if there are none
-  __device__ __forceinline__ static void params(const float* p, int cols, bool vec, float none, float (&v)[kTurns][8]) {
+  __device__ __forceinline__ static void params(const float* p, int cols, bool vec, float none, float2 (&v)[kTurns][4]) {
 #pragma unroll
     for (int i = 0; i < kTurns; ++i) {
+      float w[8];
       if constexpr (kVec) {
-        params8(p, column(i, 0), cols, vec, none, v[i]);
+        params8(p, column(i, 0), cols, vec, none, w);
       } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[i][e] = p && column(i, e) < cols ? p[column(i, e)] : none;
+        for (int e = 0; e < 8; ++e) w[e] = p && column(i, e) < cols ? p[column(i, e)] : none;
       }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[i][e] = make_float2(w[2 * e], w[2 * e + 1]);
     }
   }
 };
+
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
 
 // Sums of N values over a row's threads, in each of them, in a fixed order.  `parts` alternates between two places, so that one
 // barrier is enough: a sum's parts are read before those of the one after the next are written.
@@ -219,7 +221,7 @@ __global__ void __launch_bounds__(kBlock, 1) layer_norm_kernel(const __grid_cons
   int r = chunk * a.per + lane;
 #pragma unroll
   for (int i = 0; i < kD - 1; ++i) request(r + i * R::kLanes, i);
-  float g[kTurns][8], b[kTurns][8];
+  float2 g[kTurns][4], b[kTurns][4];
   R::params(a.gamma ? a.gamma + group * a.pstride : nullptr, a.cols, a.pvec, 1.f, g);
   R::params(a.beta ? a.beta + group * a.pstride : nullptr, a.cols, a.pvec, 0.f, b);
   const float each = 1.f / a.cols;
@@ -229,11 +231,12 @@ __global__ void __launch_bounds__(kBlock, 1) layer_norm_kernel(const __grid_cons
       request(r + (kD - 1) * R::kLanes, stage == 0 ? kD - 1 : stage - 1);
       copies_wait<kD - 1>();
     }
-    float v[kTurns][8];
+    float2 v[kTurns][4];
     R::take(fwd_smem, stage, 0, x + r * a.ldx, a.cols, v);
-    float sum[1] = {0.f}, none[1] = {0.f};
+    float2 pair = both(0.f);
 #pragma unroll
-    for (int i = 0; i < kTurns; ++i) sum[0] += ((v[i][0] + v[i][1]) + (v[i][2] + v[i][3])) + ((v[i][4] + v[i][5]) + (v[i][6] + v[i][7]));
+    for (int i = 0; i < kTurns; ++i) pair = __fadd2_rn(pair, __fadd2_rn(__fadd2_rn(v[i][0], v[i][1]), __fadd2_rn(v[i][2], v[i][3])));
+    float sum[1] = {pair.x + pair.y}, none[1] = {0.f};
     row_sums<TPR>(sum, parts[0]);
     float mean = sum[0] * each;
     mean = fmaf(fmaf(-mean, static_cast<float>(a.cols), sum[0]), each, mean);   // the quotient, whatever 1 / cols was rounded to
@@ -242,7 +245,7 @@ __global__ void __launch_bounds__(kBlock, 1) layer_norm_kernel(const __grid_cons
 #pragma unroll
       for (int i = 0; i < kTurns; ++i)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sum[0] += v[i][e] * 0x1p-32f;
+        for (int e = 0; e < 4; ++e) sum[0] += v[i][e].x * 0x1p-32f + v[i][e].y * 0x1p-32f;
       row_sums<TPR>(sum, parts[1]);
       mean = sum[0] / a.cols * 0x1p32f;
       row_sums<TPR>(none, parts[0]);   // keeps the two places in turn
@@ -250,18 +253,23 @@ __global__ void __launch_bounds__(kBlock, 1) layer_norm_kernel(const __grid_cons
     Squares sq;
 #pragma unroll
     for (int i = 0; i < kTurns; ++i) {
-      if (full) {
+      float2 s = both(0.f);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[i][e] -= mean;
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[i][e] = R::column(i, e) < a.cols ? v[i][e] - mean : 0.f;
+      for (int e = 0; e < 4; ++e) {
+        v[i][e] = __fadd2_rn(v[i][e], both(-mean));
+        if (!full) {
+          if (R::column(i, 2 * e) >= a.cols) v[i][e].x = 0.f;
+          if (R::column(i, 2 * e + 1) >= a.cols) v[i][e].y = 0.f;
+        }
+        s = __ffma2_rn(v[i][e], v[i][e], s);
       }
-      float s = 0.f;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) s = fmaf(v[i][e], v[i][e], s);
-      if (s > 1e-20f && s < 1e25f) sq.mid += s;
-      else sq.add(v[i]);
+      const float t8 = s.x + s.y;
+      if (t8 > 1e-20f && t8 < 1e25f) {
+        sq.mid += t8;
+      } else {
+        const float w[8] = {v[i][0].x, v[i][0].y, v[i][1].x, v[i][1].y, v[i][2].x, v[i][2].y, v[i][3].x, v[i][3].y};
+        sq.add(w);
+      }
     }
     float two[2] = {sq.mid, sq.big != 0.f || sq.small != 0.f ? 1.f : 0.f};
     row_sums<TPR>(two, parts[1]);
@@ -280,7 +288,7 @@ __global__ void __launch_bounds__(kBlock, 1) layer_norm_kernel(const __grid_cons
 #pragma unroll
     for (int i = 0; i < kTurns; ++i)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[i][e] = fmaf(v[i][e] * rstd, g[i][e], b[i][e]);
+      for (int e = 0; e < 4; ++e) v[i][e] = __ffma2_rn(__fmul2_rn(v[i][e], both(rstd)), g[i][e], b[i][e]);
     R::put(static_cast<T*>(a.y) + (first + r) * a.ldy, a.cols, v);
     if (++stage >= kD) stage = 0;
   }
@@ -538,11 +546,11 @@ __global__ void __launch_bounds__(kBlock, 1) norm_backward_kernel(const __grid_c
       copies_done();
     }
   };
-  float dg[kTurns][8] = {}, db[kTurns][8] = {};
+  float2 dg[kTurns][4] = {}, db[kTurns][4] = {};
   int r = chunk * a.per + lane;
 #pragma unroll
   for (int i = 0; i < kD - 1; ++i) request(r + i * kLanes, i);
-  float g[kTurns][8];
+  float2 g[kTurns][4];
   R::params(a.gamma ? a.gamma + group * a.pstride : nullptr, a.cols, a.pvec, 1.f, g);
   float mean = r < r1 ? a.mean[first + r] : 0.f, rstd = r < r1 ? a.rstd[first + r] : 0.f;
   const float each = 1.f / a.cols;
@@ -551,7 +559,7 @@ __global__ void __launch_bounds__(kBlock, 1) norm_backward_kernel(const __grid_c
       request(r + (kD - 1) * kLanes, stage == 0 ? kD - 1 : stage - 1);
       copies_wait<kD - 1>();
     }
-    float h[kTurns][8], xh[kTurns][8];
+    float2 h[kTurns][4], xh[kTurns][4];
     R::take(bwd_smem, stage, 0, dy + r * a.lddy, a.cols, h);
     R::take(bwd_smem, stage, 1, x + r * a.ldx, a.cols, xh);
     const float mu = mean, rs = rstd;
@@ -559,27 +567,26 @@ __global__ void __launch_bounds__(kBlock, 1) norm_backward_kernel(const __grid_c
       mean = a.mean[first + r + kLanes];
       rstd = a.rstd[first + r + kLanes];
     }
-    float sh = 0.f, shx = 0.f;
+    float2 sh = both(0.f), shx = both(0.f);
 #pragma unroll
     for (int i = 0; i < kTurns; ++i)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        xh[i][e] = (xh[i][e] - mu) * rs;
-        dg[i][e] = fmaf(h[i][e], xh[i][e], dg[i][e]);
-        db[i][e] += h[i][e];
-        h[i][e] *= g[i][e];
-        sh += h[i][e];
-        shx = fmaf(h[i][e], xh[i][e], shx);
+      for (int e = 0; e < 4; ++e) {
+        xh[i][e] = __fmul2_rn(__fadd2_rn(xh[i][e], both(-mu)), both(rs));
+        dg[i][e] = __ffma2_rn(h[i][e], xh[i][e], dg[i][e]);
+        db[i][e] = __fadd2_rn(db[i][e], h[i][e]);
+        h[i][e] = __fmul2_rn(h[i][e], g[i][e]);
+        sh = __fadd2_rn(sh, h[i][e]);
+        shx = __ffma2_rn(h[i][e], xh[i][e], shx);
       }
     if (a.dx) {
-      float mean_of[2] = {sh, shx};
-      row_sums<TPR>(mean_of, parts[it & 1]);
-      sh = mean_of[0] * each;
-      shx = mean_of[1] * each;
+      float means[2] = {sh.x + sh.y, shx.x + shx.y};
+      row_sums<TPR>(means, parts[it & 1]);
+      const float2 mh = both(-means[0] * each), mhx = both(-means[1] * each);
 #pragma unroll
       for (int i = 0; i < kTurns; ++i)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) h[i][e] = rs * (h[i][e] - sh - xh[i][e] * shx);
+        for (int e = 0; e < 4; ++e) h[i][e] = __fmul2_rn(both(rs), __ffma2_rn(xh[i][e], mhx, __fadd2_rn(h[i][e], mh)));
       R::put(static_cast<T*>(a.dx) + (first + r) * a.lddx, a.cols, h);
     }
     if (++stage >= kD) stage = 0;
@@ -597,8 +604,8 @@ __global__ void __launch_bounds__(kBlock, 1) norm_backward_kernel(const __grid_c
   for (int i = 0; i < kTurns; ++i)
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      sums[lane * kCap + R::column(i, e)] = dg[i][e];
-      sums[(kLanes + lane) * kCap + R::column(i, e)] = db[i][e];
+      sums[lane * kCap + R::column(i, e)] = e % 2 == 0 ? dg[i][e / 2].x : dg[i][e / 2].y;
+      sums[(kLanes + lane) * kCap + R::column(i, e)] = e % 2 == 0 ? db[i][e / 2].x : db[i][e / 2].y;
     }
   __syncthreads();
   for (int i = threadIdx.x; i < 2 * kCap; i += kBlock) {
