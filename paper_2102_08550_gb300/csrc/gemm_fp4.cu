@@ -9,7 +9,8 @@
 //
 // gemm_fp4_kernel: tcgen05 (kind::mxf4nvf4), persistent, one CTA per SM or a pair (cta_group::2), 20 warps:
 //   0       TMA of codes (128 channels and BN tokens, 256 of K) and of their scales into a ring
-//   1       copies a stage's scales to tensor memory and issues its products
+//   1       issues a stage's products
+//   3       copies its scales to tensor memory before that
 //   4-19    accumulators -> C, under the products of the next tile
 // gemm_fp4_few_kernel for one or two tokens.
 #include <atomic>
@@ -115,11 +116,11 @@ static_assert(no_cluster_beside(kLeast), "no other cluster's CTA beside this ker
 constexpr int kScaleCol = 256;                   // tensor memory: accumulators in front of it, scales of the stages behind
 
 struct Tile {
-  int BN, nt, mt, units, split, stages, accs, chunk;   // chunk: K-blocks that one accumulation takes
+  int BN, nt, mt, units, split, stages, accs;   // accs: accumulators
 };
 
 struct Bars {
-  uint64_t full[kMaxStages], empty[kMaxStages], accf[2], acce[2];
+  uint64_t full[kMaxStages], scaled[kMaxStages], empty[kMaxStages], accf[2], acce[2];
   uint32_t tmem;
   int failed;   // kSplit: a part's sums are not all there
 };
@@ -163,6 +164,10 @@ __device__ __forceinline__ void umma_commit_pair(uint64_t* bar) {
           smem_u32(bar)),
       "h"(static_cast<uint16_t>(0x3))
       : "memory");
+}
+// the same, on this CTA's barrier alone
+__device__ __forceinline__ void umma_commit_here(uint64_t* bar) {
+  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
 // An arrival on a barrier of the pair's leader, released at CTA scope: all that it has to come after are reads of this SM's
 // tensor memory, which tcgen05.wait::ld has seen finished (gemm_i8.cu).
@@ -244,6 +249,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp4_kernel(const __grid_cons
     prefetch_tmap(&mapSX);
     for (int i = 0; i < p.stages; ++i) {
       mbar_init(&bars->full[i], 1);
+      mbar_init(&bars->scaled[i], 1);
       mbar_init(&bars->empty[i], 1);
     }
     for (int i = 0; i < 2; ++i) {
@@ -305,52 +311,75 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp4_kernel(const __grid_cons
       for (int i = it > p.stages ? it - p.stages : 0; i < it; ++i)
         mbar_wait_keep(limit, &bars->full[i % p.stages], (i / p.stages) & 1, nullptr, kDevTimeoutFull);
   } else if (warp == 1 && rank == 0) {
-    // ---- scales to tensor memory, products (the leader's, of a pair); the warp stays converged and one elected lane issues
+    // ---- products (the leader's, of a pair); the warp stays converged and one elected lane issues
     const uint32_t idesc = idesc_fp4(128 * CL, p.BN, kMx), ring0 = smem_u32(ring);
     const int cols = (1 + xt) * kTk * 4;           // of a stage's scales
-    int s = 0, ph = 0, t = 0;                      // t: accumulations begun
+    int s = 0, ph = 0, t = 0;                      // t: tiles begun
     uint32_t limit = kSpinLimit;
-    for (int u = u0; u < p.units; u += ustep) {
-      for (int c0 = k0; c0 < k1; c0 += p.chunk, ++t) {
-        const int b = t % p.accs, c1 = c0 + p.chunk < k1 ? c0 + p.chunk : k1;
-        if (t >= p.accs) mbar_wait_keep(limit, &bars->acce[b], (t / p.accs + 1) & 1, nullptr, kDevTimeoutAccum);
+    for (int u = u0; u < p.units; u += ustep, ++t) {
+      const int b = t % p.accs;
+      if (t >= p.accs) mbar_wait_keep(limit, &bars->acce[b], (t / p.accs + 1) & 1, nullptr, kDevTimeoutAccum);
+      tc_fence_after();
+      const uint32_t acc = tmem + b * 128;
+      for (int kb = k0; kb < k1; ++kb) {
+        mbar_wait_keep(limit, &bars->scaled[s], ph, nullptr, kDevTimeoutFull);
         tc_fence_after();
-        const uint32_t acc = tmem + b * 128;
-        for (int kb = c0; kb < c1; ++kb) {
-          mbar_wait_keep(limit, &bars->full[s], ph, nullptr, kDevTimeoutFull);
-          tc_fence_after();
-          if (elect_one() && limit > 1) {
-            const uint32_t at = ring0 + s * stage_bytes, sw = tmem + kScaleCol + s * cols, sx = sw + 4 * kTk;
-            const uint64_t wd = smem_desc_k128(at), xd = smem_desc_k128(at + x_at);
-            const uint64_t swd = scale_desc(at + sw_at), sxd = scale_desc(at + sx_at);
-            const int left = a.K - kb * kK, n = left >= kK ? 4 : (left + 63) / 64;
-            // a stage's columns were last read by products that have ended: its copies have been waited for
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-              if (j < n) {
-                const int tile = kMx ? j / 2 : j;
-                if (!kMx || j % 2 == 0) {
-                  copy_scales<CL>(sw + 4 * tile, swd + tile * 32);
-                  for (int i = 0; i < xt; ++i) copy_scales<CL>(sx + 4 * (tile * xt + i), sxd + (i * kTk + tile) * 32);
-                }
-                umma_fp4<CL, kMx>(acc, wd + 2 * j, xd + 2 * j, idesc | (kMx ? scale_id(j % 2 * 2) : 0), sw + 4 * tile, sx + 4 * tile * xt, (kb > c0) | (j > 0));
-              }
-            if (CL > 1) umma_commit_pair(&bars->empty[s]);
-            else umma_commit(&bars->empty[s]);
-          }
-          __syncwarp();
-          if (++s == p.stages) {
-            s = 0;
-            ph ^= 1;
-          }
-        }
         if (elect_one() && limit > 1) {
-          if (CL > 1) umma_commit_pair(&bars->accf[b]);
-          else umma_commit(&bars->accf[b]);
+          const uint32_t at = ring0 + s * stage_bytes, sw = tmem + kScaleCol + s * cols, sx = sw + 4 * kTk;
+          const uint64_t wd = smem_desc_k128(at), xd = smem_desc_k128(at + x_at);
+          const int left = a.K - kb * kK, n = left >= kK ? 4 : (left + 63) / 64;
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (j < n) {
+              const int tile = kMx ? j / 2 : j;
+              umma_fp4<CL, kMx>(acc, wd + 2 * j, xd + 2 * j, idesc | (kMx ? scale_id(j % 2 * 2) : 0), sw + 4 * tile, sx + 4 * tile * xt,
+                                (kb > k0) | (j > 0));
+            }
+          if (CL > 1) umma_commit_pair(&bars->empty[s]);
+          else umma_commit(&bars->empty[s]);
         }
         __syncwarp();
+        if (++s == p.stages) {
+          s = 0;
+          ph ^= 1;
+        }
       }
+      if (elect_one() && limit > 1) {
+        if (CL > 1) umma_commit_pair(&bars->accf[b]);
+        else umma_commit(&bars->accf[b]);
+      }
+      __syncwarp();
     }
+  } else if (warp == 3 && rank == 0) {
+    // ---- scales to tensor memory, ahead of the products
+    const uint32_t ring0 = smem_u32(ring);
+    const int cols = (1 + xt) * kTk * 4;
+    int s = 0, ph = 0;
+    uint32_t limit = kSpinLimit;
+    for (int u = u0; u < p.units; u += ustep)
+      for (int kb = k0; kb < k1; ++kb) {
+        // a stage's columns were last read by products that have ended: its copies were begun after those
+        mbar_wait_keep(limit, &bars->full[s], ph, nullptr, kDevTimeoutFull);
+        tc_fence_after();
+        if (elect_one() && limit > 1) {
+          const uint32_t at = ring0 + s * stage_bytes, sw = tmem + kScaleCol + s * cols, sx = sw + 4 * kTk;
+          const uint64_t swd = scale_desc(at + sw_at), sxd = scale_desc(at + sx_at);
+          const int left = a.K - kb * kK, n = left >= kK ? 4 : (left + 63) / 64;
+#pragma unroll
+          for (int j = 0; j < kTk; ++j)
+            if (j * (kMx ? 2 : 1) < n) {
+              copy_scales<CL>(sw + 4 * j, swd + j * 32);
+              for (int i = 0; i < xt; ++i) copy_scales<CL>(sx + 4 * (j * xt + i), sxd + (i * kTk + j) * 32);
+            }
+          if (CL > 1) umma_commit_here(&bars->scaled[s]);
+          else umma_commit(&bars->scaled[s]);
+        }
+        __syncwarp();
+        if (++s == p.stages) {
+          s = 0;
+          ph ^= 1;
+        }
+      }
   } else if (warp >= 4) {
     // ---- C: thread = one channel and a quarter of the tile's tokens (16 of fewer than 64)
     const int quarter = warp & 3, span = p.BN > 64 ? p.BN / 4 : 16, cb = (warp / 4 - 1) * span;
@@ -374,22 +403,13 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp4_kernel(const __grid_cons
         far = __any_sync(0xffffffffu, far);
       }
       float sum[kSpan / 16][16];
-#pragma unroll
-      for (int g = 0; g < kSpan / 16; ++g)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) sum[g][e] = 0.f;
-      for (int c0 = k0; c0 < k1; c0 += p.chunk, ++t) {
-        const int b = t % p.accs;
-        if (!(ok = mbar_wait_warp(&bars->accf[b], (t / p.accs) & 1, nullptr, kDevTimeoutAccum))) break;
-        tc_fence_after();
+      const int b = t % p.accs;
+      ok = mbar_wait_warp(&bars->accf[b], (t / p.accs) & 1, nullptr, kDevTimeoutAccum);
+      tc_fence_after();
+      if (ok) {
 #pragma unroll
         for (int g = 0; g < kSpan / 16; ++g)
-          if (works && 16 * g < span) {
-            float v[16];
-            tmem_ld_32x32b_x16(row0 + b * 128 + 16 * g, v);
-#pragma unroll
-            for (int e = 0; e < 16; ++e) sum[g][e] += v[e];
-          }
+          if (works && 16 * g < span) tmem_ld_32x32b_x16(row0 + b * 128 + 16 * g, sum[g]);
         tc_fence_before();
         __syncwarp();
         if (lane == 0) {
@@ -397,6 +417,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp4_kernel(const __grid_cons
           else mbar_arrive(&bars->acce[b]);
         }
       }
+      ++t;
       if (!ok) {   // every wait that runs out in this CTA ends in one of the accumulator's; its peers then leave the tile alone too
         if (kSplit && lane < p.split) st_peer(&bars->failed, lane, 1);
         break;
@@ -557,7 +578,6 @@ void choose(const Fp4Args& a, int sms, int pairs, Tile& p, int& cl) {
     }
   }
   p.accs = p.BN > 128 ? 1 : 2;
-  p.chunk = nk;
 }
 
 template <bool kMx>
