@@ -4,13 +4,14 @@
 //
 // A product of two codes is a multiple of 1/4 up to 36, so a block's sum is exact in fp32.
 //
-// The product is computed as rows = channels (B), columns = tokens (A): the accumulator's lanes then run along a row of C,
-// so that a store of a token's 32 channels is coalesced as it leaves the registers, whatever C's alignment.
+// Which operand gives the accumulator's rows (its lanes, 128 a CTA) and which its columns is chosen for each call.  With channels
+// as rows, the lanes run along a row of C, so that a store of a token's 32 channels is coalesced as it leaves the registers,
+// whatever C's alignment.  With tokens as rows, a thread holds a piece of a row of C, which goes through shared memory and leaves by
+// TMA: a third of the instructions, with which the warp that issues the products has to share its scheduler.
 //
 // gemm_fp4_kernel: tcgen05 (kind::mxf4nvf4), persistent, one CTA per SM or a pair (cta_group::2), 20 warps:
 //   0       TMA of codes (128 channels and BN tokens, 256 of K) and of their scales into a ring
-//   1       issues a stage's products
-//   3       copies its scales to tensor memory before that
+//   1       copies a stage's scales to tensor memory and issues its products
 //   4-19    accumulators -> C, under the products of the next tile
 // gemm_fp4_few_kernel for one or two tokens.
 #include <atomic>
@@ -115,12 +116,14 @@ constexpr size_t kLeast = 164 * 1024;            // one CTA an SM, and no other 
 static_assert(no_cluster_beside(kLeast), "no other cluster's CTA beside this kernel's");
 constexpr int kScaleCol = 256;                   // tensor memory: accumulators in front of it, scales of the stages behind
 
+constexpr int kBox = 32 * 64, kTokenBytes = kEpiWarps * kBox + 4 * 2 * kSpan * 4;   // of the epilogue, with tokens as rows
+
 struct Tile {
-  int BN, nt, mt, units, split, stages, accs;   // accs: accumulators
+  int BN, nt, mt, units, split, stages, accs, tokens;   // accs: accumulators; tokens: they are the rows
 };
 
 struct Bars {
-  uint64_t full[kMaxStages], scaled[kMaxStages], empty[kMaxStages], accf[2], acce[2];
+  uint64_t full[kMaxStages], empty[kMaxStages], accf[2], acce[2];
   uint32_t tmem;
   int failed;   // kSplit: a part's sums are not all there
 };
@@ -164,10 +167,6 @@ __device__ __forceinline__ void umma_commit_pair(uint64_t* bar) {
           smem_u32(bar)),
       "h"(static_cast<uint16_t>(0x3))
       : "memory");
-}
-// the same, on this CTA's barrier alone
-__device__ __forceinline__ void umma_commit_here(uint64_t* bar) {
-  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
 // An arrival on a barrier of the pair's leader, released at CTA scope: all that it has to come after are reads of this SM's
 // tensor memory, which tcgen05.wait::ld has seen finished (gemm_i8.cu).
@@ -219,19 +218,80 @@ __device__ __forceinline__ void store_tokens(const Fp4Args& a, T* C, int m0, int
     }
 }
 
-template <int CL, bool kSplit, bool kMx>
+// 8 values of shared memory, in pairs, read here and not earlier (all of a tile's at once do not fit the registers)
+__device__ __forceinline__ void lds8(const float* from, float2 (&v)[4]) {
+  const uint32_t at = smem_u32(from);
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];"
+                 : "=f"(v[2 * i].x), "=f"(v[2 * i].y), "=f"(v[2 * i + 1].x), "=f"(v[2 * i + 1].y)
+                 : "r"(at + 16 * i)
+                 : "memory");
+}
+// A warp's 32 tokens from row on, channels n0 ... n0 + span: 64 bytes of each token at a time go to the warp's box in shared
+// memory (64-byte swizzle) and by TMA to C, which clips them at its edges.  `scale`: [channel scale | bias][kSpan]
+template <typename T>
+__device__ __forceinline__ void store_channels(const Fp4Args& a, const CUtensorMap* mapC, uint8_t* box, int row, int n0, int span,
+                                               const float (&sum)[kSpan / 16][16], const float* scale, float ra, float far) {
+  constexpr int kCols = 64 / sizeof(T);
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int c0 = 0; c0 < kSpan; c0 += kCols)
+    if (c0 < span && n0 + c0 < a.N) {
+      if (lane == 0) bulk_wait_read_all();   // the box is free
+      __syncwarp();
+#pragma unroll
+      for (int i = 0; i < kCols; i += 8) {
+        const int at = c0 + i;
+        float2 v[4], c[4];
+        lds8(scale + at, c);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          v[e] = __fmul2_rn(__fmul2_rn(__fmul2_rn(make_float2(sum[at / 16][at % 16 + 2 * e], sum[at / 16][at % 16 + 2 * e + 1]), make_float2(ra, ra)), c[e]),
+                            make_float2(far, far));
+        if (a.bias) {
+          lds8(scale + kSpan + at, c);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = __fadd2_rn(v[e], c[e]);
+        }
+        if (a.relu) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = make_float2(v[e].x < 0.f ? 0.f : v[e].x, v[e].y < 0.f ? 0.f : v[e].y);
+        }
+        auto put = [&](int chunk, uint4 w) { *reinterpret_cast<uint4*>(box + lane * 64 + ((chunk ^ ((lane >> 1) & 3)) << 4)) = w; };
+        if constexpr (sizeof(T) == 2) {
+          put(i / 8, make_uint4(pack_bf16x2(v[0].x, v[0].y), pack_bf16x2(v[1].x, v[1].y), pack_bf16x2(v[2].x, v[2].y), pack_bf16x2(v[3].x, v[3].y)));
+        } else {
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+            put(i / 4 + h, make_uint4(__float_as_uint(v[2 * h].x), __float_as_uint(v[2 * h].y), __float_as_uint(v[2 * h + 1].x), __float_as_uint(v[2 * h + 1].y)));
+        }
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) {
+        tma_store_3d(mapC, box, n0 + c0, row, 0);
+        bulk_commit_group();
+      }
+    }
+}
+
+// Rows (W): channels, or, with kTokens, tokens; columns (X): the other.
+template <int CL, bool kSplit, bool kMx, bool kTokens>
 __global__ void __launch_bounds__(kThreads, 1) gemm_fp4_kernel(const __grid_constant__ CUtensorMap mapW, const __grid_constant__ CUtensorMap mapX,
                                                                const __grid_constant__ CUtensorMap mapSW, const __grid_constant__ CUtensorMap mapSX,
+                                                               const __grid_constant__ CUtensorMap mapC,
                                                                const __grid_constant__ Fp4Args a, const __grid_constant__ Tile p) {
   extern __shared__ uint8_t fp4_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(fp4_raw) + 1023) & ~uintptr_t(1023));
   constexpr int kTk = kMx ? 2 : 4;                 // scale tiles of a row tile in a K-block
-  const int bn = p.BN / CL, xt = p.BN > 128 ? 2 : 1;   // this CTA's tokens of a tile; row tiles of the tokens' scales
+  const int bn = p.BN / CL, xt = p.BN > 128 ? 2 : 1;   // this CTA's rows of X in a tile; row tiles of their scales
   const int x_at = 128 * 128, sw_at = x_at + bn * 128, sx_at = sw_at + kTk * 512, stage_bytes = (sx_at + xt * kTk * 512 + 1023) & ~1023;
   const int copied = sx_at + xt * kTk * 512;
   uint8_t* ring = smem;
   uint8_t* recv = smem + p.stages * stage_bytes;   // kSplit: the parts' sums of this CTA's tokens [part][BN / split][128]
-  Bars* bars = reinterpret_cast<Bars*>(recv + (kSplit ? p.BN * 512 : 0));
+  uint8_t* boxes = recv;                           // kTokens: a box for each warp of the epilogue, and four quarters' scales and biases
+  Bars* bars = reinterpret_cast<Bars*>(recv + (kSplit ? p.BN * 512 : kTokens ? kTokenBytes : 0));
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const int part = kSplit ? static_cast<int>(cluster_ctarank()) : 0;
   const int rank = CL > 1 ? static_cast<int>(cluster_ctarank()) : 0;
@@ -240,7 +300,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp4_kernel(const __grid_cons
   const int k1 = kSplit ? static_cast<int>(static_cast<int64_t>(nk) * (part + 1) / p.split) : nk;
   const int per = kSplit ? p.split : CL;           // CTAs of a tile
   const int u0 = blockIdx.x / per, ustep = gridDim.x / per;
-  const int mu = p.mt / CL;                        // row tiles (of channels); rows fastest
+  const int mu = p.mt / CL;                        // row tiles; rows fastest
 
   if (threadIdx.x == 0) {
     prefetch_tmap(&mapW);
@@ -249,7 +309,6 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp4_kernel(const __grid_cons
     prefetch_tmap(&mapSX);
     for (int i = 0; i < p.stages; ++i) {
       mbar_init(&bars->full[i], 1);
-      mbar_init(&bars->scaled[i], 1);
       mbar_init(&bars->empty[i], 1);
     }
     for (int i = 0; i < 2; ++i) {
@@ -274,7 +333,9 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp4_kernel(const __grid_cons
   if (CL > 1 || kSplit) cluster_sync();   // the peers run, and their barriers are initialised
   else __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = bars->tmem;
+  // all of tensor memory is this CTA's, so its columns start at 0: written so, addresses stay in uniform registers and an
+  // instruction takes its issue slot instead of 40 clocks (8192 x 4096 x 4096: @@)
+  constexpr uint32_t tmem = 0;
   pdl_wait();
   pdl_trigger();
 
@@ -283,7 +344,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp4_kernel(const __grid_cons
     int it = 0, s = 0, ph = 1;
     uint32_t limit = kSpinLimit;
     for (int u = u0; u < p.units; u += ustep) {
-      const int n0 = ((u % mu) * CL + rank) * 128, m0 = (u / mu) * p.BN;
+      const int r0 = ((u % mu) * CL + rank) * 128, c0 = (u / mu) * p.BN;
       for (int kb = k0; kb < k1; ++kb, ++it) {
         if (it >= p.stages) mbar_wait_keep(limit, &bars->empty[s], ph, nullptr, kDevTimeoutEmpty);
         if (elect_one() && limit > 1) {
@@ -294,10 +355,10 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp4_kernel(const __grid_cons
             if (CL > 1) tma_load_3d_pair(at + to, map, c0, c1, c2, bar);
             else tma_load_3d(at + to, map, c0, c1, c2, bar);
           };
-          load(0, &mapW, kb * 128, n0, 0);
-          load(x_at, &mapX, kb * 128, m0 + rank * bn, 0);
-          load(sw_at, &mapSW, 0, kb * kTk, n0 >> 7);
-          load(sx_at, &mapSX, 0, kb * kTk, m0 >> 7);
+          load(0, &mapW, kb * 128, r0, 0);
+          load(x_at, &mapX, kb * 128, c0 + rank * bn, 0);
+          load(sw_at, &mapSW, 0, kb * kTk, r0 >> 7);
+          load(sx_at, &mapSX, 0, kb * kTk, c0 >> 7);
         }
         __syncwarp();
         if (++s == p.stages) {
@@ -311,30 +372,56 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp4_kernel(const __grid_cons
       for (int i = it > p.stages ? it - p.stages : 0; i < it; ++i)
         mbar_wait_keep(limit, &bars->full[i % p.stages], (i / p.stages) & 1, nullptr, kDevTimeoutFull);
   } else if (warp == 1 && rank == 0) {
-    // ---- products (the leader's, of a pair); the warp stays converged and one elected lane issues
+    // ---- scales to tensor memory, products (the leader's, of a pair); the warp stays converged and one elected lane issues
     const uint32_t idesc = idesc_fp4(128 * CL, p.BN, kMx), ring0 = smem_u32(ring);
     const int cols = (1 + xt) * kTk * 4;           // of a stage's scales
     int s = 0, ph = 0, t = 0;                      // t: tiles begun
     uint32_t limit = kSpinLimit;
     for (int u = u0; u < p.units; u += ustep, ++t) {
       const int b = t % p.accs;
-      if (t >= p.accs) mbar_wait_keep(limit, &bars->acce[b], (t / p.accs + 1) & 1, nullptr, kDevTimeoutAccum);
-      tc_fence_after();
       const uint32_t acc = tmem + b * 128;
       for (int kb = k0; kb < k1; ++kb) {
-        mbar_wait_keep(limit, &bars->scaled[s], ph, nullptr, kDevTimeoutFull);
+        mbar_wait_keep(limit, &bars->full[s], ph, nullptr, kDevTimeoutFull);
         tc_fence_after();
+        const uint32_t at = ring0 + s * stage_bytes, sw = tmem + kScaleCol + s * cols, sx = sw + 4 * kTk;
         if (elect_one() && limit > 1) {
-          const uint32_t at = ring0 + s * stage_bytes, sw = tmem + kScaleCol + s * cols, sx = sw + 4 * kTk;
-          const uint64_t wd = smem_desc_k128(at), xd = smem_desc_k128(at + x_at);
-          const int left = a.K - kb * kK, n = left >= kK ? 4 : (left + 63) / 64;
+                    const uint64_t swd = scale_desc(at + sw_at), sxd = scale_desc(at + sx_at);
+          // a stage's columns were last read by products that have ended: its copies have been waited for.  Tiles behind the
+          // last are zeros that no product takes
+          if (xt == 2) {
 #pragma unroll
-          for (int j = 0; j < 4; ++j)
-            if (j < n) {
-              const int tile = kMx ? j / 2 : j;
-              umma_fp4<CL, kMx>(acc, wd + 2 * j, xd + 2 * j, idesc | (kMx ? scale_id(j % 2 * 2) : 0), sw + 4 * tile, sx + 4 * tile * xt,
-                                (kb > k0) | (j > 0));
+            for (int j = 0; j < kTk; ++j) {
+              copy_scales<CL>(sw + 4 * j, swd + j * 32);
+              copy_scales<CL>(sx + 8 * j, sxd + j * 32);
+              copy_scales<CL>(sx + 8 * j + 4, sxd + (kTk + j) * 32);
             }
+          } else {
+#pragma unroll
+            for (int j = 0; j < kTk; ++j) {
+              copy_scales<CL>(sw + 4 * j, swd + j * 32);
+              copy_scales<CL>(sx + 4 * j, sxd + j * 32);
+            }
+          }
+        }
+        __syncwarp();
+        if (kb == k0) {   // the accumulator is free
+          if (t >= p.accs) mbar_wait_keep(limit, &bars->acce[b], (t / p.accs + 1) & 1, nullptr, kDevTimeoutAccum);
+          tc_fence_after();
+        }
+        if (elect_one() && limit > 1) {
+          const uint64_t wd = smem_desc_k128(at), xd = smem_desc_k128(at + x_at);
+          const int left = a.K - kb * kK;
+          auto product = [&](int j) {
+            const int tile = kMx ? j / 2 : j;
+            umma_fp4<CL, kMx>(acc, wd + 2 * j, xd + 2 * j, idesc | (kMx ? scale_id(j % 2 * 2) : 0), sw + 4 * tile, sx + 4 * tile * xt,
+                              (kb > k0) | (j > 0));
+          };
+          if (left >= kK) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) product(j);
+          } else {
+            for (int j = 0; j * 64 < left; ++j) product(j);
+          }
           if (CL > 1) umma_commit_pair(&bars->empty[s]);
           else umma_commit(&bars->empty[s]);
         }
@@ -350,55 +437,35 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp4_kernel(const __grid_cons
       }
       __syncwarp();
     }
-  } else if (warp == 3 && rank == 0) {
-    // ---- scales to tensor memory, ahead of the products
-    const uint32_t ring0 = smem_u32(ring);
-    const int cols = (1 + xt) * kTk * 4;
-    int s = 0, ph = 0;
-    uint32_t limit = kSpinLimit;
-    for (int u = u0; u < p.units; u += ustep)
-      for (int kb = k0; kb < k1; ++kb) {
-        // a stage's columns were last read by products that have ended: its copies were begun after those
-        mbar_wait_keep(limit, &bars->full[s], ph, nullptr, kDevTimeoutFull);
-        tc_fence_after();
-        if (elect_one() && limit > 1) {
-          const uint32_t at = ring0 + s * stage_bytes, sw = tmem + kScaleCol + s * cols, sx = sw + 4 * kTk;
-          const uint64_t swd = scale_desc(at + sw_at), sxd = scale_desc(at + sx_at);
-          const int left = a.K - kb * kK, n = left >= kK ? 4 : (left + 63) / 64;
-#pragma unroll
-          for (int j = 0; j < kTk; ++j)
-            if (j * (kMx ? 2 : 1) < n) {
-              copy_scales<CL>(sw + 4 * j, swd + j * 32);
-              for (int i = 0; i < xt; ++i) copy_scales<CL>(sx + 4 * (j * xt + i), sxd + (i * kTk + j) * 32);
-            }
-          if (CL > 1) umma_commit_here(&bars->scaled[s]);
-          else umma_commit(&bars->scaled[s]);
-        }
-        __syncwarp();
-        if (++s == p.stages) {
-          s = 0;
-          ph ^= 1;
-        }
-      }
   } else if (warp >= 4) {
-    // ---- C: thread = one channel and a quarter of the tile's tokens (16 of fewer than 64)
+    // ---- C: thread = one row and a quarter of the tile's columns (16 of fewer than 64)
     const int quarter = warp & 3, span = p.BN > 64 ? p.BN / 4 : 16, cb = (warp / 4 - 1) * span;
     const bool works = cb < p.BN;
     int t = 0;
     bool ok = true;
     for (int u = u0; ok && u < p.units; u += ustep) {
-      const int n = ((u % mu) * CL + rank) * 128 + 32 * quarter + lane, m0 = (u / mu) * p.BN + cb;
+      const int row = ((u % mu) * CL + rank) * 128 + 32 * quarter + lane, col0 = (u / mu) * p.BN + cb;
       const uint32_t row0 = tmem + (static_cast<uint32_t>(32 * quarter) << 16) + cb;
-      float rb = 1.f, bias = 0.f, ra[kSpan / 32];   // lane l: tokens l, 32 + l, ...
+      // of the row; of the columns, lane l those of l, 32 + l, ...
+      float mine = 1.f, bias = 0.f, theirs[kSpan / 32];
       bool far = false;
-      if (!kSplit) {
-        if (a.rb && n < a.N) rb = __ldg(a.rb + n);
-        if (a.bias && n < a.N) bias = __ldg(a.bias + n);
+      const int group = warp / 4 - 1;   // the four warps that have the same columns
+      float* scale = reinterpret_cast<float*>(boxes + kEpiWarps * kBox) + group * 2 * kSpan;
+      if constexpr (kTokens) {
+        if (a.ra && row < a.M) mine = __ldg(a.ra + row);
+        bar_named(1 + group, 128);      // they are done with the tile before
+        const int i = threadIdx.x & 127, n = col0 + (i & (kSpan - 1));
+        if (i < kSpan) scale[i] = a.rb && n < a.N ? __ldg(a.rb + n) : 1.f;
+        else scale[i] = a.bias && n < a.N ? __ldg(a.bias + n) : 0.f;
+        bar_named(1 + group, 128);
+      } else if (!kSplit) {
+        if (a.rb && row < a.N) mine = __ldg(a.rb + row);
+        if (a.bias && row < a.N) bias = __ldg(a.bias + row);
 #pragma unroll
         for (int i = 0; i < kSpan / 32; ++i) {
-          ra[i] = a.ra && m0 + 32 * i + lane < a.M && 32 * i < span ? __ldg(a.ra + m0 + 32 * i + lane) : 1.f;
-          far |= ra[i] != 0.f && back(ra[i]) != 1.f;
-          ra[i] = near_one(ra[i]);
+          theirs[i] = a.ra && col0 + 32 * i + lane < a.M && 32 * i < span ? __ldg(a.ra + col0 + 32 * i + lane) : 1.f;
+          far |= theirs[i] != 0.f && back(theirs[i]) != 1.f;
+          theirs[i] = near_one(theirs[i]);
         }
         far = __any_sync(0xffffffffu, far);
       }
@@ -407,9 +474,15 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp4_kernel(const __grid_cons
       ok = mbar_wait_warp(&bars->accf[b], (t / p.accs) & 1, nullptr, kDevTimeoutAccum);
       tc_fence_after();
       if (ok) {
+        const uint32_t from = row0 + b * 128;
+        if (span == kSpan) {
 #pragma unroll
-        for (int g = 0; g < kSpan / 16; ++g)
-          if (works && 16 * g < span) tmem_ld_32x32b_x16(row0 + b * 128 + 16 * g, sum[g]);
+          for (int g = 0; g < kSpan / 16; g += 2) tmem_ld_32x32b_x16_pair(from + 16 * g, sum[g], from + 16 * (g + 1), sum[g + 1]);
+        } else if (works) {
+#pragma unroll
+          for (int g = 0; g < kSpan / 32; ++g)
+            if (16 * g < span) tmem_ld_32x32b_x16(from + 16 * g, sum[g]);
+        }
         tc_fence_before();
         __syncwarp();
         if (lane == 0) {
@@ -434,15 +507,23 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp4_kernel(const __grid_cons
               st_peer(recv + ((part * owned + tok % owned) * 128 + 32 * quarter + lane) * 4, tok / owned, __float_as_uint(sum[g][e]));
             }
           }
+      } else if constexpr (kTokens) {
+        const float ra = near_one(mine), to = back(mine);
+        uint8_t* box = boxes + (warp - 4) * kBox;
+        if (row - lane < a.M) {
+          if (a.bf16) store_channels<__nv_bfloat16>(a, &mapC, box, row - lane, col0, span, sum, scale, ra, to);
+          else store_channels<float>(a, &mapC, box, row - lane, col0, span, sum, scale, ra, to);
+        }
       } else if (far) {
-        if (a.bf16) store_tokens<true>(a, static_cast<__nv_bfloat16*>(a.C), m0, n, span, sum, ra, rb, bias);
-        else store_tokens<true>(a, static_cast<float*>(a.C), m0, n, span, sum, ra, rb, bias);
+        if (a.bf16) store_tokens<true>(a, static_cast<__nv_bfloat16*>(a.C), col0, row, span, sum, theirs, mine, bias);
+        else store_tokens<true>(a, static_cast<float*>(a.C), col0, row, span, sum, theirs, mine, bias);
       } else if (a.bf16) {
-        store_tokens<false>(a, static_cast<__nv_bfloat16*>(a.C), m0, n, span, sum, ra, rb, bias);
+        store_tokens<false>(a, static_cast<__nv_bfloat16*>(a.C), col0, row, span, sum, theirs, mine, bias);
       } else {
-        store_tokens<false>(a, static_cast<float*>(a.C), m0, n, span, sum, ra, rb, bias);
+        store_tokens<false>(a, static_cast<float*>(a.C), col0, row, span, sum, theirs, mine, bias);
       }
     }
+    if (kTokens && lane == 0) bulk_wait_all();
   }
   tc_fence_before();
   if (CL > 1 || kSplit) cluster_sync();   // the pair's products and arrivals are done in both CTAs; every part's sums are there
@@ -464,8 +545,8 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp4_kernel(const __grid_cons
   }
   if (warp == 2) {
     tc_fence_after();
-    if (CL == 1) tmem_dealloc(tmem, 512);
-    else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+    if (CL == 1) tmem_dealloc(bars->tmem, 512);
+    else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(bars->tmem), "r"(512) : "memory");
   }
 }
 
@@ -503,9 +584,9 @@ void device_room(int& sms, int& pairs) {
   if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || sms < 1) sms = 1;
   cudaLaunchAttribute attr[1];
   pairs = 0;
-  if (allow_smem(gemm_fp4_kernel<2, false, false>, kSmem) == cudaSuccess) {
+  if (allow_smem(gemm_fp4_kernel<2, false, false, false>, kSmem) == cudaSuccess) {
     cudaLaunchConfig_t cfg = config(attr, 2, 2, kSmem, nullptr);
-    if (cudaOccupancyMaxActiveClusters(&pairs, gemm_fp4_kernel<2, false, false>, &cfg) != cudaSuccess) pairs = 0;
+    if (cudaOccupancyMaxActiveClusters(&pairs, gemm_fp4_kernel<2, false, false, false>, &cfg) != cudaSuccess) pairs = 0;
   }
   cudaGetLastError();
   if (pairs < 1) pairs = 1;
@@ -513,24 +594,24 @@ void device_room(int& sms, int& pairs) {
   g_dev[dev].pairs.store(pairs, std::memory_order_relaxed);
 }
 
-template <int CL, bool kSplit, bool kMx>
-cudaError_t launch_fp4(const CUtensorMap (&m)[4], const Fp4Args& a, Tile p, int grid, cudaStream_t s) {
+template <int CL, bool kSplit, bool kMx, bool kTokens>
+cudaError_t launch_fp4(const CUtensorMap (&m)[5], const Fp4Args& a, Tile p, int grid, cudaStream_t s) {
   const int tk = kMx ? 2 : 4, xt = p.BN > 128 ? 2 : 1;
-  const int stage = (128 * 128 + p.BN / CL * 128 + (1 + xt) * tk * 512 + 1023) & ~1023, sums = kSplit ? p.BN * 512 : 0;
+  const int stage = (128 * 128 + p.BN / CL * 128 + (1 + xt) * tk * 512 + 1023) & ~1023, sums = kSplit ? p.BN * 512 : kTokens ? kTokenBytes : 0;
   p.stages = (kSmem - 1024 - kBarBytes - sums) / stage;
   if (p.stages > kMaxStages) p.stages = kMaxStages;
   const int cols = (1 + xt) * tk * 4;
   if (p.stages > (512 - kScaleCol) / cols) p.stages = (512 - kScaleCol) / cols;
   size_t smem = 1024 + static_cast<size_t>(p.stages) * stage + sums + kBarBytes;
   if (smem < kLeast) smem = kLeast;
-  cudaError_t e = allow_smem(gemm_fp4_kernel<CL, kSplit, kMx>, kSmem);
+  cudaError_t e = allow_smem(gemm_fp4_kernel<CL, kSplit, kMx, kTokens>, kSmem);
   if (e != cudaSuccess) return e;
   cudaLaunchAttribute attr[2];
   cudaLaunchConfig_t cfg = config(attr, kSplit ? p.split : CL, grid, smem, s);
   attr[cfg.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[cfg.numAttrs].val.programmaticStreamSerializationAllowed = 1;
   ++cfg.numAttrs;
-  return cudaLaunchKernelEx(&cfg, gemm_fp4_kernel<CL, kSplit, kMx>, m[0], m[1], m[2], m[3], a, p);
+  return cudaLaunchKernelEx(&cfg, gemm_fp4_kernel<CL, kSplit, kMx, kTokens>, m[0], m[1], m[2], m[3], m[4], a, p);
 }
 
 bool code_map(CUtensorMap* m, const uint8_t* base, int64_t ld, int K, int rows, int box_rows) {
@@ -547,32 +628,47 @@ bool scale_map(CUtensorMap* m, const uint8_t* base, int tiles, int rows, int box
   return encode_map(m, CU_TENSOR_MAP_DATA_TYPE_UINT32, 3, base, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_NONE);
 }
 
+// C in boxes of 32 rows of 64 bytes
+bool result_map(CUtensorMap* m, void* C, int64_t ldc, int M, int N, bool bf16) {
+  const cuuint64_t dims[3] = {static_cast<cuuint64_t>(N), static_cast<cuuint64_t>(M), 1};
+  const cuuint64_t stride = static_cast<cuuint64_t>(ldc) * (bf16 ? 2 : 4), strides[2] = {stride, stride};
+  const cuuint32_t box[3] = {bf16 ? 32u : 16u, 32, 1};
+  return encode_map(m, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, C, dims, strides, box,
+                    CU_TENSOR_MAP_SWIZZLE_64B);
+}
+
 // The shape with the least estimated time: waves of tiles times the longer of a K-block's products (2 BN clocks, or 130 for
-// the channels' reads) and its loads (45 bytes a clock), plus fixed parts
-void choose(const Fp4Args& a, int sms, int pairs, Tile& p, int& cl) {
+// the rows' reads) and its loads (45 bytes a clock), plus fixed parts
+void choose(const Fp4Args& a, bool boxes, int sms, int pairs, Tile& p, int& cl) {
   const int nk = (a.K + kK - 1) / kK;
   double best = 0.0;
-  for (int c = 1; c <= 2; ++c) {
-    const int mt = ((a.N + 127) / 128 + c - 1) / c * c;
-    for (int bn = c == 1 ? 16 : 64; bn <= kMaxBN; bn *= 2) {
-      if (bn < 128 && a.M > bn) continue;   // a product takes a scale tile from its first row on
-      const int64_t nt = (static_cast<int64_t>(a.M) + bn - 1) / bn, units = mt / c * nt;
-      const int room = c == 2 ? pairs : sms;
-      const double bytes = (128 + bn / c) * 128 + 512 * (a.mx ? 2 : 4) * (bn > 128 ? 3 : 2);
-      double kb = 2.0 * bn;
-      kb = kb > 130.0 ? kb : 130.0;
-      kb = kb > bytes / 45.0 ? kb : bytes / 45.0;
-      for (int split = 1; split <= (c == 1 ? 8 : 1); split *= 2) {
-        if (split > 1 && (units * split > sms * 7 / 8 || nk < 2 * split || bn < 2 * split || bn > 128)) break;
-        const double waves = split > 1 ? 1.0 : static_cast<double>((units + room - 1) / room);
-        const double cost = waves * ((nk + split - 1) / split * kb + 600.0) + 15.0 * bn + (c == 2 ? 1500.0 : 0.0) + (split > 1 ? 3000.0 : 0.0);
-        if (best == 0.0 || cost < best) {
-          best = cost;
-          cl = c;
-          p.BN = bn;
-          p.mt = mt;
-          p.nt = static_cast<int>(nt);
-          p.split = split;
+  for (int tokens = 0; tokens <= (boxes ? 1 : 0); ++tokens) {
+    const int64_t rows = tokens ? a.M : a.N, cols = tokens ? a.N : a.M;
+    for (int c = 1; c <= 2; ++c) {
+      const int64_t mt = ((rows + 127) / 128 + c - 1) / c * c;
+      for (int bn = c == 1 ? 16 : 64; bn <= kMaxBN; bn *= 2) {
+        // a product takes a scale tile from its first row on, and a warp's columns are whole boxes
+        if (bn < 128 && (cols > bn || tokens)) continue;
+        const int64_t nt = (cols + bn - 1) / bn, units = mt / c * nt;
+        const int room = c == 2 ? pairs : sms;
+        const double bytes = (128 + bn / c) * 128 + 512 * (a.mx ? 2 : 4) * (bn > 128 ? 3 : 2);
+        double kb = 2.0 * bn;
+        kb = kb > 130.0 ? kb : 130.0;
+        kb = kb > bytes / 45.0 ? kb : bytes / 45.0;
+        for (int split = 1; split <= (c == 1 && !tokens ? 8 : 1); split *= 2) {
+          if (split > 1 && (units * split > sms * 7 / 8 || nk < 2 * split || bn < 2 * split || bn > 128)) break;
+          const double waves = split > 1 ? 1.0 : static_cast<double>((units + room - 1) / room);
+          const double cost = waves * ((nk + split - 1) / split * kb + 600.0) + (tokens ? 5.0 : 15.0) * bn + (c == 2 ? 1500.0 : 0.0) +
+                              (split > 1 ? 3000.0 : 0.0);
+          if (best == 0.0 || cost < best) {
+            best = cost;
+            cl = c;
+            p.BN = bn;
+            p.mt = static_cast<int>(mt);
+            p.nt = static_cast<int>(nt);
+            p.split = split;
+            p.tokens = tokens;
+          }
         }
       }
     }
@@ -581,11 +677,12 @@ void choose(const Fp4Args& a, int sms, int pairs, Tile& p, int& cl) {
 }
 
 template <bool kMx>
-cudaError_t launch_tile(const CUtensorMap (&m)[4], const Fp4Args& a, const Tile& p, int cl, int room, cudaStream_t s) {
+cudaError_t launch_tile(const CUtensorMap (&m)[5], const Fp4Args& a, const Tile& p, int cl, int room, cudaStream_t s) {
   const int grid = (p.units < room ? p.units : room) * cl;
-  return p.split > 1 ? launch_fp4<1, true, kMx>(m, a, p, p.units * p.split, s)
-         : cl == 2   ? launch_fp4<2, false, kMx>(m, a, p, grid, s)
-                     : launch_fp4<1, false, kMx>(m, a, p, grid, s);
+  if (p.tokens) return cl == 2 ? launch_fp4<2, false, kMx, true>(m, a, p, grid, s) : launch_fp4<1, false, kMx, true>(m, a, p, grid, s);
+  return p.split > 1 ? launch_fp4<1, true, kMx, false>(m, a, p, p.units * p.split, s)
+         : cl == 2   ? launch_fp4<2, false, kMx, false>(m, a, p, grid, s)
+                     : launch_fp4<1, false, kMx, false>(m, a, p, grid, s);
 }
 
 bool at_bytes(const void* p, int n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
@@ -620,14 +717,19 @@ oscars_status oscars_gemm_fp4_nt(const uint8_t* A, int64_t lda, const uint8_t* s
   int sms, pairs, cl = 1;
   device_room(sms, pairs);
   Tile p{};
-  choose(a, sms, pairs, p, cl);
+  const int size = dtype == OSCARS_F32 ? 4 : 2;
+  // TMA stores rows of 16 bytes' alignment, and its strides end at 2^40
+  choose(a, at_bytes(C, 16) && ldc * size % 16 == 0 && ldc < (int64_t(1) << 37), sms, pairs, p, cl);
   const int64_t units = static_cast<int64_t>(p.mt / cl) * p.nt;
   if (units > INT32_MAX / 2) return OSCARS_EINVAL;
   p.units = static_cast<int>(units);
   const int tk = a.mx ? 2 : 4;
-  CUtensorMap m[4];
-  if (!code_map(&m[0], B, ldb, K, N, 128) || !code_map(&m[1], A, lda, K, M, p.BN / cl) || !scale_map(&m[2], scales_b, a.tiles, N, tk, 1) ||
-      !scale_map(&m[3], scales_a, a.tiles, M, tk, p.BN > 128 ? 2 : 1))
+  CUtensorMap m[5] = {};
+  const int boxes[2] = {128, p.BN / cl}, tiles[2] = {1, p.BN > 128 ? 2 : 1};   // of the rows' operand, of the columns'
+  const int of_a = p.tokens ? 0 : 1, of_b = 1 - of_a;
+  if (!code_map(&m[of_a], A, lda, K, M, boxes[of_a]) || !code_map(&m[of_b], B, ldb, K, N, boxes[of_b]) ||
+      !scale_map(&m[2 + of_a], scales_a, a.tiles, M, tk, tiles[of_a]) || !scale_map(&m[2 + of_b], scales_b, a.tiles, N, tk, tiles[of_b]) ||
+      (p.tokens && !result_map(&m[4], C, ldc, M, N, dtype == OSCARS_BF16)))
     return OSCARS_ECUDA;
   const int room = cl == 2 ? pairs : sms;
   const cudaError_t e = a.mx ? launch_tile<true>(m, a, p, cl, room, s) : launch_tile<false>(m, a, p, cl, room, s);
