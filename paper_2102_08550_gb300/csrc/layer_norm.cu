@@ -72,15 +72,15 @@ struct Rows {
   static constexpr int kDepth = kVec ? (196608 / kStage < 6 ? 196608 / kStage : 6) : 1;
   static constexpr int kBytes = kVec ? kDepth * kStage : 0;
 
+  static constexpr int kPer = kVec ? 16 / static_cast<int>(sizeof(T)) : 1;         // neighbouring columns of a thread
   __device__ __forceinline__ static int column(int i, int e) {
-    const int t = threadIdx.x % TPR;
-    return kVec ? (i * TPR + t) * 8 + e : (i * 8 + e) * TPR + t;
+    const int t = threadIdx.x % TPR, c = i * 8 + e;
+    return (c / kPer * TPR + t) * kPer + c % kPer;
   }
   // whether all of this thread's columns are inside the row
   __device__ __forceinline__ static bool inside(int cols) { return column(kTurns - 1, 7) < cols; }
   // begin the copy of row `row` of matrix m to a stage
   __device__ __forceinline__ static void request(uint8_t* ring, int stage, int m, const T* row, int cols) {
-    constexpr int kPer = 16 / sizeof(T);                   // columns of a piece
     uint8_t* to = ring + stage * kStage + (m * kPieces * kBlock + threadIdx.x) * 16;
     if (inside(cols)) {
 #pragma unroll
@@ -122,8 +122,11 @@ struct Rows {
 #pragma unroll
     for (int i = 0; i < kTurns; ++i) {
       const float w[8] = {v[i][0].x, v[i][0].y, v[i][1].x, v[i][1].y, v[i][2].x, v[i][2].y, v[i][3].x, v[i][3].y};
-      if constexpr (kVec) {
+      if constexpr (kVec && sizeof(T) == 2) {
         store8(row + column(i, 0), all ? 8 : cols - column(i, 0), true, w);
+      } else if (kVec && all) {
+#pragma unroll
+        for (int h = 0; h < 8; h += 4) *reinterpret_cast<float4*>(row + column(i, h)) = make_float4(w[h], w[h + 1], w[h + 2], w[h + 3]);
       } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
@@ -136,8 +139,12 @@ struct Rows {
 #pragma unroll
     for (int i = 0; i < kTurns; ++i) {
       float w[8];
-      if constexpr (kVec) {
-        params8(p, column(i, 0), cols, vec, none, w);
+      if (kVec && p && vec && inside(cols)) {
+#pragma unroll
+        for (int h = 0; h < 8; h += 4) {
+          const float4 f = *reinterpret_cast<const float4*>(p + column(i, h));
+          w[h] = f.x, w[h + 1] = f.y, w[h + 2] = f.z, w[h + 3] = f.w;
+        }
       } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e) w[e] = p && column(i, e) < cols ? p[column(i, e)] : none;
