@@ -50,7 +50,9 @@ __device__ __forceinline__ void params8(const float* p, int at, int cols, bool v
 // ------------------------------------------------------------------ rows through shared memory
 // Up to 8192 columns: TPR threads take a row, a block 512 / TPR rows at a time; a thread owns 8 kTurns columns.  kMats matrices'
 // rows come through a ring in shared memory in which each thread reads what it has copied itself (cp.async, no barrier).
-// Where rows are not 16-byte aligned, neighbouring threads take neighbouring columns and load them when they are due.
+// Where rows are not 16-byte aligned, they are copied from the 16 bytes on in which they begin, neighbouring threads take
+// neighbouring columns of them, and a barrier of the row's threads comes in between (12 x 332 x 5115 bf16 backward: loads of
+// single values when they are due 104 us).
 constexpr int kBlock = 512;
 
 __device__ __forceinline__ void copy16(void* to, const void* from, int bytes) {   // zeros behind the first `bytes`
@@ -66,11 +68,12 @@ __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_grou
 
 template <typename T, int TPR, int kTurns, bool kVec, int kMats>
 struct Rows {
-  static constexpr int kLanes = kBlock / TPR, kCap = TPR * kTurns * 8;
-  static constexpr int kPieces = kTurns * static_cast<int>(sizeof(T)) / 2;          // of 16 bytes, of a thread's columns of one matrix
-  static constexpr int kStage = kMats * kPieces * kBlock * 16;
-  static constexpr int kDepth = kVec ? (196608 / kStage < 6 ? 196608 / kStage : 6) : 1;
-  static constexpr int kBytes = kVec ? kDepth * kStage : 0;
+  static constexpr int kSize = sizeof(T), kLanes = kBlock / TPR, kCap = TPR * kTurns * 8;
+  static constexpr int kPieces = kTurns * kSize / 2;          // of 16 bytes, of a thread's columns of one matrix
+  static constexpr int kRow = kCap * kSize + 16;              // a row and what lies in front of it in its first 16 bytes
+  static constexpr int kStage = kMats * (kVec ? kPieces * kBlock * 16 : kLanes * kRow);
+  static constexpr int kDepth = 200704 / kStage < 6 ? 200704 / kStage : 6;
+  static constexpr int kBytes = kDepth * kStage;
 
   static constexpr int kPer = kVec ? 16 / static_cast<int>(sizeof(T)) : 1;         // neighbouring columns of a thread
   __device__ __forceinline__ static int column(int i, int e) {
@@ -79,8 +82,27 @@ struct Rows {
   }
   // whether all of this thread's columns are inside the row
   __device__ __forceinline__ static bool inside(int cols) { return column(kTurns - 1, 7) < cols; }
-  // begin the copy of row `row` of matrix m to a stage
-  __device__ __forceinline__ static void request(uint8_t* ring, int stage, int m, const T* row, int cols) {
+  __device__ __forceinline__ static int in_front(const T* row) { return static_cast<int>(reinterpret_cast<uintptr_t>(row) & 15); }
+  __device__ __forceinline__ static uint8_t* lane_row(uint8_t* ring, int stage, int m) {
+    return ring + stage * kStage + (m * kLanes + threadIdx.x / TPR) * kRow;
+  }
+  // a row's threads are here, and each of them sees what the others have copied
+  __device__ __forceinline__ static void meet() {
+    if (TPR == 32) __syncwarp();
+    else bar_named(1 + threadIdx.x / TPR, TPR);
+  }
+  // begin the copy of row `row` of a matrix that starts at `first` to a stage
+  __device__ __forceinline__ static void request(uint8_t* ring, int stage, int m, const T* row, const T* first, int cols) {
+    if constexpr (!kVec) {   // whole 16 bytes, with a piece of the row before in front; the matrix's own first ones one at a time
+      const int t = threadIdx.x % TPR, front = in_front(row), bytes = front + cols * kSize;
+      uint8_t* to = lane_row(ring, stage, m);
+      const uint8_t* from = reinterpret_cast<const uint8_t*>(row) - front;
+      const bool inside = from >= reinterpret_cast<const uint8_t*>(first);
+      if (!inside && t < (16 - front) / kSize && t < cols) reinterpret_cast<T*>(to + front)[t] = row[t];
+      for (int at = t * 16; at < bytes; at += TPR * 16)
+        if (inside || at > 0) copy16(to + at, from + at, bytes - at >= 16 ? 16 : bytes - at);
+      return;
+    }
     uint8_t* to = ring + stage * kStage + (m * kPieces * kBlock + threadIdx.x) * 16;
     if (inside(cols)) {
 #pragma unroll
@@ -94,7 +116,7 @@ struct Rows {
     }
   }
   // this thread's columns of it (zeros behind the row's end)
-  __device__ __forceinline__ static void take(const uint8_t* ring, int stage, int m, const T* row, int cols, float2 (&v)[kTurns][4]) {
+  __device__ __forceinline__ static void take(uint8_t* ring, int stage, int m, const T* row, int cols, float2 (&v)[kTurns][4]) {
     if constexpr (kVec) {
 #pragma unroll
       for (int p = 0; p < kPieces; ++p) {
@@ -109,12 +131,13 @@ struct Rows {
         }
       }
     } else {
+      const T* from = reinterpret_cast<const T*>(lane_row(ring, stage, m) + in_front(row));
 #pragma unroll
       for (int i = 0; i < kTurns; ++i)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          v[i][e] = make_float2(column(i, 2 * e) < cols ? to_f32(row[column(i, 2 * e)]) : 0.f,
-                                column(i, 2 * e + 1) < cols ? to_f32(row[column(i, 2 * e + 1)]) : 0.f);
+          v[i][e] = make_float2(column(i, 2 * e) < cols ? to_f32(from[column(i, 2 * e)]) : 0.f,
+                                column(i, 2 * e + 1) < cols ? to_f32(from[column(i, 2 * e + 1)]) : 0.f);
     }
   }
   __device__ __forceinline__ static void put(T* row, int cols, const float2 (&v)[kTurns][4]) {
@@ -220,10 +243,8 @@ __global__ void __launch_bounds__(kBlock, 1) layer_norm_kernel(const __grid_cons
   pdl_trigger();
   const T* x = static_cast<const T*>(a.x) + first * a.ldx;
   auto request = [&](int r, int stage) {
-    if constexpr (kVec) {
-      if (r < r1) R::request(fwd_smem, stage, 0, x + r * a.ldx, a.cols);
-      copies_done();
-    }
+    if (r < r1) R::request(fwd_smem, stage, 0, x + r * a.ldx, static_cast<const T*>(a.x), a.cols);
+    copies_done();
   };
   int r = chunk * a.per + lane;
 #pragma unroll
@@ -234,10 +255,9 @@ __global__ void __launch_bounds__(kBlock, 1) layer_norm_kernel(const __grid_cons
   const float each = 1.f / a.cols;
   const bool full = R::inside(a.cols);
   for (int stage = 0; r < r1; r += R::kLanes) {
-    if constexpr (kVec) {
-      request(r + (kD - 1) * R::kLanes, stage == 0 ? kD - 1 : stage - 1);
-      copies_wait<kD - 1>();
-    }
+    request(r + (kD - 1) * R::kLanes, stage == 0 ? kD - 1 : stage - 1);
+    copies_wait<kD - 1>();
+    if constexpr (!kVec) R::meet();
     float2 v[kTurns][4];
     R::take(fwd_smem, stage, 0, x + r * a.ldx, a.cols, v);
     float2 pair = both(0.f);
@@ -545,13 +565,11 @@ __global__ void __launch_bounds__(kBlock, 1) norm_backward_kernel(const __grid_c
   pdl_trigger();
   const T *dy = static_cast<const T*>(a.dy) + first * a.lddy, *x = static_cast<const T*>(a.x) + first * a.ldx;
   auto request = [&](int r, int stage) {
-    if constexpr (kVec) {
-      if (r < r1) {
-        R::request(bwd_smem, stage, 0, dy + r * a.lddy, a.cols);
-        R::request(bwd_smem, stage, 1, x + r * a.ldx, a.cols);
-      }
-      copies_done();
+    if (r < r1) {
+      R::request(bwd_smem, stage, 0, dy + r * a.lddy, static_cast<const T*>(a.dy), a.cols);
+      R::request(bwd_smem, stage, 1, x + r * a.ldx, static_cast<const T*>(a.x), a.cols);
     }
+    copies_done();
   };
   float2 dg[kTurns][4] = {}, db[kTurns][4] = {};
   int r = chunk * a.per + lane;
@@ -562,10 +580,9 @@ __global__ void __launch_bounds__(kBlock, 1) norm_backward_kernel(const __grid_c
   float mean = r < r1 ? a.mean[first + r] : 0.f, rstd = r < r1 ? a.rstd[first + r] : 0.f;
   const float each = 1.f / a.cols;
   for (int it = 0, stage = 0; r < r1; r += kLanes, ++it) {
-    if constexpr (kVec) {
-      request(r + (kD - 1) * kLanes, stage == 0 ? kD - 1 : stage - 1);
-      copies_wait<kD - 1>();
-    }
+    request(r + (kD - 1) * kLanes, stage == 0 ? kD - 1 : stage - 1);
+    copies_wait<kD - 1>();
+    if constexpr (!kVec) R::meet();
     float2 h[kTurns][4], xh[kTurns][4];
     R::take(bwd_smem, stage, 0, dy + r * a.lddy, a.cols, h);
     R::take(bwd_smem, stage, 1, x + r * a.ldx, a.cols, xh);
@@ -595,6 +612,8 @@ __global__ void __launch_bounds__(kBlock, 1) norm_backward_kernel(const __grid_c
 #pragma unroll
         for (int e = 0; e < 4; ++e) h[i][e] = __fmul2_rn(both(rs), __ffma2_rn(xh[i][e], mhx, __fadd2_rn(h[i][e], mh)));
       R::put(static_cast<T*>(a.dx) + (first + r) * a.lddx, a.cols, h);
+    } else if constexpr (!kVec) {
+      R::meet();   // the stage has been read
     }
     if (++stage >= kD) stage = 0;
   }
@@ -604,7 +623,7 @@ __global__ void __launch_bounds__(kBlock, 1) norm_backward_kernel(const __grid_c
   }
 
   // the rows' lanes, then the chunks
-  if constexpr (kVec) copies_wait<0>();
+  copies_wait<0>();
   __syncthreads();
   float* sums = reinterpret_cast<float*>(bwd_smem);   // [2][kLanes][kCap]
 #pragma unroll

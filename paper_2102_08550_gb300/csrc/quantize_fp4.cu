@@ -31,13 +31,16 @@ Divide divide_by(uint32_t d) {
 }
 __device__ __forceinline__ uint32_t operator/(uint32_t n, const Divide& v) { return (__umulhi(n, v.m) + n) >> v.s; }
 
-// 16 values of a row as they were read (n of them are inside it).  wide: 32 for 32-byte accesses, 16 for 16-byte ones.
+// 16 values of a row as they were read (n of them are inside it).  wide: 32 for 32-byte accesses, 16 for 16-byte ones, 0 for a
+// matrix from `begin` to `end` whose rows start anywhere: the 16 bytes that hold the values are read and shifted.
 template <typename T>
 struct Held {
   static constexpr int kWords = kUnit * sizeof(T) / 4;
   uint32_t w[kWords];
 
-  __device__ __forceinline__ void load(const T* p, int n, int wide) {
+  __device__ __forceinline__ void load(const T* p, int n, int wide, const void* begin, const void* end) {
+    const int front = static_cast<int>(reinterpret_cast<uintptr_t>(p) & 15);
+    const uint8_t* from = reinterpret_cast<const uint8_t*>(p) - front;
     if (n >= kUnit && wide == 32) {
 #pragma unroll
       for (int i = 0; i < kWords; i += 8)
@@ -45,12 +48,27 @@ struct Held {
                      : "=r"(w[i]), "=r"(w[i + 1]), "=r"(w[i + 2]), "=r"(w[i + 3]), "=r"(w[i + 4]), "=r"(w[i + 5]), "=r"(w[i + 6]), "=r"(w[i + 7])
                      : "l"(reinterpret_cast<const uint32_t*>(p) + i)
                      : "memory");
-    } else if (n >= kUnit) {
+    } else if (n >= kUnit && wide == 16) {
 #pragma unroll
       for (int i = 0; i < kWords; i += 4) {
         const uint4 a = *reinterpret_cast<const uint4*>(reinterpret_cast<const uint32_t*>(p) + i);
         w[i] = a.x, w[i + 1] = a.y, w[i + 2] = a.z, w[i + 3] = a.w;
       }
+    } else if (wide == 0 && n >= kUnit && from >= static_cast<const uint8_t*>(begin) &&
+               from + 4 * kWords + 16 <= static_cast<const uint8_t*>(end)) {
+      uint32_t r[kWords + 4];
+#pragma unroll
+      for (int i = 0; i < kWords + 4; i += 4) {
+        const uint4 a = *reinterpret_cast<const uint4*>(from + 4 * i);
+        r[i] = a.x, r[i + 1] = a.y, r[i + 2] = a.z, r[i + 3] = a.w;
+      }
+      const bool two = front & 8, one = front & 4;
+#pragma unroll
+      for (int i = 0; i < kWords + 2; ++i) r[i] = two ? r[i + 2] : r[i];
+#pragma unroll
+      for (int i = 0; i < kWords + 1; ++i) r[i] = one ? r[i + 1] : r[i];
+#pragma unroll
+      for (int i = 0; i < kWords; ++i) w[i] = sizeof(T) == 4 ? r[i] : __funnelshift_r(r[i], r[i + 1], (front & 2) * 8);
     } else if constexpr (sizeof(T) == 4) {
 #pragma unroll
       for (int i = 0; i < kWords; ++i) w[i] = i < n ? reinterpret_cast<const uint32_t*>(p)[i] : 0u;
@@ -95,31 +113,9 @@ struct Held {
 };
 
 // Rows that are not 16-byte aligned: the G lanes of a group, whose units lie one behind the other from `base` on (n values up to
-// the row's end), read neighbouring values and exchange them through the warp's own part of shared memory.
+// the row's end), exchange them through the warp's own part of shared memory and write neighbouring ones.
 constexpr int kPitch = kUnit + 1, kExchange = 32 * kPitch;
 
-template <int G, typename T>
-__device__ __forceinline__ void load_apart(Held<T>& h, const T* base, int n, uint32_t* room) {
-  const int lane = threadIdx.x & 31, l = lane % G;
-  room += lane / G * G * kPitch;
-  uint32_t v[kUnit];
-#pragma unroll
-  for (int j = 0; j < kUnit; ++j) {
-    const int e = j * G + l;
-    if constexpr (sizeof(T) == 4) v[j] = e < n ? reinterpret_cast<const uint32_t*>(base)[e] : 0u;
-    else v[j] = e < n ? reinterpret_cast<const unsigned short*>(base)[e] : 0u;
-  }
-  __syncwarp();
-#pragma unroll
-  for (int j = 0; j < kUnit; ++j) {
-    const int e = j * G + l;
-    room[e + e / kUnit] = v[j];
-  }
-  __syncwarp();
-  const uint32_t* mine = room + l * kPitch;
-#pragma unroll
-  for (int i = 0; i < Held<T>::kWords; ++i) h.w[i] = sizeof(T) == 4 ? mine[i] : mine[2 * i] | mine[2 * i + 1] << 16;
-}
 template <int G, typename T>
 __device__ __forceinline__ void store_apart(const float (&f)[kUnit], T* base, int n, float* room) {
   const int lane = threadIdx.x & 31, l = lane % G;
@@ -136,7 +132,7 @@ __device__ __forceinline__ void store_apart(const float (&f)[kUnit], T* base, in
 }
 
 struct QuantArgs {
-  const void* x;
+  const void *x, *end;   // end: behind the last value
   uint8_t *q, *scales;
   float* row_scale;
   int64_t ldx, ldq;
@@ -149,7 +145,6 @@ struct QuantArgs {
 // Blocks are on their own: a thread takes kN units, whose loads are in flight together.
 template <typename T, int kN>
 __global__ void __launch_bounds__(kThreads) quantize_mx_kernel(const __grid_constant__ QuantArgs a) {
-  __shared__ uint32_t room[kThreads / 32][kExchange];
   pdl_wait();
   pdl_trigger();
   const int lane = threadIdx.x & 31;
@@ -162,13 +157,7 @@ __global__ void __launch_bounds__(kThreads) quantize_mx_kernel(const __grid_cons
     const uint32_t u = u0 + i * kThreads;
     row[i] = u < a.units ? u / a.per : 0;
     at[i] = u < a.units ? static_cast<int>(u - row[i] * a.per.d) * kUnit : -1;
-    const T* x = static_cast<const T*>(a.x) + row[i] * a.ldx;
-    if (a.wide) {
-      held[i].load(x + (at[i] < a.cols ? at[i] : 0), at[i] < 0 ? 0 : a.cols - at[i], a.wide);
-    } else {
-      const int tile = at[i] < 0 ? a.cols : at[i] / 128 * 128;
-      load_apart<8>(held[i], x + tile, a.cols - tile, room[threadIdx.x >> 5]);
-    }
+    held[i].load(static_cast<const T*>(a.x) + row[i] * a.ldx + (at[i] < a.cols ? at[i] : 0), at[i] < 0 ? 0 : a.cols - at[i], a.wide, a.x, a.end);
   }
 #pragma unroll
   for (int i = 0; i < kN; ++i) {
@@ -192,10 +181,10 @@ __global__ void __launch_bounds__(kThreads) quantize_mx_kernel(const __grid_cons
 // A row on TPR threads; up to kKeep turns stay in registers between the row's maximum and the codes.
 constexpr int kKeep = 2;
 
-template <typename T, int TPR, bool kWide>
+template <typename T, int TPR>
 __global__ void __launch_bounds__(kThreads) quantize_nv_kernel(const __grid_constant__ QuantArgs a) {
   constexpr int kRows = kThreads / TPR;
-  __shared__ uint32_t part[kThreads / 32], room[kWide ? 1 : kThreads / 32][kWide ? 1 : kExchange];
+  __shared__ uint32_t part[kThreads / 32];
   pdl_wait();
   pdl_trigger();
   const int64_t row = static_cast<int64_t>(blockIdx.x) * kRows + threadIdx.x / TPR;
@@ -204,9 +193,8 @@ __global__ void __launch_bounds__(kThreads) quantize_nv_kernel(const __grid_cons
   const bool live = row < a.rows;
   const T* x = static_cast<const T*>(a.x) + (live ? row : 0) * a.ldx;
   auto load = [&](Held<T>& h, int i) {
-    const int at = (i * TPR + t) * kUnit, warp = (i * TPR + t / 32 * 32) * kUnit;
-    if constexpr (kWide) h.load(x + (at < a.cols ? at : 0), a.cols - at, a.wide);
-    else load_apart<32>(h, x + (warp < a.cols ? warp : 0), a.cols - warp, room[threadIdx.x >> 5]);
+    const int at = (i * TPR + t) * kUnit;
+    h.load(x + (at < a.cols ? at : 0), a.cols - at, a.wide, a.x, a.end);
   };
   Held<T> held[kKeep];
   uint32_t m = 0;
@@ -364,13 +352,6 @@ cudaError_t by_units(uint32_t units, F&& f) {
   return f(std::integral_constant<int, 1>());
 }
 
-template <typename T, bool kWide>
-cudaError_t quantize_nv(const QuantArgs& a, cudaStream_t s) {
-  if (a.cols <= 32 * kUnit * kKeep) return launch_dependent(quantize_nv_kernel<T, 32, kWide>, dim3((a.rows + 7) / 8), kThreads, 0, s, a);
-  if (a.cols <= 128 * kUnit * kKeep) return launch_dependent(quantize_nv_kernel<T, 128, kWide>, dim3((a.rows + 1) / 2), kThreads, 0, s, a);
-  return launch_dependent(quantize_nv_kernel<T, kThreads, kWide>, dim3(a.rows), kThreads, 0, s, a);
-}
-
 template <typename T>
 cudaError_t quantize(const QuantArgs& a, int format, cudaStream_t s) {
   if (format == OSCARS_MXFP4) {
@@ -388,7 +369,9 @@ cudaError_t quantize(const QuantArgs& a, int format, cudaStream_t s) {
       });
     });
   }
-  return a.wide ? quantize_nv<T, true>(a, s) : quantize_nv<T, false>(a, s);
+  if (a.cols <= 32 * kUnit * kKeep) return launch_dependent(quantize_nv_kernel<T, 32>, dim3((a.rows + 7) / 8), kThreads, 0, s, a);
+  if (a.cols <= 128 * kUnit * kKeep) return launch_dependent(quantize_nv_kernel<T, 128>, dim3((a.rows + 1) / 2), kThreads, 0, s, a);
+  return launch_dependent(quantize_nv_kernel<T, kThreads>, dim3(a.rows), kThreads, 0, s, a);
 }
 
 template <typename T>
@@ -431,7 +414,8 @@ oscars_status oscars_quantize_fp4(const void* x, int64_t ldx, int32_t dtype, int
   if (!x || !q || !scales || !at_bytes(x, size) || !at_bytes(q, 16) || !at_bytes(scales, 16) || !at_bytes(row_scale, 4) ||
       (format == OSCARS_NVFP4) != (row_scale != nullptr))
     return OSCARS_EINVAL;
-  QuantArgs a{x, q, scales, row_scale, ldx, ldq, 0, {}, rows, cols, fp4_tiles(cols, format), wide_rows(x, ldx, size)};
+  const uint8_t* end = static_cast<const uint8_t*>(x) + ((rows - 1) * ldx + cols) * size;
+  QuantArgs a{x, end, q, scales, row_scale, ldx, ldq, 0, {}, rows, cols, fp4_tiles(cols, format), wide_rows(x, ldx, size)};
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const cudaError_t e = dtype == OSCARS_F32 ? quantize<float>(a, format, s) : quantize<__nv_bfloat16>(a, format, s);
   return e == cudaSuccess ? OSCARS_OK : OSCARS_ECUDA;
