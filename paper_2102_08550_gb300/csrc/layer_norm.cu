@@ -50,9 +50,9 @@ __device__ __forceinline__ void params8(const float* p, int at, int cols, bool v
 // ------------------------------------------------------------------ rows through shared memory
 // Up to 8192 columns: TPR threads take a row, a block 512 / TPR rows at a time; a thread owns 8 kTurns columns.  kMats matrices'
 // rows come through a ring in shared memory in which each thread reads what it has copied itself (cp.async, no barrier).
-// Where rows are not 16-byte aligned, they are copied from the 16 bytes on in which they begin, neighbouring threads take
-// neighbouring columns of them, and a barrier of the row's threads comes in between (12 x 332 x 5115 bf16 backward: loads of
-// single values when they are due 104 us).
+// Where rows are not 16-byte aligned, neighbouring threads take neighbouring columns.  Up to four rows at a time are copied from
+// the 16 bytes on in which they begin, with a barrier of the row's threads in between (2991 x 5541 fp32 backward 47 us, 56
+// without); more rows at a time hide the latency of loads of single values when they are due (16030 x 22 fp32 7.8 us, 11 copied).
 constexpr int kBlock = 512;
 
 __device__ __forceinline__ void copy16(void* to, const void* from, int bytes) {   // zeros behind the first `bytes`
@@ -71,9 +71,10 @@ struct Rows {
   static constexpr int kSize = sizeof(T), kLanes = kBlock / TPR, kCap = TPR * kTurns * 8;
   static constexpr int kPieces = kTurns * kSize / 2;          // of 16 bytes, of a thread's columns of one matrix
   static constexpr int kRow = kCap * kSize + 16;              // a row and what lies in front of it in its first 16 bytes
+  static constexpr bool kDirect = !kVec && kLanes > 4;
   static constexpr int kStage = kMats * (kVec ? kPieces * kBlock * 16 : kLanes * kRow);
-  static constexpr int kDepth = 200704 / kStage < 6 ? 200704 / kStage : 6;
-  static constexpr int kBytes = kDepth * kStage;
+  static constexpr int kDepth = kDirect ? 1 : 200704 / kStage < 6 ? 200704 / kStage : 6;
+  static constexpr int kBytes = kDirect ? 0 : kDepth * kStage;
 
   static constexpr int kPer = kVec ? 16 / static_cast<int>(sizeof(T)) : 1;         // neighbouring columns of a thread
   __device__ __forceinline__ static int column(int i, int e) {
@@ -93,6 +94,7 @@ struct Rows {
   }
   // begin the copy of row `row` of a matrix that starts at `first` to a stage
   __device__ __forceinline__ static void request(uint8_t* ring, int stage, int m, const T* row, const T* first, int cols) {
+    if constexpr (kDirect) return;
     if constexpr (!kVec) {   // whole 16 bytes, with a piece of the row before in front; the matrix's own first ones one at a time
       const int t = threadIdx.x % TPR, front = in_front(row), bytes = front + cols * kSize;
       uint8_t* to = lane_row(ring, stage, m);
@@ -131,7 +133,7 @@ struct Rows {
         }
       }
     } else {
-      const T* from = reinterpret_cast<const T*>(lane_row(ring, stage, m) + in_front(row));
+      const T* from = kDirect ? row : reinterpret_cast<const T*>(lane_row(ring, stage, m) + in_front(row));
 #pragma unroll
       for (int i = 0; i < kTurns; ++i)
 #pragma unroll
@@ -257,7 +259,7 @@ __global__ void __launch_bounds__(kBlock, 1) layer_norm_kernel(const __grid_cons
   for (int stage = 0; r < r1; r += R::kLanes) {
     request(r + (kD - 1) * R::kLanes, stage == 0 ? kD - 1 : stage - 1);
     copies_wait<kD - 1>();
-    if constexpr (!kVec) R::meet();
+    if constexpr (!kVec && !R::kDirect) R::meet();
     float2 v[kTurns][4];
     R::take(fwd_smem, stage, 0, x + r * a.ldx, a.cols, v);
     float2 pair = both(0.f);
@@ -582,7 +584,7 @@ __global__ void __launch_bounds__(kBlock, 1) norm_backward_kernel(const __grid_c
   for (int it = 0, stage = 0; r < r1; r += kLanes, ++it) {
     request(r + (kD - 1) * kLanes, stage == 0 ? kD - 1 : stage - 1);
     copies_wait<kD - 1>();
-    if constexpr (!kVec) R::meet();
+    if constexpr (!kVec && !R::kDirect) R::meet();
     float2 h[kTurns][4], xh[kTurns][4];
     R::take(bwd_smem, stage, 0, dy + r * a.lddy, a.cols, h);
     R::take(bwd_smem, stage, 1, x + r * a.ldx, a.cols, xh);
@@ -612,7 +614,7 @@ __global__ void __launch_bounds__(kBlock, 1) norm_backward_kernel(const __grid_c
 #pragma unroll
         for (int e = 0; e < 4; ++e) h[i][e] = __fmul2_rn(both(rs), __ffma2_rn(xh[i][e], mhx, __fadd2_rn(h[i][e], mh)));
       R::put(static_cast<T*>(a.dx) + (first + r) * a.lddx, a.cols, h);
-    } else if constexpr (!kVec) {
+    } else if constexpr (!kVec && !R::kDirect) {
       R::meet();   // the stage has been read
     }
     if (++stage >= kD) stage = 0;
@@ -665,13 +667,13 @@ __global__ void __launch_bounds__(kBlock, 1) norm_backward_kernel(const __grid_c
 
 // ------------------------------------------------------------------ backward, how it is split
 constexpr int kCtas = 152;        // chunks of all groups: one CTA an SM
-constexpr int kCluster = 8;
+constexpr int kCluster = 8, kFewRows = 8;
 
 struct Split {
   int chunks, per, clustered;
 };
 // One pass: a chunk for each SM, each with a row for all of its lanes at least.  Up to 16 chunks of a group are made eight, which
-// meet in a cluster: no second launch.
+// meet in a cluster, where they are short: up to kFewRows turns cost less than a second launch.
 // Wide rows: chunks of columns' tiles enough to fill the card, each of 64 rows or more.
 Split split_rows(int groups, int rows, int cols) {
   int64_t want, most;
@@ -686,7 +688,7 @@ Split split_rows(int groups, int rows, int cols) {
   }
   want = want < most ? want : most;
   if (want < 1) want = 1;
-  if (cols <= kWide && want > kCluster && want <= 2 * kCluster) want = kCluster;
+  if (cols <= kWide && want > kCluster && want <= 2 * kCluster && most <= kFewRows * kCluster) want = kCluster;
   Split s;
   s.per = static_cast<int>((rows + want - 1) / want);
   if (s.per < 1) s.per = 1;
