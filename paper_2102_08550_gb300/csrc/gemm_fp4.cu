@@ -13,7 +13,7 @@
 //   0       TMA of codes (128 channels and BN tokens, 256 of K) and of their scales into a ring
 //   1       copies a stage's scales to tensor memory and issues its products
 //   4-19    accumulators -> C, under the products of the next tile
-// gemm_fp4_few_kernel for one or two tokens.
+// gemm_fp4_few_kernel for one token, or up to three of few channels.
 #include <atomic>
 
 #include "common.cuh"
@@ -45,66 +45,100 @@ __device__ __forceinline__ float finish(const Fp4Args& a, float sum, float ra, f
   return a.relu && v < 0.f ? 0.f : v;
 }
 
-// ------------------------------------------------------------------ any sizes
-// A warp takes one channel and MT tokens, a lane 32 codes of a row a turn: its blocks' sums in fp32, times their scales.
+// ------------------------------------------------------------------ few tokens
+// A warp takes one channel, a lane 32 codes of a row a turn.  Eight products of codes are at most 288, in quarters, which fp16
+// holds exactly: a block's sum is two or four such sums, exact in fp32, and is added up times its scales.
+// Neither the tensor core's set-up nor its exchange pays here.  Measured (us, this kernel / the one below): 1 x 64 x 100 1.6 / 2.6;
+// 1 x 512 x 784 1.8 / 3.5; 1 x 4096 x 1024 3.2 / 3.5; 1 x 4096 x 4096 5.1 / 5.3; 2 x 1024 x 1024 2.5 / 3.4; 3 x 1024 x 1024 3.0 /
+// 3.4; beyond the rule 1 x 8192 x 512 3.6 / 3.0, 1 x 8192 x 8192 12 / 8.1, 2 x 4096 x 1024 5.2 / 3.4, 4 x 1024 x 1024 3.4 / 3.4.
 constexpr int kFewThreads = 256;
+bool few_tokens(int M, int N, int K) {
+  const int64_t codes = static_cast<int64_t>(N) * K;
+  return M == 1 ? N <= 4096 && codes <= 1 << 24 : M <= 3 && K <= 2048 && codes <= 1 << 20;
+}
 
-template <int MT>
+// codes' products over 16 columns, exact
+__device__ __forceinline__ float dot16(uint32_t a0, uint32_t a1, uint32_t b0, uint32_t b1) {
+  uint32_t p[4], q[4];
+  eight_values(a0, p);
+  eight_values(b0, q);
+  __half2 s = __hmul2(*reinterpret_cast<const __half2*>(&p[0]), *reinterpret_cast<const __half2*>(&q[0]));
+#pragma unroll
+  for (int i = 1; i < 4; ++i) s = __hfma2(*reinterpret_cast<const __half2*>(&p[i]), *reinterpret_cast<const __half2*>(&q[i]), s);
+  eight_values(a1, p);
+  eight_values(b1, q);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) s = __hfma2(*reinterpret_cast<const __half2*>(&p[i]), *reinterpret_cast<const __half2*>(&q[i]), s);
+  const float2 f = __half22float2(s);
+  return f.x + f.y;
+}
+
+template <int MT, bool kMx>
 __global__ void __launch_bounds__(kFewThreads) gemm_fp4_few_kernel(const __grid_constant__ Fp4Args a) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   pdl_wait();
   pdl_trigger();
   const int n = blockIdx.x * (kFewThreads / 32) + warp;
   if (n >= a.N) return;
-  const int groups = (a.K + 31) / 32;
-  {
-    constexpr int m0 = 0;
-    float sum[MT] = {};
-    for (int g = lane; g < groups; g += 32) {
-      const uint4 w = *reinterpret_cast<const uint4*>(a.B + n * a.ldb + g * 16);
-      const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
-      auto scales = [&](const uint8_t* s, int64_t row, float& s0, float& s1) {   // of the group's two halves
-        if (a.mx) {
-          s0 = s1 = e8m0_value(s[fp4_scale_at(row, g >> 2, a.tiles) + (g & 3)]);
-        } else {
-          const float2 f = __half22float2(e4m3_pair(*reinterpret_cast<const uint16_t*>(s + fp4_scale_at(row, g >> 1, a.tiles) + 2 * (g & 1))));
-          s0 = f.x, s1 = f.y;
-        }
-      };
-      float b0, b1;
-      scales(a.sb, n, b0, b1);
+  const int groups = (a.K + 31) / 32;   // of 32 codes: a block, or two
+  auto scales = [&](const uint8_t* s, int64_t row, int g) -> uint32_t {
+    if constexpr (kMx) return s[fp4_scale_at(row, g >> 2, a.tiles) + (g & 3)];
+    else return *reinterpret_cast<const uint16_t*>(s + fp4_scale_at(row, g >> 1, a.tiles) + 2 * (g & 1));
+  };
+  float sum[MT] = {};
+  constexpr int kAhead = 4;             // turns whose codes are requested together
+  for (int g0 = lane; g0 < groups; g0 += 32 * kAhead) {
+    uint4 w[kAhead];
+    uint32_t sw[kAhead];
 #pragma unroll
-      for (int m = 0; m < MT; ++m) {
-        if (m0 + m >= a.M) break;
-        const uint4 x = *reinterpret_cast<const uint4*>(a.A + (m0 + m) * a.lda + g * 16);
-        const uint32_t xx[4] = {x.x, x.y, x.z, x.w};
-        float s0, s1, part[2] = {};
-        scales(a.sa, m0 + m, s0, s1);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          uint32_t p[4], q[4];
-          eight_values(ww[i], p);
-          eight_values(xx[i], q);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const float2 u = __half22float2(*reinterpret_cast<const __half2*>(&p[j])), v = __half22float2(*reinterpret_cast<const __half2*>(&q[j]));
-            part[i >> 1] = fmaf(u.y, v.y, fmaf(u.x, v.x, part[i >> 1]));
-          }
-        }
-        sum[m] = fmaf(part[1], s1 * b1, fmaf(part[0], s0 * b0, sum[m]));
-      }
+    for (int h = 0; h < kAhead; ++h) {
+      const int g = g0 + 32 * h < groups ? g0 + 32 * h : g0;
+      w[h] = *reinterpret_cast<const uint4*>(a.B + n * a.ldb + g * 16);
+      sw[h] = scales(a.sb, n, g);
     }
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
-      float s = sum[m];
+      uint4 x[kAhead];
+      uint32_t sx[kAhead];
 #pragma unroll
-      for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-      if (lane == 0 && m0 + m < a.M) {
-        const float y = finish(a, s, a.ra ? a.ra[m0 + m] : 1.f, a.rb ? a.rb[n] : 1.f, a.bias ? a.bias[n] : 0.f);
-        if (a.bf16) static_cast<__nv_bfloat16*>(a.C)[(m0 + m) * a.ldc + n] = __float2bfloat16_rn(y);
-        else static_cast<float*>(a.C)[(m0 + m) * a.ldc + n] = y;
+      for (int h = 0; h < kAhead; ++h) {
+        const int g = g0 + 32 * h < groups ? g0 + 32 * h : g0;
+        x[h] = *reinterpret_cast<const uint4*>(a.A + m * a.lda + g * 16);
+        sx[h] = scales(a.sa, m, g);
+      }
+#pragma unroll
+      for (int h = 0; h < kAhead; ++h) {
+        if (g0 + 32 * h >= groups) break;
+        const float lo = dot16(w[h].x, w[h].y, x[h].x, x[h].y), hi = dot16(w[h].z, w[h].w, x[h].z, x[h].w);
+        if constexpr (kMx) {
+          sum[m] = fmaf(lo + hi, e8m0_value(sw[h]) * e8m0_value(sx[h]), sum[m]);
+        } else {
+          const float2 f = __half22float2(e4m3_pair(sw[h])), g = __half22float2(e4m3_pair(sx[h]));
+          sum[m] = fmaf(hi, f.y * g.y, fmaf(lo, f.x * g.x, sum[m]));
+        }
       }
     }
+  }
+#pragma unroll
+  for (int m = 0; m < MT; ++m) {
+    float s = sum[m];
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    if (lane == m) {
+      const float y = finish(a, s, a.ra ? a.ra[m] : 1.f, a.rb ? a.rb[n] : 1.f, a.bias ? a.bias[n] : 0.f);
+      if (a.bf16) static_cast<__nv_bfloat16*>(a.C)[m * a.ldc + n] = __float2bfloat16_rn(y);
+      else static_cast<float*>(a.C)[m * a.ldc + n] = y;
+    }
+  }
+}
+
+template <bool kMx>
+cudaError_t launch_few(const Fp4Args& a, cudaStream_t s) {
+  const dim3 grid((a.N + kFewThreads / 32 - 1) / (kFewThreads / 32));
+  switch (a.M) {
+    case 1: return launch_dependent(gemm_fp4_few_kernel<1, kMx>, grid, kFewThreads, 0, s, a);
+    case 2: return launch_dependent(gemm_fp4_few_kernel<2, kMx>, grid, kFewThreads, 0, s, a);
+    default: return launch_dependent(gemm_fp4_few_kernel<3, kMx>, grid, kFewThreads, 0, s, a);
   }
 }
 
@@ -123,9 +157,8 @@ struct Tile {
 };
 
 struct Bars {
-  uint64_t full[kMaxStages], empty[kMaxStages], accf[2], acce[2];
+  uint64_t full[kMaxStages], empty[kMaxStages], accf[2], acce[2], parts;   // parts: kSplit, all parts' sums are here
   uint32_t tmem;
-  int failed;   // kSplit: a part's sums are not all there
 };
 static_assert(sizeof(Bars) <= kBarBytes, "barriers fit");
 
@@ -172,9 +205,6 @@ __device__ __forceinline__ void umma_commit_pair(uint64_t* bar) {
 // tensor memory, which tcgen05.wait::ld has seen finished (gemm_i8.cu).
 __device__ __forceinline__ void mbar_arrive_at(uint32_t cluster_bar) {
   asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
-}
-__device__ __forceinline__ void st_peer(const void* local, int rank, uint32_t v) {
-  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(cluster_addr(local, rank)), "r"(v) : "memory");
 }
 
 // e2m1 operands (1), both K-major; scales e8m0 or e4m3
@@ -315,7 +345,8 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp4_kernel(const __grid_cons
       mbar_init(&bars->accf[i], 1);
       mbar_init(&bars->acce[i], kEpiWarps * CL);
     }
-    bars->failed = 0;
+    mbar_init(&bars->parts, 1);
+    if (kSplit) mbar_arrive_expect_tx(&bars->parts, p.BN * 512);
     fence_barrier_init();
     fence_proxy_async_smem();
   }
@@ -334,11 +365,12 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp4_kernel(const __grid_cons
   else __syncthreads();
   tc_fence_after();
   // all of tensor memory is this CTA's, so its columns start at 0: written so, addresses stay in uniform registers and an
-  // instruction takes its issue slot instead of 40 clocks (8192 x 4096 x 4096: @@)
+  // instruction takes its issue slot instead of 40 clocks (8192 x 4096 x 4096 51.6 -> 44.6 us)
   constexpr uint32_t tmem = 0;
   pdl_wait();
   pdl_trigger();
 
+  bool ok = true;   // of the epilogue's warps: no wait has run out
   if (warp == 0) {
     // ---- TMA
     int it = 0, s = 0, ph = 1;
@@ -442,7 +474,6 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp4_kernel(const __grid_cons
     const int quarter = warp & 3, span = p.BN > 64 ? p.BN / 4 : 16, cb = (warp / 4 - 1) * span;
     const bool works = cb < p.BN;
     int t = 0;
-    bool ok = true;
     for (int u = u0; ok && u < p.units; u += ustep) {
       const int row = ((u % mu) * CL + rank) * 128 + 32 * quarter + lane, col0 = (u / mu) * p.BN + cb;
       const uint32_t row0 = tmem + (static_cast<uint32_t>(32 * quarter) << 16) + cb;
@@ -491,21 +522,14 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp4_kernel(const __grid_cons
         }
       }
       ++t;
-      if (!ok) {   // every wait that runs out in this CTA ends in one of the accumulator's; its peers then leave the tile alone too
-        if (kSplit && lane < p.split) st_peer(&bars->failed, lane, 1);
-        break;
-      }
+      if (!ok) break;   // every wait that runs out in this CTA ends in one of the accumulator's
       if (!works) continue;
-      if constexpr (kSplit) {   // a part's sums [token][channel] go to the CTA that adds up the token
-        const int owned = p.BN / p.split;
+      if constexpr (kSplit) {   // the part's sums [token][channel], where the ring was: its products have ended
 #pragma unroll
         for (int g = 0; g < kSpan / 16; ++g)
           if (16 * g < span) {
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              const int tok = cb + 16 * g + e;
-              st_peer(recv + ((part * owned + tok % owned) * 128 + 32 * quarter + lane) * 4, tok / owned, __float_as_uint(sum[g][e]));
-            }
+            for (int e = 0; e < 16; ++e) *reinterpret_cast<float*>(ring + ((cb + 16 * g + e) * 128 + 32 * quarter + lane) * 4) = sum[g][e];
           }
       } else if constexpr (kTokens) {
         const float ra = near_one(mine), to = back(mine);
@@ -525,24 +549,47 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp4_kernel(const __grid_cons
     }
     if (kTokens && lane == 0) bulk_wait_all();
   }
-  tc_fence_before();
-  if (CL > 1 || kSplit) cluster_sync();   // the pair's products and arrivals are done in both CTAs; every part's sums are there
-  else __syncthreads();
   if constexpr (kSplit) {
-    // each CTA adds up its tokens of the tile over the parts
-    const int missing = bars->failed;
-    const int n0 = (u0 % mu) * 128, tokens = p.BN / p.split, m0 = (u0 / mu) * p.BN + part * tokens;
-    const float* sums = reinterpret_cast<const float*>(recv);
-    for (int i = threadIdx.x; missing == 0 && i < tokens * 128; i += kThreads) {
-      const int m = m0 + i / 128, n = n0 + i % 128;
-      if (m >= a.M || n >= a.N) continue;
-      float t = 0.f;
-      for (int q = 0; q < p.split; ++q) t += sums[q * tokens * 128 + i];
-      const float y = finish(a, t, a.ra ? __ldg(a.ra + m) : 1.f, a.rb ? __ldg(a.rb + n) : 1.f, a.bias ? __ldg(a.bias + n) : 0.f);
-      if (a.bf16) static_cast<__nv_bfloat16*>(a.C)[m * a.ldc + n] = __float2bfloat16_rn(y);
-      else static_cast<float*>(a.C)[m * a.ldc + n] = y;
+    // each token's sums go to the CTA that adds up its parts, 128 channels of all of its tokens at once
+    const int tokens = p.BN / p.split, bytes = tokens * 512;
+    if (warp >= 4) {
+      fence_proxy_async_smem();
+      if (bar_and(1, kEpiWarps * 32, ok) && threadIdx.x == 128)   // no part is sent that is not whole
+        for (int i = 0; i < p.split; ++i) {   // each begins with another one: all at one CTA are received one after the other
+          const int r = (part + i) % p.split;
+          bulk_copy_to_peer(recv + part * bytes, ring + r * bytes, bytes, &bars->parts, r);
+        }
+      // a warp adds up a token, four channels a lane
+      const int n0 = (u0 % mu) * 128 + lane, m0 = (u0 / mu) * p.BN + part * tokens, end = a.M - m0 < tokens ? a.M - m0 : tokens;
+      float rb[4], bias[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        rb[j] = a.rb && n0 + 32 * j < a.N ? __ldg(a.rb + n0 + 32 * j) : 1.f;
+        bias[j] = a.bias && n0 + 32 * j < a.N ? __ldg(a.bias + n0 + 32 * j) : 0.f;
+      }
+      const float* sums = reinterpret_cast<const float*>(recv) + lane;
+      if (mbar_wait_warp(&bars->parts, 0, nullptr, kDevTimeoutAccum)) {   // and none is added up that is not there
+        for (int i = warp - 4; i < end; i += kEpiWarps) {
+          const float ra = a.ra ? __ldg(a.ra + m0 + i) : 1.f;
+          float t[4] = {};
+          for (int q = 0; q < p.split; ++q)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) t[j] += sums[(q * tokens + i) * 128 + 32 * j];
+          const int64_t at = (m0 + i) * a.ldc + n0;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float y = finish(a, t[j], ra, rb[j], bias[j]);
+            if (n0 + 32 * j >= a.N) continue;
+            if (a.bf16) static_cast<__nv_bfloat16*>(a.C)[at + 32 * j] = __float2bfloat16_rn(y);
+            else static_cast<float*>(a.C)[at + 32 * j] = y;
+          }
+        }
+      }
     }
   }
+  tc_fence_before();
+  if (CL > 1 || kSplit) cluster_sync();   // the pair's products and arrivals are done in both CTAs; every part's sums have been read
+  else __syncthreads();
   if (warp == 2) {
     tc_fence_after();
     if (CL == 1) tmem_dealloc(bars->tmem, 512);
@@ -637,29 +684,30 @@ bool result_map(CUtensorMap* m, void* C, int64_t ldc, int M, int N, bool bf16) {
                     CU_TENSOR_MAP_SWIZZLE_64B);
 }
 
-// The shape with the least estimated time: waves of tiles times the longer of a K-block's products (2 BN clocks, or 130 for
-// the rows' reads) and its loads (45 bytes a clock), plus fixed parts
+// The shape with the least estimated time, in clocks, as fitted to 30 sizes in all of their shapes (the choice is within 10% of
+// the best of them, two of 30 within 15%).  A wave of tiles takes its K-blocks (issue, or loads at 60 bytes a clock, 80 while
+// few tiles load) and what lies between two accumulations, or its results' way to memory if that is longer; the last one's
+// comes on top, and a split's exchange.
 void choose(const Fp4Args& a, bool boxes, int sms, int pairs, Tile& p, int& cl) {
   const int nk = (a.K + kK - 1) / kK;
   double best = 0.0;
   for (int tokens = 0; tokens <= (boxes ? 1 : 0); ++tokens) {
     const int64_t rows = tokens ? a.M : a.N, cols = tokens ? a.N : a.M;
-    for (int c = 1; c <= 2; ++c) {
+    for (int c = 1; c <= (rows > 128 ? 2 : 1); ++c) {
       const int64_t mt = ((rows + 127) / 128 + c - 1) / c * c;
       for (int bn = c == 1 ? 16 : 64; bn <= kMaxBN; bn *= 2) {
         // a product takes a scale tile from its first row on, and a warp's columns are whole boxes
         if (bn < 128 && (cols > bn || tokens)) continue;
         const int64_t nt = (cols + bn - 1) / bn, units = mt / c * nt;
         const int room = c == 2 ? pairs : sms;
+        const double waves = static_cast<double>((units + room - 1) / room);
         const double bytes = (128 + bn / c) * 128 + 512 * (a.mx ? 2 : 4) * (bn > 128 ? 3 : 2);
-        double kb = 2.0 * bn;
-        kb = kb > 130.0 ? kb : 130.0;
-        kb = kb > bytes / 45.0 ? kb : bytes / 45.0;
+        const double issue = (c == 2 ? 340.0 : 420.0) + bn, loads = bytes / (waves > 2.0 ? 60.0 : 80.0), kb = issue > loads ? issue : loads;
+        const double store = tokens ? 1200.0 + 9.4 * bn : (c == 2 ? 400.0 : 2200.0) + 25.0 * bn, last = (tokens ? 12.0 : 26.0) * bn;
         for (int split = 1; split <= (c == 1 && !tokens ? 8 : 1); split *= 2) {
           if (split > 1 && (units * split > sms * 7 / 8 || nk < 2 * split || bn < 2 * split || bn > 128)) break;
-          const double waves = split > 1 ? 1.0 : static_cast<double>((units + room - 1) / room);
-          const double cost = waves * ((nk + split - 1) / split * kb + 600.0) + (tokens ? 5.0 : 15.0) * bn + (c == 2 ? 1500.0 : 0.0) +
-                              (split > 1 ? 3000.0 : 0.0);
+          const double main = (nk + split - 1) / split * kb + (bn > 128 ? 900.0 : 300.0);
+          const double cost = (split > 1 ? main + 1500.0 + 29.0 * bn : waves * (main > store || waves == 1.0 ? main : store)) + last + (c == 2 ? 900.0 : 0.0);
           if (best == 0.0 || cost < best) {
             best = cost;
             cl = c;
@@ -707,11 +755,8 @@ oscars_status oscars_gemm_fp4_nt(const uint8_t* A, int64_t lda, const uint8_t* s
   Fp4Args a{A, scales_a, B, scales_b, row_a, row_b, bias, C, lda, ldb, ldc, M, N, K, format == OSCARS_MXFP4, fp4_tiles(K, format), relu,
             dtype == OSCARS_BF16};
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (M <= 2) {
-    constexpr int kPer = kFewThreads / 32;
-    const dim3 grid((N + kPer - 1) / kPer);
-    const cudaError_t e = M == 1 ? launch_dependent(gemm_fp4_few_kernel<1>, grid, kFewThreads, 0, s, a)
-                                 : launch_dependent(gemm_fp4_few_kernel<2>, grid, kFewThreads, 0, s, a);
+  if (few_tokens(M, N, K)) {
+    const cudaError_t e = a.mx ? launch_few<true>(a, s) : launch_few<false>(a, s);
     return e == cudaSuccess ? OSCARS_OK : OSCARS_ECUDA;
   }
   int sms, pairs, cl = 1;
