@@ -124,10 +124,22 @@ __device__ __forceinline__ void store_apart(const float (&f)[kUnit], T* base, in
 #pragma unroll
   for (int i = 0; i < kUnit; ++i) room[l * kPitch + i] = f[i];
   __syncwarp();
+  if constexpr (sizeof(T) == 4) {
 #pragma unroll
-  for (int j = 0; j < kUnit; ++j) {
-    const int e = j * G + l;
-    if (e < n) base[e] = static_cast<T>(room[e + e / kUnit]);
+    for (int j = 0; j < kUnit; ++j) {
+      const int e = j * G + l;
+      if (e < n) base[e] = room[e + e / kUnit];
+    }
+  } else {   // in words of two; the first and the last may be half the neighbours'
+    const int odd = static_cast<int>(reinterpret_cast<uintptr_t>(base) >> 1 & 1), most = n < G * kUnit ? n : G * kUnit;
+#pragma unroll
+    for (int j = 0; j <= kUnit / 2; ++j) {
+      const int e = (j * G + l) * 2 - odd, f = e + 1;
+      const float a = e >= 0 && e < most ? room[e + e / kUnit] : 0.f, b = f < most ? room[f + f / kUnit] : 0.f;
+      if (e >= 0 && f < most) *reinterpret_cast<uint32_t*>(base + e) = pack_bf16x2(a, b);
+      else if (e >= 0 && e < most) base[e] = static_cast<T>(a);
+      else if (f >= 0 && f < most) base[f] = static_cast<T>(b);
+    }
   }
 }
 
@@ -182,7 +194,7 @@ __global__ void __launch_bounds__(kThreads) quantize_mx_kernel(const __grid_cons
 constexpr int kKeep = 2;
 
 template <typename T, int TPR>
-__global__ void __launch_bounds__(kThreads) quantize_nv_kernel(const __grid_constant__ QuantArgs a) {
+__global__ void __launch_bounds__(kThreads / TPR * TPR) quantize_nv_kernel(const __grid_constant__ QuantArgs a) {
   constexpr int kRows = kThreads / TPR;
   __shared__ uint32_t part[kThreads / 32];
   pdl_wait();
@@ -369,9 +381,17 @@ cudaError_t quantize(const QuantArgs& a, int format, cudaStream_t s) {
       });
     });
   }
-  if (a.cols <= 32 * kUnit * kKeep) return launch_dependent(quantize_nv_kernel<T, 32>, dim3((a.rows + 7) / 8), kThreads, 0, s, a);
-  if (a.cols <= 128 * kUnit * kKeep) return launch_dependent(quantize_nv_kernel<T, 128>, dim3((a.rows + 1) / 2), kThreads, 0, s, a);
-  return launch_dependent(quantize_nv_kernel<T, kThreads>, dim3(a.rows), kThreads, 0, s, a);
+  auto rows = [&](auto tpr) {
+    constexpr int kRows = kThreads / tpr();
+    return launch_dependent(quantize_nv_kernel<T, tpr()>, dim3((a.rows + kRows - 1) / kRows), kRows * tpr(), 0, s, a);
+  };
+  // the least whole warps that keep a row in registers
+  const int warps = (a.cols + 32 * kUnit * kKeep - 1) / (32 * kUnit * kKeep);
+  if (warps <= 1) return rows(std::integral_constant<int, 32>());
+  if (warps <= 2) return rows(std::integral_constant<int, 64>());
+  if (warps <= 4) return rows(std::integral_constant<int, 128>());
+  if (warps <= 6) return rows(std::integral_constant<int, 192>());
+  return rows(std::integral_constant<int, 256>());
 }
 
 template <typename T>
