@@ -733,6 +733,7 @@ cudaError_t launch_tile(const CUtensorMap (&m)[5], const Fp4Args& a, const Tile&
                      : launch_fp4<1, false, kMx, false>(m, a, p, grid, s);
 }
 
+constexpr int64_t kMaxStride = int64_t(1) << 40;   // of a tensor map
 bool at_bytes(const void* p, int n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 
 }  // namespace
@@ -748,6 +749,7 @@ oscars_status oscars_gemm_fp4_nt(const uint8_t* A, int64_t lda, const uint8_t* s
   if (M < 0 || M > kFp4MaxSide || N < 1 || N > kFp4MaxSide || K < 1 || K > kFp4MaxSide || lda % 16 || ldb % 16 || lda < fp4_row_bytes(K) ||
       ldb < fp4_row_bytes(K) || ldc < N || (format != OSCARS_MXFP4 && format != OSCARS_NVFP4) || (dtype != OSCARS_F32 && dtype != OSCARS_BF16))
     return OSCARS_EINVAL;
+  if (lda >= kMaxStride || ldb >= kMaxStride) return OSCARS_EINVAL;
   if (M == 0) return OSCARS_OK;
   if (!A || !B || !C || !scales_a || !scales_b || !at_bytes(A, 16) || !at_bytes(B, 16) || !at_bytes(scales_a, 16) || !at_bytes(scales_b, 16) ||
       !at_bytes(row_a, 4) || !at_bytes(row_b, 4) || !at_bytes(bias, 4) || !at_bytes(C, dtype == OSCARS_F32 ? 4 : 2))
@@ -763,8 +765,8 @@ oscars_status oscars_gemm_fp4_nt(const uint8_t* A, int64_t lda, const uint8_t* s
   device_room(sms, pairs);
   Tile p{};
   const int size = dtype == OSCARS_F32 ? 4 : 2;
-  // TMA stores rows of 16 bytes' alignment, and its strides end at 2^40
-  choose(a, at_bytes(C, 16) && ldc * size % 16 == 0 && ldc < (int64_t(1) << 37), sms, pairs, p, cl);
+  // TMA stores rows of 16 bytes' alignment
+  choose(a, at_bytes(C, 16) && ldc * size % 16 == 0 && ldc < kMaxStride / 8, sms, pairs, p, cl);
   const int64_t units = static_cast<int64_t>(p.mt / cl) * p.nt;
   if (units > INT32_MAX / 2) return OSCARS_EINVAL;
   p.units = static_cast<int>(units);

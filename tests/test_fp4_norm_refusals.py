@@ -42,7 +42,7 @@ def product(a=4096, lda=32, sa=4096, b=4096, ldb=32, sb=4096, fmt=P.MXFP4, c=409
 @pytest.mark.parametrize("kw", [dict(a=0), dict(a=4097), dict(lda=24), dict(lda=16), dict(sa=0), dict(sa=4100), dict(b=0), dict(b=4104),
                                 dict(ldb=0), dict(ldb=33), dict(sb=0), dict(sb=4097), dict(fmt=3), dict(c=0), dict(c=4098),
                                 dict(c=4097, dtype=P.BF16), dict(ldc=7), dict(dtype=5), dict(M=-1), dict(M=BIG), dict(N=0), dict(N=BIG, ldc=BIG),
-                                dict(K=0), dict(K=BIG), dict(K=65), dict(row_scale_a_ptr=4097), dict(row_scale_b_ptr=4098), dict(bias_ptr=4099)])
+                                dict(K=0), dict(K=BIG), dict(K=65), dict(lda=1 << 40), dict(ldb=1 << 40), dict(row_scale_a_ptr=4097), dict(row_scale_b_ptr=4098), dict(bias_ptr=4099)])
 def test_product(oscars_lib, kw):
     refused(lambda: product(**kw))
 

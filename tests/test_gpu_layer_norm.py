@@ -137,7 +137,7 @@ def make(groups, rows, cols, dtype, dev, seed=0, pad=0, shift=0):
 SHAPES = [(1, 1, 1, 0, 0), (1, 1, 512, 0, 0), (1, 3, 2, 0, 0), (1, 5, 7, 3, 1), (2, 4, 8, 0, 0), (3, 5, 33, 7, 2), (16, 64, 512, 0, 0),
           (1, 1003, 777, 6, 0), (7, 33, 1000, 0, 0), (1, 130, 1024, 0, 0), (4, 70, 1025, 1, 3), (1, 9, 4096, 8, 0), (2, 100, 4097, 0, 0),
           (1, 40, 8192, 0, 0), (3, 7, 8191, 1, 0), (1, 12, 8200, 0, 0), (2, 3, 20001, 3, 5), (1, 2, 70000, 0, 0), (300, 2, 65, 0, 0),
-          (1, 2500, 130, 0, 0), (32, 100, 96, 8, 8), (1, 700, 2048, 0, 0), (5, 257, 256, 0, 0), (65535, 1, 3, 0, 0), (2, 1500, 640, 0, 0)]
+          (2, 6, 3001, 2, 1), (1, 5, 5001, 3, 3), (3, 4, 8001, 0, 5), (1, 2500, 130, 0, 0), (32, 100, 96, 8, 8), (1, 700, 2048, 0, 0), (5, 257, 256, 0, 0), (65535, 1, 3, 0, 0), (2, 1500, 640, 0, 0)]
 
 
 @pytest.mark.parametrize("dtype", TYPES)
