@@ -383,9 +383,9 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp4_kernel(const __grid_cons
           uint8_t* at = ring + s * stage_bytes;
           uint64_t* bar = &bars->full[s];
           if (rank == 0) mbar_arrive_expect_tx(bar, CL * copied);   // a pair's bytes count on the leader's
-          auto load = [&](int to, const CUtensorMap* map, int c0, int c1, int c2) {
-            if (CL > 1) tma_load_3d_pair(at + to, map, c0, c1, c2, bar);
-            else tma_load_3d(at + to, map, c0, c1, c2, bar);
+          auto load = [&](int to, const CUtensorMap* map, int x, int y, int z) {
+            if (CL > 1) tma_load_3d_pair(at + to, map, x, y, z, bar);
+            else tma_load_3d(at + to, map, x, y, z, bar);
           };
           load(0, &mapW, kb * 128, r0, 0);
           load(x_at, &mapX, kb * 128, c0 + rank * bn, 0);
@@ -399,10 +399,9 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp4_kernel(const __grid_cons
         }
       }
     }
-    // the copies have landed before this CTA ends (a pair's end together)
-    if (rank == 0)
-      for (int i = it > p.stages ? it - p.stages : 0; i < it; ++i)
-        mbar_wait_keep(limit, &bars->full[i % p.stages], (i / p.stages) & 1, nullptr, kDevTimeoutFull);
+    // no copy and no commit of the leader may still be on its way to this CTA when it ends
+    for (int i = it > p.stages ? it - p.stages : 0; i < it; ++i)
+      mbar_wait_keep(limit, &bars->empty[i % p.stages], (i / p.stages) & 1, nullptr, kDevTimeoutEmpty);
   } else if (warp == 1 && rank == 0) {
     // ---- scales to tensor memory, products (the leader's, of a pair); the warp stays converged and one elected lane issues
     const uint32_t idesc = idesc_fp4(128 * CL, p.BN, kMx), ring0 = smem_u32(ring);
@@ -417,7 +416,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp4_kernel(const __grid_cons
         tc_fence_after();
         const uint32_t at = ring0 + s * stage_bytes, sw = tmem + kScaleCol + s * cols, sx = sw + 4 * kTk;
         if (elect_one() && limit > 1) {
-                    const uint64_t swd = scale_desc(at + sw_at), sxd = scale_desc(at + sx_at);
+          const uint64_t swd = scale_desc(at + sw_at), sxd = scale_desc(at + sx_at);
           // a stage's columns were last read by products that have ended: its copies have been waited for.  Tiles behind the
           // last are zeros that no product takes
           if (xt == 2) {
@@ -684,8 +683,8 @@ bool result_map(CUtensorMap* m, void* C, int64_t ldc, int M, int N, bool bf16) {
                     CU_TENSOR_MAP_SWIZZLE_64B);
 }
 
-// The shape with the least estimated time, in clocks, as fitted to 30 sizes in all of their shapes (the choice is within 10% of
-// the best of them, two of 30 within 15%).  A wave of tiles takes its K-blocks (issue, or loads at 60 bytes a clock, 80 while
+// The shape with the least estimated time, in clocks, as fitted to 31 sizes in all of their shapes (the choice is within 10% of
+// the best of them, one within 15%).  A wave of tiles takes its K-blocks (issue, or loads at 60 bytes a clock, 80 while
 // few tiles load) and what lies between two accumulations, or its results' way to memory if that is longer; the last one's
 // comes on top, and a split's exchange.
 void choose(const Fp4Args& a, bool boxes, int sms, int pairs, Tile& p, int& cl) {
@@ -703,7 +702,8 @@ void choose(const Fp4Args& a, bool boxes, int sms, int pairs, Tile& p, int& cl) 
         const double waves = static_cast<double>((units + room - 1) / room);
         const double bytes = (128 + bn / c) * 128 + 512 * (a.mx ? 2 : 4) * (bn > 128 ? 3 : 2);
         const double issue = (c == 2 ? 340.0 : 420.0) + bn, loads = bytes / (waves > 2.0 ? 60.0 : 80.0), kb = issue > loads ? issue : loads;
-        const double store = tokens ? 1200.0 + 9.4 * bn : (c == 2 ? 400.0 : 2200.0) + 25.0 * bn, last = (tokens ? 12.0 : 26.0) * bn;
+        const double wide = a.bf16 ? 1.0 : 1.6;
+        const double store = tokens ? 1200.0 + 9.4 * wide * bn : (c == 2 ? 400.0 : 2200.0) + 25.0 * bn, last = (tokens ? 12.0 * wide : 26.0) * bn;
         for (int split = 1; split <= (c == 1 && !tokens ? 8 : 1); split *= 2) {
           if (split > 1 && (units * split > sms * 7 / 8 || nk < 2 * split || bn < 2 * split || bn > 128)) break;
           const double main = (nk + split - 1) / split * kb + (bn > 128 ? 900.0 : 300.0);
