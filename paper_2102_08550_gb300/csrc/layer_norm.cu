@@ -4,7 +4,9 @@
 //   dx = rstd (h - mean(h) - xh mean(h xh)),  h = dy gamma,  xh = (x - mean) rstd
 //   dgamma = sum over the group's rows of dy xh,  dbeta = sum of dy
 //
-// Bound by memory: forward reads x and writes y, backward reads dy and x and writes dx.
+// Bound by memory: forward reads x and writes y, backward reads dy and x and writes dx.  8192 x 4096 bf16 forward 24.3 us (5.5
+// TB/s; a copy of as many bytes 21.1), 16384 x 4096 bf16 backward 67.4 us (6.0 TB/s; twice the rows 124 us, 6.5 TB/s).
+// Additions, products and their sums go two at a time (f32x2), which takes half the issue slots.
 #include <type_traits>
 
 #include "../../include/oscars.h"
@@ -19,21 +21,16 @@ namespace {
 constexpr int kMaxSide = 1 << 30, kMaxGroups = 65535;
 constexpr int kThreads = 256;
 
-// the sum of a value over the TPR threads of a row, in each of them, in a fixed order (a barrier of the row's threads
-// alone: rows of one block may differ in how many sums they take)
-template <int TPR>
-__device__ __forceinline__ float row_sum(float v, float* part) {
+// the sum of a value over a block of kThreads, in each of them, in a fixed order
+__device__ __forceinline__ float block_sum(float v, float* part) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  if (TPR > 32) {
-    const int r = threadIdx.x / TPR;
-    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
-    bar_named(1 + r, TPR);
-    v = 0.f;
+  if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
+  __syncthreads();
+  v = 0.f;
 #pragma unroll
-    for (int i = 0; i < TPR / 32; ++i) v += part[r * (TPR / 32) + i];
-    bar_named(1 + r, TPR);
-  }
+  for (int i = 0; i < kThreads / 32; ++i) v += part[i];
+  __syncthreads();
   return v;
 }
 
@@ -95,8 +92,16 @@ struct Rows {
   // begin the copy of row `row` of a matrix that starts at `first` to a stage (kFull: all of the warp's columns are inside the row)
   template <bool kFull>
   __device__ __forceinline__ static void request(uint8_t* ring, int stage, int m, const T* row, const T* first, int cols) {
-    if constexpr (kDirect) return;
-    if constexpr (!kVec) {   // whole 16 bytes, with a piece of the row before in front; the matrix's own first ones one at a time
+    constexpr int kPiece = 16 / kSize;                       // columns of 16 bytes
+    if constexpr (kVec) {
+      uint8_t* to = ring + stage * kStage + (m * kPieces * kBlock + threadIdx.x) * 16;
+#pragma unroll
+      for (int p = 0; p < kPieces; ++p) {
+        const int at = column(p * kPiece / 8, p * kPiece % 8), left = (cols - at) * kSize;
+        if constexpr (kFull) copy16(to + p * kBlock * 16, row + at);
+        else copy16(to + p * kBlock * 16, row + (left > 0 ? at : 0), left >= 16 ? 16 : left > 0 ? left : 0);
+      }
+    } else if constexpr (!kDirect) {   // whole 16 bytes, with a piece of the row before in front; the matrix's own first ones one at a time
       const int t = threadIdx.x % TPR, front = in_front(row), bytes = front + cols * kSize;
       uint8_t* to = lane_row(ring, stage, m);
       const uint8_t* from = reinterpret_cast<const uint8_t*>(row) - front;
@@ -104,18 +109,6 @@ struct Rows {
       if (!inside && t < (16 - front) / kSize && t < cols) reinterpret_cast<T*>(to + front)[t] = row[t];
       for (int at = t * 16; at < bytes; at += TPR * 16)
         if (inside || at > 0) copy16(to + at, from + at, bytes - at >= 16 ? 16 : bytes - at);
-      return;
-    }
-    uint8_t* to = ring + stage * kStage + (m * kPieces * kBlock + threadIdx.x) * 16;
-    if constexpr (kFull) {
-#pragma unroll
-      for (int p = 0; p < kPieces; ++p) copy16(to + p * kBlock * 16, row + column(p * kPer / 8, p * kPer % 8));
-      return;
-    }
-#pragma unroll
-    for (int p = 0; p < kPieces; ++p) {
-      const int at = column(p * kPer / 8, p * kPer % 8), left = (cols - at) * static_cast<int>(sizeof(T));
-      copy16(to + p * kBlock * 16, row + (left > 0 ? at : 0), left >= 16 ? 16 : left > 0 ? left : 0);
     }
   }
   // this thread's columns of it (zeros behind the row's end)
@@ -233,6 +226,8 @@ __device__ __forceinline__ float inverse_std(const Squares& s, int cols, float e
   return static_cast<float>(1.0 / sqrt(s.total() / cols + eps));
 }
 
+// Mean and squares of deviations from registers: two exchanges between a row's threads, each behind one barrier, are what a row
+// waits for, so that four rows at a time or more are under way.
 template <typename T, int TPR, int kTurns, bool kVec>
 __global__ void __launch_bounds__(kBlock, 1) layer_norm_kernel(const __grid_constant__ FwdArgs a) {
   using R = Rows<T, TPR, kTurns, kVec, 1>;
@@ -248,87 +243,87 @@ __global__ void __launch_bounds__(kBlock, 1) layer_norm_kernel(const __grid_cons
   const T* x = static_cast<const T*>(a.x) + first * a.ldx;
   // warps of which all columns are inside the row go without bounds (8192 x 4096 bf16 30.0 -> 24.2 us)
   auto all_rows = [&](auto with) {
-  constexpr bool kFull = with();
-  auto request = [&](int r, int stage) {
-    if (r < r1) R::template request<kFull>(fwd_smem, stage, 0, x + r * a.ldx, static_cast<const T*>(a.x), a.cols);
-    copies_done();
-  };
-  int r = chunk * a.per + lane;
+    constexpr bool kFull = with();
+    auto request = [&](int r, int stage) {
+      if (r < r1) R::template request<kFull>(fwd_smem, stage, 0, x + r * a.ldx, static_cast<const T*>(a.x), a.cols);
+      copies_done();
+    };
+    int r = chunk * a.per + lane;
 #pragma unroll
-  for (int i = 0; i < kD - 1; ++i) request(r + i * R::kLanes, i);
-  float2 g[kTurns][4], b[kTurns][4];
-  R::params(a.gamma ? a.gamma + group * a.pstride : nullptr, a.cols, a.pvec, 1.f, g);
-  R::params(a.beta ? a.beta + group * a.pstride : nullptr, a.cols, a.pvec, 0.f, b);
-  const float each = 1.f / a.cols;
-  for (int stage = 0; r < r1; r += R::kLanes) {
-    request(r + (kD - 1) * R::kLanes, stage == 0 ? kD - 1 : stage - 1);
-    copies_wait<kD - 1>();
-    if constexpr (!kVec && !R::kDirect) R::meet();
-    float2 v[kTurns][4];
-    R::template take<kFull>(fwd_smem, stage, 0, x + r * a.ldx, a.cols, v);
-    float2 pair = both(0.f);
+    for (int i = 0; i < kD - 1; ++i) request(r + i * R::kLanes, i);
+    float2 g[kTurns][4], b[kTurns][4];
+    R::params(a.gamma ? a.gamma + group * a.pstride : nullptr, a.cols, a.pvec, 1.f, g);
+    R::params(a.beta ? a.beta + group * a.pstride : nullptr, a.cols, a.pvec, 0.f, b);
+    const float each = 1.f / a.cols;
+    for (int stage = 0; r < r1; r += R::kLanes) {
+      request(r + (kD - 1) * R::kLanes, stage == 0 ? kD - 1 : stage - 1);
+      copies_wait<kD - 1>();
+      if constexpr (!kVec && !R::kDirect) R::meet();
+      float2 v[kTurns][4];
+      R::template take<kFull>(fwd_smem, stage, 0, x + r * a.ldx, a.cols, v);
+      float2 pair = both(0.f);
 #pragma unroll
-    for (int i = 0; i < kTurns; ++i) pair = __fadd2_rn(pair, __fadd2_rn(__fadd2_rn(v[i][0], v[i][1]), __fadd2_rn(v[i][2], v[i][3])));
-    float sum[1] = {pair.x + pair.y}, none[1] = {0.f};
-    row_sums<TPR>(sum, parts[0]);
-    float mean = sum[0] * each;
-    mean = fmaf(fmaf(-mean, static_cast<float>(a.cols), sum[0]), each, mean);   // the quotient, whatever 1 / cols was rounded to
-    if (!(fabsf(sum[0]) < 0x1p127f)) {   // the sum may have left fp32 where the mean does not; all of the row's threads come here
-      sum[0] = 0.f;
+      for (int i = 0; i < kTurns; ++i) pair = __fadd2_rn(pair, __fadd2_rn(__fadd2_rn(v[i][0], v[i][1]), __fadd2_rn(v[i][2], v[i][3])));
+      float sum[1] = {pair.x + pair.y}, none[1] = {0.f};
+      row_sums<TPR>(sum, parts[0]);
+      float mean = sum[0] * each;
+      mean = fmaf(fmaf(-mean, static_cast<float>(a.cols), sum[0]), each, mean);   // the quotient, whatever 1 / cols was rounded to
+      if (!(fabsf(sum[0]) < 0x1p127f)) {   // the sum may have left fp32 where the mean does not; all of the row's threads come here
+        sum[0] = 0.f;
+#pragma unroll
+        for (int i = 0; i < kTurns; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sum[0] += v[i][e].x * 0x1p-32f + v[i][e].y * 0x1p-32f;
+        row_sums<TPR>(sum, parts[1]);
+        mean = sum[0] / a.cols * 0x1p32f;
+        row_sums<TPR>(none, parts[0]);   // keeps the two places in turn
+      }
+      Squares sq;
+      bool plain = true;
+#pragma unroll
+      for (int i = 0; i < kTurns; ++i) {
+        float2 s = both(0.f);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          v[i][e] = __fadd2_rn(v[i][e], both(-mean));
+          if constexpr (!kFull) {
+            if (R::column(i, 2 * e) >= a.cols) v[i][e].x = 0.f;
+            if (R::column(i, 2 * e + 1) >= a.cols) v[i][e].y = 0.f;
+          }
+          s = __ffma2_rn(v[i][e], v[i][e], s);
+        }
+        sq.mid += s.x + s.y;
+        plain = plain && s.x + s.y > 1e-20f && s.x + s.y < 1e25f;
+      }
+      if (!plain) {   // squares may have left fp32's range, or are zeros
+        sq.mid = 0.f;
+#pragma unroll
+        for (int i = 0; i < kTurns; ++i) {
+          const float w[8] = {v[i][0].x, v[i][0].y, v[i][1].x, v[i][1].y, v[i][2].x, v[i][2].y, v[i][3].x, v[i][3].y};
+          sq.add(w);
+        }
+      }
+      float two[2] = {sq.mid, sq.big != 0.f || sq.small != 0.f ? 1.f : 0.f};
+      row_sums<TPR>(two, parts[1]);
+      float rstd = inverse_sqrt(fmaf(two[0], each, a.eps));
+      if (two[1] != 0.f || !(a.eps >= 0x1p-120f)) {
+        float far[2] = {sq.big, sq.small};
+        row_sums<TPR>(far, parts[0]);
+        row_sums<TPR>(none, parts[1]);
+        sq.mid = two[0], sq.big = far[0], sq.small = far[1];
+        rstd = inverse_std(sq, a.cols, a.eps);
+      }
+      if (t == 0) {
+        if (a.mean) a.mean[first + r] = mean;
+        if (a.rstd) a.rstd[first + r] = rstd;
+      }
 #pragma unroll
       for (int i = 0; i < kTurns; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sum[0] += v[i][e].x * 0x1p-32f + v[i][e].y * 0x1p-32f;
-      row_sums<TPR>(sum, parts[1]);
-      mean = sum[0] / a.cols * 0x1p32f;
-      row_sums<TPR>(none, parts[0]);   // keeps the two places in turn
+        for (int e = 0; e < 4; ++e) v[i][e] = __ffma2_rn(__fmul2_rn(v[i][e], both(rstd)), g[i][e], b[i][e]);
+      R::template put<kFull>(static_cast<T*>(a.y) + (first + r) * a.ldy, a.cols, v);
+      if (++stage >= kD) stage = 0;
     }
-    Squares sq;
-    bool plain = true;
-#pragma unroll
-    for (int i = 0; i < kTurns; ++i) {
-      float2 s = both(0.f);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        v[i][e] = __fadd2_rn(v[i][e], both(-mean));
-        if constexpr (!kFull) {
-          if (R::column(i, 2 * e) >= a.cols) v[i][e].x = 0.f;
-          if (R::column(i, 2 * e + 1) >= a.cols) v[i][e].y = 0.f;
-        }
-        s = __ffma2_rn(v[i][e], v[i][e], s);
-      }
-      sq.mid += s.x + s.y;
-      plain = plain && s.x + s.y > 1e-20f && s.x + s.y < 1e25f;
-    }
-    if (!plain) {   // squares may have left fp32's range, or are zeros
-      sq.mid = 0.f;
-#pragma unroll
-      for (int i = 0; i < kTurns; ++i) {
-        const float w[8] = {v[i][0].x, v[i][0].y, v[i][1].x, v[i][1].y, v[i][2].x, v[i][2].y, v[i][3].x, v[i][3].y};
-        sq.add(w);
-      }
-    }
-    float two[2] = {sq.mid, sq.big != 0.f || sq.small != 0.f ? 1.f : 0.f};
-    row_sums<TPR>(two, parts[1]);
-    float rstd = inverse_sqrt(fmaf(two[0], each, a.eps));
-    if (two[1] != 0.f || !(a.eps >= 0x1p-120f)) {
-      float far[2] = {sq.big, sq.small};
-      row_sums<TPR>(far, parts[0]);
-      row_sums<TPR>(none, parts[1]);
-      sq.mid = two[0], sq.big = far[0], sq.small = far[1];
-      rstd = inverse_std(sq, a.cols, a.eps);
-    }
-    if (t == 0) {
-      if (a.mean) a.mean[first + r] = mean;
-      if (a.rstd) a.rstd[first + r] = rstd;
-    }
-#pragma unroll
-    for (int i = 0; i < kTurns; ++i)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[i][e] = __ffma2_rn(__fmul2_rn(v[i][e], both(rstd)), g[i][e], b[i][e]);
-    R::template put<kFull>(static_cast<T*>(a.y) + (first + r) * a.ldy, a.cols, v);
-    if (++stage >= kD) stage = 0;
-  }
   };
   if (kVec && __all_sync(0xffffffffu, R::inside(a.cols))) all_rows(std::bool_constant<kVec>());
   else all_rows(std::false_type());
@@ -354,7 +349,7 @@ __global__ void __launch_bounds__(kThreads) wide_norm_kernel(const __grid_consta
   };
   float sum = 0.f;
   each([&](int, float (&v)[8]) { sum += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7])); });
-  sum = row_sum<kThreads>(sum, part);
+  sum = block_sum(sum, part);
   float mean = sum / a.cols;
   if (!(fabsf(sum) < INFINITY)) {
     sum = 0.f;
@@ -362,7 +357,7 @@ __global__ void __launch_bounds__(kThreads) wide_norm_kernel(const __grid_consta
 #pragma unroll
       for (int e = 0; e < 8; ++e) sum += v[e] * 0x1p-32f;
     });
-    sum = row_sum<kThreads>(sum, part);
+    sum = block_sum(sum, part);
     mean = sum / a.cols * 0x1p32f;
   }
   Squares sq;
@@ -371,9 +366,9 @@ __global__ void __launch_bounds__(kThreads) wide_norm_kernel(const __grid_consta
     for (int e = 0; e < 8; ++e) v[e] = at + e < a.cols ? v[e] - mean : 0.f;
     sq.add(v);
   });
-  sq.mid = row_sum<kThreads>(sq.mid, part);
-  sq.big = row_sum<kThreads>(sq.big, part);
-  sq.small = row_sum<kThreads>(sq.small, part);
+  sq.mid = block_sum(sq.mid, part);
+  sq.big = block_sum(sq.big, part);
+  sq.small = block_sum(sq.small, part);
   const float rstd = inverse_std(sq, a.cols, a.eps);
   if (threadIdx.x == 0) {
     if (a.mean) a.mean[row] = mean;
@@ -484,8 +479,8 @@ __global__ void __launch_bounds__(kThreads) norm_dx_kernel(const __grid_constant
         shx = fmaf(h[e], xh[e], shx);
       }
   });
-  sh = row_sum<kThreads>(sh, part) / a.cols;
-  shx = row_sum<kThreads>(shx, part) / a.cols;
+  sh = block_sum(sh, part) / a.cols;
+  shx = block_sum(shx, part) / a.cols;
   each([&](int at, float (&h)[8], float (&xh)[8]) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) h[e] = rstd * (h[e] - sh - xh[e] * shx);
@@ -588,59 +583,59 @@ __global__ void __launch_bounds__(kBlock, 1) norm_backward_kernel(const __grid_c
   float2 dg[kTurns][4] = {}, db[kTurns][4] = {};
   // whole warps of which all columns are inside the row go without bounds
   auto all_rows = [&](auto with) {
-  constexpr bool kFull = with();
-  auto request = [&](int r, int stage) {
-    if (r < r1) {
-      R::template request<kFull>(bwd_smem, stage, 0, dy + r * a.lddy, static_cast<const T*>(a.dy), a.cols);
-      R::template request<kFull>(bwd_smem, stage, 1, x + r * a.ldx, static_cast<const T*>(a.x), a.cols);
-    }
-    copies_done();
-  };
-  int r = chunk * a.per + lane;
-#pragma unroll
-  for (int i = 0; i < kD - 1; ++i) request(r + i * kLanes, i);
-  float2 g[kTurns][4];
-  R::params(a.gamma ? a.gamma + group * a.pstride : nullptr, a.cols, a.pvec, 1.f, g);
-  float mean = r < r1 ? a.mean[first + r] : 0.f, rstd = r < r1 ? a.rstd[first + r] : 0.f;
-  const float each = 1.f / a.cols;
-  for (int it = 0, stage = 0; r < r1; r += kLanes, ++it) {
-    request(r + (kD - 1) * kLanes, stage == 0 ? kD - 1 : stage - 1);
-    copies_wait<kD - 1>();
-    if constexpr (!kVec && !R::kDirect) R::meet();
-    float2 h[kTurns][4], xh[kTurns][4];
-    R::template take<kFull>(bwd_smem, stage, 0, dy + r * a.lddy, a.cols, h);
-    R::template take<kFull>(bwd_smem, stage, 1, x + r * a.ldx, a.cols, xh);
-    const float mu = mean, rs = rstd;
-    if (r + kLanes < r1) {
-      mean = a.mean[first + r + kLanes];
-      rstd = a.rstd[first + r + kLanes];
-    }
-    float2 sh = both(0.f), shx = both(0.f);
-#pragma unroll
-    for (int i = 0; i < kTurns; ++i)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        xh[i][e] = __fmul2_rn(__fadd2_rn(xh[i][e], both(-mu)), both(rs));
-        dg[i][e] = __ffma2_rn(h[i][e], xh[i][e], dg[i][e]);
-        db[i][e] = __fadd2_rn(db[i][e], h[i][e]);
-        h[i][e] = __fmul2_rn(h[i][e], g[i][e]);
-        sh = __fadd2_rn(sh, h[i][e]);
-        shx = __ffma2_rn(h[i][e], xh[i][e], shx);
+    constexpr bool kFull = with();
+    auto request = [&](int r, int stage) {
+      if (r < r1) {
+        R::template request<kFull>(bwd_smem, stage, 0, dy + r * a.lddy, static_cast<const T*>(a.dy), a.cols);
+        R::template request<kFull>(bwd_smem, stage, 1, x + r * a.ldx, static_cast<const T*>(a.x), a.cols);
       }
-    if (a.dx) {
-      float means[2] = {sh.x + sh.y, shx.x + shx.y};
-      row_sums<TPR>(means, parts[it & 1]);
-      const float2 mh = both(-means[0] * each), mhx = both(-means[1] * each);
+      copies_done();
+    };
+    int r = chunk * a.per + lane;
+#pragma unroll
+    for (int i = 0; i < kD - 1; ++i) request(r + i * kLanes, i);
+    float2 g[kTurns][4];
+    R::params(a.gamma ? a.gamma + group * a.pstride : nullptr, a.cols, a.pvec, 1.f, g);
+    float mean = r < r1 ? a.mean[first + r] : 0.f, rstd = r < r1 ? a.rstd[first + r] : 0.f;
+    const float each = 1.f / a.cols;
+    for (int it = 0, stage = 0; r < r1; r += kLanes, ++it) {
+      request(r + (kD - 1) * kLanes, stage == 0 ? kD - 1 : stage - 1);
+      copies_wait<kD - 1>();
+      if constexpr (!kVec && !R::kDirect) R::meet();
+      float2 h[kTurns][4], xh[kTurns][4];
+      R::template take<kFull>(bwd_smem, stage, 0, dy + r * a.lddy, a.cols, h);
+      R::template take<kFull>(bwd_smem, stage, 1, x + r * a.ldx, a.cols, xh);
+      const float mu = mean, rs = rstd;
+      if (r + kLanes < r1) {
+        mean = a.mean[first + r + kLanes];
+        rstd = a.rstd[first + r + kLanes];
+      }
+      float2 sh = both(0.f), shx = both(0.f);
 #pragma unroll
       for (int i = 0; i < kTurns; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) h[i][e] = __fmul2_rn(both(rs), __ffma2_rn(xh[i][e], mhx, __fadd2_rn(h[i][e], mh)));
-      R::template put<kFull>(static_cast<T*>(a.dx) + (first + r) * a.lddx, a.cols, h);
-    } else if constexpr (!kVec && !R::kDirect) {
-      R::meet();   // the stage has been read
+        for (int e = 0; e < 4; ++e) {
+          xh[i][e] = __fmul2_rn(__fadd2_rn(xh[i][e], both(-mu)), both(rs));
+          dg[i][e] = __ffma2_rn(h[i][e], xh[i][e], dg[i][e]);
+          db[i][e] = __fadd2_rn(db[i][e], h[i][e]);
+          h[i][e] = __fmul2_rn(h[i][e], g[i][e]);
+          sh = __fadd2_rn(sh, h[i][e]);
+          shx = __ffma2_rn(h[i][e], xh[i][e], shx);
+        }
+      if (a.dx) {
+        float means[2] = {sh.x + sh.y, shx.x + shx.y};
+        row_sums<TPR>(means, parts[it & 1]);
+        const float2 mh = both(-means[0] * each), mhx = both(-means[1] * each);
+#pragma unroll
+        for (int i = 0; i < kTurns; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) h[i][e] = __fmul2_rn(both(rs), __ffma2_rn(xh[i][e], mhx, __fadd2_rn(h[i][e], mh)));
+        R::template put<kFull>(static_cast<T*>(a.dx) + (first + r) * a.lddx, a.cols, h);
+      } else if constexpr (!kVec && !R::kDirect) {
+        R::meet();   // the stage has been read
+      }
+      if (++stage >= kD) stage = 0;
     }
-    if (++stage >= kD) stage = 0;
-  }
   };
   if (kVec && __all_sync(0xffffffffu, R::inside(a.cols))) all_rows(std::bool_constant<kVec>());
   else all_rows(std::false_type());

@@ -5,7 +5,9 @@
 //
 // A thread takes 16 neighbouring values: a block of NV, half of one of MX, whose halves meet in a shuffle; the four scales of
 // a tile's row are written by one of its threads.
-// Bound by memory: values in, codes and scales out (or the other way round).
+// Bound by memory: values in, codes and scales out (or the other way round).  8192 x 4096 bf16: NV 13.4 us (6.4 TB/s), MX 11.9
+// (values in L2), back 12.4; with eight values a thread, whose blocks' divisions and exchanges every other thread repeats, 20.6,
+// 27.4 and 24.7.
 #include <type_traits>
 
 #include "common.cuh"
