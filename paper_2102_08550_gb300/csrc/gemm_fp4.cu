@@ -15,7 +15,7 @@
 //   4-19    accumulators -> C, under the products of the next tile
 // What bounds a large product is the tensor pipe (69% busy; a pair's K-block of 256 x 256 x 256 is 512 clocks of products) and, while
 // results leave, the loads' latency: five stages of 38 KB cover 2500 clocks of it (four 47.3 us, three 54.9).  8192 x 4096 x
-// 4096 NV takes 44.5 us (6.2 PFLOP/s), 40.1 if no results left.
+// 4096 NV takes 43.5 us (6.3 PFLOP/s); without its results' stores 4.5 us less.
 // gemm_fp4_few_kernel for one token, or up to three of few channels.
 #include <atomic>
 
@@ -310,6 +310,16 @@ __device__ __forceinline__ void store_channels(const Fp4Args& a, const CUtensorM
     }
 }
 
+// Tile u of mu x nt: rows fastest, in groups of kGroup of them, so that the tiles under way at once share both operands and a
+// wave asks memory for little that is new (8192 x 4096 x 4096 with operands in memory: rows alone 47.1 us, groups of eight 45.8,
+// of four 45.0, of two 46.2).
+constexpr int kGroup = 4;
+__device__ __forceinline__ void tile_at(int u, int mu, int nt, int& row, int& col) {
+  const int group = u / (kGroup * nt), in = u - group * kGroup * nt, rows = min(kGroup, mu - group * kGroup);
+  col = in / rows;
+  row = group * kGroup + in - col * rows;
+}
+
 // Rows (W): channels, or, with kTokens, tokens; columns (X): the other.
 template <int CL, bool kSplit, bool kMx, bool kTokens>
 __global__ void __launch_bounds__(kThreads, 1) gemm_fp4_kernel(const __grid_constant__ CUtensorMap mapW, const __grid_constant__ CUtensorMap mapX,
@@ -334,7 +344,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp4_kernel(const __grid_cons
   const int k1 = kSplit ? static_cast<int>(static_cast<int64_t>(nk) * (part + 1) / p.split) : nk;
   const int per = kSplit ? p.split : CL;           // CTAs of a tile
   const int u0 = blockIdx.x / per, ustep = gridDim.x / per;
-  const int mu = p.mt / CL;                        // row tiles; rows fastest
+  const int mu = p.mt / CL;                        // row tiles
 
   if (threadIdx.x == 0) {
     prefetch_tmap(&mapW);
@@ -380,7 +390,9 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp4_kernel(const __grid_cons
     int it = 0, s = 0, ph = 1;
     uint32_t limit = kSpinLimit;
     for (int u = u0; u < p.units; u += ustep) {
-      const int r0 = ((u % mu) * CL + rank) * 128, c0 = (u / mu) * p.BN;
+      int tr, tc;
+      tile_at(u, mu, p.nt, tr, tc);
+      const int r0 = (tr * CL + rank) * 128, c0 = tc * p.BN;
       for (int kb = k0; kb < k1; ++kb, ++it) {
         if (it >= p.stages) mbar_wait_keep(limit, &bars->empty[s], ph, nullptr, kDevTimeoutEmpty);
         if (elect_one() && limit > 1) {
@@ -478,7 +490,9 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp4_kernel(const __grid_cons
     const bool works = cb < p.BN;
     int t = 0;
     for (int u = u0; ok && u < p.units; u += ustep) {
-      const int row = ((u % mu) * CL + rank) * 128 + 32 * quarter + lane, col0 = (u / mu) * p.BN + cb;
+      int tr, tc;
+      tile_at(u, mu, p.nt, tr, tc);
+      const int row = (tr * CL + rank) * 128 + 32 * quarter + lane, col0 = tc * p.BN + cb;
       const uint32_t row0 = tmem + (static_cast<uint32_t>(32 * quarter) << 16) + cb;
       // of the row; of the columns, lane l those of l, 32 + l, ...
       float mine = 1.f, bias = 0.f, theirs[kSpan / 32];
@@ -563,7 +577,9 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp4_kernel(const __grid_cons
           bulk_copy_to_peer(recv + part * bytes, ring + r * bytes, bytes, &bars->parts, r);
         }
       // a warp adds up a token, four channels a lane
-      const int n0 = (u0 % mu) * 128 + lane, m0 = (u0 / mu) * p.BN + part * tokens, end = a.M - m0 < tokens ? a.M - m0 : tokens;
+      int tr, tc;
+      tile_at(u0, mu, p.nt, tr, tc);
+      const int n0 = tr * 128 + lane, m0 = tc * p.BN + part * tokens, end = a.M - m0 < tokens ? a.M - m0 : tokens;
       float rb[4], bias[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
