@@ -276,3 +276,38 @@ def test_more_pieces_than_a_launch_takes(cuda_device):
         assert torch.equal(x[r], dequantize(wq, ws, None, cols, P.MXFP4, torch.bfloat16)[0])
     for r in (1, 129, 700001, 825854, 825858, 900001, rows - 2):
         assert (x[r] == 0).all()
+
+
+def test_beside_the_8_bit_products_and_updates(cuda_device):
+    """Streams with 4-bit products (pairs, clusters of eight) beside 8-bit products and orthogonalised updates, which all want an SM's
+    tensor memory: each ends, with its own bits."""
+    g = torch.Generator(device=cuda_device).manual_seed(1)
+    jobs = []
+    for i, (M, N, K) in enumerate([(100, 128, 5000), (700, 700, 700), (16, 600, 3000)]):
+        A, B = Kept.random(M, K, FORMATS[i % 2], cuda_device, i), Kept.random(N, K, FORMATS[i % 2], cuda_device, i + 9)
+        out = torch.empty(M, N, device=cuda_device)
+        jobs.append((lambda A=A, B=B, out=out: product(A, B, torch.float32, C=out), out))
+    for M, N, K in ((300, 500, 800), (40, 300, 2000)):
+        A, B = (torch.randint(-128, 128, (r, K), dtype=torch.int8, generator=g, device=cuda_device) for r in (M, N))
+        sa, sb, out = torch.rand(M, device=cuda_device), torch.rand(N, device=cuda_device), torch.empty(M, N, device=cuda_device)
+        jobs.append((lambda A=A, B=B, sa=sa, sb=sb, out=out, n=(M, N, K): P.oscars_gemm_i8_nt(
+            A.data_ptr(), n[2], sa.data_ptr(), B.data_ptr(), n[2], sb.data_ptr(), out.data_ptr(), n[1], P.F32, *n, stream=stream()), out))
+    G, out = torch.randn(300, 400, generator=g, device=cuda_device), torch.empty(300, 400, device=cuda_device)
+    ws = torch.empty(P.oscars_orthogonalize_workspace(1, 300, 400, P.F32), dtype=torch.uint8, device=cuda_device)
+    jobs.append((lambda: P.oscars_orthogonalize(G.data_ptr(), 400, 0, out.data_ptr(), 400, 0, 1, 300, 400, P.F32, 5, ws.data_ptr(), ws.numel(),
+                                                stream=stream()), out))
+    want = []
+    for call, o in jobs:
+        call()
+        torch.cuda.synchronize()
+        want.append(o.clone())
+        o.zero_()
+    streams = [torch.cuda.Stream(priority=-(i % 2)) for i in range(len(jobs))]
+    torch.cuda.synchronize()
+    for _ in range(40):
+        for s, (call, _) in zip(streams, jobs):
+            with torch.cuda.stream(s):
+                call()
+    torch.cuda.synchronize()
+    for (_, o), w in zip(jobs, want):
+        assert torch.equal(o, w)
