@@ -78,8 +78,6 @@ struct Rows {
     const int t = threadIdx.x % TPR, c = i * 8 + e;
     return (c / kPer * TPR + t) * kPer + c % kPer;
   }
-  // whether all of this thread's columns are inside the row
-  __device__ __forceinline__ static bool inside(int cols) { return column(kTurns - 1, 7) < cols; }
   __device__ __forceinline__ static int in_front(const T* row) { return static_cast<int>(reinterpret_cast<uintptr_t>(row) & 15); }
   __device__ __forceinline__ static uint8_t* lane_row(uint8_t* ring, int stage, int m) {
     return ring + stage * kStage + (m * kLanes + threadIdx.x / TPR) * kRow;
@@ -89,7 +87,17 @@ struct Rows {
     if (TPR == 32) __syncwarp();
     else bar_named(1 + threadIdx.x / TPR, TPR);
   }
-  // begin the copy of row `row` of a matrix that starts at `first` to a stage (kFull: all of the warp's columns are inside the row)
+  // whether all of this thread's columns are inside the row
+  __device__ __forceinline__ static bool inside(int cols) { return column(kTurns - 1, 7) < cols; }
+  // Turn i's columns are those from i TPR 8 on, of all of a row's threads: none of them, some or all are inside the row, the same
+  // for all threads.  kFull: all are, of every turn.  (With two turns alone the questions cost more than they save: 4104 columns of
+  // bf16 backward 89 us for 75.)
+  static constexpr bool kByTurn = kTurns > 2;
+  template <bool kFull>
+  __device__ __forceinline__ static bool none(int i, int cols) { return kByTurn && !kFull && i * TPR * 8 >= cols; }
+  template <bool kFull>
+  __device__ __forceinline__ static bool whole(int i, int cols) { return kFull || (kByTurn && (i + 1) * TPR * 8 <= cols); }
+  // begin the copy of row `row` of a matrix that starts at `first` to a stage
   template <bool kFull>
   __device__ __forceinline__ static void request(uint8_t* ring, int stage, int m, const T* row, const T* first, int cols) {
     constexpr int kPiece = 16 / kSize;                       // columns of 16 bytes
@@ -97,9 +105,11 @@ struct Rows {
       uint8_t* to = ring + stage * kStage + (m * kPieces * kBlock + threadIdx.x) * 16;
 #pragma unroll
       for (int p = 0; p < kPieces; ++p) {
+        constexpr int kAtOnce = 8 / kPiece;                    // pieces of a turn
         const int at = column(p * kPiece / 8, p * kPiece % 8), left = (cols - at) * kSize;
-        if constexpr (kFull) copy16(to + p * kBlock * 16, row + at);
-        else copy16(to + p * kBlock * 16, row + (left > 0 ? at : 0), left >= 16 ? 16 : left > 0 ? left : 0);
+        if (none<kFull>(p / kAtOnce, cols)) continue;
+        if (kFull || left >= 16) copy16(to + p * kBlock * 16, row + at);
+        else copy16(to + p * kBlock * 16, row + (left > 0 ? at : 0), left > 0 ? left : 0);
       }
     } else if constexpr (!kDirect) {   // whole 16 bytes, with a piece of the row before in front; the matrix's own first ones one at a time
       const int t = threadIdx.x % TPR, front = in_front(row), bytes = front + cols * kSize;
@@ -111,12 +121,13 @@ struct Rows {
         if (inside || at > 0) copy16(to + at, from + at, bytes - at >= 16 ? 16 : bytes - at);
     }
   }
-  // this thread's columns of it (zeros behind the row's end)
+  // this thread's columns of it, of turns that have some (zeros behind the row's end)
   template <bool kFull>
   __device__ __forceinline__ static void take(uint8_t* ring, int stage, int m, const T* row, int cols, float2 (&v)[kTurns][4]) {
     if constexpr (kVec) {
 #pragma unroll
       for (int p = 0; p < kPieces; ++p) {
+        if (none<kFull>(p * kTurns / kPieces, cols)) continue;
         const uint4 w = *reinterpret_cast<const uint4*>(ring + stage * kStage + ((m * kPieces + p) * kBlock + threadIdx.x) * 16);
         const uint32_t u[4] = {w.x, w.y, w.z, w.w};
         if constexpr (sizeof(T) == 4) {
@@ -130,27 +141,38 @@ struct Rows {
     } else {
       const T* from = kDirect ? row : reinterpret_cast<const T*>(lane_row(ring, stage, m) + in_front(row));
 #pragma unroll
-      for (int i = 0; i < kTurns; ++i)
+      for (int i = 0; i < kTurns; ++i) {
+        if (none<kFull>(i, cols)) continue;
+        if (whole<kFull>(i, cols)) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          v[i][e] = make_float2(kFull || column(i, 2 * e) < cols ? to_f32(from[column(i, 2 * e)]) : 0.f,
-                                kFull || column(i, 2 * e + 1) < cols ? to_f32(from[column(i, 2 * e + 1)]) : 0.f);
+          for (int e = 0; e < 4; ++e) v[i][e] = make_float2(to_f32(from[column(i, 2 * e)]), to_f32(from[column(i, 2 * e + 1)]));
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            v[i][e] = make_float2(column(i, 2 * e) < cols ? to_f32(from[column(i, 2 * e)]) : 0.f,
+                                  column(i, 2 * e + 1) < cols ? to_f32(from[column(i, 2 * e + 1)]) : 0.f);
+        }
+      }
     }
   }
   template <bool kFull>
   __device__ __forceinline__ static void put(T* row, int cols, const float2 (&v)[kTurns][4]) {
 #pragma unroll
     for (int i = 0; i < kTurns; ++i) {
+      if (none<kFull>(i, cols)) continue;
       const float w[8] = {v[i][0].x, v[i][0].y, v[i][1].x, v[i][1].y, v[i][2].x, v[i][2].y, v[i][3].x, v[i][3].y};
-      if constexpr (kVec && sizeof(T) == 2) {
-        store8(row + column(i, 0), kFull ? 8 : cols - column(i, 0), true, w);
-      } else if constexpr (kVec && kFull) {
+      if (!kFull && column(i, 7) >= cols) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (column(i, e) < cols) row[column(i, e)] = static_cast<T>(w[e]);
+      } else if constexpr (kVec && sizeof(T) == 2) {
+        store8(row + column(i, 0), 8, true, w);
+      } else if constexpr (kVec) {
 #pragma unroll
         for (int h = 0; h < 8; h += 4) *reinterpret_cast<float4*>(row + column(i, h)) = make_float4(w[h], w[h + 1], w[h + 2], w[h + 3]);
       } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (kFull || column(i, e) < cols) row[column(i, e)] = static_cast<T>(w[e]);
+        for (int e = 0; e < 8; ++e) row[column(i, e)] = static_cast<T>(w[e]);
       }
     }
   }
@@ -159,7 +181,7 @@ struct Rows {
 #pragma unroll
     for (int i = 0; i < kTurns; ++i) {
       float w[8];
-      if (kVec && p && vec && inside(cols)) {
+      if (kVec && p && vec && (i + 1) * TPR * 8 <= cols) {
 #pragma unroll
         for (int h = 0; h < 8; h += 4) {
           const float4 f = *reinterpret_cast<const float4*>(p + column(i, h));
@@ -227,8 +249,9 @@ __device__ __forceinline__ float inverse_std(const Squares& s, int cols, float e
 }
 
 // Mean and squares of deviations from registers: two exchanges between a row's threads, each behind one barrier, are what a row
-// waits for, so that four rows at a time or more are under way.
-template <typename T, int TPR, int kTurns, bool kVec>
+// waits for, so that four rows at a time or more are under way.  Rows that fill all turns (kFull) go without bounds: 8192 x 4096 bf16
+// 30.0 -> 24.2 us.
+template <typename T, int TPR, int kTurns, bool kVec, bool kFull>
 __global__ void __launch_bounds__(kBlock, 1) layer_norm_kernel(const __grid_constant__ FwdArgs a) {
   using R = Rows<T, TPR, kTurns, kVec, 1>;
   constexpr int kD = R::kDepth;
@@ -241,92 +264,95 @@ __global__ void __launch_bounds__(kBlock, 1) layer_norm_kernel(const __grid_cons
   pdl_wait();
   pdl_trigger();
   const T* x = static_cast<const T*>(a.x) + first * a.ldx;
-  // warps of which all columns are inside the row go without bounds (8192 x 4096 bf16 30.0 -> 24.2 us)
-  auto all_rows = [&](auto with) {
-    constexpr bool kFull = with();
-    auto request = [&](int r, int stage) {
-      if (r < r1) R::template request<kFull>(fwd_smem, stage, 0, x + r * a.ldx, static_cast<const T*>(a.x), a.cols);
-      copies_done();
-    };
-    int r = chunk * a.per + lane;
+  auto request = [&](int r, int stage) {
+    if (r < r1) R::template request<kFull>(fwd_smem, stage, 0, x + r * a.ldx, static_cast<const T*>(a.x), a.cols);
+    copies_done();
+  };
+  int r = chunk * a.per + lane;
 #pragma unroll
-    for (int i = 0; i < kD - 1; ++i) request(r + i * R::kLanes, i);
-    float2 g[kTurns][4], b[kTurns][4];
-    R::params(a.gamma ? a.gamma + group * a.pstride : nullptr, a.cols, a.pvec, 1.f, g);
-    R::params(a.beta ? a.beta + group * a.pstride : nullptr, a.cols, a.pvec, 0.f, b);
-    const float each = 1.f / a.cols;
-    for (int stage = 0; r < r1; r += R::kLanes) {
-      request(r + (kD - 1) * R::kLanes, stage == 0 ? kD - 1 : stage - 1);
-      copies_wait<kD - 1>();
-      if constexpr (!kVec && !R::kDirect) R::meet();
-      float2 v[kTurns][4];
-      R::template take<kFull>(fwd_smem, stage, 0, x + r * a.ldx, a.cols, v);
-      float2 pair = both(0.f);
+  for (int i = 0; i < kD - 1; ++i) request(r + i * R::kLanes, i);
+  float2 g[kTurns][4], b[kTurns][4];
+  R::params(a.gamma ? a.gamma + group * a.pstride : nullptr, a.cols, a.pvec, 1.f, g);
+  R::params(a.beta ? a.beta + group * a.pstride : nullptr, a.cols, a.pvec, 0.f, b);
+  const float each = 1.f / a.cols;
+  for (int stage = 0; r < r1; r += R::kLanes) {
+    request(r + (kD - 1) * R::kLanes, stage == 0 ? kD - 1 : stage - 1);
+    copies_wait<kD - 1>();
+    if constexpr (!kVec && !R::kDirect) R::meet();
+    float2 v[kTurns][4];
+    R::template take<kFull>(fwd_smem, stage, 0, x + r * a.ldx, a.cols, v);
+    float2 pair = both(0.f);
 #pragma unroll
-      for (int i = 0; i < kTurns; ++i) pair = __fadd2_rn(pair, __fadd2_rn(__fadd2_rn(v[i][0], v[i][1]), __fadd2_rn(v[i][2], v[i][3])));
-      float sum[1] = {pair.x + pair.y}, none[1] = {0.f};
-      row_sums<TPR>(sum, parts[0]);
-      float mean = sum[0] * each;
-      mean = fmaf(fmaf(-mean, static_cast<float>(a.cols), sum[0]), each, mean);   // the quotient, whatever 1 / cols was rounded to
-      if (!(fabsf(sum[0]) < 0x1p127f)) {   // the sum may have left fp32 where the mean does not; all of the row's threads come here
-        sum[0] = 0.f;
-#pragma unroll
-        for (int i = 0; i < kTurns; ++i)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) sum[0] += v[i][e].x * 0x1p-32f + v[i][e].y * 0x1p-32f;
-        row_sums<TPR>(sum, parts[1]);
-        mean = sum[0] / a.cols * 0x1p32f;
-        row_sums<TPR>(none, parts[0]);   // keeps the two places in turn
-      }
-      Squares sq;
-      bool plain = true;
+    for (int i = 0; i < kTurns; ++i)
+      if (!R::template none<kFull>(i, a.cols)) pair = __fadd2_rn(pair, __fadd2_rn(__fadd2_rn(v[i][0], v[i][1]), __fadd2_rn(v[i][2], v[i][3])));
+    float sum[1] = {pair.x + pair.y}, none[1] = {0.f};
+    row_sums<TPR>(sum, parts[0]);
+    float mean = sum[0] * each;
+    mean = fmaf(fmaf(-mean, static_cast<float>(a.cols), sum[0]), each, mean);   // the quotient, whatever 1 / cols was rounded to
+    if (!(fabsf(sum[0]) < 0x1p127f)) {   // the sum may have left fp32 where the mean does not; all of the row's threads come here
+      sum[0] = 0.f;
 #pragma unroll
       for (int i = 0; i < kTurns; ++i) {
-        float2 s = both(0.f);
+        if (R::template none<kFull>(i, a.cols)) continue;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[0] += v[i][e].x * 0x1p-32f + v[i][e].y * 0x1p-32f;
+      }
+      row_sums<TPR>(sum, parts[1]);
+      mean = sum[0] / a.cols * 0x1p32f;
+      row_sums<TPR>(none, parts[0]);   // keeps the two places in turn
+    }
+    Squares sq;
+    bool plain = true;
+#pragma unroll
+    for (int i = 0; i < kTurns; ++i) {
+      if (R::template none<kFull>(i, a.cols)) continue;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[i][e] = __fadd2_rn(v[i][e], both(-mean));
+      if (!kFull && R::column(i, 7) >= a.cols) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          v[i][e] = __fadd2_rn(v[i][e], both(-mean));
-          if constexpr (!kFull) {
-            if (R::column(i, 2 * e) >= a.cols) v[i][e].x = 0.f;
-            if (R::column(i, 2 * e + 1) >= a.cols) v[i][e].y = 0.f;
-          }
-          s = __ffma2_rn(v[i][e], v[i][e], s);
-        }
-        sq.mid += s.x + s.y;
-        plain = plain && s.x + s.y > 1e-20f && s.x + s.y < 1e25f;
-      }
-      if (!plain) {   // squares may have left fp32's range, or are zeros
-        sq.mid = 0.f;
-#pragma unroll
-        for (int i = 0; i < kTurns; ++i) {
-          const float w[8] = {v[i][0].x, v[i][0].y, v[i][1].x, v[i][1].y, v[i][2].x, v[i][2].y, v[i][3].x, v[i][3].y};
-          sq.add(w);
+          if (R::column(i, 2 * e) >= a.cols) v[i][e].x = 0.f;
+          if (R::column(i, 2 * e + 1) >= a.cols) v[i][e].y = 0.f;
         }
       }
-      float two[2] = {sq.mid, sq.big != 0.f || sq.small != 0.f ? 1.f : 0.f};
-      row_sums<TPR>(two, parts[1]);
-      float rstd = inverse_sqrt(fmaf(two[0], each, a.eps));
-      if (two[1] != 0.f || !(a.eps >= 0x1p-120f)) {
-        float far[2] = {sq.big, sq.small};
-        row_sums<TPR>(far, parts[0]);
-        row_sums<TPR>(none, parts[1]);
-        sq.mid = two[0], sq.big = far[0], sq.small = far[1];
-        rstd = inverse_std(sq, a.cols, a.eps);
-      }
-      if (t == 0) {
-        if (a.mean) a.mean[first + r] = mean;
-        if (a.rstd) a.rstd[first + r] = rstd;
-      }
+      float2 s = both(0.f);
 #pragma unroll
-      for (int i = 0; i < kTurns; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[i][e] = __ffma2_rn(__fmul2_rn(v[i][e], both(rstd)), g[i][e], b[i][e]);
-      R::template put<kFull>(static_cast<T*>(a.y) + (first + r) * a.ldy, a.cols, v);
-      if (++stage >= kD) stage = 0;
+      for (int e = 0; e < 4; ++e) s = __ffma2_rn(v[i][e], v[i][e], s);
+      sq.mid += s.x + s.y;
+      plain = plain && ((s.x + s.y > 1e-20f && s.x + s.y < 1e25f) || R::column(i, 0) >= a.cols);
     }
-  };
-  if (kVec && __all_sync(0xffffffffu, R::inside(a.cols))) all_rows(std::bool_constant<kVec>());
-  else all_rows(std::false_type());
+    if (!plain) {   // squares may have left fp32's range, or are zeros
+      sq.mid = 0.f;
+#pragma unroll
+      for (int i = 0; i < kTurns; ++i) {
+        if (R::template none<kFull>(i, a.cols)) continue;
+        const float w[8] = {v[i][0].x, v[i][0].y, v[i][1].x, v[i][1].y, v[i][2].x, v[i][2].y, v[i][3].x, v[i][3].y};
+        sq.add(w);
+      }
+    }
+    float two[2] = {sq.mid, sq.big != 0.f || sq.small != 0.f ? 1.f : 0.f};
+    row_sums<TPR>(two, parts[1]);
+    float rstd = inverse_sqrt(fmaf(two[0], each, a.eps));
+    if (two[1] != 0.f || !(a.eps >= 0x1p-120f)) {
+      float far[2] = {sq.big, sq.small};
+      row_sums<TPR>(far, parts[0]);
+      row_sums<TPR>(none, parts[1]);
+      sq.mid = two[0], sq.big = far[0], sq.small = far[1];
+      rstd = inverse_std(sq, a.cols, a.eps);
+    }
+    if (t == 0) {
+      if (a.mean) a.mean[first + r] = mean;
+      if (a.rstd) a.rstd[first + r] = rstd;
+    }
+#pragma unroll
+    for (int i = 0; i < kTurns; ++i) {
+      if (R::template none<kFull>(i, a.cols)) continue;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[i][e] = __ffma2_rn(__fmul2_rn(v[i][e], both(rstd)), g[i][e], b[i][e]);
+    }
+    R::template put<kFull>(static_cast<T*>(a.y) + (first + r) * a.ldy, a.cols, v);
+    if (++stage >= kD) stage = 0;
+  }
 }
 
 // Wide rows: a block each, read again from L2 for the squares and for the result.
@@ -415,9 +441,12 @@ template <typename T, bool kVec>
 cudaError_t forward_rows(const FwdArgs& a, cudaStream_t s) {
   return by_width<kForward>(a.cols, [&](auto tpr, auto turns) {
     constexpr int kBytes = Rows<T, tpr(), turns(), kVec, 1>::kBytes;
-    auto kernel = layer_norm_kernel<T, tpr(), turns(), kVec>;
-    const cudaError_t e = allow_smem(kernel, kBytes);
-    return e != cudaSuccess ? e : launch_dependent(kernel, dim3(static_cast<unsigned>(a.groups) * a.chunks), kBlock, kBytes, s, a);
+    auto launch = [&](auto kernel) {
+      const cudaError_t e = allow_smem(kernel, kBytes);
+      return e != cudaSuccess ? e : launch_dependent(kernel, dim3(static_cast<unsigned>(a.groups) * a.chunks), kBlock, kBytes, s, a);
+    };
+    if (kVec && a.cols == tpr() * turns() * 8) return launch(layer_norm_kernel<T, tpr(), turns(), kVec, kVec>);
+    return launch(layer_norm_kernel<T, tpr(), turns(), kVec, false>);
   });
 }
 
@@ -581,7 +610,7 @@ __global__ void __launch_bounds__(kBlock, 1) norm_backward_kernel(const __grid_c
   pdl_trigger();
   const T *dy = static_cast<const T*>(a.dy) + first * a.lddy, *x = static_cast<const T*>(a.x) + first * a.ldx;
   float2 dg[kTurns][4] = {}, db[kTurns][4] = {};
-  // whole warps of which all columns are inside the row go without bounds
+  // warps of which all columns are inside the row go without bounds
   auto all_rows = [&](auto with) {
     constexpr bool kFull = with();
     auto request = [&](int r, int stage) {
@@ -612,7 +641,8 @@ __global__ void __launch_bounds__(kBlock, 1) norm_backward_kernel(const __grid_c
       }
       float2 sh = both(0.f), shx = both(0.f);
 #pragma unroll
-      for (int i = 0; i < kTurns; ++i)
+      for (int i = 0; i < kTurns; ++i) {
+        if (R::template none<kFull>(i, a.cols)) continue;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           xh[i][e] = __fmul2_rn(__fadd2_rn(xh[i][e], both(-mu)), both(rs));
@@ -622,6 +652,7 @@ __global__ void __launch_bounds__(kBlock, 1) norm_backward_kernel(const __grid_c
           sh = __fadd2_rn(sh, h[i][e]);
           shx = __ffma2_rn(h[i][e], xh[i][e], shx);
         }
+      }
       if (a.dx) {
         float means[2] = {sh.x + sh.y, shx.x + shx.y};
         row_sums<TPR>(means, parts[it & 1]);
@@ -629,7 +660,8 @@ __global__ void __launch_bounds__(kBlock, 1) norm_backward_kernel(const __grid_c
 #pragma unroll
         for (int i = 0; i < kTurns; ++i)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) h[i][e] = __fmul2_rn(both(rs), __ffma2_rn(xh[i][e], mhx, __fadd2_rn(h[i][e], mh)));
+          for (int e = 0; e < 4; ++e)
+            if (!R::template none<kFull>(i, a.cols)) h[i][e] = __fmul2_rn(both(rs), __ffma2_rn(xh[i][e], mhx, __fadd2_rn(h[i][e], mh)));
         R::template put<kFull>(static_cast<T*>(a.dx) + (first + r) * a.lddx, a.cols, h);
       } else if constexpr (!kVec && !R::kDirect) {
         R::meet();   // the stage has been read
