@@ -60,8 +60,8 @@ struct Held {
                from + 4 * kWords + 16 <= static_cast<const uint8_t*>(end)) {
       uint32_t r[kWords + 4];
 #pragma unroll
-      for (int i = 0; i < kWords + 4; i += 4) {
-        const uint4 a = *reinterpret_cast<const uint4*>(from + 4 * i);
+      for (int i = 0; i < kWords + 4; i += 4) {   // the last 16 bytes hold none of the values if the first hold all of theirs
+        const uint4 a = i < kWords || front > 0 ? *reinterpret_cast<const uint4*>(from + 4 * i) : make_uint4(0u, 0u, 0u, 0u);
         r[i] = a.x, r[i + 1] = a.y, r[i + 2] = a.z, r[i + 3] = a.w;
       }
       const bool two = front & 8, one = front & 4;
@@ -150,8 +150,9 @@ struct QuantArgs {
   uint8_t *q, *scales;
   float* row_scale;
   int64_t ldx, ldq;
-  uint32_t units;       // OSCARS_MXFP4: threads, eight for each tile of a row
+  uint32_t units;       // OSCARS_MXFP4: threads, eight for each tile of a row, of rows from `first` on
   Divide per;           // of a row
+  int64_t first;
   int rows, cols, tiles, wide;
 };
 
@@ -187,7 +188,7 @@ __global__ void __launch_bounds__(kThreads) quantize_mx_kernel(const __grid_cons
     uint2 c = held[i].codes(__uint_as_float((254 - byte) << 23));   // 2^-e: from 2^127 (byte 0) to 2^-125
     if (!number) c = make_uint2(0u, 0u);
     if (at[i] / 32 * 32 < a.cols) *reinterpret_cast<uint2*>(a.q + row[i] * a.ldq + at[i] / 2) = c;
-    if (lane % 8 == 0) *reinterpret_cast<uint32_t*>(a.scales + fp4_scale_at(row[i], at[i] / 128, a.tiles)) = word;
+    if (lane % 8 == 0) *reinterpret_cast<uint32_t*>(a.scales + fp4_scale_at(a.first + row[i], at[i] / 128, a.tiles)) = word;
   }
 }
 
@@ -267,8 +268,9 @@ struct DequantArgs {
   const float* row_scale;
   void* x;
   int64_t ldq, ldx;
-  uint32_t units;       // of 16 columns
+  uint32_t units;       // of 16 columns, of rows from `first` on
   Divide per;           // of a row
+  int64_t first;
   int rows, cols, tiles, wide, mx;
 };
 
@@ -290,7 +292,7 @@ __global__ void __launch_bounds__(kThreads) dequantize_kernel(const __grid_const
     const int from = at[i] < a.cols ? at[i] : 0;
     w[i] = *reinterpret_cast<const uint2*>(a.q + row[i] * a.ldq + from / 2);
     const int block = from / (a.mx ? 32 : 16);
-    byte[i] = a.scales[fp4_scale_at(row[i], block / 4, a.tiles) + block % 4];
+    byte[i] = a.scales[fp4_scale_at(a.first + row[i], block / 4, a.tiles) + block % 4];
     t[i] = a.row_scale ? a.row_scale[row[i]] : 1.f;
   }
 #pragma unroll
@@ -345,11 +347,10 @@ bool sizes_ok(int rows, int cols, int format) {
 int wide_rows(const void* p, int64_t ld, int size) {
   return at_bytes(p, 32) && ld * size % 32 == 0 ? 32 : at_bytes(p, 16) && ld * size % 16 == 0 ? 16 : 0;
 }
-// f(first row, rows) over pieces of a matrix that have fewer than 2^30 units: rows from a tile's first on
+// f(first row, rows) over pieces of a matrix that have up to 2^30 units (a row has up to 2^26)
 template <typename F>
 cudaError_t by_rows(int rows, int per, F&& f) {
-  int64_t most = (int64_t(1) << 30) / per / 128 * 128;
-  if (most < 128) most = 128;
+  const int64_t most = (int64_t(1) << 30) / per;
   for (int64_t r = 0; r < rows; r += most) {
     const cudaError_t e = f(r, static_cast<int>(rows - r < most ? rows - r : most));
     if (e != cudaSuccess) return e;
@@ -374,7 +375,7 @@ cudaError_t quantize(const QuantArgs& a, int format, cudaStream_t s) {
       QuantArgs p = a;
       p.x = static_cast<const T*>(a.x) + r * a.ldx;
       p.q += r * a.ldq;
-      p.scales += fp4_scale_at(r, 0, a.tiles);
+      p.first = r;
       p.rows = rows;
       p.units = static_cast<uint32_t>(rows) * per;
       p.per = divide_by(per);
@@ -403,7 +404,7 @@ cudaError_t dequantize(const DequantArgs& a, cudaStream_t s) {
     DequantArgs p = a;
     p.x = static_cast<T*>(a.x) + r * a.ldx;
     p.q += r * a.ldq;
-    p.scales += fp4_scale_at(r, 0, a.tiles);
+    p.first = r;
     if (a.row_scale) p.row_scale += r;
     p.rows = rows;
     p.units = static_cast<uint32_t>(rows) * per;
@@ -437,7 +438,7 @@ oscars_status oscars_quantize_fp4(const void* x, int64_t ldx, int32_t dtype, int
       (format == OSCARS_NVFP4) != (row_scale != nullptr))
     return OSCARS_EINVAL;
   const uint8_t* end = static_cast<const uint8_t*>(x) + ((rows - 1) * ldx + cols) * size;
-  QuantArgs a{x, end, q, scales, row_scale, ldx, ldq, 0, {}, rows, cols, fp4_tiles(cols, format), wide_rows(x, ldx, size)};
+  QuantArgs a{x, end, q, scales, row_scale, ldx, ldq, 0, {}, 0, rows, cols, fp4_tiles(cols, format), wide_rows(x, ldx, size)};
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const cudaError_t e = dtype == OSCARS_F32 ? quantize<float>(a, format, s) : quantize<__nv_bfloat16>(a, format, s);
   return e == cudaSuccess ? OSCARS_OK : OSCARS_ECUDA;
@@ -450,7 +451,7 @@ oscars_status oscars_dequantize_fp4(const uint8_t* q, int64_t ldq, const uint8_t
   if (rows == 0) return OSCARS_OK;
   const int size = dtype == OSCARS_F32 ? 4 : 2;
   if (!x || !q || !scales || !at_bytes(x, size) || !at_bytes(q, 16) || !at_bytes(scales, 16) || !at_bytes(row_scale, 4)) return OSCARS_EINVAL;
-  DequantArgs a{q, scales, row_scale, x, ldq, ldx, 0, {}, rows, cols, fp4_tiles(cols, format), wide_rows(x, ldx, size), format == OSCARS_MXFP4};
+  DequantArgs a{q, scales, row_scale, x, ldq, ldx, 0, {}, 0, rows, cols, fp4_tiles(cols, format), wide_rows(x, ldx, size), format == OSCARS_MXFP4};
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const cudaError_t e = dtype == OSCARS_F32 ? dequantize<float>(a, s) : dequantize<__nv_bfloat16>(a, s);
   return e == cudaSuccess ? OSCARS_OK : OSCARS_ECUDA;

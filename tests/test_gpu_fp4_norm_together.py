@@ -256,12 +256,13 @@ def test_offsets_beyond_32_bits(cuda_device):
         del x, dy, y
 
 
-def test_more_pieces_than_a_launch_takes(cuda_device):
-    """1.3 x 2^30 pieces of 16 columns: two launches, the second from a tile's first row on."""
-    rows, cols = 1 << 20, 20800
+@pytest.mark.parametrize("rows,cols,at", [(1 << 20, 20800, [0, 127, 128, 700000, 823420, 823421, 825954, 825955, 900000, (1 << 20) - 1]),
+                                          (70, (1 << 28) + 40, [0, 62, 63, 64, 69])])
+def test_more_pieces_than_a_launch_takes(cuda_device, rows, cols, at):
+    """1.3 x 2^30 and 1.1 x 2^30 pieces of 16 columns: two launches, the second from inside a scale tile on (MX: 2^30 / 1304 =
+    823421 rows of eight pieces a tile, back: 2^30 / 1300 = 825955; of the wide matrix 63 rows)."""
     x = torch.zeros(rows, cols, dtype=torch.bfloat16, device=cuda_device)
     g = torch.Generator(device=cuda_device).manual_seed(2)
-    at = [0, 127, 128, 700000, 825855, 825856, 825857, 900000, rows - 1]
     values = torch.randn(len(at), cols, generator=g, device=cuda_device).bfloat16()
     x[at] = values
     q = torch.empty(rows, (cols + 31) // 32 * 16, dtype=torch.uint8, device=cuda_device)
@@ -274,7 +275,7 @@ def test_more_pieces_than_a_launch_takes(cuda_device):
     P.oscars_dequantize_fp4(q.data_ptr(), q.stride(0), s.data_ptr(), None, P.MXFP4, rows, cols, x.data_ptr(), cols, P.BF16, stream())
     for r, (wq, ws, _) in zip(at, want):
         assert torch.equal(x[r], dequantize(wq, ws, None, cols, P.MXFP4, torch.bfloat16)[0])
-    for r in (1, 129, 700001, 825854, 825858, 900001, rows - 2):
+    for r in (1, 61, 65, rows // 2, rows - 2):
         assert (x[r] == 0).all()
 
 
