@@ -153,7 +153,7 @@ def _pack(codes, byte, rows):
     q = flat[:, 0::2] | (flat[:, 1::2] << 4)
     tiles = torch.nn.functional.pad(byte, (0, -byte.shape[1] % 4, 0, -rows % 128))
     s = tiles.reshape(tiles.shape[0] // 128, 4, 32, -1, 4).permute(0, 3, 2, 1, 4).contiguous()
-    return q.to(torch.uint8).contiguous(), s.reshape(-1)   # bytes, as the calls take them
+    return q.contiguous(), s.reshape(-1)
 
 
 def _unpack(q, s, rows, cols, fmt):
@@ -319,6 +319,7 @@ def _run_own(state):
         return {"dx": out, "dgamma": dgamma, "dbeta": dbeta}
     fmt = lib.MXFP4 if case["format"] == "mx" else lib.NVFP4
     q, s, t = state["A"]
+    q = q.to(torch.uint8)   # the calls take codes as bytes (what quantisation writes is bytes already)
     tp = t.data_ptr() if t is not None else None
     if k != "product":
         x = state["x"]
@@ -330,6 +331,9 @@ def _run_own(state):
             return out
     M, N, K = case["M"], case["N"], case["K"]
     qb, sb, tb = state["B"]
+    if "weight" not in state:   # laid out once, as a program keeps its weights
+        state["weight"] = qb.to(torch.uint8)
+    qb = state["weight"]
     C = state["C"]
     lib.oscars_gemm_fp4_nt(q.data_ptr(), q.stride(0), s.data_ptr(), qb.data_ptr(), qb.stride(0), sb.data_ptr(), fmt, C.data_ptr(), N, dt,
                            M, N, K, row_scale_a_ptr=tp, row_scale_b_ptr=tb.data_ptr() if tb is not None else None,
