@@ -665,7 +665,8 @@ oscars_status oscars_dequantize_fp4(const uint8_t* q, int64_t ldq, const uint8_t
  * sum is kept in fp32 (a block's sum is exact; where block scales' products leave
  * fp32's normal numbers, so does the sum).  bias: device, N fp32, or NULL.  relu != 0:
  * act = max(0, .) (NaN stays).  C: device, element (m, n) at C[m ldc + n], of `dtype`,
- * any alignment; row scales, bias and act are fp32, rounded once to `dtype`.  M = 0 does
+ * any alignment; row scales, bias and act are fp32, rounded once to `dtype` (a result
+ * in fp32's range is right however far apart the sum and its two scales lie).  M = 0 does
  * nothing.  Equal calls give equal bits.  Allocates nothing and can be captured
  * (after a first call on the device, which loads the kernels).  Ordered on `stream`.
  * A wait inside the kernel that runs out (none is known to) is not reported, as in

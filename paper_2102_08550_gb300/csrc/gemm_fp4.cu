@@ -37,16 +37,44 @@ struct Fp4Args {
   int M, N, K, mx, tiles, relu, bf16;
 };
 
-// sum x ra x rb: NV's sums lie between 2^-20 and 2^62 (or are 0), so their products with a row scale in [2^-96, 2^64] stay
-// among fp32's normal numbers and only the result can leave them.  Other row scales are taken 2^64 nearer to 1, and the result
-// gets that back.
-__device__ __forceinline__ float near_one(float s) { return fabsf(s) > 0x1p64f ? s * 0x1p-64f : fabsf(s) < 0x1p-96f ? s * 0x1p64f : s; }
-__device__ __forceinline__ float back(float s) { return fabsf(s) > 0x1p64f ? 0x1p64f : fabsf(s) < 0x1p-96f ? 0x1p-64f : 1.f; }
+// sum x ra x rb, in this order.  The first product may leave fp32's normal numbers where the result does not: then all of it is
+// taken in 64 bits, of this element alone, so that a row knows nothing of its neighbours.  (A call, so that it stays behind a
+// branch: 40 x 4096 x 4096 MX takes 9.1 us for 6.8 with both sides computed.)
+__device__ __noinline__ float scaled_64(float sum, float ra, float rb) { return static_cast<float>(static_cast<double>(sum) * ra * rb); }
+__device__ __forceinline__ float scaled(float sum, float ra, float rb) {
+  const float t = sum * ra, m = fabsf(t);   // (a sum of 0 takes the other way to the same 0)
+  return m >= 0x1p-126f && m < INFINITY ? t * rb : scaled_64(sum, ra, rb);
+}
+// Whether it may do so, asked once for many elements (a call without row_a or row_b has one product alone): sums between 2^-20 and
+// 2^62, or 0, by scales in [2^-96, 2^64], or 0, stay in [2^-116, 2^126].  NV's sums are all of this kind: multiples of 2^-20,
+// and up to 2^30 x 2688^2.
+__device__ __forceinline__ bool far_scale(float s) { return s != 0.f && !(fabsf(s) >= 0x1p-96f && fabsf(s) <= 0x1p64f); }
+__device__ __forceinline__ bool far_sums(const float (&s)[16]) {   // by their bits without the sign, 0 behind all others in `least`
+  uint32_t least = ~0u, most = 0;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) {
+    const uint32_t u = __float_as_uint(s[e]) << 1;
+    least = min(least, u - 1);
+    most = max(most, u);
+  }
+  return least < ((127u - 20) << 24) - 1 || most > (127u + 62) << 24;
+}
 
-__device__ __forceinline__ float finish(const Fp4Args& a, float sum, float ra, float rb, float bias) {
-  float v = sum * near_one(ra) * rb * back(ra);
-  if (a.bias) v += bias;
-  return a.relu && v < 0.f ? 0.f : v;
+// N channels' results of a token
+template <bool kMx, int N>
+__device__ __forceinline__ void finish(const Fp4Args& a, float (&v)[N], float ra, const float (&rb)[N], const float (&bias)[N]) {
+  if (__builtin_expect(a.ra && a.rb && (kMx || far_scale(ra)), 0)) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) v[j] = scaled(v[j], ra, rb[j]);
+  } else {
+#pragma unroll
+    for (int j = 0; j < N; ++j) v[j] = v[j] * ra * rb[j];
+  }
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    if (a.bias) v[j] += bias[j];
+    if (a.relu && v[j] < 0.f) v[j] = 0.f;
+  }
 }
 
 // ------------------------------------------------------------------ few tokens
@@ -129,9 +157,11 @@ __global__ void __launch_bounds__(kFewThreads) gemm_fp4_few_kernel(const __grid_
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
     if (lane == m) {
-      const float y = finish(a, s, a.ra ? a.ra[m] : 1.f, a.rb ? a.rb[n] : 1.f, a.bias ? a.bias[n] : 0.f);
-      if (a.bf16) static_cast<__nv_bfloat16*>(a.C)[m * a.ldc + n] = __float2bfloat16_rn(y);
-      else static_cast<float*>(a.C)[m * a.ldc + n] = y;
+      float y[1] = {s};
+      const float rb[1] = {a.rb ? a.rb[n] : 1.f}, bias[1] = {a.bias ? a.bias[n] : 0.f};
+      finish<kMx>(a, y, a.ra ? a.ra[m] : 1.f, rb, bias);
+      if (a.bf16) static_cast<__nv_bfloat16*>(a.C)[m * a.ldc + n] = __float2bfloat16_rn(y[0]);
+      else static_cast<float*>(a.C)[m * a.ldc + n] = y[0];
     }
   }
 }
@@ -154,7 +184,7 @@ constexpr size_t kLeast = 164 * 1024;            // one CTA an SM, and no other 
 static_assert(no_cluster_beside(kLeast), "no other cluster's CTA beside this kernel's");
 constexpr int kScaleCol = 256;                   // tensor memory: accumulators in front of it, scales of the stages behind
 
-constexpr int kBox = 32 * 64, kTokenBytes = kEpiWarps * kBox + 4 * 2 * kSpan * 4;   // of the epilogue, with tokens as rows
+constexpr int kBox = 32 * 64, kTokenBytes = kEpiWarps * kBox + (4 * 2 + 1) * kSpan * 4;   // of the epilogue, with tokens as rows
 
 struct Tile {
   int BN, nt, mt, units, split, stages, accs, tokens;   // accs: accumulators; tokens: they are the rows
@@ -218,8 +248,8 @@ __host__ __device__ constexpr uint32_t idesc_fp4(int M, int N, bool mx) {
 // which of a tile's four scales a product takes (0, 2), of both operands
 __host__ __device__ constexpr uint32_t scale_id(int id) { return static_cast<uint32_t>(id) << 4 | static_cast<uint32_t>(id) << 29; }
 
-// A thread's channel n of tokens m0 ... m0 + span (kFar: some of the tokens' row scales are near_one's)
-template <bool kFar, typename T>
+// A thread's channel n of tokens m0 ... m0 + span
+template <typename T>
 __device__ __forceinline__ void store_tokens(const Fp4Args& a, T* C, int m0, int n, int span, const float (&sum)[kSpan / 16][16],
                                              const float (&ra)[kSpan / 32], float rb, float bias) {
   T* at = C + m0 * a.ldc + n;
@@ -230,12 +260,6 @@ __device__ __forceinline__ void store_tokens(const Fp4Args& a, T* C, int m0, int
       float v[16];
 #pragma unroll
       for (int e = 0; e < 16; ++e) v[e] = sum[g][e] * __shfl_sync(0xffffffffu, ra[g / 2], (g & 1) * 16 + e) * rb;
-      if constexpr (kFar) {
-        const int m = m0 + 16 * g + (threadIdx.x & 15);
-        const float to = m < a.M && a.ra ? back(__ldg(a.ra + m)) : 1.f;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) v[e] *= __shfl_sync(0xffffffffu, to, e);
-      }
       if (a.bias) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) v[e] += bias;
@@ -263,10 +287,10 @@ __device__ __forceinline__ void lds8(const float* from, float2 (&v)[4]) {
                  : "memory");
 }
 // A warp's 32 tokens from row on, channels n0 ... n0 + span: 64 bytes of each token at a time go to the warp's box in shared
-// memory (64-byte swizzle) and by TMA to C, which clips them at its edges.  `scale`: [channel scale | bias][kSpan]
+// memory (64-byte swizzle) and by TMA to C, which clips them at its edges.  `scale`, `bias`: the channels' [kSpan]
 template <typename T>
 __device__ __forceinline__ void store_channels(const Fp4Args& a, const CUtensorMap* mapC, uint8_t* box, int row, int n0, int span,
-                                               const float (&sum)[kSpan / 16][16], const float* scale, float ra, float far) {
+                                               const float (&sum)[kSpan / 16][16], const float* scale, const float* bias, float ra) {
   constexpr int kCols = 64 / sizeof(T);
   const int lane = threadIdx.x & 31;
 #pragma unroll
@@ -281,10 +305,9 @@ __device__ __forceinline__ void store_channels(const Fp4Args& a, const CUtensorM
         lds8(scale + at, c);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          v[e] = __fmul2_rn(__fmul2_rn(__fmul2_rn(make_float2(sum[at / 16][at % 16 + 2 * e], sum[at / 16][at % 16 + 2 * e + 1]), make_float2(ra, ra)), c[e]),
-                            make_float2(far, far));
+          v[e] = __fmul2_rn(__fmul2_rn(make_float2(sum[at / 16][at % 16 + 2 * e], sum[at / 16][at % 16 + 2 * e + 1]), make_float2(ra, ra)), c[e]);
         if (a.bias) {
-          lds8(scale + kSpan + at, c);
+          lds8(bias + at, c);
 #pragma unroll
           for (int e = 0; e < 4; ++e) v[e] = __fadd2_rn(v[e], c[e]);
         }
@@ -334,7 +357,8 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp4_kernel(const __grid_cons
   const int copied = sx_at + xt * kTk * 512;
   uint8_t* ring = smem;
   uint8_t* recv = smem + p.stages * stage_bytes;   // kSplit: the parts' sums of this CTA's tokens [part][BN / split][128]
-  uint8_t* boxes = recv;                           // kTokens: a box for each warp of the epilogue, and four quarters' scales and biases
+  uint8_t* boxes = recv;                           // kTokens: a box for each warp of the epilogue, four quarters' scales and biases, ones
+  float* ones = reinterpret_cast<float*>(boxes + kEpiWarps * kBox) + 4 * 2 * kSpan;
   Bars* bars = reinterpret_cast<Bars*>(recv + (kSplit ? p.BN * 512 : kTokens ? kTokenBytes : 0));
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const int part = kSplit ? static_cast<int>(cluster_ctarank()) : 0;
@@ -364,6 +388,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp4_kernel(const __grid_cons
     fence_barrier_init();
     fence_proxy_async_smem();
   }
+  if (kTokens && threadIdx.x >= 128 && threadIdx.x < 128 + kSpan) ones[threadIdx.x - 128] = 1.f;
   if (warp == 2) {
     if (CL == 1) {
       tmem_alloc(&bars->tmem, 512);
@@ -496,7 +521,6 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp4_kernel(const __grid_cons
       const uint32_t row0 = tmem + (static_cast<uint32_t>(32 * quarter) << 16) + cb;
       // of the row; of the columns, lane l those of l, 32 + l, ...
       float mine = 1.f, bias = 0.f, theirs[kSpan / 32];
-      bool far = false;
       const int group = warp / 4 - 1;   // the four warps that have the same columns
       float* scale = reinterpret_cast<float*>(boxes + kEpiWarps * kBox) + group * 2 * kSpan;
       if constexpr (kTokens) {
@@ -510,12 +534,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp4_kernel(const __grid_cons
         if (a.rb && row < a.N) mine = __ldg(a.rb + row);
         if (a.bias && row < a.N) bias = __ldg(a.bias + row);
 #pragma unroll
-        for (int i = 0; i < kSpan / 32; ++i) {
-          theirs[i] = a.ra && col0 + 32 * i + lane < a.M && 32 * i < span ? __ldg(a.ra + col0 + 32 * i + lane) : 1.f;
-          far |= theirs[i] != 0.f && back(theirs[i]) != 1.f;
-          theirs[i] = near_one(theirs[i]);
-        }
-        far = __any_sync(0xffffffffu, far);
+        for (int i = 0; i < kSpan / 32; ++i) theirs[i] = a.ra && col0 + 32 * i + lane < a.M && 32 * i < span ? __ldg(a.ra + col0 + 32 * i + lane) : 1.f;
       }
       float sum[kSpan / 16][16];
       const int b = t % p.accs;
@@ -548,20 +567,46 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp4_kernel(const __grid_cons
 #pragma unroll
             for (int e = 0; e < 16; ++e) *reinterpret_cast<float*>(ring + ((cb + 16 * g + e) * 128 + 32 * quarter + lane) * 4) = sum[g][e];
           }
-      } else if constexpr (kTokens) {
-        const float ra = near_one(mine), to = back(mine);
-        uint8_t* box = boxes + (warp - 4) * kBox;
-        if (row - lane < a.M) {
-          if (a.bf16) store_channels<__nv_bfloat16>(a, &mapC, box, row - lane, col0, span, sum, scale, ra, to);
-          else store_channels<float>(a, &mapC, box, row - lane, col0, span, sum, scale, ra, to);
-        }
-      } else if (far) {
-        if (a.bf16) store_tokens<true>(a, static_cast<__nv_bfloat16*>(a.C), col0, row, span, sum, theirs, mine, bias);
-        else store_tokens<true>(a, static_cast<float*>(a.C), col0, row, span, sum, theirs, mine, bias);
-      } else if (a.bf16) {
-        store_tokens<false>(a, static_cast<__nv_bfloat16*>(a.C), col0, row, span, sum, theirs, mine, bias);
       } else {
-        store_tokens<false>(a, static_cast<float*>(a.C), col0, row, span, sum, theirs, mine, bias);
+        bool apart = false;
+        if (a.ra && a.rb) {   // the same for all
+          if constexpr (kTokens) {
+            apart = far_scale(mine);
+          } else {
+#pragma unroll
+            for (int i = 0; i < kSpan / 32; ++i) apart |= far_scale(theirs[i]);
+          }
+          if constexpr (kMx) {
+#pragma unroll
+            for (int g = 0; g < kSpan / 16; ++g)
+              if (16 * g < span) apart |= far_sums(sum[g]);
+          }
+          apart = __any_sync(0xffffffffu, apart);
+        }
+        if (__builtin_expect(apart, 0)) {   // the scales are taken here, and ones below
+#pragma unroll
+          for (int g = 0; g < kSpan / 16; ++g)
+            if (16 * g < span) {
+#pragma unroll
+              for (int e = 0; e < 16; ++e)
+                sum[g][e] = kTokens ? scaled(sum[g][e], mine, scale[16 * g + e])
+                                    : scaled(sum[g][e], __shfl_sync(0xffffffffu, theirs[g / 2], (g & 1) * 16 + e), mine);
+            }
+          mine = 1.f;
+#pragma unroll
+          for (int i = 0; i < kSpan / 32; ++i) theirs[i] = 1.f;
+        }
+        if constexpr (kTokens) {
+          uint8_t* box = boxes + (warp - 4) * kBox;
+          const float* rb = apart ? ones : scale;
+          if (row - lane < a.M) {
+            if (a.bf16) store_channels<__nv_bfloat16>(a, &mapC, box, row - lane, col0, span, sum, rb, scale + kSpan, mine);
+            else store_channels<float>(a, &mapC, box, row - lane, col0, span, sum, rb, scale + kSpan, mine);
+          }
+        } else {
+          if (a.bf16) store_tokens(a, static_cast<__nv_bfloat16*>(a.C), col0, row, span, sum, theirs, mine, bias);
+          else store_tokens(a, static_cast<float*>(a.C), col0, row, span, sum, theirs, mine, bias);
+        }
       }
     }
     if (kTokens && lane == 0) bulk_wait_all();
@@ -594,13 +639,13 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp4_kernel(const __grid_cons
           for (int q = 0; q < p.split; ++q)
 #pragma unroll
             for (int j = 0; j < 4; ++j) t[j] += sums[(q * tokens + i) * 128 + 32 * j];
+          finish<kMx>(a, t, ra, rb, bias);
           const int64_t at = (m0 + i) * a.ldc + n0;
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const float y = finish(a, t[j], ra, rb[j], bias[j]);
             if (n0 + 32 * j >= a.N) continue;
-            if (a.bf16) static_cast<__nv_bfloat16*>(a.C)[at + 32 * j] = __float2bfloat16_rn(y);
-            else static_cast<float*>(a.C)[at + 32 * j] = y;
+            if (a.bf16) static_cast<__nv_bfloat16*>(a.C)[at + 32 * j] = __float2bfloat16_rn(t[j]);
+            else static_cast<float*>(a.C)[at + 32 * j] = t[j];
           }
         }
       }
