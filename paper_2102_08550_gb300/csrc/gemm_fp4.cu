@@ -514,7 +514,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp4_kernel(const __grid_cons
     const int quarter = warp & 3, span = p.BN > 64 ? p.BN / 4 : 16, cb = (warp / 4 - 1) * span;
     const bool works = cb < p.BN;
     int t = 0;
-    for (int u = u0; ok && u < p.units; u += ustep) {
+    for (int u = u0; (kTokens || ok) && u < p.units; u += ustep) {
       int tr, tc;
       tile_at(u, mu, p.nt, tr, tc);
       const int row = (tr * CL + rank) * 128 + 32 * quarter + lane, col0 = tc * p.BN + cb;
@@ -525,7 +525,9 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp4_kernel(const __grid_cons
       float* scale = reinterpret_cast<float*>(boxes + kEpiWarps * kBox) + group * 2 * kSpan;
       if constexpr (kTokens) {
         if (a.ra && row < a.M) mine = __ldg(a.ra + row);
-        bar_named(1 + group, 128);      // they are done with the tile before
+        // They are done with the tile before.  A wait may have run out in one of them alone, which then comes here once more, and
+        // all four leave together: none waits for one that has gone.
+        if (!bar_and(1 + group, 128, ok)) break;
         const int i = threadIdx.x & 127, n = col0 + (i & (kSpan - 1));
         if (i < kSpan) scale[i] = a.rb && n < a.N ? __ldg(a.rb + n) : 1.f;
         else scale[i] = a.bias && n < a.N ? __ldg(a.bias + n) : 0.f;
@@ -558,7 +560,10 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_fp4_kernel(const __grid_cons
         }
       }
       ++t;
-      if (!ok) break;   // every wait that runs out in this CTA ends in one of the accumulator's
+      if (!ok) {   // every wait that runs out in this CTA ends in one of the accumulator's
+        if constexpr (kTokens) continue;
+        else break;
+      }
       if (!works) continue;
       if constexpr (kSplit) {   // the part's sums [token][channel], where the ring was: its products have ended
 #pragma unroll
