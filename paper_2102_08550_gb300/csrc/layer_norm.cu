@@ -569,6 +569,24 @@ __global__ void __launch_bounds__(kThreads) norm_columns_kernel(const __grid_con
   }
 }
 
+// The sums of up to eight chunks, a column a thread, in their order.
+constexpr int kFewChunks = 8;
+__global__ void __launch_bounds__(kThreads) norm_join_few_kernel(const __grid_constant__ BwdArgs a) {
+  pdl_wait();
+  pdl_trigger();
+  const int64_t col = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
+  const int group = blockIdx.z, which = blockIdx.y;
+  float* to = which == 0 ? a.dgamma : a.dbeta;
+  if (!to || col >= a.cols) return;
+  const float* from = a.part + (static_cast<int64_t>(group) * a.chunks * 2 + which) * a.cols + col;
+  float v[kFewChunks];
+#pragma unroll
+  for (int i = 0; i < kFewChunks; ++i) v[i] = i < a.chunks ? from[static_cast<int64_t>(i) * 2 * a.cols] : 0.f;
+#pragma unroll
+  for (int i = 1; i < kFewChunks; ++i) v[0] += v[i];
+  to[group * a.dstride + col] = v[0];
+}
+
 // The chunks' sums of a column, kJoinLanes threads a column, in a fixed order.  32 where a call has more chunks than 64, so that
 // they are requested together (152 chunks of 16384 x 4096: 67.7 us for 69.5 with eight; 64 of 64 x 8192 fp32: 8.8 us for 7.6).
 template <int kJoinLanes>
@@ -763,25 +781,39 @@ struct Split {
 // One pass: a chunk for each SM, each with a row for all of its lanes at least.  Up to 16 chunks of a group are made eight, which
 // meet in a cluster, where they are short: up to kFewRows turns cost less than a second launch.
 // Wide rows: chunks of columns' tiles enough to fill the card, each of 64 rows or more.
+// In both a thread adds up so few rows of its columns in sequence that a term takes at most 256 + rows / 64 additions in all (the
+// lanes, and chunks 16 at most).  Where a chunk for each SM would have more: as many as take the least time in waves of an SM
+// each, whose beginning and end cost as much as 16 rows (77 x 1000 x 4104 bf16 803 us with a chunk an SM, 614 with as few as the
+// bound allows, 479 so; 152 x 700 x 4200, which fills the card without, 578 and 592).
 Split split_rows(int groups, int rows, int cols) {
   int64_t want, most;
+  const int lanes = cols <= kWide ? lanes_of<kBackward>(cols) : kRowLanes;
+  const int64_t run = lanes * (236 - lanes + rows / 64), need = (rows + run - 1) / run;
+  bool waves = false;
   if (cols <= kWide) {
-    const int lanes = lanes_of<kBackward>(cols);
     want = kCtas / groups;
+    waves = want < need;
+    if (waves) {
+      auto time = [&](int64_t c) { return (groups * c + kCtas - 1) / kCtas * (rows / (c * lanes) + 16); };
+      want = need;
+      for (int64_t c = need + 1; c <= 4 * need; ++c)
+        if (time(c) < time(want)) want = c;
+    }
     most = (static_cast<int64_t>(rows) + lanes - 1) / lanes;
   } else {
     const int64_t tiles = (static_cast<int64_t>(cols) + kColTile - 1) / kColTile * groups;
     want = (1216 + tiles - 1) / tiles;
+    want = want > need ? want : need;
     most = (static_cast<int64_t>(rows) + 63) / 64;
   }
   want = want < most ? want : most;
   if (want < 1) want = 1;
-  if (cols <= kWide && want > kCluster && want <= 2 * kCluster && most <= kFewRows * kCluster) want = kCluster;
+  if (cols <= kWide && !waves && want > kCluster && want <= 2 * kCluster && most <= kFewRows * kCluster) want = kCluster;
   Split s;
   s.per = static_cast<int>((rows + want - 1) / want);
   if (s.per < 1) s.per = 1;
   s.chunks = rows > 0 ? (rows + s.per - 1) / s.per : 1;
-  s.clustered = cols <= kWide && s.chunks > 1 && s.chunks <= kCluster;
+  s.clustered = cols <= kWide && !waves && s.chunks > 1 && s.chunks <= kCluster;
   return s;
 }
 
@@ -815,7 +847,9 @@ cudaError_t one_pass(const BwdArgs& a, cudaStream_t s) {
   });
 }
 
+// (few chunks by blocks of 32 columns too: 100 x 300 x 8192 fp32, three each, 520 us for 475)
 cudaError_t join(const BwdArgs& a, cudaStream_t s) {
+  if (a.chunks <= kFewChunks) return launch_dependent(norm_join_few_kernel, dim3((a.cols + kThreads - 1) / kThreads, 2, a.groups), kThreads, 0, s, a);
   const dim3 grid((a.cols + kColTile - 1) / kColTile, 2, a.groups);
   return a.chunks > 64 ? launch_dependent(norm_join_kernel<32>, grid, kColTile * 32, 0, s, a)
                        : launch_dependent(norm_join_kernel<8>, grid, kColTile * 8, 0, s, a);
