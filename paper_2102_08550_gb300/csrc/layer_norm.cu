@@ -518,13 +518,13 @@ __global__ void __launch_bounds__(kThreads) norm_dx_kernel(const __grid_constant
     }
   };
   float sh = 0.f, shx = 0.f;
-  each([&](int at, float (&h)[8], float (&xh)[8]) {
+  each([&](int at, float (&h)[8], float (&xh)[8]) {   // eight at a time: n / 2048 additions in sequence
+    float t = 0.f;
 #pragma unroll
     for (int e = 0; e < 8; ++e)
-      if (at + e < a.cols) {
-        sh += h[e];
-        shx = fmaf(h[e], xh[e], shx);
-      }
+      if (at + e < a.cols) t = fmaf(h[e], xh[e], t);   // (h is 0 behind the row's end, and xh may be infinite)
+    sh += ((h[0] + h[1]) + (h[2] + h[3])) + ((h[4] + h[5]) + (h[6] + h[7]));
+    shx += t;
   });
   sh = block_sum(sh, part) / a.cols;
   shx = block_sum(shx, part) / a.cols;
