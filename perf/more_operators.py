@@ -319,7 +319,6 @@ def _run_own(state):
         return {"dx": out, "dgamma": dgamma, "dbeta": dbeta}
     fmt = lib.MXFP4 if case["format"] == "mx" else lib.NVFP4
     q, s, t = state["A"]
-    q = q.to(torch.uint8)   # the calls take codes as bytes (what quantisation writes is bytes already)
     tp = t.data_ptr() if t is not None else None
     if k != "product":
         x = state["x"]
@@ -329,6 +328,10 @@ def _run_own(state):
             out = state["out"]
             lib.oscars_dequantize_fp4(q.data_ptr(), q.stride(0), s.data_ptr(), tp, fmt, rows, cols, out.data_ptr(), cols, dt, stream=stream)
             return out
+    else:   # the calls take codes as bytes (what quantisation writes is bytes already)
+        if "bytes" not in state:   # a buffer of the program's, written in each pass
+            state["bytes"] = torch.empty(q.shape, device=DEV, dtype=torch.uint8)
+        q = state["bytes"].copy_(q)
     M, N, K = case["M"], case["N"], case["K"]
     qb, sb, tb = state["B"]
     if "weight" not in state:   # laid out once, as a program keeps its weights
