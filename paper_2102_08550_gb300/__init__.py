@@ -386,13 +386,14 @@ def oscars_fp4_scale_bytes(rows: int, cols: int, fmt: int) -> int:
 
 def oscars_quantize_fp4(x_ptr: int, ldx: int, dtype: int, rows: int, cols: int, fmt: int, q_ptr: int, ldq: int, scales_ptr: int,
                         row_scale_ptr: Optional[int] = None, stream: Optional[int] = None):
-    """Rows in 4 bits with a scale for each block (ldx in elements, ldq in bytes)."""
+    """Rows in 4 bits with a scale for each block (ldx in elements, ldq in bytes).  Codes and block scales are bytes: buffers
+    of torch.uint8, whose addresses and strides these calls take as they are."""
     _check(lib().oscars_quantize_fp4(x_ptr, ldx, dtype, rows, cols, fmt, q_ptr, ldq, scales_ptr, row_scale_ptr, stream))
 
 
 def oscars_dequantize_fp4(q_ptr: int, ldq: int, scales_ptr: int, row_scale_ptr: Optional[int], fmt: int, rows: int, cols: int,
                           x_ptr: int, ldx: int, dtype: int, stream: Optional[int] = None):
-    """The values of rows in 4 bits (ldq in bytes, ldx in elements)."""
+    """The values of rows in 4 bits (ldq in bytes, ldx in elements; codes and block scales in torch.uint8)."""
     _check(lib().oscars_dequantize_fp4(q_ptr, ldq, scales_ptr, row_scale_ptr, fmt, rows, cols, x_ptr, ldx, dtype, stream))
 
 
@@ -400,7 +401,7 @@ def oscars_gemm_fp4_nt(a_ptr: int, lda: int, scales_a_ptr: int, b_ptr: int, ldb:
                        ldc: int, dtype: int, M: int, N: int, K: int, row_scale_a_ptr: Optional[int] = None,
                        row_scale_b_ptr: Optional[int] = None, bias_ptr: Optional[int] = None, relu: bool = False,
                        stream: Optional[int] = None):
-    """4-bit product with scales, bias and ReLU (lda, ldb in bytes, ldc in elements)."""
+    """4-bit product with scales, bias and ReLU (lda, ldb in bytes, ldc in elements; codes and block scales in torch.uint8)."""
     _check(lib().oscars_gemm_fp4_nt(a_ptr, lda, scales_a_ptr, row_scale_a_ptr, b_ptr, ldb, scales_b_ptr, row_scale_b_ptr, fmt,
                                     bias_ptr, int(relu), c_ptr, ldc, dtype, M, N, K, stream))
 

@@ -15,7 +15,8 @@
 //   4-19    accumulators -> C, under the products of the next tile
 // What bounds a large product is the tensor pipe (69% busy; a pair's K-block of 256 x 256 x 256 is 512 clocks of products) and, while
 // results leave, the loads' latency: five stages of 38 KB cover 2500 clocks of it (four 47.3 us, three 54.9).  8192 x 4096 x
-// 4096 NV takes 43.5 us (6.3 PFLOP/s); without its results' stores 4.5 us less.
+// 4096 NV takes 43.5 us in a burst (6.3 PFLOP/s), 48 to 50 back to back for seconds under the power cap; without its results'
+// stores 4.5 us less.
 // gemm_fp4_few_kernel for one token, or up to three of few channels.
 #include <atomic>
 

@@ -21,7 +21,9 @@ namespace {
 
 constexpr int kThreads = 256, kUnit = 16;
 
-// n / d for n < 2^31 by a multiplication (d of a launch is one number)
+// n / d for n < 2^31 by a multiplication (d of a launch is one number): T. Granlund, P. L. Montgomery, "Division by invariant
+// integers using multiplication", 1994, their multiplier less 2^32, which n < 2^31
+// lets be added without a carry
 struct Divide {
   uint32_t d, m;
   int s;
