@@ -711,7 +711,8 @@ oscars_status oscars_layer_norm(const void* x, int64_t ldx, const float* gamma, 
  * dgamma[g dparam_stride + j], overwritten (rows = 0: zeros).  dx, dgamma and dbeta
  * may each be NULL: not wanted.  All sums are in fp32 and in a fixed order: equal calls
  * give equal bits; a value of a row goes through at most 40 + cols / 1024 additions, a
- * term of dgamma or dbeta through 256 + rows / 64.  (Where xh leaves a row no freedom, as with two columns, dx is
+ * term of dgamma or dbeta through 256 + rows / 64.  A row's sums of h and h xh
+ * have to stay inside fp32.  (Where xh leaves a row no freedom, as with two columns, dx is
  * what fp32 leaves of terms that cancel.)
  * workspace: device, 16-byte aligned, at least the bytes that
  * oscars_layer_norm_backward_workspace gives for the same sizes (it may be 0, then
